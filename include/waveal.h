@@ -1,11 +1,16 @@
 /* waveal - WaveAlign-scheduled block-sparse attention for NVIDIA B200 (sm_100a).
  *
- * C ABI of the library.  Two groups of calls:
+ * C ABI of the library.  Groups of calls:
  *   planning   waveal_plan_bitmap / waveal_plan_csr : block mask -> per-head execution order
  *              of the query blocks (Algorithm 2 of the WaveAlign paper, with the adaptive
  *              skip of Section 4.5 in front);
  *   attention  waveal_bsattn_fwd : block-sparse FlashAttention-style forward (Sections
  *              2.2-2.3) whose persistent CTAs walk that order head by head.
+ * and, for programs that continue one long sequence in several ways,
+ *   positions  waveal_rope : rotary positions of queries and keys, forwards and backwards;
+ *   cache      waveal_cache_append : new keys (rotated on the way) and values into a paged cache;
+ *   attention  waveal_prefix_attn : a batch of queries over a prefix that all of them share and over
+ *              each sequence's own keys, both in that cache.
  *
  * Conventions for every call
  *   - "dev" pointers are device pointers on the current CUDA device, "host" pointers are
@@ -28,7 +33,7 @@
  *
  * Shape of the interface (choices of this library, fixed here so that callers need not guess)
  *   - batch is flattened into `heads`, so strides have two entries {head, token};
- *   - bf16 is the only element type, so there is no dtype field;
+ *   - bf16 is the only element type of waveal_bsattn_fwd, so its descriptor has no dtype field;
  *   - a plan call's outputs are grouped in one struct, waveal_plan_out: one required, the rest optional;
  *   - workspace sizes depend on the descriptor alone, never on the number of selected blocks;
  *   - dev_status has four int32 words {code, site, head or block, value};
@@ -272,6 +277,138 @@ waveal_status waveal_scatter_rows(int32_t heads, int32_t n_blocks, int32_t block
                                   const void* src /*dev*/, const int64_t* src_stride_bytes /*host [2]*/,
                                   void* dst /*dev*/, const int64_t* dst_stride_bytes /*host [2]*/,
                                   const int32_t* row_order /*dev [heads][n_blocks]*/, void* cuda_stream);
+
+/* ---------------------------------------------------------------- rotary positions, paged cache, shared prefix
+ *
+ * Tensors of these calls are [heads][tokens][head_dim] with strides {head, token} in elements, head_dim
+ * contiguous, any order and gaps.  They have no counterpart in the WaveAlign paper: they are what a program that
+ * generates a clip piece by piece, or several continuations of one, needs around its attention. */
+
+typedef enum { WAVEAL_BF16 = 0, WAVEAL_FP16 = 1, WAVEAL_FP32 = 2 } waveal_dtype;
+
+/* Which channels form a pair: (i, i + rot_dim/2), or (2i, 2i + 1). */
+#define WAVEAL_PAIRS_HALVES 0
+#define WAVEAL_PAIRS_INTERLEAVED 1
+
+/* The rotation of the first rot_dim channels of every head; the others pass unchanged.  Pair i is turned by
+ *     angle = 2 pi * frac(position * freqs[i] / 2^64),   (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ * freqs: int64 [rot_dim/2], turns per position in units of 2^-64 turns (waveal_rope_freqs makes them): the product
+ * cut to 64 bits has no rounding, so the angle is as exact at position 2^31 as at 1.
+ * axes: how many positions a token has (1 for a sequence, 3 for frame, height and width of a video); the first
+ * axis_pairs[0] pairs turn with the first, the next axis_pairs[1] with the second and so on. */
+typedef struct waveal_rotation {
+  int32_t rot_dim;        /* even, 2 .. head_dim                                              */
+  int32_t pairs;          /* WAVEAL_PAIRS_*                                                   */
+  int32_t axes;           /* 1 .. 3                                                           */
+  int32_t axis_pairs[3];  /* adding up to rot_dim/2; those of unused axes 0                   */
+  int32_t inverse;        /* 1: by -angle.  With the same amplitude that is the gradient: the rotation is linear, and its
+                             transpose is the rotation backwards                              */
+  float amplitude;        /* factor on the rotated channels (1, or what a scaling asks for)   */
+} waveal_rotation;
+
+/* Frequencies for contexts longer than the trained one.  base^(-2i/rot_dim) radians a position, then
+ *   NONE    as they are;
+ *   LINEAR  divided by factor (positions are interpolated);
+ *   NTK     with base * factor^(rot_dim/(rot_dim-2)): the slowest pair is stretched by factor, the fastest not at all;
+ *   PARTS   (as in YaRN) by how often a pair turns in the trained length: >= 32 times as it is, <= once divided by factor,
+ *           linearly in between; *amplitude becomes 0.1 ln(factor) + 1. */
+typedef enum { WAVEAL_ROPE_NONE = 0, WAVEAL_ROPE_LINEAR = 1, WAVEAL_ROPE_NTK = 2, WAVEAL_ROPE_PARTS = 3 } waveal_rope_scaling;
+
+/* Fills freqs[0 .. rot_dim/2) (host; one axis: a caller with several calls it for each and lays them one behind the other)
+ * and *amplitude (host or NULL; 1 but for PARTS).  trained_len: used by PARTS.  Host-only. */
+waveal_status waveal_rope_freqs(int32_t rot_dim, double base, waveal_rope_scaling scaling, double factor, int64_t trained_len,
+                                int64_t* freqs /*host*/, float* amplitude /*host or NULL*/);
+
+typedef struct waveal_rope_desc {
+  int32_t tokens, head_dim;      /* tokens >= 0, head_dim 2 .. 512                            */
+  int32_t q_heads, k_heads;      /* k_heads 0: one tensor                                     */
+  int32_t dtype;                 /* waveal_dtype                                              */
+  waveal_rotation rot;
+  int64_t q_stride[2], q_out_stride[2], k_stride[2], k_out_stride[2];   /* elements: {head, token} */
+} waveal_rope_desc;
+
+/* Rotates q (and k) by their positions.  positions: dev int32 [axes][tokens], the same for every head.  An output may be
+ * its own input (same pointer and strides: the channels behind rot_dim are then left alone); any other overlap is not
+ * allowed.  Arithmetic in fp32, one rounding on the way out.  Any alignment of the elements' own size works; 16-byte
+ * aligned rows are read and written 16 bytes at a time.  No workspace. */
+waveal_status waveal_rope(const waveal_rope_desc* desc /*host*/, const void* q, void* q_out, const void* k /*or NULL*/,
+                          void* k_out /*or NULL*/, const int32_t* positions /*dev*/, const int64_t* freqs /*dev*/,
+                          void* cuda_stream);
+
+/* A paged cache: keys and values [n_pages][kv_heads][page_size][head_dim], each with strides {page, head, token} in
+ * elements (so a page may hold its tokens head by head or token by token).  Key i of a sequence lies in page
+ * table[i / page_size], slot i % page_size. */
+typedef struct waveal_cache_desc {
+  int32_t n_pages;
+  int32_t page_size;      /* power of two, 16 .. 65536                                        */
+  int32_t kv_heads;
+  int32_t head_dim;       /* append: 2 .. 512; attention: 64 or 128                           */
+  int32_t dtype;          /* WAVEAL_BF16 or WAVEAL_FP16                                       */
+  int64_t k_stride[3], v_stride[3];
+} waveal_cache_desc;
+
+/* The batch that append and attention are called for.
+ *   seq_start  dev int32 [batch + 1]: the new tokens of sequence b are tokens seq_start[b] .. seq_start[b+1] - 1 of the
+ *              call's tensors (0 <= seq_start[b] <= seq_start[b+1] <= tokens; tokens behind the last one's are not touched)
+ *   kv_len     dev int32 [batch]: the sequence's own keys, the new ones among them (they are its last)
+ *   page_table dev int32 [batch][table_stride]: the pages of its own keys, max_pages a row at most
+ * All three are read on the device, so a captured call follows what they hold when it is replayed.  What is malformed
+ * (a decreasing or too large seq_start, a negative kv_len or one beyond max_pages * page_size, kv_len smaller than the new
+ * tokens in append, a page outside [0, n_pages)) is reported in dev_status as {WAVEAL_ERR_BAD_MASK, site, sequence, value};
+ * the sequence then counts as having no new tokens, or no own keys, or the page is not written / reads as zeros. */
+typedef struct waveal_batch_desc {
+  int32_t batch, tokens;  /* sequences, new tokens of all of them (both may be 0)             */
+  int32_t q_heads;        /* append: 0 where queries are not passed; attention: a multiple of kv_heads, at most 128 times as many */
+  int32_t max_pages;      /* 0 where no sequence has own keys                                 */
+  int32_t prefix_len;     /* keys of the shared prefix (append: what the default positions start from) */
+  int32_t flags;          /* attention: WAVEAL_PREFIX_CAUSAL                                  */
+  int64_t table_stride;
+} waveal_batch_desc;
+
+/* New token i (from 0) of n sees its sequence's own keys 0 .. kv_len - n + i only; without the flag all kv_len. */
+#define WAVEAL_PREFIX_CAUSAL 1
+/* Self-test of the kernel's failure handling, as WAVEAL_ATTN_SELFTEST_LOST_TILE: thread block 0 never loads its first K tile and
+ * waits give up after about 2 ms; dev_status then reports WAVEAL_ERR_TIMEOUT, o is undefined, the next call works. */
+#define WAVEAL_PREFIX_SELFTEST_LOST_TILE 256
+
+typedef struct waveal_append_strides {
+  int64_t k[2], v[2], q[2], q_out[2];  /* {head, token} */
+} waveal_append_strides;
+
+/* Writes the new tokens' keys, rotated, and values to their places in the cache, and the rotated queries to q_out.
+ * rot: NULL for no rotation (q must then be NULL).  positions: dev int32 [axes][tokens], or NULL: prefix_len + the token's place
+ * among its sequence's own keys, on every axis.  q, q_out: NULL where the queries are rotated elsewhere; q_out may be q.
+ * Two tokens must not go to the same slot (sequences that share a page which both write to).  No workspace. */
+waveal_status waveal_cache_append(const waveal_cache_desc* cache /*host*/, const waveal_batch_desc* batch /*host*/,
+                                  const waveal_rotation* rot /*host or NULL*/, const waveal_append_strides* strides /*host*/,
+                                  const void* k, const void* v, const void* q, void* q_out, void* k_cache, void* v_cache,
+                                  const int32_t* seq_start, const int32_t* kv_len, const int32_t* page_table,
+                                  const int32_t* positions, const int64_t* freqs, int32_t* dev_status /*dev [4] or NULL*/,
+                                  void* cuda_stream);
+
+/* Bytes of device workspace waveal_prefix_attn needs.  It depends on the descriptors alone, not on the lengths. */
+waveal_status waveal_prefix_attn_workspace_bytes(const waveal_cache_desc* cache /*host*/, const waveal_batch_desc* batch /*host*/,
+                                                 size_t* bytes /*host*/);
+
+/* o = softmax(scale * q K^T) V of every new token over the keys of the shared prefix and those of its own sequence
+ * (query head h reads key head h / (q_heads / kv_heads)).  The rows of all sequences that read a key head go through the
+ * prefix together, so its keys and values are read once for up to 256 of them; each sequence's own keys are read by its own rows.  Both are
+ * split over the SMs by their length; the parts are joined by their maxima and sums.
+ * prefix_pages: dev int32 [ceil(prefix_len / page_size)] or NULL with prefix_len 0.  Slots of a page behind the last key may hold
+ * anything, NaN included; so may pages and table entries behind it, which are not read.
+ * q, o: 16-byte aligned, strides multiples of 8 elements; the cache likewise.  q's and o's type is the cache's.
+ * At most 2^30 keys in the prefix and in a row of the page table, 10^9 rows (tokens * q_heads).
+ * lse: dev float [q_heads][tokens] or NULL, the natural log of the sum of exponentials; a token that sees no key has o = 0
+ * and -inf.  A row whose scores hold +infinity or NaN gives NaN; values of keys that a token does not see through
+ * WAVEAL_PREFIX_CAUSAL must be finite all the same (they are multiplied by zero).
+ * scale <= 0 means 1/sqrt(head_dim).  Scores and sums are fp32; the probabilities enter the second product in the tensors' type.
+ * ws: 256-byte aligned, not shared with a call that may run at the same time; needs no clearing.  dev_status: dev int32 [4] or
+ * NULL, zeroed by the caller; also {WAVEAL_ERR_TIMEOUT, site, thread block, thread} when a bounded wait ran out. */
+waveal_status waveal_prefix_attn(const waveal_cache_desc* cache /*host*/, const waveal_batch_desc* batch /*host*/, const void* q,
+                                 const int64_t* q_stride /*host [2]*/, const void* k_cache, const void* v_cache, void* o,
+                                 const int64_t* o_stride /*host [2]*/, float* lse, const int32_t* seq_start,
+                                 const int32_t* kv_len, const int32_t* page_table, const int32_t* prefix_pages, float scale,
+                                 void* ws, size_t ws_bytes, int32_t* dev_status, void* cuda_stream);
 
 /* Number of query-block tasks the attention kernel keeps in flight on the current device
  * (SM count x CTAs per SM): the W to plan with (Section 6.1).  Returns <= 0 on failure. */

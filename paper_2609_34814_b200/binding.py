@@ -21,6 +21,7 @@ FLAG_SKIPPED, FLAG_SHORT_SEQ, FLAG_TOO_SPARSE, FLAG_ALREADY_LOCAL = 1, 2, 4, 8
 EXPORTS = ["waveal_plan_desc_default", "waveal_plan_workspace_bytes", "waveal_plan_bitmap", "waveal_plan_csr",
            "waveal_bitmap_to_csr", "waveal_bitmap_to_csr_noalloc", "waveal_noalloc_max_rows",
            "waveal_gather_rows", "waveal_scatter_rows", "waveal_bsattn_workspace_bytes", "waveal_bsattn_fwd",
+           "waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
            "waveal_default_wave_size", "waveal_last_launch_count", "waveal_status_string", "waveal_last_error"]
 
 
@@ -44,6 +45,35 @@ class AttnDesc(ctypes.Structure):
                 ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2),
                 ("o_stride", ctypes.c_int64 * 2), ("order_heads_interleaved", ctypes.c_int32),
                 ("flags", ctypes.c_int32)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("axis_pairs", ctypes.c_int32 * 3), ("inverse", ctypes.c_int32), ("amplitude", ctypes.c_float)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("k_heads", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rot", Rotation),
+                ("q_stride", ctypes.c_int64 * 2), ("q_out_stride", ctypes.c_int64 * 2),
+                ("k_stride", ctypes.c_int64 * 2), ("k_out_stride", ctypes.c_int64 * 2)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3)]
+
+
+class BatchDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("prefix_len", ctypes.c_int32), ("flags", ctypes.c_int32),
+                ("table_stride", ctypes.c_int64)]
+
+
+class AppendStrides(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int64 * 2), ("v", ctypes.c_int64 * 2), ("q", ctypes.c_int64 * 2),
+                ("q_out", ctypes.c_int64 * 2)]
 
 
 class WavealError(RuntimeError):
@@ -79,7 +109,16 @@ def load() -> ctypes.CDLL:
         lib.waveal_bsattn_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(ctypes.c_size_t)]
         lib.waveal_bsattn_fwd.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, P, P, P, ctypes.c_float, P,
                                           ctypes.c_size_t, P, P]
-        for name in ["waveal_plan_workspace_bytes", "waveal_plan_bitmap", "waveal_plan_csr", "waveal_bitmap_to_csr",
+        lib.waveal_rope_freqs.argtypes = [I32, ctypes.c_double, ctypes.c_int, ctypes.c_double, I64, P, ctypes.POINTER(ctypes.c_float)]
+        lib.waveal_rope.argtypes = [ctypes.POINTER(RopeDesc), P, P, P, P, P, P, P]
+        lib.waveal_cache_append.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc), ctypes.POINTER(Rotation),
+                                            ctypes.POINTER(AppendStrides), P, P, P, P, P, P, P, P, P, P, P, P, P]
+        lib.waveal_prefix_attn_workspace_bytes.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc),
+                                                           ctypes.POINTER(ctypes.c_size_t)]
+        lib.waveal_prefix_attn.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc), P, ctypes.POINTER(I64), P, P, P,
+                                           ctypes.POINTER(I64), P, P, P, P, P, ctypes.c_float, P, ctypes.c_size_t, P, P]
+        for name in ["waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
+                     "waveal_plan_workspace_bytes", "waveal_plan_bitmap", "waveal_plan_csr", "waveal_bitmap_to_csr",
                      "waveal_gather_rows", "waveal_scatter_rows", "waveal_bsattn_workspace_bytes", "waveal_bsattn_fwd", "waveal_default_wave_size",
                      "waveal_last_launch_count"]:
             getattr(lib, name).restype = ctypes.c_int
@@ -310,3 +349,211 @@ def bsattn_fwd(desc: AttnDesc, q, k, v, o, kv_row_ptr, kv_block_indices, row_ord
                                  _ptr(kv_block_indices), _ptr(row_order), ctypes.c_float(scale), _ptr(workspace),
                                  workspace.numel(), _ptr(dev_status), _stream(stream)))
     return workspace
+
+
+# ------------------------------------------------------------------ rotary positions, paged cache, shared prefix
+
+BF16, FP16, FP32 = range(3)
+PAIRS_HALVES, PAIRS_INTERLEAVED = range(2)
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+PREFIX_CAUSAL = 1
+PREFIX_SELFTEST_LOST_TILE = 256
+
+
+_dtypes = None
+
+
+def _dtype(t) -> int:
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
+    if t.dtype not in _dtypes:
+        raise TypeError(f"{t.dtype} is not supported")
+    return _dtypes[t.dtype]
+
+
+def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained_len: int = 0, device="cuda"):
+    """waveal_rope_freqs.  Returns (freqs, amplitude): an int64 tensor of rot_dim/2 phase steps on `device` and the
+    factor that the scaling puts on the rotated channels.  Several axes: one call each, torch.cat of the steps."""
+    import torch
+    freqs = torch.empty((rot_dim // 2,), dtype=torch.int64)
+    amplitude = ctypes.c_float(1.0)
+    _check(load().waveal_rope_freqs(rot_dim, base, ROPE_SCALINGS[scaling], factor, trained_len, freqs.data_ptr(),
+                                    ctypes.byref(amplitude)))
+    return freqs.to(device), float(amplitude.value)
+
+
+def _rotation(freqs, interleaved, axis_pairs, amplitude, inverse=False) -> Rotation:
+    pairs = freqs.shape[0]
+    n = len(axis_pairs) if axis_pairs is not None else 1
+    if n > 3:
+        raise ValueError("at most three axes")
+    own = (pairs, 0, 0) if axis_pairs is None else (*axis_pairs, 0, 0)[:3]
+    return Rotation(2 * pairs, 1 if interleaved else 0, n, own, 1 if inverse else 0, amplitude)
+
+
+def _int32(t, name):
+    import torch
+    if t is not None and (t.dtype != torch.int32 or not t.is_cuda):
+        raise TypeError(f"{name} must be an int32 cuda tensor")
+    return t
+
+
+def _rows(name, t, head_dim=None):
+    """strides {head, token} of a [heads, tokens, head_dim] cuda tensor"""
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{name} must be a [heads, tokens, head_dim] cuda tensor")
+    h, n, d = t.stride()
+    if d != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name}: head_dim must be contiguous")
+    if head_dim is not None and t.shape[2] != head_dim:
+        raise ValueError(f"{name} has head_dim {t.shape[2]}, expected {head_dim}")
+    return h, n
+
+
+def _positions(positions, axes, tokens):
+    _int32(positions, "positions")
+    if positions.dim() == 1:
+        positions = positions[None]
+    if tuple(positions.shape) != (axes, tokens) or not positions.is_contiguous():
+        raise ValueError(f"positions must be contiguous [{axes}, {tokens}], got {tuple(positions.shape)}")
+    return positions
+
+
+def _freqs(freqs):
+    import torch
+    if freqs.dtype != torch.int64 or not freqs.is_cuda or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise TypeError("freqs must be a contiguous int64 cuda tensor [rot_dim/2]")
+    return freqs
+
+
+def rope(q, positions, freqs, k=None, q_out=None, k_out=None, interleaved: bool = False, axis_pairs=None, amplitude: float = 1.0,
+         inverse: bool = False, stream=None):
+    """waveal_rope.  q (and k): [heads, tokens, head_dim] cuda tensors, head_dim contiguous, any other strides (a
+    [tokens, heads, head_dim] tensor is passed as x.transpose(0, 1)); positions: int32 [axes, tokens] ([tokens] for one axis);
+    freqs: from rope_freqs.  Returns (q_out, k_out): new tensors unless given (q_out=q turns in place).  inverse=True is the
+    gradient: pass those of the outputs, get those of the inputs."""
+    import torch
+    rot = _rotation(_freqs(freqs), interleaved, axis_pairs, amplitude, inverse)
+    d = RopeDesc()
+    d.q_heads, d.tokens, d.head_dim = q.shape
+    d.dtype = _dtype(q)
+    d.rot = rot
+    positions = _positions(positions, rot.axes, d.tokens)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    d.q_stride, d.q_out_stride = _rows("q", q), _rows("q_out", q_out)
+    if q_out.shape != q.shape or q_out.dtype != q.dtype:
+        raise ValueError("q_out must have q's shape and type")
+    if k is not None:
+        if k.shape[1:] != q.shape[1:] or k.dtype != q.dtype:
+            raise ValueError("k must have q's tokens, head_dim and type")
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        if k_out.shape != k.shape or k_out.dtype != k.dtype:
+            raise ValueError("k_out must have k's shape and type")
+        d.k_heads = k.shape[0]
+        d.k_stride, d.k_out_stride = _rows("k", k), _rows("k_out", k_out)
+    _check(load().waveal_rope(ctypes.byref(d), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), _ptr(positions), _ptr(freqs), _stream(stream)))
+    return q_out, k_out
+
+
+class PagedCache:
+    """A paged cache of the caller's tensors: k, v [n_pages, kv_heads, page_size, head_dim], bf16 or fp16, head_dim
+    contiguous, any other strides ([n_pages, page_size, kv_heads, head_dim] tensors are passed as x.transpose(1, 2))."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not (k.is_cuda and v.is_cuda):
+            raise ValueError("k and v must be cuda tensors [n_pages, kv_heads, page_size, head_dim] of one shape and type")
+        if k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("head_dim must be contiguous")
+        self.k, self.v = k, v
+        n, h, page, dim = k.shape
+        self.desc = CacheDesc(n, page, h, dim, _dtype(k), k.stride()[:3], v.stride()[:3])
+
+
+def _batch(q_heads, tokens, seq_start, kv_len, page_table, prefix_len, flags=0) -> BatchDesc:
+    batch = kv_len.shape[0]
+    _int32(kv_len, "kv_len"), _int32(seq_start, "seq_start")
+    if seq_start.shape != (batch + 1,) or kv_len.dim() != 1 or not (seq_start.is_contiguous() and kv_len.is_contiguous()):
+        raise ValueError("seq_start must be a contiguous [batch + 1], kv_len a contiguous [batch]")
+    if page_table is None:
+        return BatchDesc(batch, tokens, q_heads, 0, prefix_len, flags, 0)
+    _int32(page_table, "page_table")
+    if page_table.dim() != 2 or page_table.shape[0] != batch or page_table.stride(1) != 1 and page_table.shape[1] > 1:
+        raise ValueError("page_table must be [batch, pages], a row's pages contiguous")
+    return BatchDesc(batch, tokens, q_heads, page_table.shape[1], prefix_len, flags, max(page_table.stride(0), page_table.shape[1]) if batch < 2
+                     else page_table.stride(0))
+
+
+def cache_append(cache: PagedCache, k, v, seq_start, kv_len, page_table, positions=None, freqs=None, q=None, q_out=None,
+                 prefix_len: int = 0, interleaved: bool = False, axis_pairs=None, amplitude: float = 1.0, dev_status=None, stream=None):
+    """waveal_cache_append.  k, v: [kv_heads, tokens, head_dim] of the new tokens; kv_len counts them in.  With freqs the keys
+    are rotated on the way (positions None: prefix_len + place among the sequence's own keys), and q [q_heads, tokens, head_dim],
+    where given, into q_out (a new tensor unless given; q_out=q turns in place), which is returned."""
+    import torch
+    d = cache.desc
+    heads, tokens, dim = k.shape
+    if v.shape != k.shape or heads != d.kv_heads or dim != d.head_dim:
+        raise ValueError("k and v must be [kv_heads, tokens, head_dim] of the cache")
+    if k.dtype != cache.k.dtype or v.dtype != cache.k.dtype:
+        raise TypeError("k and v must have the cache's type")
+    strides = AppendStrides()
+    strides.k, strides.v = _rows("k", k), _rows("v", v)
+    rot = None
+    if freqs is not None:
+        rot = _rotation(_freqs(freqs), interleaved, axis_pairs, amplitude)
+        if positions is not None:
+            positions = _positions(positions, rot.axes, tokens)
+    if q is not None:
+        if q.shape[1:] != k.shape[1:] or q.dtype != k.dtype:
+            raise ValueError("q must have k's tokens, head_dim and type")
+        if q_out is None:
+            q_out = torch.empty_like(q)
+        if q_out.shape != q.shape or q_out.dtype != q.dtype:
+            raise ValueError("q_out must have q's shape and type")
+        strides.q, strides.q_out = _rows("q", q), _rows("q_out", q_out)
+    b = _batch(0 if q is None else q.shape[0], tokens, seq_start, kv_len, page_table, prefix_len)
+    _check(load().waveal_cache_append(ctypes.byref(d), ctypes.byref(b), None if rot is None else ctypes.byref(rot), ctypes.byref(strides),
+                                      _ptr(k), _ptr(v), _ptr(q), _ptr(q_out), _ptr(cache.k), _ptr(cache.v), _ptr(seq_start), _ptr(kv_len),
+                                      _ptr(page_table), _ptr(positions), _ptr(freqs), _ptr(dev_status), _stream(stream)))
+    return q_out
+
+
+def prefix_attn_workspace_bytes(cache: PagedCache, batch: BatchDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().waveal_prefix_attn_workspace_bytes(ctypes.byref(cache.desc), ctypes.byref(batch), ctypes.byref(n)))
+    return int(n.value)
+
+
+def prefix_attn(cache: PagedCache, q, seq_start, kv_len, page_table=None, prefix_pages=None, prefix_len: int = 0, o=None, lse=None,
+                return_lse: bool = False, causal: bool = True, scale: float = 0.0, workspace=None, dev_status=None, flags: int = 0, stream=None):
+    """waveal_prefix_attn.  q: [q_heads, tokens, head_dim], the new tokens of all sequences one after another; prefix_pages:
+    int32 pages of the first prefix_len keys, seen by all; page_table int32 [batch, pages] and kv_len: each sequence's
+    own keys, its new ones last.  Returns o (laid out like q unless given), or (o, lse) with return_lse."""
+    import torch
+    lib = load()
+    heads, tokens, dim = q.shape
+    if q.dtype != cache.k.dtype:
+        raise TypeError("q must have the cache's type")
+    b = _batch(heads, tokens, seq_start, kv_len, page_table, prefix_len, (PREFIX_CAUSAL if causal else 0) | flags)
+    if prefix_pages is not None:
+        _int32(prefix_pages, "prefix_pages")
+        if prefix_pages.dim() != 1 or not prefix_pages.is_contiguous() or prefix_pages.shape[0] * cache.desc.page_size < prefix_len:
+            raise ValueError("prefix_pages must be a contiguous list of all of the prefix's pages")
+    if o is None:
+        o = torch.empty_like(q)
+    if o.shape != q.shape or o.dtype != q.dtype:
+        raise ValueError("o must have q's shape and type")
+    if lse is None and return_lse:
+        lse = torch.empty((heads, tokens), dtype=torch.float32, device=q.device)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (heads, tokens) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 [q_heads, tokens]")
+    if workspace is None:
+        workspace = torch.empty((prefix_attn_workspace_bytes(cache, b),), dtype=torch.uint8, device=q.device)
+    qs, os_ = (ctypes.c_int64 * 2)(*_rows("q", q, cache.desc.head_dim)), (ctypes.c_int64 * 2)(*_rows("o", o))
+    _check(lib.waveal_prefix_attn(ctypes.byref(cache.desc), ctypes.byref(b), _ptr(q), qs, _ptr(cache.k), _ptr(cache.v), _ptr(o), os_,
+                                  _ptr(lse), _ptr(seq_start), _ptr(kv_len), _ptr(page_table), _ptr(prefix_pages), ctypes.c_float(scale),
+                                  _ptr(workspace), workspace.numel(), _ptr(dev_status), _stream(stream)))
+    return (o, lse) if return_lse else o

@@ -45,6 +45,24 @@ inline cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, int thre
 }
 #endif
 
+// what append and attention ask of the cache and of the batch
+inline waveal_status check_cache(const waveal_cache_desc* c) {
+  if (c->n_pages <= 0 || c->kv_heads <= 0) return fail(WAVEAL_ERR_INVALID_ARG, "n_pages and kv_heads must be positive");
+  if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
+    return fail(WAVEAL_ERR_UNSUPPORTED, "page_size %d (supported: powers of two, 16 .. 65536)", c->page_size);
+  if (c->kv_heads > (1 << 20)) return fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^20 heads");
+  if (c->dtype != WAVEAL_BF16 && c->dtype != WAVEAL_FP16)
+    return fail(WAVEAL_ERR_UNSUPPORTED, "dtype %d (a cache holds WAVEAL_BF16 or WAVEAL_FP16)", c->dtype);
+  return WAVEAL_OK;
+}
+
+inline waveal_status check_batch(const waveal_batch_desc* b) {
+  if (b->batch < 0 || b->tokens < 0 || b->max_pages < 0 || b->prefix_len < 0)
+    return fail(WAVEAL_ERR_INVALID_ARG, "batch, tokens, max_pages and prefix_len must not be negative");
+  if (b->table_stride < b->max_pages) return fail(WAVEAL_ERR_INVALID_ARG, "table_stride is smaller than max_pages");
+  return WAVEAL_OK;
+}
+
 #define WAVEAL_CUDA_OK(expr)                                                                 \
   do {                                                                                       \
     cudaError_t e__ = (expr);                                                                \
