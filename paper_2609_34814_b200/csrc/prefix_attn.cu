@@ -15,11 +15,11 @@
 // the lengths are.  A unit that a cut goes through leaves a part on either side; k_join_parts adds them up.  The line
 // is worked out from the lengths by every CTA itself at its start (a scan over the batch), so the lengths may live on the device.
 //
-// Inside a CTA (384 threads) there are two slots, each with its own S and O accumulators in tensor memory, its own issuing
-// warp and its own four softmax warps:
+// Inside a CTA (640 threads) there are two slots, each with its own S and O accumulators in tensor memory and its own eight
+// softmax warps:
 //   warp 0   items (pieces of units), Q tiles and K tiles by TMA        warp 3   V tiles by TMA
-//   warp 1, 2  slot 0, 1: S = Q K^T, O += P V (tcgen05, P in tensor memory over the columns of S)
-//   warps 4-7, 8-11  slot 0, 1: online softmax, one thread a row; the epilogue
+//   warp 1   S = Q K^T of both slots in turn     warp 2   O += P V (tcgen05, P in tensor memory over the columns of S)
+//   warps 4-7 and 12-15, 8-11 and 16-19  slot 0, 1: online softmax, two threads a row; the epilogue
 // With more than 128 rows the slots have a row tile each and share every K and V tile; with at most 128 they take the key tiles
 // in turn and join their accumulators in the epilogue (both slots' warps reach the same lanes of tensor memory).  Either
 // way one slot's products run while the other's softmax does.  O is rescaled only when a row's maximum has grown by more than 2^8.
@@ -36,13 +36,15 @@ namespace {
 
 using namespace waveal::sm100;
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;
 constexpr int kVLoadWarp = 3, kSoftmaxWarp0 = 4;
 constexpr int kTile = 128;                           // keys of a tile, rows of a slot
-constexpr int kItems = 4;                            // items in flight between the loader and the others
-constexpr int kItemReaders = 11;                     // V loader, two issuers, eight softmax warps
+constexpr int kItems = 16;                           // items between the loader and the others
+constexpr int kBatch = 8;                            // of them worked out at a time, a lane each
+constexpr int kItemReaders = 19;                     // V loader, two issuers, sixteen softmax warps
 constexpr long long kTimeoutCycles = 4000000000ll;   // ~2 s at boost clock
 constexpr long long kSelfTestCycles = 4000000ll;     // ~2 ms
+constexpr int kMaxColumns = 32;                      // rows of an item that is computed with its keys as rows (below)
 constexpr float kGrowth = 8.0f;                      // log2 of how far a row's maximum may outgrow its reference
 
 // Costs on the line of tiles: a key tile of a unit of up to 128 rows, of up to 256, and the start and end of a unit.
@@ -54,8 +56,11 @@ template <int D> struct Geo {
   static constexpr int SLABS = D / 64;               // 128-byte-swizzled slabs of 64 channels
   static constexpr int SLAB_BYTES = kTile * 128;
   static constexpr int TILE_BYTES = SLABS * SLAB_BYTES;
-  static constexpr int NKS = D == 128 ? 3 : 6, NVS = D == 128 ? 2 : 6;
-  static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NKS * TILE_BYTES, OFF_END = OFF_V + NVS * TILE_BYTES;
+  static constexpr int NKS = D == 128 ? 2 : 4, NVS = NKS;
+  // P of items of few rows: two halves of 64 keys for each slot
+  static constexpr int P_HALF = kMaxColumns * 128, P_SLOT = 2 * P_HALF;
+  static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NKS * TILE_BYTES, OFF_P = OFF_V + NVS * TILE_BYTES;
+  static constexpr int OFF_END = OFF_P + 2 * P_SLOT;
   static constexpr int S_COL = 0, O_COL = 256;       // tensor memory: S 0-127, 128-255, O 256.., 384..
 };
 
@@ -104,8 +109,9 @@ struct PrefixLine {
   __device__ int find(long long x) const {           // the unit that position x of the line lies in
     x += before(whole);
     const long long head = (per_head - 1) * cost + last_cost;
-    const int h = (int)(x / head);
-    return h * per_head + min((int)((x - h * head) / cost), per_head - 1);
+    const int h = x >> 32 ? (int)(x / head) : (int)((unsigned)x / (unsigned)min(head, 0xffffffffll));
+    const long long in = x - h * head;
+    return h * per_head + min(in >> 32 ? (int)(in / cost) : (int)((unsigned)in / (unsigned)min(cost, 0xffffffffll)), per_head - 1);
   }
 };
 
@@ -153,21 +159,33 @@ __device__ inline long long own_head_cost(const Shape& s, const Sequence& q) {
   return c;
 }
 
-// the line cut into pieces
+// the line cut into pieces: piece c begins at floor(c * total / pieces)
 struct Cuts {
-  long long total;
-  int pieces;
-  __device__ Cuts(long long total_, int ctas) : total(total_) {
+  long long each;          // total / pieces
+  int rest, pieces;        // total % pieces
+  __device__ Cuts(long long total, int ctas) {
     pieces = (int)min((long long)ctas, max(1ll, total / kMinPiece));
+    if (total >> 32) {
+      each = total / pieces;
+    } else {
+      each = (unsigned)total / (unsigned)pieces;               // (a 64-bit division takes 1,000 clk)
+    }
+    rest = (int)(total - each * pieces);
   }
-  __device__ long long begin(int c) const { return c * total / pieces; }
-  __device__ int piece(long long x) const { return (int)(((x + 1) * pieces - 1) / total); }
-  // tiles [from, to) of a unit at `at` that begin in piece c
-  __device__ int first_tile(int c, long long at, int tiles, int weight) const {
-    const long long d = begin(c) - at;
-    return d <= 0 ? 0 : (int)min((long long)tiles, (d + weight - 1) / weight);
+  __device__ long long begin(int c) const { return each * c + (unsigned)(rest * c) / (unsigned)pieces; }
+  __device__ int piece(long long x) const {                    // the last one that begins at x or before
+    int c = (int)min((float)x / ((float)each + (float)rest / (float)pieces), (float)(pieces - 1));
+    while (c > 0 && begin(c) > x) --c;
+    while (c + 1 < pieces && begin(c + 1) <= x) ++c;
+    return c;
   }
 };
+// of a unit at `at`: its first tile that begins at x or behind
+__device__ inline int first_tile(long long x, long long at, int tiles, int weight) {
+  const long long d = x - at;
+  return d <= 0 ? 0 : d >= (long long)tiles * weight ? tiles : (int)(weight == kCostWide ? (d + kCostWide - 1) / kCostWide : d);
+}
+static_assert(kCostNarrow == 1, "first_tile");
 
 // Where the parts of a row lie.  Units follow each other on the line in the order of their rows (prefix: head, token, query head
 // of the group; own: sequence, key head, token, query head), and so do pieces: row + piece * (rows of the largest unit) is
@@ -193,7 +211,128 @@ struct Item {
   int sees;                // keys that the first token sees (below 1: none); every token sees one more. kAll: all of them see all
   int direct;              // 1: no other part of these rows exists, o is written at once
   int row;                 // of the parts
+  int columns;             // 0: rows of S are query rows; 16 or 32: they are keys, and its columns the item's up to 32 rows
 };
+
+__device__ inline int columns_of(const Item& im, int group) {
+  const int rows = im.n0 * group;
+  return im.wide || rows > kMaxColumns ? 0 : rows > 16 ? 32 : 16;
+}
+
+// How far a CTA is on its way through its units: whole ones, its piece's prefix units, its piece's own units.
+struct Walk {
+  PrefixLine line;
+  long long w0, w1;        // its piece of the line
+  long long base, at;      // where the sequence, the next unit begin
+  Sequence q;
+  OwnUnit own;             // its first unit
+  int piece, whole, unit;
+  int seq, head, i, units; // head -1: the sequence has not been looked at; units: of a head
+};
+
+// The next items, up to kBatch, a lane each (a whole warp calls it): 3,000 clk of index arithmetic, for one item or for all of them.
+// Returns the lanes that have one; none at the end.
+__device__ __noinline__ unsigned next_units(const Shape& s, Walk& w, Item& im, int lane) {
+  const PrefixLine& line = w.line;
+  for (;;) {
+    bool have = false;
+    __syncwarp();
+    if (w.whole < line.whole || w.unit < line.units) {
+      const bool whole = w.whole < line.whole;
+      const int u = whole ? w.whole + lane * s.ctas : w.unit + lane;
+      int j0 = 0, j1 = line.tiles;
+      const int h = u / line.per_head, i = u - h * line.per_head;
+      bool past = false;                             // behind this CTA's piece
+      if (whole) {
+        have = lane < kBatch && u < line.whole;
+      } else {
+        const long long at = line.at(u);
+        past = u >= line.units || at >= w.w1;
+        j0 = first_tile(w.w0, at, line.tiles, line.weight(i)), j1 = first_tile(w.w1, at, line.tiles, line.weight(i));
+        have = lane < kBatch && !past && j0 < j1;
+      }
+      if (have) {
+        im.tiles = j1 - j0;
+        im.head = h, im.token = i * 2 * s.tq;
+        im.n0 = min(s.tq, s.tokens - im.token), im.n1 = min(s.tq, s.tokens - im.token - im.n0);
+        im.first_key = j0 * kTile, im.keys = min(s.prefix_len, j1 * kTile);
+        im.list = -1, im.sees = kAll;
+        im.direct = 0;
+        im.row = (int)part_row(s, prefix_row(s, h, im.token), whole ? 0 : w.piece);
+      }
+      const bool end = __any_sync(0xffffffffu, past && lane <= kBatch);
+      if (lane == 0) {
+        if (whole) w.whole += kBatch * s.ctas;
+        else w.unit = end ? line.units : w.unit + kBatch;
+      }
+    } else if (w.seq < s.batch) {
+      if (w.head < 0) {
+        if (w.base >= w.w1) return 0;
+        const Sequence q = read_sequence(s, w.seq, nullptr);
+        const int units = ceil_div(q.n, 2 * s.tq);
+        const OwnUnit own = own_unit(s, q, 0);
+        const long long cost = units == 0 ? 0 : units == 1 ? own.cost : own_head_cost(s, q);
+        const long long skip = w.w0 - w.base;
+        const int head = cost && skip > 0 ? (int)min((long long)s.kv_heads, skip / cost) : 0;
+        __syncwarp();
+        if (lane == 0) {
+          w.q = q, w.own = own, w.units = units;
+          w.at = w.base + head * cost;
+          w.base += cost * s.kv_heads;
+          w.head = head, w.i = 0;
+          if (cost == 0) ++w.seq, w.head = -1;
+        }
+        continue;
+      }
+      // a sequence of one unit: its next heads; else the next units of the head
+      const Sequence q = w.q;
+      const bool one = w.units == 1;
+      const int h = one ? w.head + lane : w.head, i = one ? 0 : w.i + lane;
+      OwnUnit u = w.own;
+      if (!one) u = own_unit(s, q, min(i, w.units - 1));
+      const bool real = lane < kBatch && (one ? h < s.kv_heads : i < w.units);
+      long long to = real ? u.cost : 0;
+#pragma unroll
+      for (int d = 1; d < kBatch; d *= 2) {
+        const long long x = __shfl_up_sync(0xffffffffu, to, d);
+        if (lane >= d) to += x;
+      }
+      const long long at = w.at + to - (real ? u.cost : 0), last = w.at + __shfl_sync(0xffffffffu, to, kBatch - 1);
+      const int j0 = first_tile(w.w0, at, u.tiles, u.weight), j1 = first_tile(w.w1, at, u.tiles, u.weight);
+      have = real && at < w.w1 && j0 < j1;
+      if (have) {
+        im.tiles = j1 - j0;
+        im.head = h, im.token = q.start + u.first;
+        im.n0 = u.n0, im.n1 = u.n1;
+        im.first_key = j0 * kTile, im.keys = min(u.keys, j1 * kTile);
+        im.list = w.seq;
+        im.sees = s.causal ? q.len - q.n + u.first + 1 : kAll;
+        im.direct = line.tiles == 0 && j0 == 0 && j1 == u.tiles;
+        im.row = (int)part_row(s, own_row(s, q, h, u.first), w.piece);
+      }
+      __syncwarp();
+      if (lane == 0) {
+        w.at = last;
+        if (one) {
+          w.head += kBatch;
+        } else if ((w.i += kBatch) >= w.units) {
+          w.i = 0, ++w.head;
+        }
+        if (last >= w.w1) w.seq = s.batch;
+        else if (w.head >= s.kv_heads) ++w.seq, w.head = -1;
+      }
+    } else {
+      return 0;
+    }
+    if (have) {
+      im.wide = im.n1 > 0;
+      im.columns = columns_of(im, s.group);
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, have);
+    __syncwarp();
+    if (who) return who;
+  }
+}
 
 struct Params {
   Shape s;
@@ -249,7 +388,19 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm,
       : "memory");
 }
 
-// D[tmem] (+)= A[smem] * B[smem]; both operands of the tensors' type
+// D[tmem] (+)= A[smem] * B[smem], both of the tensors' type: four products along K, 32 bytes of A and B further each, by one elected lane
+__device__ __forceinline__ void umma4_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .b32 rx;\n\t.reg .pred e, p, t;\n\t.reg .b64 a, b;\n\t"
+      "elect.sync rx|e, 0xFFFFFFFF;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, %3, %3;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
 __device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   if (elect_one())
     asm volatile(
@@ -258,6 +409,18 @@ __device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a_desc, uint64
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
+}
+// four products with A in tensor memory, 8 columns further each, and B 16 keys further each
+__device__ __forceinline__ void umma4_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .b32 rx, a;\n\t.reg .pred e, p, t;\n\t.reg .b64 b;\n\t"
+      "elect.sync rx|e, 0xFFFFFFFF;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, %3, %3;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "add.u32 a, %1, 8;\n\tadd.s64 b, %2, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.u32 a, %1, 16;\n\tadd.s64 b, %2, 256;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.u32 a, %1, 24;\n\tadd.s64 b, %2, 384;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
 }
 
 template <class T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -269,21 +432,44 @@ template <class T> __device__ __forceinline__ uint32_t pack2(float lo, float hi)
   return r;
 }
 
+constexpr int kStages = 4;                            // of a ring, at most
 enum {
   B_ITEM_FULL = 0, B_ITEM_EMPTY = B_ITEM_FULL + kItems, B_Q_FULL = B_ITEM_EMPTY + kItems, B_Q_EMPTY = B_Q_FULL + 2,
-  B_K_FULL = B_Q_EMPTY + 2, B_K_EMPTY = B_K_FULL + 6, B_V_FULL = B_K_EMPTY + 6, B_V_EMPTY = B_V_FULL + 6,
-  B_S_FULL = B_V_EMPTY + 6, B_P_FULL = B_S_FULL + 2, B_PV_DONE = B_P_FULL + 4, B_O_EMPTY = B_PV_DONE + 2, B_SUMS = B_O_EMPTY + 2,
-  B_FINAL = B_SUMS + 2, B_COUNT = B_FINAL + 2
+  B_K_FULL = B_Q_EMPTY + 2, B_K_EMPTY = B_K_FULL + kStages, B_V_FULL = B_K_EMPTY + kStages, B_V_EMPTY = B_V_FULL + kStages,
+  B_S_FULL = B_V_EMPTY + kStages, B_P_FULL = B_S_FULL + 4, B_PV_DONE = B_P_FULL + 4, B_O_EMPTY = B_PV_DONE + 4, B_SUMS = B_O_EMPTY + 2,
+  B_SUMS_READ, B_VOTE, B_PAIR = B_VOTE + 4, B_REF = B_PAIR + 8, B_FINAL = B_REF + 8, B_COUNT = B_FINAL + 2
 };
 
 // what lies behind the tiles in shared memory
+// 8 consecutive columns of this thread's lane of tensor memory
+#define WAVEAL_TMEM_LD8(taddr, v)                                                                                      \
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"                         \
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])        \
+               : "r"(taddr) : "memory")
+#define WAVEAL_TMEM_WAIT_LD8(v)                                                                                        \
+  asm volatile("tcgen05.wait::ld.sync.aligned;"                                                                        \
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7])::"memory")
+#define WAVEAL_TMEM_ST8(taddr, v)                                                                                      \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"                         \
+               ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory")
+__device__ __forceinline__ void st_shared_u16(uint32_t addr, uint32_t x) {
+  asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"((unsigned short)x) : "memory");
+}
+
 struct Small {
   unsigned long long bar[B_COUNT];
   Item items[kItems];
-  float2 sums[2][kTile];   // slot 1's references and sums of an item whose key tiles the slots share out (two: slot 1 may be an item ahead)
+  float ref[2][kTile];                               // [slot][row]: the reference, from one half tile's owner to the next one's
+  float pair[2][2][kTile];                           // [slot][owner][row]: sums
+  float warp_max[2][2][4][kMaxColumns / 2];          // few rows: [slot][half of the rows][warp]: maxima, at the end slot 0's sums
+  union {                                            // what slot 1 leaves of an item whose key tiles the slots share out
+    float2 sums[kTile];                              // a row's reference and sum
+    struct { float sum[4][kMaxColumns], ref[kMaxColumns]; } cols;
+  };
+  int vote[2][2][2];
   long long warp_sum[kThreads / 32];
-  long long own_total, start_base;
-  int start_seq;
+  alignas(16) unsigned char walk_space[sizeof(Walk)];
+  __device__ Walk& walk() { return *reinterpret_cast<Walk*>(walk_space); }
   uint32_t tmem;
   int abort;
 };
@@ -296,20 +482,23 @@ struct TileLoader {
   uint32_t it = 0, armed = 0, parity = 0;
   int page = 0;
 
+  // boxes of a tile: log2 of the box's rows, how many, and which one (and which slab of it) is this lane's
+  __device__ static int box_shift(const Params& p) { return min(p.s.page_shift, 7); }
+  __device__ static int boxes(const Params& p, const Item& im, int key) {
+    return (min(kTile, im.keys - key) + (1 << box_shift(p)) - 1) >> box_shift(p);
+  }
   __device__ int read_page(const Params& p, const Item& im, int key, int lane) const {
-    const int shift = p.s.page_shift, box = min(1 << shift, kTile);
-    const int nb = ceil_div(min(kTile, im.keys - key), box);
-    const int k = key + (lane % max(nb, 1)) * box;
-    if (lane >= nb * G::SLABS || key >= im.keys) return 0;
+    if (key >= im.keys) return 0;
+    const int nb = boxes(p, im, key), i = lane < nb ? lane : lane - nb;
+    if (lane >= nb * G::SLABS) return 0;
     const int* list = im.list < 0 ? p.prefix_pages : p.page_table + im.list * p.s.table_stride;
-    return __ldg(list + (k >> shift));
+    return __ldg(list + ((key + (i << box_shift(p))) >> p.s.page_shift));
   }
   template <int STAGES>
   __device__ bool load(const Ctx& c, const Params& p, const Item& im, int key, bool last, bool drop, int lane, uint32_t smem,
                        uint32_t full, uint32_t empty, const CUtensorMap* tm, int site) {
     const uint32_t st = it % STAGES, ph = it / STAGES & 1;
-    const int shift = p.s.page_shift, box = min(1 << shift, kTile);
-    const int nb = ceil_div(min(kTile, im.keys - key), box);
+    const int shift = p.s.page_shift, box = 1 << box_shift(p), nb = boxes(p, im, key);
     int pg = page;
     if (!last) page = read_page(p, im, key + kTile, lane);
     if (it >= STAGES && !warp_wait(c, empty + 8 * st, ph ^ 1, site)) return false;
@@ -320,7 +509,7 @@ struct TileLoader {
     parity = (parity & ~(1u << st)) | ph << st;
     __syncwarp();
     if (lane < nb * G::SLABS) {
-      const int slab = lane / nb, i = lane - slab * nb;
+      const int slab = lane >= nb, i = lane - slab * nb;
       if (pg < 0 || pg >= p.s.n_pages) {
         report(p.dev_status, WAVEAL_ERR_BAD_MASK, 52, im.list, pg);
         pg = p.s.n_pages;                            // beyond the cache: the copy engine fills in zeros
@@ -333,7 +522,7 @@ struct TileLoader {
   }
   // (after a wait gave up) leaves no copy in flight
   __device__ void drain(const Params& p, uint32_t full) const {
-    for (int st = 0; st < 6; ++st)
+    for (int st = 0; st < kStages; ++st)
       if (armed >> st & 1) {
         const long long t0 = clock64();
         while (!mbar_try_wait(full + 8 * st, parity >> st & 1) && clock64() - t0 < p.wait_limit / 4) {}
@@ -358,20 +547,14 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (warp == 1) {
     tmem_alloc(smem_u32(&sm.tmem), 512);
     tmem_relinquish();
-  } else if (warp == 2 && lane == 0) {
-    for (int i = 0; i < kItems; ++i) mbar_init(BAR(B_ITEM_FULL + i), 1), mbar_init(BAR(B_ITEM_EMPTY + i), kItemReaders);
-    for (int i = 0; i < 6; ++i) {
-      mbar_init(BAR(B_K_FULL + i), 1), mbar_init(BAR(B_K_EMPTY + i), 2);
-      mbar_init(BAR(B_V_FULL + i), 1), mbar_init(BAR(B_V_EMPTY + i), 2);
+  } else if (warp == 2) {
+    for (int i = lane; i < B_COUNT; i += 32) {
+      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps4 = (i >= B_P_FULL && i < B_P_FULL + 4) || (i >= B_VOTE && i < B_VOTE + 4);
+      const bool warps8 = (i >= B_O_EMPTY && i < B_O_EMPTY + 2) || i == B_SUMS || i == B_SUMS_READ, warps2 = i >= B_PAIR && i < B_PAIR + 8;
+      mbar_init(BAR(i), item ? kItemReaders : warps4 ? 4 : warps8 ? 8 : warps2 ? 2 : 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(BAR(B_Q_FULL + i), 1), mbar_init(BAR(B_Q_EMPTY + i), 2);
-      mbar_init(BAR(B_S_FULL + i), 1), mbar_init(BAR(B_P_FULL + 2 * i), 4), mbar_init(BAR(B_P_FULL + 2 * i + 1), 4);
-      mbar_init(BAR(B_PV_DONE + i), 1), mbar_init(BAR(B_O_EMPTY + i), 4), mbar_init(BAR(B_FINAL + i), 1);
-      mbar_init(BAR(B_SUMS + i), 4);
-    }
-    sm.abort = 0;
-    sm.start_seq = s.batch;
+    if (lane < 8) (&sm.vote[0][0][0])[lane] = 0;
+    if (lane == 0) sm.abort = 0, sm.walk().seq = s.batch;
     fence_mbar_init();
   } else if (warp == 3 && lane == 0) {
     prefetch_tmap(&tmQ), prefetch_tmap(&tmQ1), prefetch_tmap(&tmK), prefetch_tmap(&tmV);
@@ -395,15 +578,17 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   }
   if (lane == 31) sm.warp_sum[warp] = upto;
   __syncthreads();
-  long long own_total = 0;
+  long long sums = lane < kThreads / 32 ? sm.warp_sum[lane] : 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) upto += sm.warp_sum[w];
-    own_total += sm.warp_sum[w];
+  for (int d = 1; d < 32; d *= 2) {
+    const long long x = __shfl_up_sync(0xffffffffu, sums, d);
+    if (lane >= d) sums += x;
   }
+  const long long own_total = __shfl_sync(0xffffffffu, sums, 31), before = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
+  if (warp) upto += before;
   const Cuts cuts(max(line.total() + own_total, 1ll), s.ctas);
   const int piece = blockIdx.x;
-  const bool has_piece = piece < cuts.pieces && line.total() + own_total > 0;
+  const bool has_piece = piece < cuts.pieces;
   const long long w0 = has_piece ? cuts.begin(piece) : 0, w1 = has_piece ? cuts.begin(piece + 1) : 0;
   {
     const long long from = max(w0 - line.total(), 0ll);
@@ -411,11 +596,18 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     if (blockIdx.x == 0 || (base <= from && from < upto))
       for (int b = b0; b < b1; ++b) {
         const long long c = own_head_cost(s, read_sequence(s, b, nullptr)) * s.kv_heads;
-        if (base <= from && from < base + c) sm.start_seq = b, sm.start_base = base;
+        if (has_piece && base <= from && from < base + c) sm.walk().seq = b, sm.walk().base = line.total() + base;
         if (blockIdx.x == 0) p.parts.own_base[b] = base;
         base += c;
       }
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.parts.total = own_total;
+    if (threadIdx.x == 0) {
+      Walk& w = sm.walk();
+      w.w0 = w0, w.w1 = w1;
+      w.piece = piece, w.whole = blockIdx.x, w.unit = has_piece && w0 < line.total() ? line.find(w0) : line.units;
+      w.head = -1;
+      w.line = line;
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -426,14 +618,17 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
   // the next item, for everyone but the loader: false when there is none or a wait gave up
   uint32_t item_no = 0;
-  auto next_item = [&](Item& im) {
+  // (it stays in shared memory: the softmax warps have no registers to spare for it)
+  auto next_item = [&](const Item*& im) {
     const uint32_t slot = item_no % kItems;
     if (!warp_wait(ctx, BAR(B_ITEM_FULL + slot), item_no / kItems & 1, 60)) return ok = false;
-    im = sm.items[slot];
+    im = &sm.items[slot];
+    return im->tiles > 0;
+  };
+  auto item_done = [&] {
     __syncwarp();
-    if (lane == 0) mbar_arrive(BAR(B_ITEM_EMPTY + slot));
+    if (lane == 0) mbar_arrive(BAR(B_ITEM_EMPTY + item_no % kItems));
     ++item_no;
-    return im.tiles > 0;
   };
 
   if (warp == 0) {
@@ -454,87 +649,31 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       __syncwarp();
       return true;
     };
-    auto publish = [&](const Item& im) {
-      const uint32_t slot = item_no % kItems;
-      if (item_no >= kItems && !warp_wait(ctx, BAR(B_ITEM_EMPTY + slot), (item_no / kItems & 1) ^ 1, 62)) return false;
-      if (lane == 0) {
-        sm.items[slot] = im;
+    for (bool more = true; ok && more;) {
+      Item next;
+      const unsigned who = next_units(s, sm.walk(), next, lane);
+      const int count = max(__popc(who), 1), nth = __popc(who & ((1u << lane) - 1));   // (at the end: one item without tiles)
+      more = who != 0;
+      const uint32_t first = item_no;
+      for (int i = 0; ok && i < count; ++i, ++item_no)
+        if (item_no >= kItems) ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + item_no % kItems), (item_no / kItems & 1) ^ 1, 62);
+      if (!ok) break;
+      if (more ? who >> lane & 1 : lane == 0) {
+        const uint32_t slot = (first + nth) % kItems;
+        if (!more) next.tiles = 0;
+        sm.items[slot] = next;
         mbar_arrive(BAR(B_ITEM_FULL + slot));
       }
       __syncwarp();
-      ++item_no;
-      return true;
-    };
-    auto emit = [&](Item im) {
-      loader.page = loader.read_page(p, im, im.first_key, lane);
-      if (!publish(im)) return false;
-      if (!load_q(im.n0 == 1 ? &tmQ1 : &tmQ, im.token, im.head * s.group, im.n0 == 1 ? 1 : s.tq)) return false;
-      if (im.wide && !load_q(im.n1 == 1 ? &tmQ1 : &tmQ, im.token + s.tq, im.head * s.group, im.n1 == 1 ? 1 : s.tq)) return false;
-      for (int j = 0; j < im.tiles; ++j)
-        if (!loader.template load<G::NKS>(ctx, p, im, im.first_key + j * kTile, j == im.tiles - 1, p.drop_tile && blockIdx.x == 0 && loader.it == 0,
-                                          lane, sbase + G::OFF_K, BAR(B_K_FULL), BAR(B_K_EMPTY), &tmK, 63))
-          return false;
-      return true;
-    };
-    auto prefix_item = [&](int u, int j0, int j1, int at_piece) {
-      const int h = u / line.per_head, i = u - h * line.per_head;
-      Item im;
-      im.tiles = j1 - j0;
-      im.head = h, im.token = i * 2 * s.tq;
-      im.n0 = min(s.tq, s.tokens - im.token), im.n1 = min(s.tq, s.tokens - im.token - im.n0);
-      im.wide = im.n1 > 0;
-      im.first_key = j0 * kTile, im.keys = min(s.prefix_len, j1 * kTile);
-      im.list = -1, im.sees = kAll;
-      im.direct = 0;
-      im.row = (int)part_row(s, prefix_row(s, h, im.token), at_piece);
-      return emit(im);
-    };
-    // whole units
-    for (int u = blockIdx.x; ok && u < line.whole; u += s.ctas) ok = prefix_item(u, 0, line.tiles, 0);
-    // this CTA's piece of the line: prefix units ...
-    if (ok && has_piece && w0 < line.total()) {
-      for (int u = line.find(w0); ok && u < line.units; ++u) {
-        const long long at = line.at(u);
-        if (at >= w1) break;
-        const int wt = line.weight(u % line.per_head);
-        const int j0 = cuts.first_tile(piece, at, line.tiles, wt), j1 = cuts.first_tile(piece + 1, at, line.tiles, wt);
-        if (j0 < j1) ok = prefix_item(u, j0, j1, piece);
+      for (int i = 0; ok && more && i < count; ++i) {
+        const Item im = sm.items[(first + i) % kItems];
+        loader.page = loader.read_page(p, im, im.first_key, lane);
+        if (!(ok = load_q(im.n0 == 1 ? &tmQ1 : &tmQ, im.token, im.head * s.group, im.n0 == 1 ? 1 : s.tq))) break;
+        if (im.wide && !(ok = load_q(im.n1 == 1 ? &tmQ1 : &tmQ, im.token + s.tq, im.head * s.group, im.n1 == 1 ? 1 : s.tq))) break;
+        for (int j = 0; ok && j < im.tiles; ++j)
+          ok = loader.template load<G::NKS>(ctx, p, im, im.first_key + j * kTile, j == im.tiles - 1, p.drop_tile && blockIdx.x == 0 && loader.it == 0,
+                                            lane, sbase + G::OFF_K, BAR(B_K_FULL), BAR(B_K_EMPTY), &tmK, 63);
       }
-    }
-    // ... and own units
-    long long base = sm.start_base;
-    for (int b = sm.start_seq; ok && has_piece && b < s.batch; ++b) {
-      if (line.total() + base >= w1) break;
-      const Sequence q = read_sequence(s, b, nullptr);
-      const long long head_cost = own_head_cost(s, q);
-      const int m = ceil_div(q.n, 2 * s.tq);
-      const long long skip = w0 - line.total() - base;
-      int h = head_cost && skip > 0 ? (int)min((long long)s.kv_heads, skip / head_cost) : 0;
-      for (; ok && head_cost && h < s.kv_heads; ++h) {
-        long long at = line.total() + base + h * head_cost;
-        if (at >= w1) break;
-        for (int i = 0; ok && i < m && at < w1; ++i) {
-          const OwnUnit u = own_unit(s, q, i);
-          const int j0 = cuts.first_tile(piece, at, u.tiles, u.weight), j1 = cuts.first_tile(piece + 1, at, u.tiles, u.weight);
-          at += u.cost;
-          if (j0 >= j1) continue;
-          Item im;
-          im.tiles = j1 - j0;
-          im.head = h, im.token = q.start + u.first;
-          im.n0 = u.n0, im.n1 = u.n1, im.wide = u.n1 > 0;
-          im.first_key = j0 * kTile, im.keys = min(u.keys, j1 * kTile);
-          im.list = b;
-          im.sees = s.causal ? q.len - q.n + u.first + 1 : kAll;
-          im.direct = line.tiles == 0 && j0 == 0 && j1 == u.tiles;
-          im.row = (int)part_row(s, own_row(s, q, h, u.first), piece);
-          ok = emit(im);
-        }
-      }
-      base += head_cost * s.kv_heads;
-    }
-    if (ok) {
-      Item im = {};
-      publish(im);
     }
     if (*ctx.abort_smem) {
       loader.drain(p, BAR(B_K_FULL));
@@ -547,8 +686,10 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   } else if (warp == kVLoadWarp) {
     // ================================================================ V
     TileLoader<D> loader;
-    Item im;
-    while (ok && next_item(im)) {
+    const Item* item;
+    while (ok && next_item(item)) {
+      const Item im = *item;
+      item_done();
       loader.page = loader.read_page(p, im, im.first_key, lane);
       for (int j = 0; ok && j < im.tiles; ++j)
         ok = loader.template load<G::NVS>(ctx, p, im, im.first_key + j * kTile, j == im.tiles - 1, false, lane, sbase + G::OFF_V, BAR(B_V_FULL),
@@ -556,274 +697,597 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     }
     if (*ctx.abort_smem) loader.drain(p, BAR(B_V_FULL));
   } else if (warp < kVLoadWarp) {
-    // ================================================================ products of a slot
-    // Each slot has an issuing warp: what one waits for (its softmax, its last product) never holds up the other.  S and P share
-    // columns, so a slot's next S = Q K^T waits for the end of its last P V.
-    constexpr uint32_t kType = std::is_same_v<T, __half> ? 0u : (1u << 7) | (1u << 10);
-    constexpr uint32_t IDESC_QK = (make_idesc(128, kTile, false) & ~((1u << 7) | (1u << 10))) | kType;
-    constexpr uint32_t IDESC_PV = (make_idesc(128, D, true) & ~((1u << 7) | (1u << 10))) | kType;
-    const int slot = warp - 1;
-    const uint32_t d_s = tmem + G::S_COL + slot * kTile, d_o = tmem + G::O_COL + slot * kTile;
-    const uint64_t q_desc0 = make_desc(sbase + G::OFF_Q, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_K, 16, 1024);
-    const uint64_t v_desc0 = make_desc(sbase + G::OFF_V, G::SLAB_BYTES, 1024);
-    // A barrier of the rings is told from the one before last only by a parity, so every issuer waits for every Q, K and V tile in
-    // turn, its own or not, and each is given back by both (its own when the products on it have ended).
-    uint32_t g0 = 0, q_it = 0, done = 0, uses = 0;   // tiles of the CTA so far; Q tiles; tiles and items of this slot
-    auto pass_on = [&](uint32_t full, uint32_t empty, uint32_t parity, int site) {
-      if (!warp_wait(ctx, full, parity, site)) return false;
-      if (lane == 0) mbar_arrive(empty);
-      __syncwarp();
-      return true;
-    };
-    Item im;
-    while (ok && next_item(im)) {
-      const int wide = __shfl_sync(0xffffffffu, im.wide, 0), tiles = __shfl_sync(0xffffffffu, im.tiles, 0);
-      const int keys = __shfl_sync(0xffffffffu, im.keys - im.first_key, 0);
-      const int from = wide ? 0 : slot;
-      const int last = wide ? tiles - 1 : (tiles - 1 - slot) / 2 * 2 + slot;
-      uint32_t qb = 0;
-      for (int i = 0; ok && i <= wide; ++i, ++q_it) {
-        const uint32_t b = q_it & 1, ph = q_it >> 1 & 1;
-        if (from < tiles && (!wide || i == slot)) {
-          qb = b;
-          ok = warp_wait(ctx, BAR(B_Q_FULL + b), ph, 65);
-        } else {
-          ok = pass_on(BAR(B_Q_FULL + b), BAR(B_Q_EMPTY + b), ph, 65);
+    // ================================================================ products
+    // Two warps issue, one S = Q K^T, the other O += P V: what they do around the products (waits, ring positions,
+    // descriptors) takes as long as the products when one warp has it all (2,690 clk a row tile and key tile; the softmax warps leave
+    // them few issue slots).  S comes in half tiles of 64 keys, two buffers a slot: one is in its products while the other is in its
+    // softmax.  (A product of 64 columns takes 47 clk, not 32: its operands come out of shared memory at that pace.  Whole tiles, one
+    // buffer a slot: products and softmax of a slot take turns, 5,210 clk for two row tiles and a key tile.)  S and P of a half tile share columns, so
+    // a buffer's next S waits for the end of its last P V.
+    // (operands of the products come from shuffles, so that the compiler knows them to be the same in all lanes: otherwise
+    // each one is brought from vector registers and the products are issued at half the rate)
+    constexpr uint32_t kTypeBits = (1u << 7) | (1u << 10), kType = std::is_same_v<T, __half> ? 0u : kTypeBits;
+    constexpr auto typed = [](uint32_t idesc) constexpr { return (idesc & ~kTypeBits) | kType; };
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const Item* im;
+    if (warp == 1) {
+      const uint64_t q_desc0 = make_desc(sbase + G::OFF_Q, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_K, 16, 1024);
+      uint32_t k_st = 0, k_ph = 0, qb = 0, q_ph = 0, used = 0, free_ph = 0;
+      // buffer b's last product has ended
+      auto buffer_free = [&](int b) {
+        if ((used >> b & 1) && !(ok = warp_wait(ctx, BAR(B_PV_DONE + b), (free_ph >> b & 1) ^ 1, 67))) return false;
+        used |= 1u << b;
+        free_ph ^= 1u << b;
+        return true;
+      };
+      while (ok && next_item(im)) {
+        const int wide = __shfl_sync(0xffffffffu, im->wide, 0), tiles = __shfl_sync(0xffffffffu, im->tiles, 0);
+        const int keys = __shfl_sync(0xffffffffu, im->keys - im->first_key, 0), columns = __shfl_sync(0xffffffffu, im->columns, 0);
+        item_done();
+        const uint32_t qb0 = qb;
+        if (!(ok = warp_wait(ctx, BAR(B_Q_FULL + qb), q_ph, 65))) break;
+        q_ph ^= qb, qb ^= 1;
+        if (wide) {
+          if (!(ok = warp_wait(ctx, BAR(B_Q_FULL + qb), q_ph, 65))) break;
+          q_ph ^= qb, qb ^= 1;
         }
-      }
-      for (int j = 0; ok && j < tiles; ++j) {
-        const uint32_t g = g0 + j, ks = g % G::NKS, vs = g % G::NVS;
-        if (!wide && (j & 1) != slot) {
-          ok = pass_on(BAR(B_K_FULL + ks), BAR(B_K_EMPTY + ks), g / G::NKS & 1, 66) &&
-               pass_on(BAR(B_V_FULL + vs), BAR(B_V_EMPTY + vs), g / G::NVS & 1, 68);
-          continue;
-        }
-        if (!(ok = warp_wait(ctx, BAR(B_K_FULL + ks), g / G::NKS & 1, 66))) break;
-        if (done && !(ok = warp_wait(ctx, BAR(B_PV_DONE + slot), (done - 1) & 1, 67))) break;
-        tc_fence_after();
-        {
-          const uint64_t qd = q_desc0 + (uint64_t)(qb * (G::TILE_BYTES >> 4)), kd = k_desc0 + (uint64_t)(ks * (G::TILE_BYTES >> 4));
-#pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            const uint64_t at = (uint64_t)((c / 4 * G::SLAB_BYTES + c % 4 * 32) >> 4);
-            umma_ss(d_s, qd + at, kd + at, IDESC_QK, c > 0);
-          }
-          tc_commit(BAR(B_K_EMPTY + ks));
-          tc_commit(BAR(B_S_FULL + slot));
-          if (j == last) tc_commit(BAR(B_Q_EMPTY + qb));
-        }
-        if (!(ok = warp_wait(ctx, BAR(B_V_FULL + vs), g / G::NVS & 1, 68))) break;
-        const int valid = min(kTile, keys - j * kTile), steps = (valid + 15) / 16;
-        if (valid < steps * 16) {
-          // the last keys of a list: what lies behind them in the page (or was never loaded) must not meet the zeros of P
-          const int chunks = (steps * 16 - valid) * 8;
-#pragma unroll
-          for (int slab = 0; slab < G::SLABS; ++slab)
-            for (int i = lane; i < chunks; i += 32)
-              st_shared_v4(sbase + G::OFF_V + vs * G::TILE_BYTES + slab * G::SLAB_BYTES + valid * 128 + i * 16, 0, 0, 0, 0);
-          fence_proxy_async();
-          __syncwarp();
-        }
-        if (j == from && uses && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + slot), (uses - 1) & 1, 69))) break;
-        const uint64_t vd = v_desc0 + (uint64_t)(vs * (G::TILE_BYTES >> 4));
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (!(ok = warp_wait(ctx, BAR(B_P_FULL + 2 * slot + half), done & 1, 70))) break;
+        const uint64_t qd = q_desc0 + (uint64_t)(qb0 * (G::TILE_BYTES >> 4)), qd1 = q_desc0 + (uint64_t)((qb0 ^ 1) * (G::TILE_BYTES >> 4));
+        auto half_tile = [&](auto b_, uint64_t q, uint64_t kd) {
+          constexpr int b = decltype(b_)::value;
+          if (!buffer_free(b)) return;
           tc_fence_after();
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int k = half * 4 + c;
-            if (k < steps) umma_bf16_ts(d_o, d_s + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), IDESC_PV, (j != from || k > 0) ? 1u : 0u);
+          for (int slab = 0; slab < G::SLABS; ++slab)
+            umma4_ss(tm + G::S_COL + b * 64, q + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)((slab * G::SLAB_BYTES + b % 2 * 64 * 128) >> 4),
+                     typed(make_idesc(128, 64, false)), slab > 0);
+          tc_commit(BAR(B_S_FULL + b));
+        };
+        using std::integral_constant;
+        for (int j = 0; ok && j < tiles; ++j) {
+          if (!(ok = warp_wait(ctx, BAR(B_K_FULL) + 8 * k_st, k_ph, 66))) break;
+          const uint64_t kd = k_desc0 + (uint64_t)(k_st * (G::TILE_BYTES >> 4));
+          const bool two = keys - j * kTile > 64;
+          if (columns) {
+            const int slot = j & 1;
+            if (!buffer_free(2 * slot) || !buffer_free(2 * slot + 1)) break;
+            tc_fence_after();
+            const uint32_t idesc = columns == 16 ? typed(make_idesc(128, 16, false)) : typed(make_idesc(128, 32, false));
+#pragma unroll
+            for (int slab = 0; slab < G::SLABS; ++slab)
+              umma4_ss(tm + G::S_COL + slot * kTile, kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), qd + (uint64_t)(slab * G::SLAB_BYTES >> 4), idesc, slab > 0);
+            tc_commit(BAR(B_S_FULL + 2 * slot));
+            tc_commit(BAR(B_S_FULL + 2 * slot + 1));
+          } else if (wide) {
+            half_tile(integral_constant<int, 0>{}, qd, kd);
+            if (ok) half_tile(integral_constant<int, 2>{}, qd1, kd);
+            if (ok && two) half_tile(integral_constant<int, 1>{}, qd, kd);
+            if (ok && two) half_tile(integral_constant<int, 3>{}, qd1, kd);
+          } else if (j & 1) {
+            half_tile(integral_constant<int, 2>{}, qd, kd);
+            if (ok && two) half_tile(integral_constant<int, 3>{}, qd, kd);
+          } else {
+            half_tile(integral_constant<int, 0>{}, qd, kd);
+            if (ok && two) half_tile(integral_constant<int, 1>{}, qd, kd);
           }
+          if (!ok) break;
+          tc_commit(BAR(B_K_EMPTY) + 8 * k_st);
+          if (++k_st == (uint32_t)G::NKS) k_st = 0, k_ph ^= 1;
         }
-        if (!ok) break;
-        tc_commit(BAR(B_V_EMPTY + vs));
-        tc_commit(BAR(B_PV_DONE + slot));
-        ++done;
+        tc_commit(BAR(B_Q_EMPTY + qb0));
+        if (wide) tc_commit(BAR(B_Q_EMPTY + (qb0 ^ 1)));
       }
-      g0 += tiles;
-      if (from < tiles) ++uses;
+    } else {
+      const uint64_t v_desc0 = make_desc(sbase + G::OFF_V, G::SLAB_BYTES, 1024);
+      // V^T as the first operand (head_dim 64: its rows twice, for a product of 128 rows)
+      const uint64_t vt_desc0 = make_desc(sbase + G::OFF_V, D == 128 ? G::SLAB_BYTES : 0, 1024);
+      uint32_t v_st = 0, v_ph = 0, used = 0, o_ph = 0, p_ph = 0;
+      // the accumulator of the slot's last item has been read
+      auto accumulator_free = [&](int slot) {
+        if ((used >> slot & 1) && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + slot), (o_ph >> slot & 1) ^ 1, 69))) return false;
+        used |= 1u << slot;
+        o_ph ^= 1u << slot;
+        return true;
+      };
+      auto p_ready = [&](int b) {
+        if (!(ok = warp_wait(ctx, BAR(B_P_FULL + b), p_ph >> b & 1, 70))) return false;
+        p_ph ^= 1u << b;
+        return true;
+      };
+      while (ok && next_item(im)) {
+        const int wide = __shfl_sync(0xffffffffu, im->wide, 0), tiles = __shfl_sync(0xffffffffu, im->tiles, 0);
+        const int keys = __shfl_sync(0xffffffffu, im->keys - im->first_key, 0), columns = __shfl_sync(0xffffffffu, im->columns, 0);
+        item_done();
+        if (!accumulator_free(0) || ((wide || tiles > 1) && !accumulator_free(1))) break;
+        auto half_tile = [&](auto b_, uint64_t vd, int groups, bool first) {
+          constexpr int b = decltype(b_)::value, half = b % 2;
+          if (!p_ready(b)) return;
+          tc_fence_after();
+          const uint32_t d = tm + G::O_COL + b / 2 * kTile, a = tm + G::S_COL + b * 64;
+          const uint64_t v = vd + (uint64_t)(half * 64 * 128 >> 4);
+          if (groups >= 4) {
+            umma4_ts(d, a, v, typed(make_idesc(128, D, true)), !first);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 3; ++c)
+              if (c < groups) umma_bf16_ts(d, a + c * 8, v + (uint64_t)(c * 16 * 128 >> 4), typed(make_idesc(128, D, true)), !first || c > 0);
+          }
+          tc_commit(BAR(B_PV_DONE + b));
+        };
+        using std::integral_constant;
+        for (int j = 0; ok && j < tiles; ++j) {
+          if (!(ok = warp_wait(ctx, BAR(B_V_FULL) + 8 * v_st, v_ph, 68))) break;
+          const int valid = min(kTile, keys - j * kTile), groups = (valid + 15) / 16;
+          if (valid < groups * 16) {
+            // the last keys of a list: what lies behind them in the page (or was never loaded) must not meet the zeros of P
+            const int chunks = (groups * 16 - valid) * 8;
+#pragma unroll
+            for (int slab = 0; slab < G::SLABS; ++slab)
+              for (int i = lane; i < chunks; i += 32)
+                st_shared_v4(sbase + G::OFF_V + v_st * G::TILE_BYTES + slab * G::SLAB_BYTES + valid * 128 + i * 16, 0, 0, 0, 0);
+            fence_proxy_async();
+            __syncwarp();
+          }
+          const uint64_t vd = v_desc0 + (uint64_t)(v_st * (G::TILE_BYTES >> 4));
+          if (columns) {
+            const int slot = j & 1;
+            // (bit 15: the first operand's rows are contiguous)
+            const uint32_t idesc = (columns == 16 ? typed(make_idesc(128, 16, false)) : typed(make_idesc(128, 32, false))) | 1u << 15;
+            const uint64_t vt = vt_desc0 + (uint64_t)(v_st * (G::TILE_BYTES >> 4)), pd = make_desc(sbase + G::OFF_P + slot * G::P_SLOT, 16, 1024);
+            if (!p_ready(2 * slot) || !p_ready(2 * slot + 1)) break;
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              if (c < groups)
+                umma_ss(tm + G::O_COL + slot * kTile, vt + (uint64_t)(c * 16 * 128 >> 4), pd + (uint64_t)((c / 4 * G::P_HALF + c % 4 * 32) >> 4), idesc,
+                        j >= 2 || c > 0);
+            tc_commit(BAR(B_PV_DONE + 2 * slot));
+            tc_commit(BAR(B_PV_DONE + 2 * slot + 1));
+          } else if (wide) {
+            half_tile(integral_constant<int, 0>{}, vd, groups, j == 0);
+            if (ok) half_tile(integral_constant<int, 2>{}, vd, groups, j == 0);
+            if (ok && groups > 4) half_tile(integral_constant<int, 1>{}, vd, groups - 4, false);
+            if (ok && groups > 4) half_tile(integral_constant<int, 3>{}, vd, groups - 4, false);
+          } else if (j & 1) {
+            half_tile(integral_constant<int, 2>{}, vd, groups, j == 1);
+            if (ok && groups > 4) half_tile(integral_constant<int, 3>{}, vd, groups - 4, false);
+          } else {
+            half_tile(integral_constant<int, 0>{}, vd, groups, j == 0);
+            if (ok && groups > 4) half_tile(integral_constant<int, 1>{}, vd, groups - 4, false);
+          }
+          if (!ok) break;
+          tc_commit(BAR(B_V_EMPTY) + 8 * v_st);
+          if (++v_st == (uint32_t)G::NVS) v_st = 0, v_ph ^= 1;
+        }
+      }
     }
     // no product is still running when tensor memory is given back
-    tc_commit(BAR(B_FINAL + slot));
+    tc_commit(BAR(B_FINAL + warp - 1));
     __syncwarp();
     const long long t0 = clock64();
-    while (!mbar_try_wait(BAR(B_FINAL + slot), 0) && clock64() - t0 < p.wait_limit / 4) {}
+    while (!mbar_try_wait(BAR(B_FINAL + warp - 1), 0) && clock64() - t0 < p.wait_limit / 4) {}
   } else {
     // ================================================================ softmax, epilogue
-    const int slot = (warp - kSoftmaxWarp0) / 4, quad = warp & 3, r = quad * 32 + lane;
+    // Eight warps a slot, four for each of its two half tiles (a warp reaches only the 32 lanes of its quadrant): four softmax warps a
+    // scheduler hide each other's latencies.  A row has the same reference in both: the owner of a half tile takes it over
+    // from that of the one before, as soon as that one has its maximum.
+    const int sw = warp - kSoftmaxWarp0, slot = sw / 4 & 1, half = sw / 8, quad = warp & 3, r = quad * 32 + lane;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const uint32_t s_addr = tmem + lanes + G::S_COL + slot * kTile, o_addr = tmem + lanes + G::O_COL + slot * kTile;
-    uint32_t done = 0, done1 = 0, joined = 0;        // tiles of this slot, of slot 1; items whose slots were joined
-    Item im;
-    while (ok && next_item(im)) {
-      const bool wide = im.wide;
-      const int step = wide ? 1 : 2, from = wide ? 0 : slot;
-      const int tok = (wide && slot ? im.token + im.n0 : im.token) , n = wide && slot ? im.n1 : im.n0;
-      const int rows = n * s.group;
-      const bool live = r < rows, idle = quad * 32 >= rows;
-      const int row_tok = r / s.group, row_sub = r - row_tok * s.group;
-      // keys of this row, from the item's first; and those that every row of the tile sees
-      const int all = im.keys - im.first_key;
-      const int sees0 = im.sees - im.first_key + (wide && slot ? im.n0 : 0);
-      const int sees = min(all, sees0 + row_tok);
-      const int unmasked = min(all, sees0);
-      float ref = -INFINITY, l0 = 0.f, l1 = 0.f;
-      const uint32_t done1_new = done1 + (wide ? im.tiles : im.tiles / 2);
-      for (int j = from; j < im.tiles; j += step) {
-        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + slot), done & 1, 71))) break;
+    uint32_t uses[4] = {0, 0, 0, 0};                 // of the four S buffers, in the items before this one
+    uint32_t joined = 0, votes = 0, pairs = 0, refs = 0;
+
+    // Items of up to 32 rows: with query rows as rows of S one or two warps would have all the exponentials, so there the keys
+    // are the rows: S^T = K Q^T has a key a thread and NT columns, of which each half of the warps takes NH.  P^T goes through
+    // shared memory, O^T = V^T P^T has a channel a thread.  The reference of a row is the same in the four warps that
+    // have its column: they agree at a barrier whether any row has outgrown its own, and only then (in the first tile, seldom
+    // afterwards) exchange their maxima.
+    auto agree = [&] {                               // all four warps have come here
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(B_VOTE + slot * 2 + half));
+      ok = warp_wait(ctx, BAR(B_VOTE + slot * 2 + half), votes & 1, 77);
+      ++votes;
+      return ok;
+    };
+    auto few_rows = [&](auto width, const Item& im) {
+      constexpr int NH = decltype(width)::value;
+      const int tiles = im.tiles, c0 = half * NH, rows = im.n0 * s.group - c0, all = im.keys - im.first_key;   // rows: from c0 on
+      const int sees0 = im.sees - im.first_key, unmasked = min(all, sees0);
+      float ref[NH], l[NH];
+#pragma unroll
+      for (int c = 0; c < NH; ++c) ref[c] = -INFINITY, l[c] = 0.f;
+      // this thread's key in P: chunk 0 of a row, moved by the row's number mod 8 (128-byte swizzle); c0 is a multiple of 8
+      const uint32_t p_base = sbase + G::OFF_P + slot * G::P_SLOT + r / 64 * G::P_HALF + c0 * 128 + r % 8 * 2, chunk = r / 8 % 8;
+      uint32_t done = slot ? uses[2] : uses[0];
+      for (int j = slot; j < tiles; j += 2) {
+        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + 2 * slot + half), (slot ? uses[2 + half] + done - uses[2] : uses[half] + done - uses[0]) & 1, 71)))
+          return false;
         ++done;
-        if (idle) {
-          if (lane == 0) mbar_arrive(BAR(B_P_FULL + 2 * slot)), mbar_arrive(BAR(B_P_FULL + 2 * slot + 1));
-          continue;
-        }
         tc_fence_after();
-        // 64 columns at a time, loaded once for the maximum and once more for the exponentials: a whole row in registers spills
-        uint32_t sv[64];
-        const int lim = sees - j * kTile;
-        const bool masked = unmasked < (j + 1) * kTile;
-        auto load_s = [&](int half) {
-          WAVEAL_TMEM_LD32(s_addr + half * 64, sv, 0);
-          WAVEAL_TMEM_LD32(s_addr + half * 64 + 32, sv, 32);
-          WAVEAL_TMEM_WAIT_LD32(sv, 0);
-          WAVEAL_TMEM_WAIT_LD32(sv, 32);
-          if (masked) {
-#pragma unroll
-            for (int c = 0; c < 64; ++c) sv[c] = half * 64 + c < lim ? sv[c] : 0xff800000u;
-          }
-        };
-        float mx = -INFINITY;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          load_s(half);
-          float mx4[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx4[i] = __uint_as_float(sv[i]);
-#pragma unroll
-          for (int c = 4; c < 60; c += 8) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mx4[i] = fmax3(mx4[i], __uint_as_float(sv[c + 2 * i]), __uint_as_float(sv[c + 2 * i + 1]));
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx4[i] = fmaxf(mx4[i], __uint_as_float(sv[60 + i]));
-          mx = fmaxf(mx, fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), mx4[3]));
+        uint32_t sv[NH];
+        if constexpr (NH == 16) {
+          WAVEAL_TMEM_LD16(s_addr + c0, sv, 0);
+          WAVEAL_TMEM_WAIT_LD16(sv, 0);
+        } else {
+          WAVEAL_TMEM_LD8(s_addr + c0, sv);
+          WAVEAL_TMEM_WAIT_LD8(sv);
         }
-        mx *= p.sl2;
-        const bool grows = live && mx > ref + kGrowth;
-        if (__any_sync(0xffffffffu, grows)) {
-          float a = 1.0f;
-          if (grows) {
-            a = ex2(ref - mx);
-            ref = mx;
-            l0 *= a, l1 *= a;
-          }
-          if (j != from) {
-            // the rows' accumulators: not while a product still adds to them
-            if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + slot), (done - 2) & 1, 72))) break;
-            tc_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              WAVEAL_TMEM_LD32(o_addr + c, sv, 0);
-              WAVEAL_TMEM_WAIT_LD32(sv, 0);
+        float x[NH], over = -INFINITY;
+        if (unmasked < (j + 1) * kTile) {
+          const int key = j * kTile + r;
+          int g = c0 % s.group, lim = sees0 + c0 / s.group;   // a token's group of rows after the other
 #pragma unroll
-              for (int i = 0; i < 32; ++i) sv[i] = __float_as_uint(__uint_as_float(sv[i]) * a);
-              WAVEAL_TMEM_ST32(o_addr + c, sv, 0);
+          for (int c = 0; c < NH; ++c) {
+            x[c] = c < rows && key < min(all, lim) ? __uint_as_float(sv[c]) * p.sl2 : -INFINITY;
+            if (++g == s.group) g = 0, ++lim;
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < NH; ++c) x[c] = c < rows ? __uint_as_float(sv[c]) * p.sl2 : -INFINITY;
+        }
+#pragma unroll
+        for (int c = 0; c < NH; ++c) over = fmaxf(over, x[c] - ref[c]);      // (-inf - -inf: NaN, which fmaxf leaves out)
+        volatile int* vote = &sm.vote[slot][half][done & 1];
+        if (__any_sync(0xffffffffu, over > kGrowth) && lane == 0) *vote = (int)done;
+        if (!agree()) return false;
+        if (*vote == (int)done) {
+          float m[NH];
+#pragma unroll
+          for (int c = 0; c < NH; ++c) asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m[c]) : "f"(x[c]));
+          float(*wm)[kMaxColumns / 2] = sm.warp_max[slot][half];
+          if (lane == 0) {
+#pragma unroll
+            for (int c = 0; c < NH; c += 4) *reinterpret_cast<float4*>(&wm[quad][c]) = make_float4(m[c], m[c + 1], m[c + 2], m[c + 3]);
+          }
+          if (!agree()) return false;
+#pragma unroll
+          for (int c = 0; c < NH; c += 4) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const float4 y = *reinterpret_cast<const float4*>(&wm[w][c]);
+              m[c] = fmaxf(m[c], y.x), m[c + 1] = fmaxf(m[c + 1], y.y), m[c + 2] = fmaxf(m[c + 2], y.z), m[c + 3] = fmaxf(m[c + 3], y.w);
             }
+          }
+#pragma unroll
+          for (int c = 0; c < NH; ++c) {
+            const float to = m[c] > ref[c] + kGrowth ? m[c] : ref[c];
+            m[c] = to == ref[c] ? 1.0f : ex2(ref[c] - to);
+            ref[c] = to;
+            l[c] *= m[c];
+          }
+          if (j != slot) {
+            // (the last product into these accumulators has ended: this tile's S was issued behind it)
+            if constexpr (NH == 16) {
+              WAVEAL_TMEM_LD16(o_addr + c0, sv, 0);
+              WAVEAL_TMEM_WAIT_LD16(sv, 0);
+            } else {
+              WAVEAL_TMEM_LD8(o_addr + c0, sv);
+              WAVEAL_TMEM_WAIT_LD8(sv);
+            }
+#pragma unroll
+            for (int c = 0; c < NH; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * m[c]);
+            if constexpr (NH == 16) WAVEAL_TMEM_ST16(o_addr + c0, sv, 0);
+            else WAVEAL_TMEM_ST8(o_addr + c0, sv);
             tc_wait_st();
           }
         }
-        const float b = ref == -INFINITY ? 0.f : -ref;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          load_s(half);
+        for (int c = 0; c < NH; c += 2) {
+          const float e0 = ex2(x[c] - (ref[c] == -INFINITY ? 0.f : ref[c])), e1 = ex2(x[c + 1] - (ref[c + 1] == -INFINITY ? 0.f : ref[c + 1]));
+          l[c] += e0, l[c + 1] += e1;
+          const uint32_t pk = pack2<T>(e0, e1);
+          st_shared_u16(p_base + c * 128 + ((chunk ^ (c & 7)) << 4), pk);
+          st_shared_u16(p_base + (c + 1) * 128 + ((chunk ^ ((c + 1) & 7)) << 4), pk >> 16);
+        }
+        fence_proxy_async();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_P_FULL + 2 * slot + half));
+      }
+
+      // ---- epilogue: sums over the keys (a lane ends up with a row's)
+      const bool join = tiles > 1;
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            uint32_t pk[16];
+      for (int w = NH / 2, d = 16; w >= 1; w /= 2, d /= 2) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float x0, x1;
-              ffma2(x0, x1, __uint_as_float(sv[q * 32 + 2 * i]), __uint_as_float(sv[q * 32 + 2 * i + 1]), p.sl2, p.sl2, b, b);
-              x0 = ex2(x0), x1 = ex2(x1);
-              fadd2(l0, l1, l0, l1, x0, x1);
-              pk[i] = pack2<T>(x0, x1);
-            }
-            // P of a half of the keys lies over S columns that have been read by then
-            WAVEAL_TMEM_ST16(s_addr + half * 32 + q * 16, pk, 0);
-          }
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(B_P_FULL + 2 * slot + half));
+        for (int i = 0; i < w; ++i) {
+          const float give = lane & d ? l[i] : l[i + w], keep = lane & d ? l[i + w] : l[i];
+          l[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
         }
       }
-      if (!ok) break;
-      const uint32_t last_done = done - 1;
-      done1 = slot ? done : done1_new;
+#pragma unroll
+      for (int d = 16 / NH; d >= 1; d /= 2) l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+      const int sum_row = lane / (32 / NH);
+      if (slot) {
+        if (!join) return true;
+        if (joined && !(ok = warp_wait(ctx, BAR(B_SUMS_READ), (joined - 1) & 1, 76))) return false;
+        sm.cols.sum[quad][c0 + sum_row] = l[0];
+        if (quad == 0 && lane == 0) {
+#pragma unroll
+          for (int c = 0; c < NH; c += 4) *reinterpret_cast<float4*>(&sm.cols.ref[c0 + c]) = make_float4(ref[c], ref[c + 1], ref[c + 2], ref[c + 3]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_SUMS));
+        ++joined;
+        return true;
+      }
+      sm.warp_max[0][half][quad][sum_row] = l[0];
+      if (!agree()) return false;
+      // row c0 + `row`
+      const int row = lane % NH;
+      float my_ref = ref[0], my_l = 0.f, a0 = 1.0f, a1 = 0.f;
+#pragma unroll
+      for (int c = 1; c < NH; ++c) my_ref = row == c ? ref[c] : my_ref;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) my_l += sm.warp_max[0][half][w][row];
+      if (join) {
+        if (!(ok = warp_wait(ctx, BAR(B_SUMS), joined & 1, 73))) return false;
+        float other = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) other += sm.cols.sum[w][c0 + row];
+        const float other_ref = sm.cols.ref[c0 + row], m = fmaxf(my_ref, other_ref);
+        ++joined;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_SUMS_READ));
+        a0 = my_ref == -INFINITY ? 0.f : ex2(my_ref - m);
+        a1 = other_ref == -INFINITY ? 0.f : ex2(other_ref - m);
+        my_ref = m;
+        my_l = my_l * a0 + other * a1;
+        if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + 2), (uses[2] + tiles / 2 - 1) & 1, 74))) return false;
+      }
+      const bool direct = im.direct;
+      const int head0 = im.head * s.group;
+      if (direct) {
+        const float inv = my_l == 0.f ? 0.f : 1.0f / my_l;
+        a0 *= inv, a1 *= inv;
+      }
+      if (quad == 0 && lane < min(rows, NH)) {
+        if (!direct)
+          p.parts.ml[im.row + c0 + lane] = make_float2(my_ref, my_l);
+        else if (p.lse)
+          p.lse[(long long)(head0 + (c0 + lane) % s.group) * s.tokens + im.token + (c0 + lane) / s.group] =
+              my_l == 0.f ? -INFINITY : (my_ref + log2f(my_l)) * 0.69314718055994531f;
+      }
+      if (!(ok = warp_wait(ctx, BAR(B_PV_DONE), (uses[0] + (tiles + 1) / 2 - 1) & 1, 75))) return false;
+      tc_fence_after();
+      uint32_t v[NH], w[NH];
+      if constexpr (NH == 16) {
+        WAVEAL_TMEM_LD16(o_addr + c0, v, 0);
+        WAVEAL_TMEM_LD16(o_addr + kTile + c0, w, 0);             // (without a tile in slot 1: not used)
+        WAVEAL_TMEM_WAIT_LD16(v, 0);
+        WAVEAL_TMEM_WAIT_LD16(w, 0);
+      } else {
+        WAVEAL_TMEM_LD8(o_addr + c0, v);
+        WAVEAL_TMEM_LD8(o_addr + kTile + c0, w);
+        WAVEAL_TMEM_WAIT_LD8(v);
+        WAVEAL_TMEM_WAIT_LD8(w);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(BAR(B_O_EMPTY));
+        if (join) mbar_arrive(BAR(B_O_EMPTY + 1));
+      }
+      int g = c0 % s.group, tok = im.token + c0 / s.group;
+#pragma unroll
+      for (int i = 0; i < NH; ++i) {
+        const float b0 = __shfl_sync(0xffffffffu, a0, i), b1 = __shfl_sync(0xffffffffu, a1, i);
+        float y = __uint_as_float(v[i]) * b0;
+        if (join) y += __uint_as_float(w[i]) * b1;
+        if (i < rows && r < D) {
+          if (direct)
+            *reinterpret_cast<unsigned short*>(static_cast<T*>(p.o) + (head0 + g) * p.o_stride_h + tok * p.o_stride_t + r) =
+                (unsigned short)pack2<T>(y, 0.f);
+          else
+            p.parts.o[(long long)(im.row + c0 + i) * D + r] = y;
+        }
+        if (++g == s.group) g = 0, ++tok;
+      }
+      return true;
+    };
 
-      // ---- epilogue
+    // a row's other owner has come here too
+    auto pair = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(B_PAIR + slot * 4 + quad));
+      ok = warp_wait(ctx, BAR(B_PAIR + slot * 4 + quad), pairs & 1, 78);
+      ++pairs;
+      return ok;
+    };
+    const Item* im;
+    while (ok && next_item(im)) {
+      const bool wide = im->wide;
+      const int tiles = im->tiles, all = im->keys - im->first_key;
+      if (im->columns) {
+        if (im->columns == 16) few_rows(std::integral_constant<int, 8>{}, *im);
+        else few_rows(std::integral_constant<int, 16>{}, *im);
+        if (!ok) break;
+        uses[0] += (tiles + 1) / 2, uses[1] += (tiles + 1) / 2, uses[2] += tiles / 2, uses[3] += tiles / 2;
+        item_done();
+        continue;
+      }
+      // uses of the buffers by this item: every tile has a first half, and but for the last one of a list a second
+      uint32_t n[4];
+      {
+        const int seconds = (all + 63) / 64 - tiles;           // tiles with a second half (all, or all but the last)
+        n[0] = wide ? tiles : (tiles + 1) / 2, n[2] = wide ? tiles : tiles / 2;
+        n[1] = wide ? seconds : (seconds + 1) / 2, n[3] = wide ? seconds : seconds / 2;
+      }
+      const uint32_t mine = slot ? n[2 + half] : n[half], others = slot ? n[3 - half] : n[1 - half], halves = mine + others;
+      const uint32_t use0 = slot ? uses[2 + half] : uses[half], other0 = slot ? uses[3 - half] : uses[1 - half];
+      const int rows = (wide && slot ? im->n1 : im->n0) * s.group;
+      const bool idle = quad * 32 >= rows, live = r < rows;
+      // keys of this row, from the item's first; and those that every row of the tile sees
+      const int sees0 = im->sees - im->first_key + (wide && slot ? im->n0 : 0);
+      const int sees = min(all, sees0 + r / s.group), unmasked = min(all, sees0);
+      const uint32_t my_s = s_addr + half * 64;
+      float ref = -INFINITY, l0 = 0.f, l1 = 0.f;
+      for (uint32_t i = 0; i < mine; ++i) {
+        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + 2 * slot + half), (use0 + i) & 1, 71))) break;
+        if (idle) {
+          if (lane == 0) mbar_arrive(BAR(B_P_FULL + 2 * slot + half));
+          continue;
+        }
+        tc_fence_after();
+        const int key0 = (wide ? (int)i : 2 * (int)i + slot) * kTile + half * 64, lim = sees - key0;
+        const bool masked = unmasked < key0 + 64;
+        uint32_t sv[32];
+        // 32 columns at a time, loaded once for the maximum and again for the exponentials
+        auto load_s = [&](int c0) {
+          WAVEAL_TMEM_LD32(my_s + c0, sv, 0);
+          WAVEAL_TMEM_WAIT_LD32(sv, 0);
+          if (masked) {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) sv[c] = c < lim - c0 ? sv[c] : 0xff800000u;
+          }
+        };
+        float mx = -INFINITY;
+#pragma unroll 1
+        for (int c0 = 0; c0 < 64; c0 += 32) {
+          load_s(c0);
+          mx = fmaxf(mx, row_max32(sv));
+        }
+        mx *= p.sl2;
+        // half tile u of the slot: the reference that u - 1's owner left
+        const uint32_t u = 2 * i + half;
+        float now = -INFINITY;
+        if (u) {
+          if (!(ok = warp_wait(ctx, BAR(B_REF + slot * 4 + quad), (refs + u - 1) & 1, 72))) break;
+          now = sm.ref[slot][r];
+        }
+        const bool grows = live && mx > now + kGrowth;
+        const float to = grows ? mx : now;
+        sm.ref[slot][r] = to;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_REF + slot * 4 + quad));
+        if (to != ref) {
+          const float a = ex2(ref - to);
+          l0 *= a, l1 *= a;
+          ref = to;
+        }
+        if (__any_sync(0xffffffffu, grows) && u) {
+          // the accumulators, between the product before this one and this one's
+          if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + 2 * slot + (half ^ 1)), (other0 + i - (half ^ 1)) & 1, 73))) break;
+          tc_fence_after();
+          const float a = grows ? ex2(now - to) : 1.0f;
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            WAVEAL_TMEM_LD32(o_addr + c, sv, 0);
+            WAVEAL_TMEM_WAIT_LD32(sv, 0);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) sv[k] = __float_as_uint(__uint_as_float(sv[k]) * a);
+            WAVEAL_TMEM_ST32(o_addr + c, sv, 0);
+          }
+          tc_wait_st();
+        }
+        const float b = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll 1
+        for (int c0 = 0; c0 < 64; c0 += 32) {
+          load_s(c0);
+          uint32_t pk[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float x0, x1;
+            ffma2(x0, x1, __uint_as_float(sv[2 * k]), __uint_as_float(sv[2 * k + 1]), p.sl2, p.sl2, b, b);
+            x0 = ex2(x0), x1 = ex2(x1);
+            fadd2(l0, l1, l0, l1, x0, x1);
+            pk[k] = pack2<T>(x0, x1);
+          }
+          WAVEAL_TMEM_ST16(my_s + c0 / 2, pk, 0);
+        }
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_P_FULL + 2 * slot + half));
+      }
+      if (!ok) break;
+
+      // ---- epilogue: the sums of a row's owners
+      const bool join = !wide && tiles > 1;
       float l = l0 + l1;
-      const bool join = !wide && im.tiles > 1;
+      // the slot's last product
+      const uint32_t last_bar = B_PV_DONE + 2 * slot + (mine > others || (mine == others && half) ? half : half ^ 1);
+      const uint32_t last_ph = (mine > others || (mine == others && half) ? use0 + mine : other0 + others) - 1;
+      if (!idle && halves) {
+        if (!(ok = warp_wait(ctx, BAR(B_REF + slot * 4 + quad), (refs + halves - 1) & 1, 72))) break;
+        const float to = sm.ref[slot][r];
+        if (to != ref) l *= ex2(ref - to), ref = to;
+        refs += halves;
+        sm.pair[slot][half][r] = l;
+        if (!pair()) break;
+        l += sm.pair[slot][half ^ 1][r];
+        if (!pair()) break;                          // (read: the next item's may be left there)
+      }
+      // slot 1's last product of a narrow item
+      const uint32_t join_bar = B_PV_DONE + 2 + (n[2] == n[3] ? 1 : 0), join_ph = (n[2] == n[3] ? uses[3] + n[3] : uses[2] + n[2]) - 1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) uses[k] += n[k];
       if (!wide && slot) {
         if (join) {
-          if (!idle) sm.sums[joined & 1][r] = make_float2(ref, l);
+          if (joined && !(ok = warp_wait(ctx, BAR(B_SUMS_READ), (joined - 1) & 1, 76))) break;
+          if (!idle && half == 0) sm.sums[r] = make_float2(ref, l);
           __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(B_SUMS + (joined & 1)));
+          if (lane == 0) mbar_arrive(BAR(B_SUMS));
           ++joined;
         }
+        item_done();
         continue;
       }
       float a0 = 1.0f, a1 = 0.0f;
       if (join) {
-        if (!(ok = warp_wait(ctx, BAR(B_SUMS + (joined & 1)), joined >> 1 & 1, 73))) break;
-        if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + 1), (done1 - 1) & 1, 74))) break;
-        const float2 other = idle ? make_float2(0.f, 0.f) : sm.sums[joined & 1][r];
+        if (!(ok = warp_wait(ctx, BAR(B_SUMS), joined & 1, 73))) break;
+        const float2 other = idle ? make_float2(0.f, 0.f) : sm.sums[r];
         ++joined;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_SUMS_READ));
+        if (!(ok = warp_wait(ctx, BAR(join_bar), join_ph & 1, 74))) break;
         const float m = fmaxf(ref, other.x);
         a0 = ref == -INFINITY ? 0.f : ex2(ref - m);
         a1 = other.x == -INFINITY ? 0.f : ex2(other.x - m);
         ref = m;
         l = l * a0 + other.y * a1;
       }
-      if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + slot), last_done & 1, 75))) break;
+      if (!(ok = warp_wait(ctx, BAR(last_bar), last_ph & 1, 75))) break;
       tc_fence_after();
       if (!idle) {
-        const long long out_row = im.row + (long long)(wide && slot ? im.n0 * s.group : 0) + r;
+        const bool second = wide && slot, direct = im->direct;
+        const long long out_row = im->row + (long long)(second ? im->n0 * s.group : 0) + r;
         float scale_o = 1.0f;
         T* o_ptr = nullptr;
-        if (im.direct) {
+        if (direct) {
           scale_o = l == 0.f ? 0.f : 1.0f / l;
-          const int head = im.head * s.group + row_sub;
-          o_ptr = static_cast<T*>(p.o) + head * p.o_stride_h + (long long)(tok + row_tok) * p.o_stride_t;
-          if (live && p.lse) p.lse[(long long)head * s.tokens + tok + row_tok] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
-        } else if (live) {
+          const int head = im->head * s.group + r % s.group, tok = im->token + (second ? im->n0 : 0) + r / s.group;
+          o_ptr = static_cast<T*>(p.o) + head * p.o_stride_h + tok * p.o_stride_t;
+          if (live && half == 0 && p.lse)
+            p.lse[(long long)head * s.tokens + tok] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
+        } else if (live && half == 0) {
           p.parts.ml[out_row] = make_float2(ref, l);
         }
         a0 *= scale_o, a1 *= scale_o;
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t v[32], w[32];
-          WAVEAL_TMEM_LD32(o_addr + c, v, 0);
+        for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 16) {
+          uint32_t v[16], w[16];
+          WAVEAL_TMEM_LD16(o_addr + c, v, 0);
           if (join) {
-            WAVEAL_TMEM_LD32(o_addr + kTile + c, w, 0);
-            WAVEAL_TMEM_WAIT_LD32(w, 0);
+            WAVEAL_TMEM_LD16(o_addr + kTile + c, w, 0);
+            WAVEAL_TMEM_WAIT_LD16(w, 0);
           }
-          WAVEAL_TMEM_WAIT_LD32(v, 0);
+          WAVEAL_TMEM_WAIT_LD16(v, 0);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
+          for (int i = 0; i < 16; ++i) {
             float x = __uint_as_float(v[i]) * a0;
             if (join) x += __uint_as_float(w[i]) * a1;
             v[i] = __float_as_uint(x);
           }
           if (live) {
-            if (im.direct) {
+            if (direct) {
 #pragma unroll
-              for (int i = 0; i < 16; ++i) w[i] = pack2<T>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+              for (int i = 0; i < 8; ++i) w[i] = pack2<T>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
 #pragma unroll
-              for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(o_ptr + c + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+              for (int i = 0; i < 8; i += 4) *reinterpret_cast<uint4*>(o_ptr + c + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
             } else {
               float* dst = p.parts.o + out_row * D + c;
-#pragma unroll
-              for (int i = 0; i < 32; i += 8) st_global_v8(dst + i, v + i);
+              st_global_v8(dst, v);
+              st_global_v8(dst + 8, v + 8);
             }
           }
         }
@@ -834,6 +1298,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         mbar_arrive(BAR(B_O_EMPTY + slot));
         if (join) mbar_arrive(BAR(B_O_EMPTY + 1));
       }
+      item_done();
     }
   }
 
@@ -890,7 +1355,7 @@ __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Para
       if (!tiles) return;
       const int c0 = whole ? 0 : cuts.piece(at), c1 = whole ? 0 : cuts.piece(at + (long long)(tiles - 1) * weight);
       for (int c = c0; c <= c1; ++c) {
-        if (!whole && cuts.first_tile(c, at, tiles, weight) >= cuts.first_tile(c + 1, at, tiles, weight)) continue;
+        if (!whole && first_tile(cuts.begin(c), at, tiles, weight) >= first_tile(cuts.begin(c + 1), at, tiles, weight)) continue;
         if (WARPS > 1 && seen++ % WARPS != part0) continue;
         const long long at_row = part_row(s, row, c);
         const float2 ml = p.parts.ml[at_row];
