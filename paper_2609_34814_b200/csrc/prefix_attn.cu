@@ -44,23 +44,24 @@ constexpr int kBatch = 8;                            // of them worked out at a 
 constexpr int kItemReaders = 19;                     // V loader, two issuers, sixteen softmax warps
 constexpr long long kTimeoutCycles = 4000000000ll;   // ~2 s at boost clock
 constexpr long long kSelfTestCycles = 4000000ll;     // ~2 ms
-constexpr int kMaxColumns = 32;                      // rows of an item that is computed with its keys as rows (below)
+constexpr int kColumns = 16;                         // rows of an item that is computed with its keys as rows (below), at most
 constexpr float kGrowth = 8.0f;                      // log2 of how far a row's maximum may outgrow its reference
 
-// Costs on the line of tiles: a key tile of a unit of up to 128 rows, of up to 256, and the start and end of a unit.
-constexpr int kCostNarrow = 1, kCostWide = 2, kCostUnit = 1;
+// Costs on the line of tiles, about 1,000 clk each: a key tile of a unit of up to 16 rows, of up to 128, of up to 256, and the start and end
+// of such a unit.
+constexpr int kTileFew = 2, kTileNarrow = 3, kTileWide = 4, kUnitFew = 5, kUnitNarrow = 6, kUnitWide = 8;
 // a piece is not made shorter than this (below it the joining costs more than the tiles)
-constexpr int kMinPiece = 2;
+constexpr int kMinPiece = 8;
 
 template <int D> struct Geo {
   static constexpr int SLABS = D / 64;               // 128-byte-swizzled slabs of 64 channels
   static constexpr int SLAB_BYTES = kTile * 128;
   static constexpr int TILE_BYTES = SLABS * SLAB_BYTES;
   static constexpr int NKS = D == 128 ? 2 : 4, NVS = NKS;
-  // P of items of few rows: two halves of 64 keys for each slot
-  static constexpr int P_HALF = kMaxColumns * 128, P_SLOT = 2 * P_HALF;
+  // P of items of few rows: two halves of 64 keys for each of the four S buffers
+  static constexpr int P_HALF = kColumns * 128, P_TILE = 2 * P_HALF;
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NKS * TILE_BYTES, OFF_P = OFF_V + NVS * TILE_BYTES;
-  static constexpr int OFF_END = OFF_P + 2 * P_SLOT;
+  static constexpr int OFF_END = OFF_P + 4 * P_TILE;
   static constexpr int S_COL = 0, O_COL = 256;       // tensor memory: S 0-127, 128-255, O 256.., 384..
 };
 
@@ -78,13 +79,18 @@ struct Shape {
 struct Parts {
   float* o;                // [row][D], unscaled
   float2* ml;              // [row] {reference (log2), sum}
-  long long* own_base;     // [batch] where a sequence's units begin on the line, from the first own unit on
-  long long* total;        // cost of all own units
+  int2* pieces;            // [row / group] of a unit's first row: the first and the last piece that has tiles of it (left by the CTAs that
+                           // work on its first and last tile)
 };
 
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-// prefix units: 0 .. n on a head, all alike but the last
+// a unit of n0 and n1 tokens in its row tiles: 2 wide, 1 narrow, 0 few rows
+__device__ inline int unit_kind(int n0, int n1, int group) { return n1 ? 2 : n0 * group > kColumns ? 1 : 0; }
+__device__ inline int tile_cost(int kind) { return kind == 2 ? kTileWide : kind ? kTileNarrow : kTileFew; }
+__device__ inline int unit_cost(int kind) { return kind == 2 ? kUnitWide : kind ? kUnitNarrow : kUnitFew; }
+
+// prefix units: 0 .. n on a head, all alike (wide) but the last
 struct PrefixLine {
   int per_head, units, whole;     // units of a head; of all heads; dealt out whole
   int tiles, last_weight;
@@ -95,9 +101,10 @@ struct PrefixLine {
     per_head = tiles ? ceil_div(s.tokens, 2 * s.tq) : 0;
     units = per_head * s.kv_heads;
     whole = units / s.ctas * s.ctas;
-    last_weight = s.tokens - (per_head - 1) * 2 * s.tq > s.tq ? kCostWide : kCostNarrow;
-    cost = (long long)tiles * kCostWide + kCostUnit;
-    last_cost = (long long)tiles * last_weight + kCostUnit;
+    const int rest = s.tokens - (per_head - 1) * 2 * s.tq, kind = unit_kind(min(rest, s.tq), max(rest - s.tq, 0), s.group);
+    last_weight = tile_cost(kind);
+    cost = (long long)tiles * kTileWide + kUnitWide;
+    last_cost = (long long)tiles * last_weight + unit_cost(kind);
   }
   __device__ long long before(int u) const {         // cost of units 0 .. u - 1
     const int h = u / max(per_head, 1), i = u - h * per_head;
@@ -105,7 +112,7 @@ struct PrefixLine {
   }
   __device__ long long at(int u) const { return before(u) - before(whole); }
   __device__ long long total() const { return at(units); }
-  __device__ int weight(int i) const { return i == per_head - 1 ? last_weight : kCostWide; }
+  __device__ int weight(int i) const { return i == per_head - 1 ? last_weight : kTileWide; }
   __device__ int find(long long x) const {           // the unit that position x of the line lies in
     x += before(whole);
     const long long head = (per_head - 1) * cost + last_cost;
@@ -144,8 +151,9 @@ __device__ inline OwnUnit own_unit(const Shape& s, const Sequence& q, int i) {
   u.n1 = min(s.tq, q.n - u.first - u.n0);
   u.keys = s.causal ? max(0, q.len - q.n + u.first + u.n0 + u.n1) : q.len;
   u.tiles = ceil_div(u.keys, kTile);
-  u.weight = u.n1 ? kCostWide : kCostNarrow;
-  u.cost = u.tiles ? u.tiles * u.weight + kCostUnit : 0;
+  const int kind = unit_kind(u.n0, u.n1, s.group);
+  u.weight = tile_cost(kind);
+  u.cost = u.tiles ? u.tiles * u.weight + unit_cost(kind) : 0;
   return u;
 }
 __device__ inline long long own_head_cost(const Shape& s, const Sequence& q) {
@@ -173,19 +181,16 @@ struct Cuts {
     rest = (int)(total - each * pieces);
   }
   __device__ long long begin(int c) const { return each * c + (unsigned)(rest * c) / (unsigned)pieces; }
-  __device__ int piece(long long x) const {                    // the last one that begins at x or before
-    int c = (int)min((float)x / ((float)each + (float)rest / (float)pieces), (float)(pieces - 1));
-    while (c > 0 && begin(c) > x) --c;
-    while (c + 1 < pieces && begin(c + 1) <= x) ++c;
-    return c;
-  }
 };
 // of a unit at `at`: its first tile that begins at x or behind
 __device__ inline int first_tile(long long x, long long at, int tiles, int weight) {
   const long long d = x - at;
-  return d <= 0 ? 0 : d >= (long long)tiles * weight ? tiles : (int)(weight == kCostWide ? (d + kCostWide - 1) / kCostWide : d);
+  if (d <= 0 || d >= (long long)tiles * weight) return d <= 0 ? 0 : tiles;
+  const unsigned u = (unsigned)d;
+  return weight == kTileFew ? (u + kTileFew - 1) / kTileFew : weight == kTileNarrow ? (u + kTileNarrow - 1) / kTileNarrow
+                                                                                                  : (u + kTileWide - 1) / kTileWide;
 }
-static_assert(kCostNarrow == 1, "first_tile");
+static_assert(kMinPiece >= kTileWide, "a piece between two others of a unit has a tile of it");
 
 // Where the parts of a row lie.  Units follow each other on the line in the order of their rows (prefix: head, token, query head
 // of the group; own: sequence, key head, token, query head), and so do pieces: row + piece * (rows of the largest unit) is
@@ -211,13 +216,9 @@ struct Item {
   int sees;                // keys that the first token sees (below 1: none); every token sees one more. kAll: all of them see all
   int direct;              // 1: no other part of these rows exists, o is written at once
   int row;                 // of the parts
-  int columns;             // 0: rows of S are query rows; 16 or 32: they are keys, and its columns the item's up to 32 rows
+  int few;                 // 0: both slots, rows of S are query rows; 1: at most kColumns rows, which are its columns, and its keys the rows,
+  int slot;                // all in this slot
 };
-
-__device__ inline int columns_of(const Item& im, int group) {
-  const int rows = im.n0 * group;
-  return im.wide || rows > kMaxColumns ? 0 : rows > 16 ? 32 : 16;
-}
 
 // How far a CTA is on its way through its units: whole ones, its piece's prefix units, its piece's own units.
 struct Walk {
@@ -232,7 +233,7 @@ struct Walk {
 
 // The next items, up to kBatch, a lane each (a whole warp calls it): 3,000 clk of index arithmetic, for one item or for all of them.
 // Returns the lanes that have one; none at the end.
-__device__ __noinline__ unsigned next_units(const Shape& s, Walk& w, Item& im, int lane) {
+__device__ __noinline__ unsigned next_units(const Shape& s, const Parts& parts, Walk& w, Item& im, int lane) {
   const PrefixLine& line = w.line;
   for (;;) {
     bool have = false;
@@ -258,7 +259,12 @@ __device__ __noinline__ unsigned next_units(const Shape& s, Walk& w, Item& im, i
         im.first_key = j0 * kTile, im.keys = min(s.prefix_len, j1 * kTile);
         im.list = -1, im.sees = kAll;
         im.direct = 0;
-        im.row = (int)part_row(s, prefix_row(s, h, im.token), whole ? 0 : w.piece);
+        const long long row = prefix_row(s, h, im.token);
+        const int piece = whole ? 0 : w.piece;
+        im.row = (int)part_row(s, row, piece);
+        int2& pieces = parts.pieces[h * s.tokens + im.token];
+        if (j0 == 0) pieces.x = piece;
+        if (j1 == line.tiles) pieces.y = piece;
       }
       const bool end = __any_sync(0xffffffffu, past && lane <= kBatch);
       if (lane == 0) {
@@ -309,6 +315,9 @@ __device__ __noinline__ unsigned next_units(const Shape& s, Walk& w, Item& im, i
         im.sees = s.causal ? q.len - q.n + u.first + 1 : kAll;
         im.direct = line.tiles == 0 && j0 == 0 && j1 == u.tiles;
         im.row = (int)part_row(s, own_row(s, q, h, u.first), w.piece);
+        int2& pieces = parts.pieces[(s.tokens + q.start) * s.kv_heads + h * q.n + u.first];
+        if (j0 == 0) pieces.x = w.piece;
+        if (j1 == u.tiles) pieces.y = w.piece;
       }
       __syncwarp();
       if (lane == 0) {
@@ -326,7 +335,7 @@ __device__ __noinline__ unsigned next_units(const Shape& s, Walk& w, Item& im, i
     }
     if (have) {
       im.wide = im.n1 > 0;
-      im.columns = columns_of(im, s.group);
+      im.few = !im.wide && im.n0 * s.group <= kColumns;
     }
     const unsigned who = __ballot_sync(0xffffffffu, have);
     __syncwarp();
@@ -437,7 +446,7 @@ enum {
   B_ITEM_FULL = 0, B_ITEM_EMPTY = B_ITEM_FULL + kItems, B_Q_FULL = B_ITEM_EMPTY + kItems, B_Q_EMPTY = B_Q_FULL + 2,
   B_K_FULL = B_Q_EMPTY + 2, B_K_EMPTY = B_K_FULL + kStages, B_V_FULL = B_K_EMPTY + kStages, B_V_EMPTY = B_V_FULL + kStages,
   B_S_FULL = B_V_EMPTY + kStages, B_P_FULL = B_S_FULL + 4, B_PV_DONE = B_P_FULL + 4, B_O_EMPTY = B_PV_DONE + 4, B_SUMS = B_O_EMPTY + 2,
-  B_SUMS_READ, B_VOTE, B_PAIR = B_VOTE + 4, B_REF = B_PAIR + 8, B_FINAL = B_REF + 8, B_COUNT = B_FINAL + 2
+  B_SUMS_READ, B_COLS, B_COLS_READ = B_COLS + 2, B_VOTE = B_COLS_READ + 2, B_PAIR = B_VOTE + 4, B_REF = B_PAIR + 8, B_FINAL = B_REF + 8, B_COUNT = B_FINAL + 2
 };
 
 // what lies behind the tiles in shared memory
@@ -452,6 +461,13 @@ enum {
 #define WAVEAL_TMEM_ST8(taddr, v)                                                                                      \
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"                         \
                ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory")
+// 8 or 16 columns by the array's length
+__device__ __forceinline__ void tmem_load(uint32_t a, uint32_t (&v)[8]) { WAVEAL_TMEM_LD8(a, v); }
+__device__ __forceinline__ void tmem_load(uint32_t a, uint32_t (&v)[16]) { WAVEAL_TMEM_LD16(a, v, 0); }
+__device__ __forceinline__ void tmem_wait(uint32_t (&v)[8]) { WAVEAL_TMEM_WAIT_LD8(v); }
+__device__ __forceinline__ void tmem_wait(uint32_t (&v)[16]) { WAVEAL_TMEM_WAIT_LD16(v, 0); }
+__device__ __forceinline__ void tmem_store(uint32_t a, const uint32_t (&v)[8]) { WAVEAL_TMEM_ST8(a, v); }
+__device__ __forceinline__ void tmem_store(uint32_t a, const uint32_t (&v)[16]) { WAVEAL_TMEM_ST16(a, v, 0); }
 __device__ __forceinline__ void st_shared_u16(uint32_t addr, uint32_t x) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"((unsigned short)x) : "memory");
 }
@@ -461,11 +477,10 @@ struct Small {
   Item items[kItems];
   float ref[2][kTile];                               // [slot][row]: the reference, from one half tile's owner to the next one's
   float pair[2][2][kTile];                           // [slot][owner][row]: sums
-  float warp_max[2][2][4][kMaxColumns / 2];          // few rows: [slot][half of the rows][warp]: maxima, at the end slot 0's sums
-  union {                                            // what slot 1 leaves of an item whose key tiles the slots share out
-    float2 sums[kTile];                              // a row's reference and sum
-    struct { float sum[4][kMaxColumns], ref[kMaxColumns]; } cols;
-  };
+  float warp_max[4][4][kColumns];                    // few rows: [buffer][warp]
+  float warp_l[2][4][kColumns];                      // few rows, sums: [slot][warp]
+  struct { float sum[4][kColumns], ref[kColumns]; } cols[2];   // few rows: what the second half's owners leave for the first's
+  float2 sums[kTile];                                // what slot 1 leaves of an item whose key tiles the slots share out: references and sums
   int vote[2][2][2];
   long long warp_sum[kThreads / 32];
   alignas(16) unsigned char walk_space[sizeof(Walk)];
@@ -549,7 +564,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     tmem_relinquish();
   } else if (warp == 2) {
     for (int i = lane; i < B_COUNT; i += 32) {
-      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps4 = (i >= B_P_FULL && i < B_P_FULL + 4) || (i >= B_VOTE && i < B_VOTE + 4);
+      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps4 = (i >= B_P_FULL && i < B_P_FULL + 4) || (i >= B_COLS && i < B_VOTE + 4);
       const bool warps8 = (i >= B_O_EMPTY && i < B_O_EMPTY + 2) || i == B_SUMS || i == B_SUMS_READ, warps2 = i >= B_PAIR && i < B_PAIR + 8;
       mbar_init(BAR(i), item ? kItemReaders : warps4 ? 4 : warps8 ? 8 : warps2 ? 2 : 1);
     }
@@ -593,14 +608,12 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   {
     const long long from = max(w0 - line.total(), 0ll);
     long long base = upto - mine;
-    if (blockIdx.x == 0 || (base <= from && from < upto))
+    if (has_piece && base <= from && from < upto)
       for (int b = b0; b < b1; ++b) {
         const long long c = own_head_cost(s, read_sequence(s, b, nullptr)) * s.kv_heads;
-        if (has_piece && base <= from && from < base + c) sm.walk().seq = b, sm.walk().base = line.total() + base;
-        if (blockIdx.x == 0) p.parts.own_base[b] = base;
+        if (base <= from && from < base + c) sm.walk().seq = b, sm.walk().base = line.total() + base;
         base += c;
       }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *p.parts.total = own_total;
     if (threadIdx.x == 0) {
       Walk& w = sm.walk();
       w.w0 = w0, w.w1 = w1;
@@ -634,7 +647,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (warp == 0) {
     // ================================================================ items, Q, K
     TileLoader<D> loader;
-    uint32_t q_it = 0, q_armed = 0, q_parity = 0;
+    uint32_t q_it = 0, q_armed = 0, q_parity = 0, few_items = 0;
     auto load_q = [&](const CUtensorMap* tm, int token, int head, int n) {
       const uint32_t st = q_it & 1, ph = q_it >> 1 & 1;
       if (q_it >= 2 && !warp_wait(ctx, BAR(B_Q_EMPTY + st), ph ^ 1, 61)) return false;
@@ -651,20 +664,24 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     };
     for (bool more = true; ok && more;) {
       Item next;
-      const unsigned who = next_units(s, sm.walk(), next, lane);
+      const unsigned who = next_units(s, p.parts, sm.walk(), next, lane);
       const int count = max(__popc(who), 1), nth = __popc(who & ((1u << lane) - 1));   // (at the end: one item without tiles)
       more = who != 0;
       const uint32_t first = item_no;
       for (int i = 0; ok && i < count; ++i, ++item_no)
         if (item_no >= kItems) ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + item_no % kItems), (item_no / kItems & 1) ^ 1, 62);
       if (!ok) break;
+      // items of few rows take the slots in turn: one's epilogue runs beside the next one's tiles
+      const unsigned few_lanes = __ballot_sync(0xffffffffu, (who >> lane & 1) && next.few);
       if (more ? who >> lane & 1 : lane == 0) {
         const uint32_t slot = (first + nth) % kItems;
-        if (!more) next.tiles = 0;
+        if (!more) next.tiles = 0, next.few = 0;
+        next.slot = (few_items + __popc(few_lanes & ((1u << lane) - 1))) & 1;
         sm.items[slot] = next;
         mbar_arrive(BAR(B_ITEM_FULL + slot));
       }
       __syncwarp();
+      few_items += __popc(few_lanes);
       for (int i = 0; ok && more && i < count; ++i) {
         const Item im = sm.items[(first + i) % kItems];
         loader.page = loader.read_page(p, im, im.first_key, lane);
@@ -722,7 +739,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       };
       while (ok && next_item(im)) {
         const int wide = __shfl_sync(0xffffffffu, im->wide, 0), tiles = __shfl_sync(0xffffffffu, im->tiles, 0);
-        const int keys = __shfl_sync(0xffffffffu, im->keys - im->first_key, 0), columns = __shfl_sync(0xffffffffu, im->columns, 0);
+        const int keys = __shfl_sync(0xffffffffu, im->keys - im->first_key, 0), few = __shfl_sync(0xffffffffu, im->few, 0), item_slot = __shfl_sync(0xffffffffu, im->slot, 0);
         item_done();
         const uint32_t qb0 = qb;
         if (!(ok = warp_wait(ctx, BAR(B_Q_FULL + qb), q_ph, 65))) break;
@@ -747,16 +764,15 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           if (!(ok = warp_wait(ctx, BAR(B_K_FULL) + 8 * k_st, k_ph, 66))) break;
           const uint64_t kd = k_desc0 + (uint64_t)(k_st * (G::TILE_BYTES >> 4));
           const bool two = keys - j * kTile > 64;
-          if (columns) {
-            const int slot = j & 1;
-            if (!buffer_free(2 * slot) || !buffer_free(2 * slot + 1)) break;
+          if (few) {
+            const int b = 2 * item_slot + (j & 1);
+            if (!buffer_free(b)) break;
             tc_fence_after();
-            const uint32_t idesc = columns == 16 ? typed(make_idesc(128, 16, false)) : typed(make_idesc(128, 32, false));
 #pragma unroll
             for (int slab = 0; slab < G::SLABS; ++slab)
-              umma4_ss(tm + G::S_COL + slot * kTile, kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), qd + (uint64_t)(slab * G::SLAB_BYTES >> 4), idesc, slab > 0);
-            tc_commit(BAR(B_S_FULL + 2 * slot));
-            tc_commit(BAR(B_S_FULL + 2 * slot + 1));
+              umma4_ss(tm + G::S_COL + b * 64, kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), qd + (uint64_t)(slab * G::SLAB_BYTES >> 4),
+                       typed(make_idesc(128, kColumns, false)), slab > 0);
+            tc_commit(BAR(B_S_FULL + b));
           } else if (wide) {
             half_tile(integral_constant<int, 0>{}, qd, kd);
             if (ok) half_tile(integral_constant<int, 2>{}, qd1, kd);
@@ -795,9 +811,9 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       };
       while (ok && next_item(im)) {
         const int wide = __shfl_sync(0xffffffffu, im->wide, 0), tiles = __shfl_sync(0xffffffffu, im->tiles, 0);
-        const int keys = __shfl_sync(0xffffffffu, im->keys - im->first_key, 0), columns = __shfl_sync(0xffffffffu, im->columns, 0);
+        const int keys = __shfl_sync(0xffffffffu, im->keys - im->first_key, 0), few = __shfl_sync(0xffffffffu, im->few, 0), item_slot = __shfl_sync(0xffffffffu, im->slot, 0);
         item_done();
-        if (!accumulator_free(0) || ((wide || tiles > 1) && !accumulator_free(1))) break;
+        if (few ? !accumulator_free(item_slot) : !accumulator_free(0) || ((wide || tiles > 1) && !accumulator_free(1))) break;
         auto half_tile = [&](auto b_, uint64_t vd, int groups, bool first) {
           constexpr int b = decltype(b_)::value, half = b % 2;
           if (!p_ready(b)) return;
@@ -828,20 +844,19 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             __syncwarp();
           }
           const uint64_t vd = v_desc0 + (uint64_t)(v_st * (G::TILE_BYTES >> 4));
-          if (columns) {
-            const int slot = j & 1;
+          if (few) {
+            const int b = 2 * item_slot + (j & 1);
             // (bit 15: the first operand's rows are contiguous)
-            const uint32_t idesc = (columns == 16 ? typed(make_idesc(128, 16, false)) : typed(make_idesc(128, 32, false))) | 1u << 15;
-            const uint64_t vt = vt_desc0 + (uint64_t)(v_st * (G::TILE_BYTES >> 4)), pd = make_desc(sbase + G::OFF_P + slot * G::P_SLOT, 16, 1024);
-            if (!p_ready(2 * slot) || !p_ready(2 * slot + 1)) break;
+            const uint32_t idesc = typed(make_idesc(128, kColumns, false)) | 1u << 15;
+            const uint64_t vt = vt_desc0 + (uint64_t)(v_st * (G::TILE_BYTES >> 4)), pd = make_desc(sbase + G::OFF_P + b * G::P_TILE, 16, 1024);
+            if (!p_ready(b)) break;
             tc_fence_after();
 #pragma unroll
             for (int c = 0; c < 8; ++c)
               if (c < groups)
-                umma_ss(tm + G::O_COL + slot * kTile, vt + (uint64_t)(c * 16 * 128 >> 4), pd + (uint64_t)((c / 4 * G::P_HALF + c % 4 * 32) >> 4), idesc,
+                umma_ss(tm + G::O_COL + b * 64, vt + (uint64_t)(c * 16 * 128 >> 4), pd + (uint64_t)((c / 4 * G::P_HALF + c % 4 * 32) >> 4), idesc,
                         j >= 2 || c > 0);
-            tc_commit(BAR(B_PV_DONE + 2 * slot));
-            tc_commit(BAR(B_PV_DONE + 2 * slot + 1));
+            tc_commit(BAR(B_PV_DONE + b));
           } else if (wide) {
             half_tile(integral_constant<int, 0>{}, vd, groups, j == 0);
             if (ok) half_tile(integral_constant<int, 2>{}, vd, groups, j == 0);
@@ -874,104 +889,99 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const uint32_t s_addr = tmem + lanes + G::S_COL + slot * kTile, o_addr = tmem + lanes + G::O_COL + slot * kTile;
     uint32_t uses[4] = {0, 0, 0, 0};                 // of the four S buffers, in the items before this one
-    uint32_t joined = 0, votes = 0, pairs = 0, refs = 0;
+    uint32_t joined = 0, joined_few = 0, votes = 0, pairs = 0, refs = 0;
 
-    // Items of up to 32 rows: with query rows as rows of S one or two warps would have all the exponentials, so there the keys
-    // are the rows: S^T = K Q^T has a key a thread and NT columns, of which each half of the warps takes NH.  P^T goes through
-    // shared memory, O^T = V^T P^T has a channel a thread.  The reference of a row is the same in the four warps that
-    // have its column: they agree at a barrier whether any row has outgrown its own, and only then (in the first tile, seldom
-    // afterwards) exchange their maxima.
+    // Items of up to 16 rows: with query rows as rows of S one warp would have all the exponentials, so there the keys are the rows:
+    // S^T = K Q^T has a key a thread and a query row a column.  The slot's two groups of four warps take the tiles in turn, each with its
+    // own accumulator, references and sums, and the first joins them.  P^T goes through shared memory, O^T = V^T P^T has a
+    // channel a thread.  The four warps of a tile have the same references: they agree at a barrier whether any row has outgrown
+    // its own, and only then (in the first tile, seldom afterwards) exchange their maxima.
+    const int buffer = slot * 2 + half;
     auto agree = [&] {                               // all four warps have come here
       __syncwarp();
-      if (lane == 0) mbar_arrive(BAR(B_VOTE + slot * 2 + half));
-      ok = warp_wait(ctx, BAR(B_VOTE + slot * 2 + half), votes & 1, 77);
+      if (lane == 0) mbar_arrive(BAR(B_VOTE + buffer));
+      ok = warp_wait(ctx, BAR(B_VOTE + buffer), votes & 1, 77);
       ++votes;
       return ok;
     };
-    auto few_rows = [&](auto width, const Item& im) {
-      constexpr int NH = decltype(width)::value;
-      const int tiles = im.tiles, c0 = half * NH, rows = im.n0 * s.group - c0, all = im.keys - im.first_key;   // rows: from c0 on
-      const int sees0 = im.sees - im.first_key, unmasked = min(all, sees0);
-      float ref[NH], l[NH];
+    // (N: columns that are computed, at least the item's rows: a warp that runs alone pays some 6 clk for each instruction)
+    auto few_rows = [&](auto columns, const Item& im, uint32_t use0, uint32_t other0) {
+      constexpr int N = decltype(columns)::value, NL = N < 8 ? 8 : N;   // NL: columns loaded
+      const int tiles = im.tiles, rows = im.n0 * s.group, all = im.keys - im.first_key, sees0 = im.sees - im.first_key;
+      const int unmasked = min(all, sees0), mine = (tiles + 1 - half) / 2;
+      float ref[N], l[N];
 #pragma unroll
-      for (int c = 0; c < NH; ++c) ref[c] = -INFINITY, l[c] = 0.f;
-      // this thread's key in P: chunk 0 of a row, moved by the row's number mod 8 (128-byte swizzle); c0 is a multiple of 8
-      const uint32_t p_base = sbase + G::OFF_P + slot * G::P_SLOT + r / 64 * G::P_HALF + c0 * 128 + r % 8 * 2, chunk = r / 8 % 8;
-      uint32_t done = slot ? uses[2] : uses[0];
-      for (int j = slot; j < tiles; j += 2) {
-        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + 2 * slot + half), (slot ? uses[2 + half] + done - uses[2] : uses[half] + done - uses[0]) & 1, 71)))
-          return false;
-        ++done;
+      for (int c = 0; c < N; ++c) ref[c] = -INFINITY, l[c] = 0.f;
+      // this thread's key in P: chunk 0 of a row, moved by the row's number mod 8 (128-byte swizzle)
+      const uint32_t p_base = sbase + G::OFF_P + buffer * G::P_TILE + r / 64 * G::P_HALF + r % 8 * 2, chunk = r / 8 % 8;
+      const uint32_t acc = tmem + lanes + G::O_COL + buffer * 64;
+      for (int i = 0; i < mine; ++i) {
+        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + buffer), (use0 + i) & 1, 71))) return false;
         tc_fence_after();
-        uint32_t sv[NH];
-        if constexpr (NH == 16) {
-          WAVEAL_TMEM_LD16(s_addr + c0, sv, 0);
-          WAVEAL_TMEM_WAIT_LD16(sv, 0);
-        } else {
-          WAVEAL_TMEM_LD8(s_addr + c0, sv);
-          WAVEAL_TMEM_WAIT_LD8(sv);
-        }
-        float x[NH], over = -INFINITY;
-        if (unmasked < (j + 1) * kTile) {
-          const int key = j * kTile + r;
-          int g = c0 % s.group, lim = sees0 + c0 / s.group;   // a token's group of rows after the other
-#pragma unroll
-          for (int c = 0; c < NH; ++c) {
-            x[c] = c < rows && key < min(all, lim) ? __uint_as_float(sv[c]) * p.sl2 : -INFINITY;
+        uint32_t sv[NL];
+        tmem_load(tmem + lanes + G::S_COL + buffer * 64, sv);
+        // the rows that see this thread's key
+        const int key = (2 * i + half) * kTile + r;
+        unsigned seen = (1u << rows) - 1;
+        if (unmasked < (2 * i + half + 1) * kTile) {
+          int g = 0, lim = sees0;                    // a token's group of rows after the other
+          seen = 0;
+#pragma unroll 1
+          for (int c = 0; c < rows; ++c) {
+            if (key < min(all, lim)) seen |= 1u << c;
             if (++g == s.group) g = 0, ++lim;
           }
-        } else {
-#pragma unroll
-          for (int c = 0; c < NH; ++c) x[c] = c < rows ? __uint_as_float(sv[c]) * p.sl2 : -INFINITY;
         }
+        tmem_wait(sv);
+        float x[N], over = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < NH; ++c) over = fmaxf(over, x[c] - ref[c]);      // (-inf - -inf: NaN, which fmaxf leaves out)
-        volatile int* vote = &sm.vote[slot][half][done & 1];
-        if (__any_sync(0xffffffffu, over > kGrowth) && lane == 0) *vote = (int)done;
-        if (!agree()) return false;
-        if (*vote == (int)done) {
-          float m[NH];
+        for (int c = 0; c < N; ++c) {
+          x[c] = seen >> c & 1 ? __uint_as_float(sv[c]) * p.sl2 : -INFINITY;
+          over = fmaxf(over, x[c] - ref[c]);         // (-inf - -inf: NaN, which fmaxf leaves out)
+        }
+        volatile int* vote = &sm.vote[slot][half][i & 1];
+        bool grow = i == 0;
+        if (!grow) {
+          if (__any_sync(0xffffffffu, over > kGrowth) && lane == 0) *vote = (int)(use0 + i) + 1;
+          if (!agree()) return false;
+          grow = *vote == (int)(use0 + i) + 1;
+        }
+        if (grow) {
+          float m[N];
 #pragma unroll
-          for (int c = 0; c < NH; ++c) asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m[c]) : "f"(x[c]));
-          float(*wm)[kMaxColumns / 2] = sm.warp_max[slot][half];
+          for (int c = 0; c < N; ++c) asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m[c]) : "f"(x[c]));
           if (lane == 0) {
 #pragma unroll
-            for (int c = 0; c < NH; c += 4) *reinterpret_cast<float4*>(&wm[quad][c]) = make_float4(m[c], m[c + 1], m[c + 2], m[c + 3]);
+            for (int c = 0; c < N; c += 4) *reinterpret_cast<float4*>(&sm.warp_max[buffer][quad][c]) = make_float4(m[c], m[c + 1], m[c + 2], m[c + 3]);
           }
           if (!agree()) return false;
 #pragma unroll
-          for (int c = 0; c < NH; c += 4) {
+          for (int c = 0; c < N; c += 4) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-              const float4 y = *reinterpret_cast<const float4*>(&wm[w][c]);
+              const float4 y = *reinterpret_cast<const float4*>(&sm.warp_max[buffer][w][c]);
               m[c] = fmaxf(m[c], y.x), m[c + 1] = fmaxf(m[c + 1], y.y), m[c + 2] = fmaxf(m[c + 2], y.z), m[c + 3] = fmaxf(m[c + 3], y.w);
             }
           }
 #pragma unroll
-          for (int c = 0; c < NH; ++c) {
+          for (int c = 0; c < N; ++c) {
             const float to = m[c] > ref[c] + kGrowth ? m[c] : ref[c];
             m[c] = to == ref[c] ? 1.0f : ex2(ref[c] - to);
             ref[c] = to;
             l[c] *= m[c];
           }
-          if (j != slot) {
-            // (the last product into these accumulators has ended: this tile's S was issued behind it)
-            if constexpr (NH == 16) {
-              WAVEAL_TMEM_LD16(o_addr + c0, sv, 0);
-              WAVEAL_TMEM_WAIT_LD16(sv, 0);
-            } else {
-              WAVEAL_TMEM_LD8(o_addr + c0, sv);
-              WAVEAL_TMEM_WAIT_LD8(sv);
-            }
+          if (i) {
+            // (the last product into this accumulator has ended: this tile's S was issued behind it)
+            tmem_load(acc, sv);
+            tmem_wait(sv);
 #pragma unroll
-            for (int c = 0; c < NH; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * m[c]);
-            if constexpr (NH == 16) WAVEAL_TMEM_ST16(o_addr + c0, sv, 0);
-            else WAVEAL_TMEM_ST8(o_addr + c0, sv);
+            for (int c = 0; c < N; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * m[c]);
+            tmem_store(acc, sv);
             tc_wait_st();
           }
         }
 #pragma unroll
-        for (int c = 0; c < NH; c += 2) {
+        for (int c = 0; c < N; c += 2) {
           const float e0 = ex2(x[c] - (ref[c] == -INFINITY ? 0.f : ref[c])), e1 = ex2(x[c + 1] - (ref[c + 1] == -INFINITY ? 0.f : ref[c + 1]));
           l[c] += e0, l[c + 1] += e1;
           const uint32_t pk = pack2<T>(e0, e1);
@@ -981,13 +991,14 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         fence_proxy_async();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(B_P_FULL + 2 * slot + half));
+        if (lane == 0) mbar_arrive(BAR(B_P_FULL + buffer));
       }
 
-      // ---- epilogue: sums over the keys (a lane ends up with a row's)
+      // ---- epilogue: sums over the warp's keys
       const bool join = tiles > 1;
+      if (half && !join) return true;
 #pragma unroll
-      for (int w = NH / 2, d = 16; w >= 1; w /= 2, d /= 2) {
+      for (int w = N / 2, d = 16; w >= 1; w /= 2, d /= 2) {
 #pragma unroll
         for (int i = 0; i < w; ++i) {
           const float give = lane & d ? l[i] : l[i + w], keep = lane & d ? l[i + w] : l[i];
@@ -995,92 +1006,83 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         }
       }
 #pragma unroll
-      for (int d = 16 / NH; d >= 1; d /= 2) l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
-      const int sum_row = lane / (32 / NH);
-      if (slot) {
-        if (!join) return true;
-        if (joined && !(ok = warp_wait(ctx, BAR(B_SUMS_READ), (joined - 1) & 1, 76))) return false;
-        sm.cols.sum[quad][c0 + sum_row] = l[0];
+      for (int d = 16 / N; d >= 1; d /= 2) l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+      constexpr int kLanes = 32 / N;                 // that end up with a row's sum
+      auto& cols = sm.cols[slot];
+      if (half) {
+        if (joined_few && !(ok = warp_wait(ctx, BAR(B_COLS_READ + slot), (joined_few - 1) & 1, 76))) return false;
+        cols.sum[quad][lane / kLanes] = l[0];
         if (quad == 0 && lane == 0) {
 #pragma unroll
-          for (int c = 0; c < NH; c += 4) *reinterpret_cast<float4*>(&sm.cols.ref[c0 + c]) = make_float4(ref[c], ref[c + 1], ref[c + 2], ref[c + 3]);
+          for (int c = 0; c < N; c += 4) *reinterpret_cast<float4*>(&cols.ref[c]) = make_float4(ref[c], ref[c + 1], ref[c + 2], ref[c + 3]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(B_SUMS));
-        ++joined;
+        if (lane == 0) mbar_arrive(BAR(B_COLS + slot));
+        ++joined_few;
         return true;
       }
-      sm.warp_max[0][half][quad][sum_row] = l[0];
+      sm.warp_l[slot][quad][lane / kLanes] = l[0];
       if (!agree()) return false;
-      // row c0 + `row`
-      const int row = lane % NH;
+      const int row = lane % N;
       float my_ref = ref[0], my_l = 0.f, a0 = 1.0f, a1 = 0.f;
 #pragma unroll
-      for (int c = 1; c < NH; ++c) my_ref = row == c ? ref[c] : my_ref;
+      for (int c = 1; c < N; ++c) my_ref = row == c ? ref[c] : my_ref;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) my_l += sm.warp_max[0][half][w][row];
+      for (int w = 0; w < 4; ++w) my_l += sm.warp_l[slot][w][row];
       if (join) {
-        if (!(ok = warp_wait(ctx, BAR(B_SUMS), joined & 1, 73))) return false;
+        if (!(ok = warp_wait(ctx, BAR(B_COLS + slot), joined_few & 1, 73))) return false;
         float other = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) other += sm.cols.sum[w][c0 + row];
-        const float other_ref = sm.cols.ref[c0 + row], m = fmaxf(my_ref, other_ref);
-        ++joined;
+        for (int w = 0; w < 4; ++w) other += cols.sum[w][row];
+        const float other_ref = cols.ref[row], m = fmaxf(my_ref, other_ref);
+        ++joined_few;
         __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(B_SUMS_READ));
+        if (lane == 0) mbar_arrive(BAR(B_COLS_READ + slot));
         a0 = my_ref == -INFINITY ? 0.f : ex2(my_ref - m);
         a1 = other_ref == -INFINITY ? 0.f : ex2(other_ref - m);
         my_ref = m;
         my_l = my_l * a0 + other * a1;
-        if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + 2), (uses[2] + tiles / 2 - 1) & 1, 74))) return false;
       }
       const bool direct = im.direct;
-      const int head0 = im.head * s.group;
       if (direct) {
         const float inv = my_l == 0.f ? 0.f : 1.0f / my_l;
         a0 *= inv, a1 *= inv;
       }
-      if (quad == 0 && lane < min(rows, NH)) {
+      const int head0 = im.head * s.group;
+      if (quad == 0 && lane < rows) {
         if (!direct)
-          p.parts.ml[im.row + c0 + lane] = make_float2(my_ref, my_l);
+          p.parts.ml[im.row + lane] = make_float2(my_ref, my_l);
         else if (p.lse)
-          p.lse[(long long)(head0 + (c0 + lane) % s.group) * s.tokens + im.token + (c0 + lane) / s.group] =
+          p.lse[(long long)(head0 + lane % s.group) * s.tokens + im.token + lane / s.group] =
               my_l == 0.f ? -INFINITY : (my_ref + log2f(my_l)) * 0.69314718055994531f;
       }
-      if (!(ok = warp_wait(ctx, BAR(B_PV_DONE), (uses[0] + (tiles + 1) / 2 - 1) & 1, 75))) return false;
+      if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + buffer), (use0 + mine - 1) & 1, 75))) return false;
+      if (join && !(ok = warp_wait(ctx, BAR(B_PV_DONE + buffer + 1), (other0 + tiles / 2 - 1) & 1, 74))) return false;
       tc_fence_after();
-      uint32_t v[NH], w[NH];
-      if constexpr (NH == 16) {
-        WAVEAL_TMEM_LD16(o_addr + c0, v, 0);
-        WAVEAL_TMEM_LD16(o_addr + kTile + c0, w, 0);             // (without a tile in slot 1: not used)
-        WAVEAL_TMEM_WAIT_LD16(v, 0);
-        WAVEAL_TMEM_WAIT_LD16(w, 0);
-      } else {
-        WAVEAL_TMEM_LD8(o_addr + c0, v);
-        WAVEAL_TMEM_LD8(o_addr + kTile + c0, w);
-        WAVEAL_TMEM_WAIT_LD8(v);
-        WAVEAL_TMEM_WAIT_LD8(w);
-      }
+      uint32_t v[NL], w[NL];
+      tmem_load(acc, v);
+      tmem_load(acc + 64, w);                        // (of one tile alone: not used)
+      tmem_wait(v);
+      tmem_wait(w);
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(BAR(B_O_EMPTY));
-        if (join) mbar_arrive(BAR(B_O_EMPTY + 1));
-      }
-      int g = c0 % s.group, tok = im.token + c0 / s.group;
+      if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + slot)), mbar_arrive(BAR(B_O_EMPTY + slot));
+      float* part = p.parts.o + (long long)im.row * D + r;
+      T* out = static_cast<T*>(p.o) + head0 * p.o_stride_h + im.token * p.o_stride_t + r;
+      const long long next_token = p.o_stride_t - (s.group - 1) * p.o_stride_h;
+      int g = 0;
 #pragma unroll
-      for (int i = 0; i < NH; ++i) {
+      for (int i = 0; i < N; ++i) {
         const float b0 = __shfl_sync(0xffffffffu, a0, i), b1 = __shfl_sync(0xffffffffu, a1, i);
         float y = __uint_as_float(v[i]) * b0;
         if (join) y += __uint_as_float(w[i]) * b1;
         if (i < rows && r < D) {
-          if (direct)
-            *reinterpret_cast<unsigned short*>(static_cast<T*>(p.o) + (head0 + g) * p.o_stride_h + tok * p.o_stride_t + r) =
-                (unsigned short)pack2<T>(y, 0.f);
-          else
-            p.parts.o[(long long)(im.row + c0 + i) * D + r] = y;
+          if (direct) *reinterpret_cast<unsigned short*>(out) = (unsigned short)pack2<T>(y, 0.f);
+          else *part = y;
         }
-        if (++g == s.group) g = 0, ++tok;
+        part += D;
+        if (++g == s.group) g = 0, out += next_token;
+        else out += p.o_stride_h;
       }
       return true;
     };
@@ -1097,11 +1099,17 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     while (ok && next_item(im)) {
       const bool wide = im->wide;
       const int tiles = im->tiles, all = im->keys - im->first_key;
-      if (im->columns) {
-        if (im->columns == 16) few_rows(std::integral_constant<int, 8>{}, *im);
-        else few_rows(std::integral_constant<int, 16>{}, *im);
-        if (!ok) break;
-        uses[0] += (tiles + 1) / 2, uses[1] += (tiles + 1) / 2, uses[2] += tiles / 2, uses[3] += tiles / 2;
+      if (im->few) {
+        const int in = im->slot;
+        if (in == slot) {
+          const int rows = im->n0 * s.group;
+          const uint32_t use0 = slot ? uses[2 + half] : uses[half], other0 = slot ? uses[3] : uses[1];
+          if (rows <= 4) few_rows(std::integral_constant<int, 4>{}, *im, use0, other0);
+          else if (rows <= 8) few_rows(std::integral_constant<int, 8>{}, *im, use0, other0);
+          else few_rows(std::integral_constant<int, 16>{}, *im, use0, other0);
+          if (!ok) break;
+        }
+        (in ? uses[2] : uses[0]) += (tiles + 1) / 2, (in ? uses[3] : uses[1]) += tiles / 2;
         item_done();
         continue;
       }
@@ -1310,25 +1318,23 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
 // ------------------------------------------------------------------ parts -> output
 
-// WARPS warps a row (a token's query head), each with every WARPS-th part.
+// WARPS warps a row (a token's query head), with every WARPS-th part each.  The parts' references and sums are read a lane each, so that
+// only one round trip stands before the loads of the parts themselves, which do not wait for each other.
 template <int D, class T, int WARPS>
 __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Params p) {
   constexpr int C = D / 32;                          // channels of a lane
   const Shape& s = p.s;
-  const int heads = s.kv_heads * s.group, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const long long id = (long long)blockIdx.x * (4 / WARPS) + warp / WARPS;
-  const int token = (int)(id / heads), head = (int)(id - (long long)token * heads), h = head / s.group, g = head - h * s.group;
-  const int part0 = WARPS > 1 ? warp : 0;
-  __shared__ float2 ml_sh[4];
+  const unsigned heads = s.kv_heads * s.group, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const unsigned id = blockIdx.x * (4 / WARPS) + warp / WARPS;
+  const int token = id / heads, head = id - token * heads, h = head / s.group, g = head - h * s.group;
   __shared__ float o_sh[WARPS > 1 ? 3 : 1][D];
   waveal::wait_for_previous_kernel();
   bool mine = token < s.tokens;
 
   // whose token is it (a token of no sequence is left alone)
   Sequence q = {0, 0, 0};
-  int b = 0;
   if (mine) {
-    b = (int)min((long long)token * s.batch / s.tokens, (long long)s.batch - 1);
+    int b = (int)((unsigned long long)token * s.batch / s.tokens);
     q = read_sequence(s, b, nullptr);
     if (token < q.start || token >= q.start + q.n) {
       int l = 0, r = s.batch - 1;
@@ -1336,8 +1342,7 @@ __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Para
         const int m = (l + r + 1) >> 1;
         if (s.seq_start[m] <= token) l = m; else r = m - 1;
       }
-      b = l;
-      q = read_sequence(s, b, nullptr);
+      q = read_sequence(s, l, nullptr);
     }
     mine = token >= q.start && token < q.start + q.n;
   }
@@ -1347,77 +1352,59 @@ __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Para
   for (int i = 0; i < C; ++i) acc[i] = 0.f;
   bool written = false;
   if (mine) {
-    const PrefixLine line(s);
-    const long long own_total = *p.parts.total;
-    const Cuts cuts(max(line.total() + own_total, 1ll), s.ctas);
-    int seen = 0;                                    // parts so far, over all warps
-    auto add_unit = [&](long long row, bool whole, long long at, int tiles, int weight) {
-      if (!tiles) return;
-      const int c0 = whole ? 0 : cuts.piece(at), c1 = whole ? 0 : cuts.piece(at + (long long)(tiles - 1) * weight);
-      for (int c = c0; c <= c1; ++c) {
-        if (!whole && first_tile(cuts.begin(c), at, tiles, weight) >= first_tile(cuts.begin(c + 1), at, tiles, weight)) continue;
-        if (WARPS > 1 && seen++ % WARPS != part0) continue;
-        const long long at_row = part_row(s, row, c);
-        const float2 ml = p.parts.ml[at_row];
-        float v[C];
-        const float* src = p.parts.o + at_row * D + lane * C;
+    int2 shared = {0, -1}, own = {0, -1};            // pieces
+    if (s.prefix_len) shared = p.parts.pieces[h * s.tokens + token / (2 * s.tq) * 2 * s.tq];
+    const int first = (token - q.start) / (2 * s.tq) * 2 * s.tq;
+    if ((s.causal ? q.len - q.n + min(q.n, first + 2 * s.tq) : q.len) > 0) own = p.parts.pieces[(s.tokens + q.start) * s.kv_heads + h * q.n + first];
+    const int n0 = shared.y - shared.x + 1, n = n0 + own.y - own.x + 1;
+    written = s.prefix_len == 0 && n == 1;
+    const long long row0 = part_row(s, prefix_row(s, h, token) + g, shared.x), row1 = part_row(s, own_row(s, q, h, token - q.start) + g, own.x);
+    for (int base = 0; base < n && !written; base += 32) {
+      const int k = base + lane;
+      const long long at = k < n0 ? part_row(s, row0, k) : part_row(s, row1, k - n0);
+      const float2 ml = k < n ? p.parts.ml[at] : make_float2(-INFINITY, 0.f);
+      float to = fmaxf(m, ml.x);
+#pragma unroll
+      for (int d = 16; d >= 1; d /= 2) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
+      const float scale = m == -INFINITY ? 0.f : ex2(m - to), weight = ml.x == -INFINITY ? 0.f : ex2(ml.x - to);
+      float sum = ml.y * weight;
+#pragma unroll
+      for (int d = 16; d >= 1; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      m = to;
+      l = l * scale + sum;
+#pragma unroll
+      for (int i = 0; i < C; ++i) acc[i] *= scale;
+      const int count = min(32, n - base);
+#pragma unroll 4
+      for (int j = WARPS > 1 ? warp : 0; j < count; j += WARPS) {
+        const float w = __shfl_sync(0xffffffffu, weight, j);
+        const float* src = p.parts.o + __shfl_sync(0xffffffffu, at, j) * D + lane * C;
         if constexpr (C == 4) {
           const float4 x = *reinterpret_cast<const float4*>(src);
-          v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+          acc[0] += x.x * w, acc[1] += x.y * w, acc[2] += x.z * w, acc[3] += x.w * w;
         } else {
           const float2 x = *reinterpret_cast<const float2*>(src);
-          v[0] = x.x, v[1] = x.y;
+          acc[0] += x.x * w, acc[1] += x.y * w;
         }
-        const float to = fmaxf(m, ml.x);
-        const float a = m == -INFINITY ? 0.f : ex2(m - to), e = ml.x == -INFINITY ? 0.f : ex2(ml.x - to);
-        m = to;
-        l = l * a + ml.y * e;
-#pragma unroll
-        for (int i = 0; i < C; ++i) acc[i] = acc[i] * a + v[i] * e;
       }
-    };
-    if (line.tiles) {
-      const int u = h * line.per_head + token / (2 * s.tq);
-      add_unit(prefix_row(s, h, token) + g, u < line.whole, u < line.whole ? 0 : line.at(u), line.tiles, line.weight(token / (2 * s.tq)));
-    }
-    if (q.len) {
-      const int i = (token - q.start) / (2 * s.tq);
-      long long at = line.total() + p.parts.own_base[b] + h * own_head_cost(s, q);
-      if (s.causal) {
-        for (int k = 0; k < i; ++k) at += own_unit(s, q, k).cost;
-      } else {
-        at += (long long)i * own_unit(s, q, 0).cost;
-      }
-      const OwnUnit u = own_unit(s, q, i);
-      written = line.tiles == 0 && u.tiles && cuts.piece(at) == cuts.piece(at + (long long)(u.tiles - 1) * u.weight);
-      if (!written) add_unit(own_row(s, q, h, token - q.start) + g, false, at, u.tiles, u.weight);
     }
   }
   if constexpr (WARPS > 1) {
-    if (lane == 0) ml_sh[warp] = make_float2(m, l);
     if (warp) {
 #pragma unroll
       for (int i = 0; i < C; ++i) o_sh[warp - 1][lane * C + i] = acc[i];
     }
     __syncthreads();
     if (warp) return;
-    float to = m;
-    for (int w = 1; w < 4; ++w) to = fmaxf(to, ml_sh[w].x);
-    const float a = m == -INFINITY ? 0.f : ex2(m - to);
-    l *= a;
 #pragma unroll
-    for (int i = 0; i < C; ++i) acc[i] *= a;
     for (int w = 1; w < 4; ++w) {
-      const float e = ml_sh[w].x == -INFINITY ? 0.f : ex2(ml_sh[w].x - to);
-      l += ml_sh[w].y * e;
 #pragma unroll
-      for (int i = 0; i < C; ++i) acc[i] += o_sh[w - 1][lane * C + i] * e;
+      for (int i = 0; i < C; ++i) acc[i] += o_sh[w - 1][lane * C + i];
     }
-    m = to;
   }
   if (!mine || written) return;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  T* o = static_cast<T*>(p.o) + head * p.o_stride_h + (long long)token * p.o_stride_t + lane * C;
+  T* o = static_cast<T*>(p.o) + head * p.o_stride_h + token * p.o_stride_t + lane * C;
   if constexpr (C == 4)
     *reinterpret_cast<uint2*>(o) = make_uint2(pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv));
   else
@@ -1470,16 +1457,15 @@ int sm_count() {
 // pieces of the line that room is made for, whatever the device (more SMs than this are not used)
 constexpr int kMaxCtas = 192;
 
-struct Layout { size_t total, own_base, ml, o, bytes; };
+struct Layout { size_t pieces, ml, o, bytes; };
 
 Layout layout(const waveal_cache_desc* c, const waveal_batch_desc* b) {
   const int group = b->q_heads / c->kv_heads;
   const size_t rows = (size_t)b->tokens * b->q_heads * 2 + (size_t)kMaxCtas * 2 * (kTile / group) * group;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   Layout l;
-  l.total = 0;
-  l.own_base = 256;
-  l.ml = l.own_base + up((size_t)b->batch * sizeof(long long));
+  l.pieces = 0;
+  l.ml = up((size_t)b->tokens * c->kv_heads * 2 * sizeof(int2));
   l.o = l.ml + up(rows * sizeof(float2));
   l.bytes = l.o + up(rows * c->head_dim * sizeof(float));
   return l;
@@ -1571,8 +1557,7 @@ extern "C" waveal_status waveal_prefix_attn(const waveal_cache_desc* c, const wa
   p.s.seq_start = seq_start, p.s.kv_len = kv_len;
   p.s.ctas = std::min(sms, kMaxCtas);
   char* w = static_cast<char*>(ws);
-  p.parts.total = reinterpret_cast<long long*>(w + l.total);
-  p.parts.own_base = reinterpret_cast<long long*>(w + l.own_base);
+  p.parts.pieces = reinterpret_cast<int2*>(w + l.pieces);
   p.parts.ml = reinterpret_cast<float2*>(w + l.ml);
   p.parts.o = reinterpret_cast<float*>(w + l.o);
   p.page_table = page_table, p.prefix_pages = prefix_pages;
