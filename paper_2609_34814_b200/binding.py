@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -110,13 +111,11 @@ def load() -> ctypes.CDLL:
         lib.waveal_bsattn_fwd.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, P, P, P, ctypes.c_float, P,
                                           ctypes.c_size_t, P, P]
         lib.waveal_rope_freqs.argtypes = [I32, ctypes.c_double, ctypes.c_int, ctypes.c_double, I64, P, ctypes.POINTER(ctypes.c_float)]
-        lib.waveal_rope.argtypes = [ctypes.POINTER(RopeDesc), P, P, P, P, P, P, P]
-        lib.waveal_cache_append.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc), ctypes.POINTER(Rotation),
-                                            ctypes.POINTER(AppendStrides), P, P, P, P, P, P, P, P, P, P, P, P, P]
-        lib.waveal_prefix_attn_workspace_bytes.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc),
-                                                           ctypes.POINTER(ctypes.c_size_t)]
-        lib.waveal_prefix_attn.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc), P, ctypes.POINTER(I64), P, P, P,
-                                           ctypes.POINTER(I64), P, P, P, P, P, ctypes.c_float, P, ctypes.c_size_t, P, P]
+        # (the descriptors of these come as packed bytes: half the host's time of structures filled field by field)
+        lib.waveal_rope.argtypes = [P] * 8
+        lib.waveal_cache_append.argtypes = [P] * 17
+        lib.waveal_prefix_attn_workspace_bytes.argtypes = [P, P, ctypes.POINTER(ctypes.c_size_t)]
+        lib.waveal_prefix_attn.argtypes = [P] * 13 + [ctypes.c_float, P, ctypes.c_size_t, P, P]
         for name in ["waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
                      "waveal_plan_workspace_bytes", "waveal_plan_bitmap", "waveal_plan_csr", "waveal_bitmap_to_csr",
                      "waveal_gather_rows", "waveal_scatter_rows", "waveal_bsattn_workspace_bytes", "waveal_bsattn_fwd", "waveal_default_wave_size",
@@ -360,23 +359,39 @@ PREFIX_CAUSAL = 1
 PREFIX_SELFTEST_LOST_TILE = 256
 
 
-_dtypes = None
+_torch = None
+_dtypes = {}
+
+
+def _load_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _dtypes.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32})
+        _torch = torch
+    return _torch
+
+
+# waveal_rotation, waveal_rope_desc, waveal_cache_desc, waveal_batch_desc, waveal_append_strides as the C compiler lays them out
+_ROTATION = struct.Struct("iii3iif")
+_ROPE = struct.Struct("5i" + "iii3iif" + "8q")
+_CACHE = struct.Struct("5i6q")
+_BATCH = struct.Struct("6iq")
+_STRIDES = struct.Struct("8q")
+_PAIR = struct.Struct("2q")
 
 
 def _dtype(t) -> int:
-    global _dtypes
-    if _dtypes is None:
-        import torch
-        _dtypes = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
-    if t.dtype not in _dtypes:
+    d = _dtypes.get(t.dtype)
+    if d is None:
         raise TypeError(f"{t.dtype} is not supported")
-    return _dtypes[t.dtype]
+    return d
 
 
 def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained_len: int = 0, device="cuda"):
     """waveal_rope_freqs.  Returns (freqs, amplitude): an int64 tensor of rot_dim/2 phase steps on `device` and the
     factor that the scaling puts on the rotated channels.  Several axes: one call each, torch.cat of the steps."""
-    import torch
+    torch = _load_torch()
     freqs = torch.empty((rot_dim // 2,), dtype=torch.int64)
     amplitude = ctypes.c_float(1.0)
     _check(load().waveal_rope_freqs(rot_dim, base, ROPE_SCALINGS[scaling], factor, trained_len, freqs.data_ptr(),
@@ -384,48 +399,46 @@ def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "none", facto
     return freqs.to(device), float(amplitude.value)
 
 
-def _rotation(freqs, interleaved, axis_pairs, amplitude, inverse=False) -> Rotation:
+def _rotation(freqs, interleaved, axis_pairs, amplitude, inverse=False):
+    """the numbers of a waveal_rotation"""
+    if freqs.dtype is not _torch.int64 or not freqs.is_cuda or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise TypeError("freqs must be a contiguous int64 cuda tensor [rot_dim/2]")
     pairs = freqs.shape[0]
-    n = len(axis_pairs) if axis_pairs is not None else 1
+    if axis_pairs is None:
+        return 2 * pairs, 1 if interleaved else 0, 1, pairs, 0, 0, 1 if inverse else 0, amplitude
+    n = len(axis_pairs)
     if n > 3:
         raise ValueError("at most three axes")
-    own = (pairs, 0, 0) if axis_pairs is None else (*axis_pairs, 0, 0)[:3]
-    return Rotation(2 * pairs, 1 if interleaved else 0, n, own, 1 if inverse else 0, amplitude)
+    return (2 * pairs, 1 if interleaved else 0, n, axis_pairs[0], axis_pairs[1] if n > 1 else 0, axis_pairs[2] if n > 2 else 0,
+            1 if inverse else 0, amplitude)
 
 
-def _int32(t, name):
-    import torch
-    if t is not None and (t.dtype != torch.int32 or not t.is_cuda):
-        raise TypeError(f"{name} must be an int32 cuda tensor")
-    return t
-
-
-def _rows(name, t, head_dim=None):
-    """strides {head, token} of a [heads, tokens, head_dim] cuda tensor"""
-    if t.dim() != 3 or not t.is_cuda:
+def _rows(name, t):
+    """strides of a [heads, tokens, head_dim] cuda tensor"""
+    st = t.stride()
+    if len(st) != 3 or not t.is_cuda:
         raise ValueError(f"{name} must be a [heads, tokens, head_dim] cuda tensor")
-    h, n, d = t.stride()
-    if d != 1 and t.shape[2] > 1:
+    if st[2] != 1 and t.shape[2] > 1:
         raise ValueError(f"{name}: head_dim must be contiguous")
-    if head_dim is not None and t.shape[2] != head_dim:
-        raise ValueError(f"{name} has head_dim {t.shape[2]}, expected {head_dim}")
-    return h, n
+    return st
+
+
+def _output(name, out, like):
+    """a new tensor like `like`, or the caller's"""
+    if out is None:
+        return _torch.empty_like(like)
+    if out.shape != like.shape or out.dtype is not like.dtype:
+        raise ValueError(f"{name} must have its input's shape and type")
+    return out
 
 
 def _positions(positions, axes, tokens):
-    _int32(positions, "positions")
-    if positions.dim() == 1:
-        positions = positions[None]
-    if tuple(positions.shape) != (axes, tokens) or not positions.is_contiguous():
-        raise ValueError(f"positions must be contiguous [{axes}, {tokens}], got {tuple(positions.shape)}")
-    return positions
-
-
-def _freqs(freqs):
-    import torch
-    if freqs.dtype != torch.int64 or not freqs.is_cuda or freqs.dim() != 1 or not freqs.is_contiguous():
-        raise TypeError("freqs must be a contiguous int64 cuda tensor [rot_dim/2]")
-    return freqs
+    if positions.dtype is not _torch.int32 or not positions.is_cuda:
+        raise TypeError("positions must be an int32 cuda tensor")
+    shape = positions.shape
+    if not (shape == (axes, tokens) or (axes == 1 and shape == (tokens,))) or not positions.is_contiguous():
+        raise ValueError(f"positions must be contiguous [{axes}, {tokens}], got {tuple(shape)}")
+    return positions.data_ptr()
 
 
 def rope(q, positions, freqs, k=None, q_out=None, k_out=None, interleaved: bool = False, axis_pairs=None, amplitude: float = 1.0,
@@ -434,28 +447,25 @@ def rope(q, positions, freqs, k=None, q_out=None, k_out=None, interleaved: bool 
     [tokens, heads, head_dim] tensor is passed as x.transpose(0, 1)); positions: int32 [axes, tokens] ([tokens] for one axis);
     freqs: from rope_freqs.  Returns (q_out, k_out): new tensors unless given (q_out=q turns in place).  inverse=True is the
     gradient: pass those of the outputs, get those of the inputs."""
-    import torch
-    rot = _rotation(_freqs(freqs), interleaved, axis_pairs, amplitude, inverse)
-    d = RopeDesc()
-    d.q_heads, d.tokens, d.head_dim = q.shape
-    d.dtype = _dtype(q)
-    d.rot = rot
-    positions = _positions(positions, rot.axes, d.tokens)
-    if q_out is None:
-        q_out = torch.empty_like(q)
-    d.q_stride, d.q_out_stride = _rows("q", q), _rows("q_out", q_out)
-    if q_out.shape != q.shape or q_out.dtype != q.dtype:
-        raise ValueError("q_out must have q's shape and type")
-    if k is not None:
-        if k.shape[1:] != q.shape[1:] or k.dtype != q.dtype:
+    _load_torch()
+    rot = _rotation(freqs, interleaved, axis_pairs, amplitude, inverse)
+    q_st = _rows("q", q)
+    heads, tokens, dim = q.shape
+    at = _positions(positions, rot[2], tokens)
+    q_out = _output("q_out", q_out, q)
+    qo_st = _rows("q_out", q_out)
+    if k is None:
+        k_heads, k_ptr, ko_ptr, k_st, ko_st, k_out = 0, None, None, (0, 0), (0, 0), None
+    else:
+        k_st = _rows("k", k)
+        k_heads = k.shape[0]
+        if k.shape[1] != tokens or k.shape[2] != dim or k.dtype is not q.dtype:
             raise ValueError("k must have q's tokens, head_dim and type")
-        if k_out is None:
-            k_out = torch.empty_like(k)
-        if k_out.shape != k.shape or k_out.dtype != k.dtype:
-            raise ValueError("k_out must have k's shape and type")
-        d.k_heads = k.shape[0]
-        d.k_stride, d.k_out_stride = _rows("k", k), _rows("k_out", k_out)
-    _check(load().waveal_rope(ctypes.byref(d), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), _ptr(positions), _ptr(freqs), _stream(stream)))
+        k_out = _output("k_out", k_out, k)
+        ko_st = _rows("k_out", k_out)
+        k_ptr, ko_ptr = k.data_ptr(), k_out.data_ptr()
+    desc = _ROPE.pack(tokens, dim, heads, k_heads, _dtype(q), *rot, q_st[0], q_st[1], qo_st[0], qo_st[1], k_st[0], k_st[1], ko_st[0], ko_st[1])
+    _check(load().waveal_rope(desc, q.data_ptr(), q_out.data_ptr(), k_ptr, ko_ptr, at, freqs.data_ptr(), _stream(stream)))
     return q_out, k_out
 
 
@@ -464,27 +474,33 @@ class PagedCache:
     contiguous, any other strides ([n_pages, page_size, kv_heads, head_dim] tensors are passed as x.transpose(1, 2))."""
 
     def __init__(self, k, v):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not (k.is_cuda and v.is_cuda):
+        _load_torch()
+        shape, ks, vs = k.shape, k.stride(), v.stride()
+        if len(ks) != 4 or shape != v.shape or k.dtype is not v.dtype or not (k.is_cuda and v.is_cuda):
             raise ValueError("k and v must be cuda tensors [n_pages, kv_heads, page_size, head_dim] of one shape and type")
-        if k.stride(3) != 1 or v.stride(3) != 1:
+        if ks[3] != 1 or vs[3] != 1:
             raise ValueError("head_dim must be contiguous")
-        self.k, self.v = k, v
-        n, h, page, dim = k.shape
-        self.desc = CacheDesc(n, page, h, dim, _dtype(k), k.stride()[:3], v.stride()[:3])
+        self.k, self.v, self.dtype = k, v, k.dtype
+        self.n_pages, self.kv_heads, self.page_size, self.head_dim = shape
+        self.desc = _CACHE.pack(shape[0], shape[2], shape[1], shape[3], _dtype(k), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
 
 
-def _batch(q_heads, tokens, seq_start, kv_len, page_table, prefix_len, flags=0) -> BatchDesc:
+def batch_desc(q_heads: int, tokens: int, seq_start, kv_len, page_table=None, prefix_len: int = 0, flags: int = 0) -> bytes:
+    """The waveal_batch_desc of a call, from its tensors."""
+    int32 = _load_torch().int32
     batch = kv_len.shape[0]
-    _int32(kv_len, "kv_len"), _int32(seq_start, "seq_start")
+    if kv_len.dtype is not int32 or seq_start.dtype is not int32 or not (kv_len.is_cuda and seq_start.is_cuda):
+        raise TypeError("seq_start and kv_len must be int32 cuda tensors")
     if seq_start.shape != (batch + 1,) or kv_len.dim() != 1 or not (seq_start.is_contiguous() and kv_len.is_contiguous()):
         raise ValueError("seq_start must be a contiguous [batch + 1], kv_len a contiguous [batch]")
     if page_table is None:
-        return BatchDesc(batch, tokens, q_heads, 0, prefix_len, flags, 0)
-    _int32(page_table, "page_table")
-    if page_table.dim() != 2 or page_table.shape[0] != batch or page_table.stride(1) != 1 and page_table.shape[1] > 1:
+        return _BATCH.pack(batch, tokens, q_heads, 0, prefix_len, flags, 0)
+    if page_table.dtype is not int32 or not page_table.is_cuda:
+        raise TypeError("page_table must be an int32 cuda tensor")
+    pages, st = page_table.shape, page_table.stride()
+    if len(st) != 2 or pages[0] != batch or st[1] != 1 and pages[1] > 1:
         raise ValueError("page_table must be [batch, pages], a row's pages contiguous")
-    return BatchDesc(batch, tokens, q_heads, page_table.shape[1], prefix_len, flags, max(page_table.stride(0), page_table.shape[1]) if batch < 2
-                     else page_table.stride(0))
+    return _BATCH.pack(batch, tokens, q_heads, pages[1], prefix_len, flags, st[0] if batch > 1 else max(st[0], pages[1]))
 
 
 def cache_append(cache: PagedCache, k, v, seq_start, kv_len, page_table, positions=None, freqs=None, q=None, q_out=None,
@@ -492,39 +508,42 @@ def cache_append(cache: PagedCache, k, v, seq_start, kv_len, page_table, positio
     """waveal_cache_append.  k, v: [kv_heads, tokens, head_dim] of the new tokens; kv_len counts them in.  With freqs the keys
     are rotated on the way (positions None: prefix_len + place among the sequence's own keys), and q [q_heads, tokens, head_dim],
     where given, into q_out (a new tensor unless given; q_out=q turns in place), which is returned."""
-    import torch
-    d = cache.desc
-    heads, tokens, dim = k.shape
-    if v.shape != k.shape or heads != d.kv_heads or dim != d.head_dim:
+    _load_torch()
+    k_st, v_st = _rows("k", k), _rows("v", v)
+    shape = k.shape
+    heads, tokens, dim = shape
+    if v.shape != shape or heads != cache.kv_heads or dim != cache.head_dim:
         raise ValueError("k and v must be [kv_heads, tokens, head_dim] of the cache")
-    if k.dtype != cache.k.dtype or v.dtype != cache.k.dtype:
+    if k.dtype is not cache.dtype or v.dtype is not cache.dtype:
         raise TypeError("k and v must have the cache's type")
-    strides = AppendStrides()
-    strides.k, strides.v = _rows("k", k), _rows("v", v)
-    rot = None
+    rot = freqs_ptr = at = q_ptr = qo_ptr = None
     if freqs is not None:
-        rot = _rotation(_freqs(freqs), interleaved, axis_pairs, amplitude)
+        numbers = _rotation(freqs, interleaved, axis_pairs, amplitude)
+        rot, freqs_ptr = _ROTATION.pack(*numbers), freqs.data_ptr()
         if positions is not None:
-            positions = _positions(positions, rot.axes, tokens)
+            at = _positions(positions, numbers[2], tokens)
+    q_heads, q_st, qo_st = 0, (0, 0), (0, 0)
     if q is not None:
-        if q.shape[1:] != k.shape[1:] or q.dtype != k.dtype:
+        q_st = _rows("q", q)
+        q_heads = q.shape[0]
+        if q.shape[1] != tokens or q.shape[2] != dim or q.dtype is not k.dtype:
             raise ValueError("q must have k's tokens, head_dim and type")
-        if q_out is None:
-            q_out = torch.empty_like(q)
-        if q_out.shape != q.shape or q_out.dtype != q.dtype:
-            raise ValueError("q_out must have q's shape and type")
-        strides.q, strides.q_out = _rows("q", q), _rows("q_out", q_out)
-    b = _batch(0 if q is None else q.shape[0], tokens, seq_start, kv_len, page_table, prefix_len)
-    _check(load().waveal_cache_append(ctypes.byref(d), ctypes.byref(b), None if rot is None else ctypes.byref(rot), ctypes.byref(strides),
-                                      _ptr(k), _ptr(v), _ptr(q), _ptr(q_out), _ptr(cache.k), _ptr(cache.v), _ptr(seq_start), _ptr(kv_len),
-                                      _ptr(page_table), _ptr(positions), _ptr(freqs), _ptr(dev_status), _stream(stream)))
+        q_out = _output("q_out", q_out, q)
+        qo_st = _rows("q_out", q_out)
+        q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
+    batch = batch_desc(q_heads, tokens, seq_start, kv_len, page_table, prefix_len)
+    strides = _STRIDES.pack(k_st[0], k_st[1], v_st[0], v_st[1], q_st[0], q_st[1], qo_st[0], qo_st[1])
+    _check(load().waveal_cache_append(cache.desc, batch, rot, strides, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, cache.k.data_ptr(),
+                                      cache.v.data_ptr(), seq_start.data_ptr(), kv_len.data_ptr(), _ptr(page_table), at, freqs_ptr,
+                                      _ptr(dev_status), _stream(stream)))
     return q_out
 
 
-def prefix_attn_workspace_bytes(cache: PagedCache, batch: BatchDesc) -> int:
+def prefix_attn_workspace_bytes(cache: PagedCache, batch: bytes) -> int:
+    """Bytes for prefix_attn's workspace; batch: batch_desc of the call."""
     n = ctypes.c_size_t(0)
-    _check(load().waveal_prefix_attn_workspace_bytes(ctypes.byref(cache.desc), ctypes.byref(batch), ctypes.byref(n)))
-    return int(n.value)
+    _check(load().waveal_prefix_attn_workspace_bytes(cache.desc, batch, ctypes.byref(n)))
+    return n.value
 
 
 def prefix_attn(cache: PagedCache, q, seq_start, kv_len, page_table=None, prefix_pages=None, prefix_len: int = 0, o=None, lse=None,
@@ -532,28 +551,32 @@ def prefix_attn(cache: PagedCache, q, seq_start, kv_len, page_table=None, prefix
     """waveal_prefix_attn.  q: [q_heads, tokens, head_dim], the new tokens of all sequences one after another; prefix_pages:
     int32 pages of the first prefix_len keys, seen by all; page_table int32 [batch, pages] and kv_len: each sequence's
     own keys, its new ones last.  Returns o (laid out like q unless given), or (o, lse) with return_lse."""
-    import torch
-    lib = load()
+    torch = _load_torch()
+    q_st = _rows("q", q)
     heads, tokens, dim = q.shape
-    if q.dtype != cache.k.dtype:
+    if q.dtype is not cache.dtype:
         raise TypeError("q must have the cache's type")
-    b = _batch(heads, tokens, seq_start, kv_len, page_table, prefix_len, (PREFIX_CAUSAL if causal else 0) | flags)
+    if dim != cache.head_dim:
+        raise ValueError(f"q has head_dim {dim}, the cache {cache.head_dim}")
+    batch = batch_desc(heads, tokens, seq_start, kv_len, page_table, prefix_len, (PREFIX_CAUSAL if causal else 0) | flags)
+    prefix_ptr = None
     if prefix_pages is not None:
-        _int32(prefix_pages, "prefix_pages")
-        if prefix_pages.dim() != 1 or not prefix_pages.is_contiguous() or prefix_pages.shape[0] * cache.desc.page_size < prefix_len:
+        if prefix_pages.dtype is not torch.int32 or not prefix_pages.is_cuda:
+            raise TypeError("prefix_pages must be an int32 cuda tensor")
+        if prefix_pages.dim() != 1 or not prefix_pages.is_contiguous() or prefix_pages.shape[0] * cache.page_size < prefix_len:
             raise ValueError("prefix_pages must be a contiguous list of all of the prefix's pages")
-    if o is None:
-        o = torch.empty_like(q)
-    if o.shape != q.shape or o.dtype != q.dtype:
-        raise ValueError("o must have q's shape and type")
-    if lse is None and return_lse:
-        lse = torch.empty((heads, tokens), dtype=torch.float32, device=q.device)
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (heads, tokens) or not lse.is_contiguous()):
+        prefix_ptr = prefix_pages.data_ptr()
+    o = _output("o", o, q)
+    o_st = _rows("o", o)
+    if lse is None:
+        if return_lse:
+            lse = q.new_empty((heads, tokens), dtype=torch.float32)
+    elif lse.dtype is not torch.float32 or lse.shape != (heads, tokens) or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 [q_heads, tokens]")
     if workspace is None:
-        workspace = torch.empty((prefix_attn_workspace_bytes(cache, b),), dtype=torch.uint8, device=q.device)
-    qs, os_ = (ctypes.c_int64 * 2)(*_rows("q", q, cache.desc.head_dim)), (ctypes.c_int64 * 2)(*_rows("o", o))
-    _check(lib.waveal_prefix_attn(ctypes.byref(cache.desc), ctypes.byref(b), _ptr(q), qs, _ptr(cache.k), _ptr(cache.v), _ptr(o), os_,
-                                  _ptr(lse), _ptr(seq_start), _ptr(kv_len), _ptr(page_table), _ptr(prefix_pages), ctypes.c_float(scale),
-                                  _ptr(workspace), workspace.numel(), _ptr(dev_status), _stream(stream)))
+        workspace = q.new_empty((prefix_attn_workspace_bytes(cache, batch),), dtype=torch.uint8)
+    _check(load().waveal_prefix_attn(cache.desc, batch, q.data_ptr(), _PAIR.pack(q_st[0], q_st[1]), cache.k.data_ptr(), cache.v.data_ptr(),
+                                     o.data_ptr(), _PAIR.pack(o_st[0], o_st[1]), _ptr(lse), seq_start.data_ptr(), kv_len.data_ptr(),
+                                     _ptr(page_table), prefix_ptr, scale, workspace.data_ptr(), workspace.numel(), _ptr(dev_status),
+                                     _stream(stream)))
     return (o, lse) if return_lse else o

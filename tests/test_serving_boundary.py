@@ -22,6 +22,15 @@ def test_struct_layouts():
     assert ctypes.sizeof(wb.CacheDesc) == 72 and wb.CacheDesc.k_stride.offset == 24
     assert ctypes.sizeof(wb.BatchDesc) == 32 and wb.BatchDesc.table_stride.offset == 24
     assert ctypes.sizeof(wb.AppendStrides) == 64
+    # what the binding packs is laid out the same
+    assert (wb._ROTATION.size, wb._ROPE.size, wb._CACHE.size, wb._BATCH.size, wb._STRIDES.size) == (32, 120, 72, 32, 64)
+    d = wb.RopeDesc.from_buffer_copy(wb._ROPE.pack(1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 1.5, 21, 22, 23, 24, 25, 26, 27, 28))
+    assert (d.tokens, d.dtype, d.rot.rot_dim, d.rot.axis_pairs[2], d.rot.inverse, d.rot.amplitude) == (1, 5, 6, 11, 12, 1.5)
+    assert (d.q_stride[0], d.q_out_stride[1], d.k_out_stride[1]) == (21, 24, 28)
+    c = wb.CacheDesc.from_buffer_copy(wb._CACHE.pack(1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11))
+    assert (c.n_pages, c.page_size, c.kv_heads, c.head_dim, c.dtype, c.k_stride[0], c.v_stride[2]) == (1, 2, 3, 4, 5, 6, 11)
+    b = wb.BatchDesc.from_buffer_copy(wb._BATCH.pack(1, 2, 3, 4, 5, 6, 7))
+    assert (b.batch, b.tokens, b.q_heads, b.max_pages, b.prefix_len, b.flags, b.table_stride) == (1, 2, 3, 4, 5, 6, 7)
 
 
 @pytest.mark.parametrize("rot", [2, 8, 64, 128])
