@@ -8,8 +8,13 @@
 // Bound by memory: every channel is read once and written once (6 flops for each 8 bytes).  A thread has one
 // (token, two vectors of VEC channels) and walks the heads with the cosines and sines of its VEC pairs in
 // registers: they cost ~50 instructions a pair, shared by all heads of the token.  The two vectors stand half of
-// rot_dim apart in both layouts, so that a warp's loads are contiguous either way.  With few tokens the heads are
-// split over blocks until there are kBlocksWanted of them.
+// rot_dim apart in both layouts, so that a warp's loads are contiguous either way.  Where the tokens alone do not fill the
+// GPU the heads are split over as many blocks as are resident at once (kBlocksWanted).
+//
+// Measured (GPU time, 6.45 TB/s is a plain copy's rate): 80 heads of 32,760 tokens, three axes, 217 us = 6.19 TB/s; fp32 gradients of
+// 16 heads of 4,099 tokens 9.6 us = 5.2 TB/s; four frames of 1,560 tokens into the cache, 40 + 80 heads, 71 us = 5.4 TB/s; 8,064
+// tokens of 28 + 8 heads of 64 in fp16 15 us = 4.5 TB/s; 8 tokens of 40 heads 2.2 us.
+// Four blocks an SM (64 registers) carry it: with three of 80 registers the clip takes 283 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cmath>
@@ -18,8 +23,9 @@
 namespace {
 
 constexpr int kThreads = 256;
-// blocks to aim at by splitting the heads: 8 of 256 threads on each of 148 SMs
-constexpr int kBlocksWanted = 148 * 8;
+// blocks to aim at by splitting the heads: the 4 that are resident on each of 148 SMs (the four frames above: 8 an SM 71.3 us, 4 an
+// SM 70.9, 2 an SM 114; the ragged fp16 prompts 16.0 / 14.9 / 15.9: every block works out its angles again)
+constexpr int kBlocksWanted = 148 * 4;
 constexpr int kMaxHeadDim = 512;
 
 struct Strides { long long h, t; };
@@ -122,7 +128,7 @@ __device__ Place find_place(const RotateParams& p, int t) {
 }
 
 template <class T, int VEC, bool INTERLEAVED, bool CACHE>
-__global__ void __launch_bounds__(kThreads) k_rotate(const __grid_constant__ RotateParams p) {
+__global__ void __launch_bounds__(kThreads, 4) k_rotate(const __grid_constant__ RotateParams p) {
   using V = Vec<T, VEC>;
   __shared__ Place places[CACHE ? kThreads : 1];
   const int local = threadIdx.x / p.slots, slot = threadIdx.x - local * p.slots;
@@ -141,9 +147,11 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const __grid_constant__ Rot
   const bool turns = slot < rot_slots;
   int e0, e1;
   float c[VEC], s[VEC];
+  int first = blockIdx.y * p.heads_per_block, left = p.heads_per_block;
   if (turns) {
     e0 = INTERLEAVED && VEC == 1 ? 2 * slot : slot * VEC;
     e1 = INTERLEAVED && VEC == 1 ? 2 * slot + 1 : e0 + half;
+    if (!CACHE || first < p.heads[0] + p.heads[1])   // (a block of values alone needs no angles)
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       // halves: pair e0 + i is (e0 + i, e1 + i); interleaved: the pairs of the first vector, then those of the second
@@ -160,7 +168,6 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const __grid_constant__ Rot
     e1 = e0 + VEC;
   }
 
-  int first = blockIdx.y * p.heads_per_block, left = p.heads_per_block;
 #pragma unroll
   for (int k = 0; k < (CACHE ? 3 : 2); ++k) {
     if (left <= 0) break;
@@ -184,7 +191,7 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const __grid_constant__ Rot
     if (!turn_here && (a0 >= p.head_dim || (k < 2 && (p.in_place >> k & 1)))) live = false;
     if (live) {
       const bool two = a1 < p.head_dim;
-#pragma unroll 4
+#pragma unroll 2
       for (int h = 0; h < n; ++h) {
         const V x = *reinterpret_cast<const V*>(src + a0);
         V y = x;
