@@ -47,9 +47,10 @@ constexpr long long kSelfTestCycles = 4000000ll;     // ~2 ms
 constexpr int kColumns = 16;                         // rows of an item that is computed with its keys as rows (below), at most
 constexpr float kGrowth = 8.0f;                      // log2 of how far a row's maximum may outgrow its reference
 
-// Costs on the line of tiles, about 1,000 clk each: a key tile of a unit of up to 16 rows, of up to 128, of up to 256, and the start and end
-// of such a unit.
-constexpr int kTileFew = 2, kTileNarrow = 3, kTileWide = 4, kUnitFew = 5, kUnitNarrow = 6, kUnitWide = 8;
+// Costs on the line of tiles, about 1,000 clk each: a key tile of a unit of up to 16 rows, of up to 128, of up to 256; what a
+// sequence's own tile costs more where its rows are many (its keys come from memory for this unit alone, the prefix's through L2);
+// and the start and end of such a unit.
+constexpr int kTileFew = 2, kTileNarrow = 3, kTileWide = 4, kOwn = 2, kUnitFew = 5, kUnitNarrow = 8, kUnitWide = 16;
 // a piece is not made shorter than this (below it the joining costs more than the tiles)
 constexpr int kMinPiece = 8;
 
@@ -152,7 +153,7 @@ __device__ inline OwnUnit own_unit(const Shape& s, const Sequence& q, int i) {
   u.keys = s.causal ? max(0, q.len - q.n + u.first + u.n0 + u.n1) : q.len;
   u.tiles = ceil_div(u.keys, kTile);
   const int kind = unit_kind(u.n0, u.n1, s.group);
-  u.weight = tile_cost(kind);
+  u.weight = tile_cost(kind) + (kind ? kOwn : 0);
   u.cost = u.tiles ? u.tiles * u.weight + unit_cost(kind) : 0;
   return u;
 }
@@ -186,11 +187,9 @@ struct Cuts {
 __device__ inline int first_tile(long long x, long long at, int tiles, int weight) {
   const long long d = x - at;
   if (d <= 0 || d >= (long long)tiles * weight) return d <= 0 ? 0 : tiles;
-  const unsigned u = (unsigned)d;
-  return weight == kTileFew ? (u + kTileFew - 1) / kTileFew : weight == kTileNarrow ? (u + kTileNarrow - 1) / kTileNarrow
-                                                                                                  : (u + kTileWide - 1) / kTileWide;
+  return ((unsigned)d + weight - 1) / (unsigned)weight;
 }
-static_assert(kMinPiece >= kTileWide, "a piece between two others of a unit has a tile of it");
+static_assert(kMinPiece >= kTileWide + kOwn, "a piece between two others of a unit has a tile of it");
 
 // Where the parts of a row lie.  Units follow each other on the line in the order of their rows (prefix: head, token, query head
 // of the group; own: sequence, key head, token, query head), and so do pieces: row + piece * (rows of the largest unit) is
