@@ -15,14 +15,24 @@
 // the lengths are.  A unit that a cut goes through leaves a part on either side; k_join_parts adds them up.  The line
 // is worked out from the lengths by every CTA itself at its start (a scan over the batch), so the lengths may live on the device.
 //
-// Inside a CTA (640 threads) there are two slots, each with its own S and O accumulators in tensor memory and its own eight
-// softmax warps:
+// Inside a CTA (640 threads) there are two slots, each with two S buffers of 64 columns and an O accumulator in tensor memory and
+// eight softmax warps:
 //   warp 0   items (pieces of units), Q tiles and K tiles by TMA        warp 3   V tiles by TMA
-//   warp 1   S = Q K^T of both slots in turn     warp 2   O += P V (tcgen05, P in tensor memory over the columns of S)
-//   warps 4-7 and 12-15, 8-11 and 16-19  slot 0, 1: online softmax, two threads a row; the epilogue
-// With more than 128 rows the slots have a row tile each and share every K and V tile; with at most 128 they take the key tiles
-// in turn and join their accumulators in the epilogue (both slots' warps reach the same lanes of tensor memory).  Either
-// way one slot's products run while the other's softmax does.  O is rescaled only when a row's maximum has grown by more than 2^8.
+//   warp 1   S = Q K^T of both slots     warp 2   O += P V (tcgen05, P in tensor memory over the columns of S)
+//   warps 4-7 and 12-15, 8-11 and 16-19  slot 0, 1: online softmax, four warps an S buffer; the epilogue
+// Three kinds of items, by their rows:
+//   up to 256  wide: the slots have a row tile each and share every K and V tile, half a tile (64 keys) at a time;
+//   up to 128  narrow: the slots take the key tiles in turn and join their accumulators in the epilogue;
+//   up to 16   few: keys are the rows of S and query rows its columns, an item has one slot and its two buffers take the tiles in turn.
+// O is rescaled only when a row's maximum has grown by more than 2^8.
+//
+// What bounds it (1 SM, 1.9 GHz; MMA at 64 clk for 128 x 128 x 16): few and narrow items are bound by memory: 16 / 64 / 128 rows a
+// key head over 65,536 keys of 37 heads take 204 / 211 / 222 us at a floor of 193 (6.45 TB/s).  Wide items: 3,500 to 3,900 clk a
+// key tile, of which the products take 2,530 (64-column products of Q K^T 47 clk instead of 32: both operands come out of
+// shared memory) and the exponentials 2,050; 1,024 rows a head over 65,536 keys 1,120 us = 1.14 PFLOP/s, 0.69 of cuBLAS's 1.65.  The
+// softmax loop is bound by issue: exponentials on the FMA pipe, or more registers a thread, made it slower.  head_dim 64: 1,000 us
+// for half the flops, the same exponentials.  A call costs ~8 us before the first tile is there (cold instructions, lengths, the
+// first item) and ~5 us behind the last one (epilogue, join): 19 us for three tokens over 500 keys.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -715,7 +725,8 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   } else if (warp < kVLoadWarp) {
     // ================================================================ products
     // Two warps issue, one S = Q K^T, the other O += P V: what they do around the products (waits, ring positions,
-    // descriptors) takes as long as the products when one warp has it all (2,690 clk a row tile and key tile; the softmax warps leave
+    // descriptors) takes as long as the products when one warp has it all (2,690 clk a row tile and key tile;
+    // with a warp for each slot's products 2,930; the softmax warps leave
     // them few issue slots).  S comes in half tiles of 64 keys, two buffers a slot: one is in its products while the other is in its
     // softmax.  (A product of 64 columns takes 47 clk, not 32: its operands come out of shared memory at that pace.  Whole tiles, one
     // buffer a slot: products and softmax of a slot take turns, 5,210 clk for two row tiles and a key tile.)  S and P of a half tile share columns, so
@@ -1142,11 +1153,20 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         auto load_s = [&](int c0) {
           WAVEAL_TMEM_LD32(my_s + c0, sv, 0);
           WAVEAL_TMEM_WAIT_LD32(sv, 0);
-          if (masked) {
-#pragma unroll
-            for (int c = 0; c < 32; ++c) sv[c] = c < lim - c0 ? sv[c] : 0xff800000u;
-          }
         };
+        if (masked) {
+          // keys that the row does not see, once and in S itself (in the passes below it would be instructions for every tile)
+#pragma unroll 1
+          for (int c0 = 0; c0 < 64; c0 += 8) {
+            uint32_t v[8];
+            WAVEAL_TMEM_LD8(my_s + c0, v);
+            WAVEAL_TMEM_WAIT_LD8(v);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = c < lim - c0 ? v[c] : 0xff800000u;
+            WAVEAL_TMEM_ST8(my_s + c0, v);
+          }
+          tc_wait_st();
+        }
         float mx = -INFINITY;
 #pragma unroll 1
         for (int c0 = 0; c0 < 64; c0 += 32) {
