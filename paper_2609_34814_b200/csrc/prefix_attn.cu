@@ -759,17 +759,6 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           q_ph ^= qb, qb ^= 1;
         }
         const uint64_t qd = q_desc0 + (uint64_t)(qb0 * (G::TILE_BYTES >> 4)), qd1 = q_desc0 + (uint64_t)((qb0 ^ 1) * (G::TILE_BYTES >> 4));
-        auto half_tile = [&](auto b_, uint64_t q, uint64_t kd) {
-          constexpr int b = decltype(b_)::value;
-          if (!buffer_free(b)) return;
-          tc_fence_after();
-#pragma unroll
-          for (int slab = 0; slab < G::SLABS; ++slab)
-            umma4_ss(tm + G::S_COL + b * 64, q + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)((slab * G::SLAB_BYTES + b % 2 * 64 * 128) >> 4),
-                     typed(make_idesc(128, 64, false)), slab > 0);
-          tc_commit(BAR(B_S_FULL + b));
-        };
-        using std::integral_constant;
         for (int j = 0; ok && j < tiles; ++j) {
           if (!(ok = warp_wait(ctx, BAR(B_K_FULL) + 8 * k_st, k_ph, 66))) break;
           const uint64_t kd = k_desc0 + (uint64_t)(k_st * (G::TILE_BYTES >> 4));
@@ -783,17 +772,21 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               umma4_ss(tm + G::S_COL + b * 64, kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), qd + (uint64_t)(slab * G::SLAB_BYTES >> 4),
                        typed(make_idesc(128, kColumns, false)), slab > 0);
             tc_commit(BAR(B_S_FULL + b));
-          } else if (wide) {
-            half_tile(integral_constant<int, 0>{}, qd, kd);
-            if (ok) half_tile(integral_constant<int, 2>{}, qd1, kd);
-            if (ok && two) half_tile(integral_constant<int, 1>{}, qd, kd);
-            if (ok && two) half_tile(integral_constant<int, 3>{}, qd1, kd);
-          } else if (j & 1) {
-            half_tile(integral_constant<int, 2>{}, qd, kd);
-            if (ok && two) half_tile(integral_constant<int, 3>{}, qd, kd);
           } else {
-            half_tile(integral_constant<int, 0>{}, qd, kd);
-            if (ok && two) half_tile(integral_constant<int, 1>{}, qd, kd);
+            // (one copy of the code for the four buffers: eight copies did not stay in the instruction caches)
+            const int count = (two ? 2 : 1) << wide;
+#pragma unroll 1
+            for (int x = 0; ok && x < count; ++x) {
+              const int b = wide ? (x & 1) * 2 + x / 2 : (j & 1) * 2 + x;
+              if (!buffer_free(b)) break;
+              tc_fence_after();
+              const uint64_t q = wide && (x & 1) ? qd1 : qd;
+#pragma unroll
+              for (int slab = 0; slab < G::SLABS; ++slab)
+                umma4_ss(tm + G::S_COL + b * 64, q + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)((slab * G::SLAB_BYTES + (b & 1) * 64 * 128) >> 4),
+                         typed(make_idesc(128, 64, false)), slab > 0);
+              tc_commit(BAR(B_S_FULL + b));
+            }
           }
           if (!ok) break;
           tc_commit(BAR(B_K_EMPTY) + 8 * k_st);
@@ -824,22 +817,6 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const int keys = __shfl_sync(0xffffffffu, im->keys - im->first_key, 0), few = __shfl_sync(0xffffffffu, im->few, 0), item_slot = __shfl_sync(0xffffffffu, im->slot, 0);
         item_done();
         if (few ? !accumulator_free(item_slot) : !accumulator_free(0) || ((wide || tiles > 1) && !accumulator_free(1))) break;
-        auto half_tile = [&](auto b_, uint64_t vd, int groups, bool first) {
-          constexpr int b = decltype(b_)::value, half = b % 2;
-          if (!p_ready(b)) return;
-          tc_fence_after();
-          const uint32_t d = tm + G::O_COL + b / 2 * kTile, a = tm + G::S_COL + b * 64;
-          const uint64_t v = vd + (uint64_t)(half * 64 * 128 >> 4);
-          if (groups >= 4) {
-            umma4_ts(d, a, v, typed(make_idesc(128, D, true)), !first);
-          } else {
-#pragma unroll
-            for (int c = 0; c < 3; ++c)
-              if (c < groups) umma_bf16_ts(d, a + c * 8, v + (uint64_t)(c * 16 * 128 >> 4), typed(make_idesc(128, D, true)), !first || c > 0);
-          }
-          tc_commit(BAR(B_PV_DONE + b));
-        };
-        using std::integral_constant;
         for (int j = 0; ok && j < tiles; ++j) {
           if (!(ok = warp_wait(ctx, BAR(B_V_FULL) + 8 * v_st, v_ph, 68))) break;
           const int valid = min(kTile, keys - j * kTile), groups = (valid + 15) / 16;
@@ -867,17 +844,24 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 umma_ss(tm + G::O_COL + b * 64, vt + (uint64_t)(c * 16 * 128 >> 4), pd + (uint64_t)((c / 4 * G::P_HALF + c % 4 * 32) >> 4), idesc,
                         j >= 2 || c > 0);
             tc_commit(BAR(B_PV_DONE + b));
-          } else if (wide) {
-            half_tile(integral_constant<int, 0>{}, vd, groups, j == 0);
-            if (ok) half_tile(integral_constant<int, 2>{}, vd, groups, j == 0);
-            if (ok && groups > 4) half_tile(integral_constant<int, 1>{}, vd, groups - 4, false);
-            if (ok && groups > 4) half_tile(integral_constant<int, 3>{}, vd, groups - 4, false);
-          } else if (j & 1) {
-            half_tile(integral_constant<int, 2>{}, vd, groups, j == 1);
-            if (ok && groups > 4) half_tile(integral_constant<int, 3>{}, vd, groups - 4, false);
           } else {
-            half_tile(integral_constant<int, 0>{}, vd, groups, j == 0);
-            if (ok && groups > 4) half_tile(integral_constant<int, 1>{}, vd, groups - 4, false);
+            const int count = (groups > 4 ? 2 : 1) << wide;
+#pragma unroll 1
+            for (int x = 0; ok && x < count; ++x) {
+              const int b = wide ? (x & 1) * 2 + x / 2 : (j & 1) * 2 + x, half = b & 1, here = groups - 4 * half;
+              if (!p_ready(b)) break;
+              tc_fence_after();
+              const bool first = half == 0 && (wide ? j == 0 : j < 2);
+              const uint32_t d = tm + G::O_COL + b / 2 * kTile, a = tm + G::S_COL + b * 64;
+              const uint64_t v = vd + (uint64_t)(half * 64 * 128 >> 4);
+              if (here >= 4) {
+                umma4_ts(d, a, v, typed(make_idesc(128, D, true)), !first);
+              } else {
+#pragma unroll 1
+                for (int c = 0; c < here; ++c) umma_bf16_ts(d, a + c * 8, v + (uint64_t)(c * 16 * 128 >> 4), typed(make_idesc(128, D, true)), !first || c > 0);
+              }
+              tc_commit(BAR(B_PV_DONE + b));
+            }
           }
           if (!ok) break;
           tc_commit(BAR(B_V_EMPTY) + 8 * v_st);
