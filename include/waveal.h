@@ -293,7 +293,7 @@ typedef enum { WAVEAL_BF16 = 0, WAVEAL_FP16 = 1, WAVEAL_FP32 = 2 } waveal_dtype;
 /* The rotation of the first rot_dim channels of every head; the others pass unchanged.  Pair i is turned by
  *     angle = 2 pi * frac(position * freqs[i] / 2^64),   (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
  * freqs: int64 [rot_dim/2], turns per position in units of 2^-64 turns (waveal_rope_freqs makes them): the product
- * cut to 64 bits has no rounding, so the angle is as exact at position 2^31 as at 1.
+ * cut to 64 bits has no rounding, so no error grows with the position but that of the table's own last bit.
  * axes: how many positions a token has (1 for a sequence, 3 for frame, height and width of a video); the first
  * axis_pairs[0] pairs turn with the first, the next axis_pairs[1] with the second and so on. */
 typedef struct waveal_rotation {

@@ -423,10 +423,20 @@ def _rows(name, t):
     return st
 
 
-def _output(name, out, like):
+def _new(stream, make):
+    """make(), its memory belonging to the call's stream: a block of the current stream's could still be in use there, or be
+    handed on there before the call has run"""
+    if stream is None:
+        return make()
+    own = stream if isinstance(stream, _torch.cuda.Stream) else _torch.cuda.ExternalStream(stream.cuda_stream)
+    with _torch.cuda.stream(own):
+        return make()
+
+
+def _output(name, out, like, stream):
     """a new tensor like `like`, or the caller's"""
     if out is None:
-        return _torch.empty_like(like)
+        return _torch.empty_like(like) if stream is None else _new(stream, lambda: _torch.empty_like(like))
     if out.shape != like.shape or out.dtype is not like.dtype:
         raise ValueError(f"{name} must have its input's shape and type")
     return out
@@ -452,7 +462,7 @@ def rope(q, positions, freqs, k=None, q_out=None, k_out=None, interleaved: bool 
     q_st = _rows("q", q)
     heads, tokens, dim = q.shape
     at = _positions(positions, rot[2], tokens)
-    q_out = _output("q_out", q_out, q)
+    q_out = _output("q_out", q_out, q, stream)
     qo_st = _rows("q_out", q_out)
     if k is None:
         k_heads, k_ptr, ko_ptr, k_st, ko_st, k_out = 0, None, None, (0, 0), (0, 0), None
@@ -461,7 +471,7 @@ def rope(q, positions, freqs, k=None, q_out=None, k_out=None, interleaved: bool 
         k_heads = k.shape[0]
         if k.shape[1] != tokens or k.shape[2] != dim or k.dtype is not q.dtype:
             raise ValueError("k must have q's tokens, head_dim and type")
-        k_out = _output("k_out", k_out, k)
+        k_out = _output("k_out", k_out, k, stream)
         ko_st = _rows("k_out", k_out)
         k_ptr, ko_ptr = k.data_ptr(), k_out.data_ptr()
     desc = _ROPE.pack(tokens, dim, heads, k_heads, _dtype(q), *rot, q_st[0], q_st[1], qo_st[0], qo_st[1], k_st[0], k_st[1], ko_st[0], ko_st[1])
@@ -528,7 +538,7 @@ def cache_append(cache: PagedCache, k, v, seq_start, kv_len, page_table, positio
         q_heads = q.shape[0]
         if q.shape[1] != tokens or q.shape[2] != dim or q.dtype is not k.dtype:
             raise ValueError("q must have k's tokens, head_dim and type")
-        q_out = _output("q_out", q_out, q)
+        q_out = _output("q_out", q_out, q, stream)
         qo_st = _rows("q_out", q_out)
         q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     batch = batch_desc(q_heads, tokens, seq_start, kv_len, page_table, prefix_len)
@@ -550,7 +560,8 @@ def prefix_attn(cache: PagedCache, q, seq_start, kv_len, page_table=None, prefix
                 return_lse: bool = False, causal: bool = True, scale: float = 0.0, workspace=None, dev_status=None, flags: int = 0, stream=None):
     """waveal_prefix_attn.  q: [q_heads, tokens, head_dim], the new tokens of all sequences one after another; prefix_pages:
     int32 pages of the first prefix_len keys, seen by all; page_table int32 [batch, pages] and kv_len: each sequence's
-    own keys, its new ones last.  Returns o (laid out like q unless given), or (o, lse) with return_lse."""
+    own keys, its new ones last.  Returns o (laid out like q unless given), or (o, lse) with return_lse.  What the call allocates belongs
+    to its stream."""
     torch = _load_torch()
     q_st = _rows("q", q)
     heads, tokens, dim = q.shape
@@ -566,15 +577,15 @@ def prefix_attn(cache: PagedCache, q, seq_start, kv_len, page_table=None, prefix
         if prefix_pages.dim() != 1 or not prefix_pages.is_contiguous() or prefix_pages.shape[0] * cache.page_size < prefix_len:
             raise ValueError("prefix_pages must be a contiguous list of all of the prefix's pages")
         prefix_ptr = prefix_pages.data_ptr()
-    o = _output("o", o, q)
+    o = _output("o", o, q, stream)
     o_st = _rows("o", o)
     if lse is None:
         if return_lse:
-            lse = q.new_empty((heads, tokens), dtype=torch.float32)
+            lse = _new(stream, lambda: q.new_empty((heads, tokens), dtype=torch.float32))
     elif lse.dtype is not torch.float32 or lse.shape != (heads, tokens) or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 [q_heads, tokens]")
     if workspace is None:
-        workspace = q.new_empty((prefix_attn_workspace_bytes(cache, batch),), dtype=torch.uint8)
+        workspace = _new(stream, lambda: q.new_empty((prefix_attn_workspace_bytes(cache, batch),), dtype=torch.uint8))
     _check(load().waveal_prefix_attn(cache.desc, batch, q.data_ptr(), _PAIR.pack(q_st[0], q_st[1]), cache.k.data_ptr(), cache.v.data_ptr(),
                                      o.data_ptr(), _PAIR.pack(o_st[0], o_st[1]), _ptr(lse), seq_start.data_ptr(), kv_len.data_ptr(),
                                      _ptr(page_table), prefix_ptr, scale, workspace.data_ptr(), workspace.numel(), _ptr(dev_status),

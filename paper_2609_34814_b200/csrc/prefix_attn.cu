@@ -1132,12 +1132,6 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         tc_fence_after();
         const int key0 = (wide ? (int)i : 2 * (int)i + slot) * kTile + half * 64, lim = sees - key0;
         const bool masked = unmasked < key0 + 64;
-        uint32_t sv[32];
-        // 32 columns at a time, loaded once for the maximum and again for the exponentials
-        auto load_s = [&](int c0) {
-          WAVEAL_TMEM_LD32(my_s + c0, sv, 0);
-          WAVEAL_TMEM_WAIT_LD32(sv, 0);
-        };
         if (masked) {
           // keys that the row does not see, once and in S itself (in the passes below it would be instructions for every tile)
 #pragma unroll 1
@@ -1151,11 +1145,25 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           }
           tc_wait_st();
         }
-        float mx = -INFINITY;
-#pragma unroll 1
-        for (int c0 = 0; c0 < 64; c0 += 32) {
-          load_s(c0);
-          mx = fmaxf(mx, row_max32(sv));
+        // S is loaded twice, for the maximum and for the exponentials (a row of it in registers spills), 16 columns at a time, the next ones
+        // on their way while these are computed
+        float mx;
+        uint32_t w[2][16];
+        {
+          WAVEAL_TMEM_LD16(my_s, w[0], 0);
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t (&x)[16] = w[q & 1];
+            WAVEAL_TMEM_WAIT_LD16(x, 0);
+            if (q < 3) WAVEAL_TMEM_LD16(my_s + (q + 1) * 16, w[(q + 1) & 1], 0);
+#pragma unroll
+            for (int c = 0; c < 16; c += 8) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) m4[k] = fmax3(m4[k], __uint_as_float(x[c + 2 * k]), __uint_as_float(x[c + 2 * k + 1]));
+            }
+          }
+          mx = fmaxf(fmax3(m4[0], m4[1], m4[2]), m4[3]);
         }
         mx *= p.sl2;
         // half tile u of the slot: the reference that u - 1's owner left
@@ -1181,29 +1189,34 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           tc_fence_after();
           const float a = grows ? ex2(now - to) : 1.0f;
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            WAVEAL_TMEM_LD32(o_addr + c, sv, 0);
-            WAVEAL_TMEM_WAIT_LD32(sv, 0);
+          for (int c = 0; c < D; c += 16) {
+            WAVEAL_TMEM_LD16(o_addr + c, w[0], 0);
+            WAVEAL_TMEM_WAIT_LD16(w[0], 0);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) sv[k] = __float_as_uint(__uint_as_float(sv[k]) * a);
-            WAVEAL_TMEM_ST32(o_addr + c, sv, 0);
+            for (int k = 0; k < 16; ++k) w[0][k] = __float_as_uint(__uint_as_float(w[0][k]) * a);
+            WAVEAL_TMEM_ST16(o_addr + c, w[0], 0);
           }
           tc_wait_st();
         }
         const float b = ref == -INFINITY ? 0.f : -ref;
-#pragma unroll 1
-        for (int c0 = 0; c0 < 64; c0 += 32) {
-          load_s(c0);
-          uint32_t pk[16];
+        {
+          WAVEAL_TMEM_LD16(my_s, w[0], 0);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            float x0, x1;
-            ffma2(x0, x1, __uint_as_float(sv[2 * k]), __uint_as_float(sv[2 * k + 1]), p.sl2, p.sl2, b, b);
-            x0 = ex2(x0), x1 = ex2(x1);
-            fadd2(l0, l1, l0, l1, x0, x1);
-            pk[k] = pack2<T>(x0, x1);
+          for (int q = 0; q < 4; ++q) {
+            uint32_t (&x)[16] = w[q & 1];
+            WAVEAL_TMEM_WAIT_LD16(x, 0);
+            if (q < 3) WAVEAL_TMEM_LD16(my_s + (q + 1) * 16, w[(q + 1) & 1], 0);
+            uint32_t pk[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float x0, x1;
+              ffma2(x0, x1, __uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]), p.sl2, p.sl2, b, b);
+              x0 = ex2(x0), x1 = ex2(x1);
+              fadd2(l0, l1, l0, l1, x0, x1);
+              pk[k] = pack2<T>(x0, x1);
+            }
+            WAVEAL_TMEM_ST8(my_s + q * 8, pk);
           }
-          WAVEAL_TMEM_ST16(my_s + c0 / 2, pk, 0);
         }
         tc_wait_st();
         tc_fence_before();

@@ -12,8 +12,8 @@
 // GPU the heads are split over as many blocks as are resident at once (kBlocksWanted).
 //
 // Measured (GPU time, 6.45 TB/s is a plain copy's rate): 80 heads of 32,760 tokens, three axes, 217 us = 6.19 TB/s; fp32 gradients of
-// 16 heads of 4,099 tokens 9.6 us = 5.2 TB/s; four frames of 1,560 tokens into the cache, 40 + 80 heads, 71 us = 5.4 TB/s; 8,064
-// tokens of 28 + 8 heads of 64 in fp16 15 us = 4.5 TB/s; 8 tokens of 40 heads 2.2 us.
+// 16 heads of 4,099 tokens 9.6 us = 5.2 TB/s; four frames of 1,560 tokens into the cache, 40 + 80 heads, 71 us = 5.4 TB/s; 7,275
+// tokens of ragged prompts, 28 + 8 heads of 64 in fp16, 15 us = 4.5 TB/s; 8 tokens of 40 heads 2.2 us.
 // Four blocks an SM (64 registers) carry it: with three of 80 registers the clip takes 283 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -171,6 +171,26 @@ def test_other_stream():
 
 
 @pytest.mark.gpu
+def test_workspace_of_another_stream_is_not_handed_on():
+    b = Batch(new=[1, 1], own=[300, 40], prefix=500, group=4, seed=8)
+    o, _, o_tol, _ = b.expected(True)
+    b.cuda()
+    cache = wb.PagedCache(b.k, b.v)
+    size = wb.prefix_attn_workspace_bytes(cache, wb.batch_desc(b.heads, b.tokens, b.seq_start, b.kv_len, b.table, b.prefix))
+    side, busy = torch.cuda.Stream(), torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy @ busy                                  # some ms in front of the call
+    got, lse = wb.prefix_attn(cache, b.q, b.seq_start, b.kv_len, b.table, b.prefix_pages, b.prefix, return_lse=True, stream=side)
+    for _ in range(8):                                   # the current stream takes memory of the workspace's size and writes to it
+        torch.empty((size,), dtype=torch.uint8, device="cuda").fill_(255)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert bool(((got.double().cpu() - o).abs() <= o_tol).all())
+
+
+@pytest.mark.gpu
 def test_offsets_beyond_32_bits():
     # pages of 65,536 slots, 8 heads of 64: 2^25 elements each, 72 pages = 2.4e9 elements; the keys lie in the last ones
     page, heads, dim, n = 65536, 8, 64, 72
