@@ -29,10 +29,12 @@
 // What bounds it (1 SM, 1.9 GHz; MMA at 64 clk for 128 x 128 x 16): few and narrow items are bound by memory: 16 / 64 / 128 rows a
 // key head over 65,536 keys of 37 heads take 204 / 211 / 222 us at a floor of 193 (6.45 TB/s).  Wide items: 3,500 to 3,900 clk a
 // key tile, of which the products take 2,530 (64-column products of Q K^T 47 clk instead of 32: both operands come out of
-// shared memory) and the exponentials 2,050; 1,024 rows a head over 65,536 keys 1,120 us = 1.14 PFLOP/s, 0.69 of cuBLAS's 1.65.  The
-// softmax loop is bound by issue: exponentials on the FMA pipe, or more registers a thread, made it slower.  head_dim 64: 1,000 us
-// for half the flops, the same exponentials.  A call costs ~8 us before the first tile is there (cold instructions, lengths, the
-// first item) and ~5 us behind the last one (epilogue, join): 19 us for three tokens over 500 keys.
+// shared memory) and the exponentials 2,050; 1,024 rows a head over 65,536 keys 1,031 us = 1.23 PFLOP/s, 0.75 of cuBLAS's 1.65
+// (in bursts; 66 % of it with the ends of units: 6,240 rows a head over 32,760 keys and their own, 524 us).  The softmax loop is bound by issue
+// and by how its instructions arrive: a quarter of the exponentials on the FMA pipe cost 11 %, a row of S in registers 37 % (spills),
+// exponentials first and a maximum only where the sum asks for it 3 to 5 %.  head_dim 64: 908 us for half the flops, the same
+// exponentials.  A call costs ~8 us before the first tile is there (cold instructions, lengths, the first item) and ~5 us behind the
+// last one (epilogue, join): 19.6 us for three tokens over 500 keys.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
