@@ -1127,8 +1127,15 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       float ref = -INFINITY, l0 = 0.f, l1 = 0.f;
       for (uint32_t i = 0; i < mine; ++i) {
         if (!(ok = warp_wait(ctx, BAR(B_S_FULL + 2 * slot + half), (use0 + i) & 1, 71))) break;
+        // half tile u of the slot: its owner goes on from the reference that u - 1's owner left
+        const uint32_t u = 2 * i + half;
         if (idle) {
-          if (lane == 0) mbar_arrive(BAR(B_P_FULL + 2 * slot + half));
+          // a warp without rows hands the reference on all the same: the chain of hand-overs is what keeps a warp that owns no half tile of an
+          // item from testing a phase whose predecessor is not complete, which would pass by its parity and free the accumulators early
+          if (u && !(ok = warp_wait(ctx, BAR(B_REF + slot * 4 + quad), (refs + u - 1) & 1, 72))) break;
+          sm.ref[slot][r] = ref;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR(B_REF + slot * 4 + quad)), mbar_arrive(BAR(B_P_FULL + 2 * slot + half));
           continue;
         }
         tc_fence_after();
@@ -1168,8 +1175,6 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           mx = fmaxf(fmax3(m4[0], m4[1], m4[2]), m4[3]);
         }
         mx *= p.sl2;
-        // half tile u of the slot: the reference that u - 1's owner left
-        const uint32_t u = 2 * i + half;
         float now = -INFINITY;
         if (u) {
           if (!(ok = warp_wait(ctx, BAR(B_REF + slot * 4 + quad), (refs + u - 1) & 1, 72))) break;
@@ -1233,7 +1238,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       // the slot's last product
       const uint32_t last_bar = B_PV_DONE + 2 * slot + (mine > others || (mine == others && half) ? half : half ^ 1);
       const uint32_t last_ph = (mine > others || (mine == others && half) ? use0 + mine : other0 + others) - 1;
-      if (!idle && halves) {
+      if (halves) {
         if (!(ok = warp_wait(ctx, BAR(B_REF + slot * 4 + quad), (refs + halves - 1) & 1, 72))) break;
         const float to = sm.ref[slot][r];
         if (to != ref) l *= ex2(ref - to), ref = to;

@@ -109,6 +109,24 @@ def test_same_bits_every_time_and_untouched_tokens():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("new,own,group,prefix", [
+    # rows that leave warps without any (16 x 5 = 80, 33, 3 x 11 = 33 of 128), keys that end in a first half tile, many short items one behind the other
+    (26, [26 + 37 * i % 290 for i in range(83)], 8, 2),
+    (5, [5 + 61 * i % 190 for i in range(300)], 16, 0),
+    (33, [33 + 29 * i % 100 for i in range(150)], 1, 20),
+    (11, [11, 64, 65, 128, 129, 192, 40, 200] * 30, 3, 0),
+])
+def test_warps_without_rows_do_not_run_ahead(new, own, group, prefix):
+    b = Batch(new=[new] * len(own), own=own, prefix=prefix, kv_heads=4, group=group, page=256, dtype=FP16, seed=len(own))
+    check(b)
+    first, lse, _ = call(b)
+    first, lse = first.clone(), lse.clone()
+    for _ in range(20):
+        again, lse2, _ = call(b)
+        assert torch.equal(again, first) and torch.equal(lse2, lse)
+
+
+@pytest.mark.gpu
 def test_strides_of_q_and_o():
     b = Batch(new=[2, 5], own=[40, 60], prefix=130, group=2, seed=6)
     o, lse, o_tol, _ = b.expected(True)
