@@ -30,7 +30,7 @@
 // key head over 65,536 keys of 37 heads take 204 / 211 / 222 us at a floor of 193 (6.45 TB/s).  Wide items: 3,500 to 3,900 clk a
 // key tile, of which the products take 2,530 (64-column products of Q K^T 47 clk instead of 32: both operands come out of
 // shared memory) and the exponentials 2,050; 1,024 rows a head over 65,536 keys 1,031 us = 1.23 PFLOP/s, 0.75 of cuBLAS's 1.65
-// (in bursts; 66 % of it with the ends of units: 6,240 rows a head over 32,760 keys and their own, 524 us).  The softmax loop is bound by issue
+// (in bursts; 65 % of it with the ends of units: 6,240 rows a head over 32,760 keys and their own, 535 us).  The softmax loop is bound by issue
 // and by how its instructions arrive: a quarter of the exponentials on the FMA pipe cost 11 %, a row of S in registers 37 % (spills),
 // exponentials first and a maximum only where the sum asks for it 3 to 5 %.  head_dim 64: 908 us for half the flops, the same
 // exponentials.  A call costs ~8 us before the first tile is there (cold instructions, lengths, the first item) and ~5 us behind the
