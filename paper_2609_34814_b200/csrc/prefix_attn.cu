@@ -1341,6 +1341,14 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
 // ------------------------------------------------------------------ parts -> output
 
+// The pieces that have tiles of a unit.  A thread block whose wait gave up has left the words of the units that it never came to as they
+// were in the workspace, and a call that reported this still ends here: what cannot be a pair of pieces is no part, and every pair
+// of pieces stands for places inside the workspace.
+__device__ __forceinline__ int2 pieces_of(const Params& p, int unit) {
+  const int2 w = p.parts.pieces[unit];
+  return w.x >= 0 && w.x <= w.y && w.y < p.s.ctas ? w : make_int2(0, -1);
+}
+
 // WARPS warps a row (a token's query head), with every WARPS-th part each.  The parts' references and sums are read a lane each, so that
 // only one round trip stands before the loads of the parts themselves, which do not wait for each other.
 template <int D, class T, int WARPS>
@@ -1376,9 +1384,9 @@ __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Para
   bool written = false;
   if (mine) {
     int2 shared = {0, -1}, own = {0, -1};            // pieces
-    if (s.prefix_len) shared = p.parts.pieces[h * s.tokens + token / (2 * s.tq) * 2 * s.tq];
+    if (s.prefix_len) shared = pieces_of(p, h * s.tokens + token / (2 * s.tq) * 2 * s.tq);
     const int first = (token - q.start) / (2 * s.tq) * 2 * s.tq;
-    if ((s.causal ? q.len - q.n + min(q.n, first + 2 * s.tq) : q.len) > 0) own = p.parts.pieces[(s.tokens + q.start) * s.kv_heads + h * q.n + first];
+    if ((s.causal ? q.len - q.n + min(q.n, first + 2 * s.tq) : q.len) > 0) own = pieces_of(p, (s.tokens + q.start) * s.kv_heads + h * q.n + first);
     const int n0 = shared.y - shared.x + 1, n = n0 + own.y - own.x + 1;
     written = s.prefix_len == 0 && n == 1;
     const long long row0 = part_row(s, prefix_row(s, h, token) + g, shared.x), row1 = part_row(s, own_row(s, q, h, token - q.start) + g, own.x);

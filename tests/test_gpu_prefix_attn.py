@@ -272,6 +272,29 @@ def test_a_wait_that_runs_out_leaves_the_context_usable():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("fill", [0x00, 0x7f, 0xff])
+@pytest.mark.parametrize("shape", [
+    dict(new=[1] * 900, own=[5] * 900, prefix=0, kv_heads=8, group=2),            # ~48 own units of block 0, eight of them planned before it gives up
+    dict(new=[2, 1, 1], own=[10, 20, 300], prefix=300, kv_heads=160, group=1),    # a whole prefix unit, then some that are cut
+])
+def test_a_wait_that_runs_out_with_units_never_planned(shape, fill):
+    # what the workspace held before must not be taken for places of parts
+    b = Batch(**shape, dim=64, seed=12).cuda()
+    cache = wb.PagedCache(b.k, b.v)
+    ws = torch.empty((wb.prefix_attn_workspace_bytes(cache, wb.batch_desc(b.heads, b.tokens, b.seq_start, b.kv_len, b.table, b.prefix)),),
+                     dtype=torch.uint8, device="cuda")
+    want, want_lse, _ = call(b, workspace=ws)
+    want, want_lse = want.clone(), want_lse.clone()
+    ws.fill_(fill)
+    _, _, status = call(b, workspace=ws, flags=wb.PREFIX_SELFTEST_LOST_TILE)
+    torch.cuda.synchronize()
+    assert status[0].item() == wb.ERR_TIMEOUT
+    got, got_lse, status = call(b, workspace=ws)
+    assert status.tolist() == [0] * 4
+    assert torch.equal(got, want) and torch.equal(got_lse, want_lse)
+
+
+@pytest.mark.gpu
 def test_empty_calls():
     b = Batch(new=[0, 0], own=[5, 6], prefix=30, group=2).cuda()
     o, lse, status = call(b)
