@@ -349,7 +349,8 @@ typedef struct waveal_cache_desc {
 
 /* The batch that append and attention are called for.
  *   seq_start  dev int32 [batch + 1]: the new tokens of sequence b are tokens seq_start[b] .. seq_start[b+1] - 1 of the
- *              call's tensors (0 <= seq_start[b] <= seq_start[b+1] <= tokens; tokens behind the last one's are not touched)
+ *              call's tensors (0 <= seq_start[b] <= seq_start[b+1] <= tokens; tokens in front of the first one's and behind
+ *              the last one's are not touched)
  *   kv_len     dev int32 [batch]: the sequence's own keys, the new ones among them (they are its last)
  *   page_table dev int32 [batch][table_stride]: the pages of its own keys, max_pages a row at most
  * All three are read on the device, so a captured call follows what they hold when it is replayed.  What is malformed

@@ -100,9 +100,9 @@ __device__ Place find_place(const RotateParams& p, int t) {
       return w;                                   // behind the last sequence's tokens
     }
     lo = p.seq_start[b], hi = p.seq_start[b + 1];
-    if (t < lo || t >= hi) {                      // in front of the first, or a start that decreases
-      report(p.dev_status, 40, b, lo);
-      return w;
+    if (t < lo || t >= hi) {
+      if (b > 0 || t >= lo) report(p.dev_status, 40, b, lo);   // a start that decreases
+      return w;                                   // (or in front of the first sequence's tokens)
     }
   }
   if (lo < 0 || hi > p.tokens) {

@@ -221,3 +221,26 @@ def test_append_beyond_32_bits():
     wb.cache_append(cache, x, x, start, lens, torch.tensor([[71]], dtype=torch.int32, device="cuda"))
     assert torch.equal(cache.k[71, :, 65533:], x) and torch.equal(cache.v[71, :, 65533:], x)
     assert int(torch.count_nonzero(cache.k)) == int(torch.count_nonzero(x))
+
+
+def append_ones(starts, tokens, lens, prefix=0, k=None, page=16):
+    """keys and values of ones (or k) into pages b of sequence b; returns (status, slots that were written, cache)"""
+    batch = len(lens)
+    kc = torch.zeros((batch, 1, page, 64), dtype=torch.bfloat16, device="cuda")
+    cache = wb.PagedCache(kc, torch.zeros_like(kc))
+    x = torch.ones((1, tokens, 64), dtype=torch.bfloat16, device="cuda") if k is None else k
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    wb.cache_append(cache, x, x, torch.tensor(starts, dtype=torch.int32, device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                    torch.arange(batch, dtype=torch.int32, device="cuda")[:, None], freqs=wb.rope_freqs(64)[0], prefix_len=prefix, dev_status=status)
+    return status.tolist(), cache.v[:, 0, :, 0].cpu() != 0, cache
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("starts, tokens, lens", [([5, 8, 10], 10, [4, 2]), ([3, 3], 3, [2]), ([4, 4, 4], 9, [1, 2]), ([1000, 1001], 1001, [7])])
+def test_append_leaves_tokens_in_front_of_the_first_sequence_alone(starts, tokens, lens):
+    status, slots, _ = append_ones(starts, tokens, lens)
+    assert status == [0] * 4
+    want = torch.zeros_like(slots)
+    for b, n in enumerate(lens):
+        want[b, n - (starts[b + 1] - starts[b]):n] = True
+    assert torch.equal(slots, want)
