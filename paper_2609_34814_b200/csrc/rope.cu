@@ -95,20 +95,11 @@ __device__ Place find_place(const RotateParams& p, int t) {
       if (p.seq_start[m] <= t) l = m; else r = m - 1;
     }
     b = l;
-    if (b >= p.batch) {
-      if (p.seq_start[b] < 0) report(p.dev_status, 40, b, p.seq_start[b]);
-      return w;                                   // behind the last sequence's tokens
-    }
+    if (b >= p.batch) return w;                   // behind the last sequence's tokens
     lo = p.seq_start[b], hi = p.seq_start[b + 1];
-    if (t < lo || t >= hi) {
-      if (b > 0 || t >= lo) report(p.dev_status, 40, b, lo);   // a start that decreases
-      return w;                                   // (or in front of the first sequence's tokens)
-    }
   }
-  if (lo < 0 || hi > p.tokens) {
-    report(p.dev_status, 40, b, lo < 0 ? lo : hi);
-    return w;
-  }
+  // not in front of the first sequence's tokens, nor in a malformed one (check_starts reports those)
+  if (lo < 0 || t < lo || t >= hi || hi > p.tokens) return w;
   w.live = 1;
   const int len = p.kv_len[b];
   const long long place = (long long)len - (hi - lo) + (t - lo);
@@ -127,6 +118,16 @@ __device__ Place find_place(const RotateParams& p, int t) {
   return w;
 }
 
+// Starts that decrease or leave the tensors, each of them looked at by one thread of the grid: a token's way to its sequence passes a few
+// only.  The threads of a block that find places have the lowest numbers, those that look here first the highest.
+__device__ __forceinline__ void check_starts(const RotateParams& p) {
+  if (blockIdx.y) return;
+  for (long long b = (long long)blockIdx.x * kThreads + kThreads - 1 - threadIdx.x; b < p.batch; b += (long long)gridDim.x * kThreads) {
+    const int lo = p.seq_start[b], hi = p.seq_start[b + 1];
+    if (lo < 0 || hi < lo || hi > p.tokens) report(p.dev_status, 40, (int)b, lo < 0 ? lo : hi);
+  }
+}
+
 template <class T, int VEC, bool INTERLEAVED, bool CACHE>
 __global__ void __launch_bounds__(kThreads, 4) k_rotate(const __grid_constant__ RotateParams p) {
   using V = Vec<T, VEC>;
@@ -135,6 +136,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_rotate(const __grid_constant__ 
   const long long t0 = (long long)blockIdx.x * p.tokens_per_block;
   if constexpr (CACHE) {
     if (threadIdx.x < p.tokens_per_block && t0 + threadIdx.x < p.tokens) places[threadIdx.x] = find_place(p, (int)t0 + threadIdx.x);
+    check_starts(p);
     __syncthreads();
   }
   if (local >= p.tokens_per_block || t0 + local >= p.tokens) return;

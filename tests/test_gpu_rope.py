@@ -244,3 +244,17 @@ def test_append_leaves_tokens_in_front_of_the_first_sequence_alone(starts, token
     for b, n in enumerate(lens):
         want[b, n - (starts[b + 1] - starts[b]):n] = True
     assert torch.equal(slots, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("starts, tokens, bad", [
+    ([0, 6, 4, 6], 6, [(1, 4)]), ([0, 3, 9], 6, [(1, 9)]), ([0, 2, -3, 4, 6], 6, [(1, -3), (2, -3)]), ([6, 0, 6], 6, [(0, 0)]),
+    ([0] * 700 + [1, 0, 2], 2, [(700, 0)]),                       # more sequences than threads of a block, in one block
+    (list(range(4000)) + [0], 3999, [(3999, 0)]),                 # several blocks
+])
+def test_append_reports_starts_that_decrease_or_leave_the_tensors(starts, tokens, bad):
+    status, slots, _ = append_ones(starts, tokens, [16] * (len(starts) - 1))
+    assert status in [[wb.ERR_BAD_MASK, 40, b, value] for b, value in bad]
+    for b, (lo, hi) in enumerate(zip(starts, starts[1:])):
+        if lo < 0 or hi < lo or hi > tokens:
+            assert not bool(slots[b].any()), b                    # counts as having no new tokens
