@@ -356,9 +356,10 @@ typedef struct waveal_cache_desc {
  * All three are read on the device, so a captured call follows what they hold when it is replayed.  What is malformed
  * (a decreasing or too large seq_start, a negative kv_len or one beyond max_pages * page_size, kv_len smaller than the new
  * tokens in append, a page outside [0, n_pages)) is reported in dev_status as {WAVEAL_ERR_BAD_MASK, site, sequence, value};
- * the sequence then counts as having no new tokens, or no own keys, or the page is not written / reads as zeros.  (append finds a
- * token's sequence by search: where a start is malformed, tokens that two sequences claim, or that lie beside a malformed one, may be
- * written for either or for none, each in its sequence's own place.) */
+ * the sequence then counts as having no new tokens, or no own keys, or the page is not written / reads as zeros.  Where starts
+ * decrease, two sequences may claim the same tokens: in attention one whose start lies below an earlier one (of those inside 0 .. tokens) counts
+ * as having no new tokens either, so that it spoils no other's; append finds a token's sequence by search, and tokens that two claim,
+ * or that lie beside a malformed one, may be written for either or for none, each in its sequence's own place. */
 typedef struct waveal_batch_desc {
   int32_t batch, tokens;  /* sequences, new tokens of all of them (both may be 0)             */
   int32_t q_heads;        /* append: 0 where queries are not passed; attention: a multiple of kv_heads, at most 128 times as many */

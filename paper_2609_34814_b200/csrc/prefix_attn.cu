@@ -94,6 +94,7 @@ struct Parts {
   float2* ml;              // [row] {reference (log2), sum}
   int2* pieces;            // [row / group] of a unit's first row: the first and the last piece that has tiles of it (left by the CTAs that
                            // work on its first and last tile)
+  int* order;              // [0]: 1 where a start is malformed; then [1 + b]: the largest start up to b's (read_sequence); left by thread block 0
 };
 
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -137,13 +138,16 @@ struct PrefixLine {
 
 struct Sequence { int start, n, len; };              // first token, new tokens, own keys
 
+// Starts that decrease would let two sequences claim the same tokens, whose parts would then share their places.  So a sequence whose start lies
+// below an earlier one has no new tokens.  `top`: the largest start in front of sequence b of those inside the tensors; where no
+// start is malformed they ascend, and 0 does as well.
+__device__ inline int raise_top(const Shape& s, int top, int start) { return start <= s.tokens ? max(top, start) : top; }
 // bad (may be NULL): {site, value} of what is malformed
-__device__ inline Sequence read_sequence(const Shape& s, int b, int* bad) {
+__device__ inline Sequence read_sequence(const Shape& s, int b, int top, int* bad) {
   Sequence q = {s.seq_start[b], 0, 0};
   const int end = s.seq_start[b + 1], len = s.kv_len[b];
-  if (q.start < 0 || end < q.start || end > s.tokens) {
+  if (q.start < top || end < q.start || end > s.tokens) {
     if (bad) bad[0] = 50, bad[1] = q.start < 0 ? q.start : end;
-    q.start = 0;
     return q;
   }
   q.n = end - q.start;
@@ -239,6 +243,7 @@ struct Walk {
   Sequence q;
   OwnUnit own;             // its first unit
   int piece, whole, unit;
+  int top;                 // of seq (read_sequence)
   int seq, head, i, units; // head -1: the sequence has not been looked at; units: of a head
 };
 
@@ -285,7 +290,7 @@ __device__ __noinline__ unsigned next_units(const Shape& s, const Parts& parts, 
     } else if (w.seq < s.batch) {
       if (w.head < 0) {
         if (w.base >= w.w1) return 0;
-        const Sequence q = read_sequence(s, w.seq, nullptr);
+        const Sequence q = read_sequence(s, w.seq, w.top, nullptr);
         const int units = ceil_div(q.n, 2 * s.tq);
         const OwnUnit own = own_unit(s, q, 0);
         const long long cost = units == 0 ? 0 : units == 1 ? own.cost : own_head_cost(s, q);
@@ -293,6 +298,7 @@ __device__ __noinline__ unsigned next_units(const Shape& s, const Parts& parts, 
         const int head = cost && skip > 0 ? (int)min((long long)s.kv_heads, skip / cost) : 0;
         __syncwarp();
         if (lane == 0) {
+          w.top = raise_top(s, w.top, q.start);
           w.q = q, w.own = own, w.units = units;
           w.at = w.base + head * cost;
           w.base += cost * s.kv_heads;
@@ -556,6 +562,75 @@ struct TileLoader {
   }
 };
 
+// up to and including this lane
+template <class X, class Op> __device__ __forceinline__ X scan_warp(X x, int lane, Op op) {
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const X y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x = op(x, y);
+  }
+  return x;
+}
+
+// Where this thread block's piece of the line begins.  A thread has the costs of its run of sequences [b0, b1) and of its warp up to it; the
+// warps' are in sm.warp_sum.  top: of b0 (read_sequence), where ORDERED is false.
+template <bool ORDERED>
+__device__ __forceinline__ void begin_walk(const Shape& s, Small& sm, const PrefixLine& line, int b0, int b1, long long mine, long long upto, int top) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const long long sums = scan_warp(lane < kThreads / 32 ? sm.warp_sum[lane] : 0, lane, [](long long a, long long b) { return a + b; });
+  const long long own_total = __shfl_sync(0xffffffffu, sums, 31), before = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
+  if (warp) upto += before;
+  const Cuts cuts(max(line.total() + own_total, 1ll), s.ctas);
+  const int piece = blockIdx.x;
+  const bool has_piece = piece < cuts.pieces;
+  const long long w0 = has_piece ? cuts.begin(piece) : 0, w1 = has_piece ? cuts.begin(piece + 1) : 0;
+  const long long from = max(w0 - line.total(), 0ll);
+  long long base = upto - mine;
+  if (has_piece && base <= from && from < upto)
+    for (int b = b0; b < b1; ++b) {
+      const Sequence q = read_sequence(s, b, ORDERED ? 0 : top, nullptr);
+      const long long c = own_head_cost(s, q) * s.kv_heads;
+      if (base <= from && from < base + c) sm.walk().seq = b, sm.walk().base = line.total() + base, sm.walk().top = ORDERED ? 0 : top;
+      if (!ORDERED) top = raise_top(s, top, q.start);
+      base += c;
+    }
+  if (threadIdx.x == 0) {
+    Walk& w = sm.walk();
+    w.w0 = w0, w.w1 = w1;
+    w.piece = piece, w.whole = blockIdx.x, w.unit = has_piece && w0 < line.total() ? line.find(w0) : line.units;
+    w.head = -1;
+    w.line = line;
+  }
+}
+
+// All of that where a start is malformed: the costs once more, now that every thread learns of the starts in front of its run.  (All threads of
+// the block call it, behind a barrier.)
+__device__ __noinline__ void begin_out_of_order(const Params& p, Small& sm, int b0, int b1) {
+  const Shape& s = p.s;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  int m = 0;
+  for (int b = b0; b < b1; ++b) m = raise_top(s, m, s.seq_start[b]);
+  m = scan_warp(m, lane, [](int a, int b) { return max(a, b); });
+  if (lane == 31) sm.warp_sum[warp] = m;
+  int top0 = __shfl_up_sync(0xffffffffu, m, 1);
+  if (lane == 0) top0 = 0;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) top0 = max(top0, (int)sm.warp_sum[w]);
+  int top = top0;
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Sequence q = read_sequence(s, b, top, nullptr);
+    mine += own_head_cost(s, q) * s.kv_heads;
+    top = raise_top(s, top, q.start);
+    if (blockIdx.x == 0) p.parts.order[1 + b] = top;
+  }
+  const long long upto = scan_warp(mine, lane, [](long long a, long long b) { return a + b; });
+  __syncthreads();                                   // (every warp has read the others' largest starts)
+  if (lane == 31) sm.warp_sum[warp] = upto;
+  __syncthreads();
+  begin_walk<false>(s, sm, PrefixLine(s), b0, b1, mine, upto, top0);
+}
+
 template <int D, class T>
 __global__ void __launch_bounds__(kThreads, 1)
 k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQ1, const __grid_constant__ CUtensorMap tmK,
@@ -591,48 +666,19 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   const int per = ceil_div(s.batch, kThreads);
   const int b0 = min((int)threadIdx.x * per, s.batch), b1 = min(b0 + per, s.batch);
   long long mine = 0;
+  bool bad_start = false;
   for (int b = b0; b < b1; ++b) {
     int bad[2] = {0, 0};
-    mine += own_head_cost(s, read_sequence(s, b, bad)) * s.kv_heads;
+    mine += own_head_cost(s, read_sequence(s, b, 0, bad)) * s.kv_heads;
+    bad_start |= bad[0] == 50;
     if (bad[0] && blockIdx.x == 0) report(p.dev_status, WAVEAL_ERR_BAD_MASK, bad[0], b, bad[1]);
   }
-  long long upto = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const long long x = __shfl_up_sync(0xffffffffu, upto, d);
-    if (lane >= d) upto += x;
-  }
+  long long upto = scan_warp(mine, lane, [](long long a, long long b) { return a + b; });
   if (lane == 31) sm.warp_sum[warp] = upto;
-  __syncthreads();
-  long long sums = lane < kThreads / 32 ? sm.warp_sum[lane] : 0;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const long long x = __shfl_up_sync(0xffffffffu, sums, d);
-    if (lane >= d) sums += x;
-  }
-  const long long own_total = __shfl_sync(0xffffffffu, sums, 31), before = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
-  if (warp) upto += before;
-  const Cuts cuts(max(line.total() + own_total, 1ll), s.ctas);
-  const int piece = blockIdx.x;
-  const bool has_piece = piece < cuts.pieces;
-  const long long w0 = has_piece ? cuts.begin(piece) : 0, w1 = has_piece ? cuts.begin(piece + 1) : 0;
-  {
-    const long long from = max(w0 - line.total(), 0ll);
-    long long base = upto - mine;
-    if (has_piece && base <= from && from < upto)
-      for (int b = b0; b < b1; ++b) {
-        const long long c = own_head_cost(s, read_sequence(s, b, nullptr)) * s.kv_heads;
-        if (base <= from && from < base + c) sm.walk().seq = b, sm.walk().base = line.total() + base;
-        base += c;
-      }
-    if (threadIdx.x == 0) {
-      Walk& w = sm.walk();
-      w.w0 = w0, w.w1 = w1;
-      w.piece = piece, w.whole = blockIdx.x, w.unit = has_piece && w0 < line.total() ? line.find(w0) : line.units;
-      w.head = -1;
-      w.line = line;
-    }
-  }
+  const bool in_order = !__syncthreads_or(bad_start);
+  if (threadIdx.x == 0 && blockIdx.x == 0) p.parts.order[0] = !in_order;
+  if (in_order) begin_walk<true>(s, sm, line, b0, b1, mine, upto, 0);
+  else begin_out_of_order(p, sm, b0, b1);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1365,15 +1411,17 @@ __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Para
   // whose token is it (a token of no sequence is left alone)
   Sequence q = {0, 0, 0};
   if (mine) {
-    int b = (int)((unsigned long long)token * s.batch / s.tokens);
-    q = read_sequence(s, b, nullptr);
-    if (token < q.start || token >= q.start + q.n) {
+    const int b = (int)((unsigned long long)token * s.batch / s.tokens);
+    const bool in_order = p.parts.order[0] == 0;
+    q = read_sequence(s, b, 0, nullptr);
+    if (!in_order || token < q.start || token >= q.start + q.n) {
+      const int* starts = in_order ? s.seq_start : p.parts.order + 1;
       int l = 0, r = s.batch - 1;
       while (l < r) {
         const int m = (l + r + 1) >> 1;
-        if (s.seq_start[m] <= token) l = m; else r = m - 1;
+        if (starts[m] <= token) l = m; else r = m - 1;
       }
-      q = read_sequence(s, l, nullptr);
+      q = read_sequence(s, l, in_order ? 0 : starts[l], nullptr);
     }
     mine = token >= q.start && token < q.start + q.n;
   }
@@ -1488,7 +1536,7 @@ int sm_count() {
 // pieces of the line that room is made for, whatever the device (more SMs than this are not used)
 constexpr int kMaxCtas = 192;
 
-struct Layout { size_t pieces, ml, o, bytes; };
+struct Layout { size_t pieces, order, ml, o, bytes; };
 
 Layout layout(const waveal_cache_desc* c, const waveal_batch_desc* b) {
   const int group = b->q_heads / c->kv_heads;
@@ -1496,7 +1544,8 @@ Layout layout(const waveal_cache_desc* c, const waveal_batch_desc* b) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   Layout l;
   l.pieces = 0;
-  l.ml = up((size_t)b->tokens * c->kv_heads * 2 * sizeof(int2));
+  l.order = up((size_t)b->tokens * c->kv_heads * 2 * sizeof(int2));
+  l.ml = l.order + up(((size_t)b->batch + 1) * sizeof(int));
   l.o = l.ml + up(rows * sizeof(float2));
   l.bytes = l.o + up(rows * c->head_dim * sizeof(float));
   return l;
@@ -1589,6 +1638,7 @@ extern "C" waveal_status waveal_prefix_attn(const waveal_cache_desc* c, const wa
   p.s.ctas = std::min(sms, kMaxCtas);
   char* w = static_cast<char*>(ws);
   p.parts.pieces = reinterpret_cast<int2*>(w + l.pieces);
+  p.parts.order = reinterpret_cast<int*>(w + l.order);
   p.parts.ml = reinterpret_cast<float2*>(w + l.ml);
   p.parts.o = reinterpret_cast<float*>(w + l.o);
   p.page_table = page_table, p.prefix_pages = prefix_pages;

@@ -258,6 +258,39 @@ def test_malformed_is_reported_and_the_rest_is_right():
             assert bool(((got.double().cpu() - o).abs() <= o_tol)[:, keep].all()), what
 
 
+# starts that decrease: (starts, lens, sequences whose outputs are right, whom the status may name with which value)
+DECREASING = {
+    "overlaps_the_first": ([0, 10, 5, 8], [60, 20, 300], [0], [(1, 5)]),
+    "and_goes_on_behind_it": ([0, 10, 5, 8, 13, 16], [700, 20, 30, 90, 40], [0, 4], [(1, 5)]),
+    "a_start_out_of_range_between": ([0, 10, -1, 5, 13, 16], [50, 20, 30, 90, 40], [0, 4], [(1, -1), (2, -1)]),
+    "too_large_in_front_of_the_others": ([0, 100, 4, 9, 16], [40, 20, 200, 70], [2, 3], [(0, 100), (1, 4)]),
+    "from_behind": ([9, 3, 9, 16], [40, 70, 200], [2], [(0, 3)]),
+    "many": (list(range(451)) + list(range(100, 1000)), [1 + i % 90 for i in range(1350)], [i for i in range(1350) if i < 450 or i >= 801], [(450, 100)]),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prefix", [0, 200])
+@pytest.mark.parametrize("name", DECREASING)
+def test_a_start_that_decreases_spoils_no_other_sequence(name, prefix):
+    starts, own, right, named = DECREASING[name]
+    new = [starts[b + 1] - starts[b] if b in set(right) else 0 for b in range(len(own))]
+    live = [t for b in right for t in range(starts[b], starts[b + 1])]
+    tokens = min(max(starts), 2000) if name != "too_large_in_front_of_the_others" else 16
+    own = [max(n, k) for n, k in zip(new, own)]
+    b = Batch(new=new, own=own, prefix=prefix, group=2 if len(own) < 20 else 1, dim=64, seed=13, spare_tokens=tokens - sum(new))
+    b.seq_start = torch.tensor(starts, dtype=torch.int32)
+    o, lse, o_tol, lse_tol = b.expected(True)
+    b.cuda()
+    out = torch.full((b.tokens, b.heads, b.dim), 7.0, dtype=b.dtype, device="cuda").transpose(0, 1)
+    got, got_lse, status = call(b, o=out)
+    assert status.tolist() in [[wb.ERR_BAD_MASK, 50, *x] for x in named]
+    assert bool(((got.double().cpu() - o).abs() <= o_tol)[:, live].all())
+    assert bool(((got_lse.double().cpu() - lse).abs() <= lse_tol)[:, live].all())
+    others = [t for t in range(tokens) if t not in set(live)]
+    assert bool((got[:, others] == 7).all())                      # tokens of no sequence are left alone
+
+
 @pytest.mark.gpu
 def test_a_wait_that_runs_out_leaves_the_context_usable():
     b = Batch(new=[1, 1], own=[300, 40], prefix=500, group=4, seed=11)
