@@ -72,7 +72,7 @@ struct Place {
   int live;      // its queries are written
   int slot;      // place inside its page, or -1: keys and values are not written
   long long page;
-  int position;  // prefix_len + place among the own keys
+  long long position;  // prefix_len + place among the own keys (two numbers of 31 bits)
 };
 
 __device__ void report(int* status, int site, int seq, int value) {
@@ -103,7 +103,7 @@ __device__ Place find_place(const RotateParams& p, int t) {
   w.live = 1;
   const int len = p.kv_len[b];
   const long long place = (long long)len - (hi - lo) + (t - lo);
-  w.position = (int)(p.prefix_len + place);
+  w.position = p.prefix_len + place;
   if (len < hi - lo || len > ((long long)p.max_pages << p.page_shift)) {
     report(p.dev_status, 41, b, len);
     return w;
@@ -159,8 +159,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_rotate(const __grid_constant__ 
       // halves: pair e0 + i is (e0 + i, e1 + i); interleaved: the pairs of the first vector, then those of the second
       const int pair = !INTERLEAVED ? e0 + i : VEC == 1 ? slot : i < VEC / 2 ? e0 / 2 + i : e1 / 2 + i - VEC / 2;
       const int axis = pair < p.axis_end0 ? 0 : pair < p.axis_end1 ? 1 : 2;
-      const int pos = !CACHE || p.positions ? __ldg(p.positions + (long long)axis * p.tokens + t) : place.position;
-      const unsigned long long turn = (unsigned long long)((long long)pos) * (unsigned long long)__ldg(p.freqs + pair);
+      const long long pos = !CACHE || p.positions ? __ldg(p.positions + (long long)axis * p.tokens + t) : place.position;
+      const unsigned long long turn = (unsigned long long)pos * (unsigned long long)__ldg(p.freqs + pair);
       sincospif((float)(int)(turn >> 32) * 0x1p-31f, &s[i], &c[i]);
       s[i] *= p.sign * p.amplitude;
       c[i] *= p.amplitude;

@@ -258,3 +258,19 @@ def test_append_reports_starts_that_decrease_or_leave_the_tensors(starts, tokens
     for b, (lo, hi) in enumerate(zip(starts, starts[1:])):
         if lo < 0 or hi < lo or hi > tokens:
             assert not bool(slots[b].any()), b                    # counts as having no new tokens
+
+
+@pytest.mark.gpu
+def test_append_positions_beyond_31_bits():
+    # prefix_len + place passes 2^31 - 1: the positions go on, they do not turn negative
+    prefix, n = 2 ** 31 - 5, 12
+    k = torch.randn((1, n, 64), generator=torch.Generator().manual_seed(1)).bfloat16()
+    status, _, cache = append_ones([0, n], n, [n], prefix, k.cuda())
+    assert status == [0] * 4
+    positions = prefix + torch.arange(n)[None]
+    want = rotated(k.double(), positions, radians(wb.rope_freqs(64)[0]), [32], False)
+    # (the definition's angle is a product of 2^31 and a table entry in 64 bits: off by 2^-53 of 2^31 radians, 2^-22)
+    tol, unit = rotation_tolerance(k.double(), 64, False, 1.0, torch.bfloat16)
+    size = (k.double().abs() + k.double().abs().roll(32, -1)) * 2.0 ** -21
+    got = cache.k[0, :, :n].double().cpu()
+    assert bool(((got - want).abs() <= tol + size + unit * want.abs()).all())
