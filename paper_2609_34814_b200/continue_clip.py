@@ -10,7 +10,6 @@ own frames in one call.  A model would put its projections and its other layers 
 from __future__ import annotations
 
 import argparse
-import math
 
 import torch
 
@@ -65,15 +64,16 @@ class ClipLayer:
         another.  Returns their attention output, laid out the same."""
         B = self.continuations
         start = torch.arange(B + 1, dtype=torch.int32, device=self.device) * self.frame
-        positions = self.positions(self.clip // self.frame + self.seen, 1).repeat(1, B)
-        self.seen += 1
-        if self.seen > self.new_frames:
+        if self.seen >= self.new_frames:
             raise ValueError("no pages left for another frame")
-        kept = torch.full((B,), self.seen * self.frame, dtype=torch.int32, device=self.device)
+        positions = self.positions(self.clip // self.frame + self.seen, 1).repeat(1, B)
+        kept = torch.full((B,), (self.seen + 1) * self.frame, dtype=torch.int32, device=self.device)
         q = wb.cache_append(self.cache, k, v, start, kept, self.table, positions=positions, freqs=self.freqs, q=q, prefix_len=self.clip,
                             interleaved=True, axis_pairs=self.axis_pairs, dev_status=self.status)
         # (a frame's tokens see each other: no causal mask inside it)
-        return wb.prefix_attn(self.cache, q, start, kept, self.table, self.clip_pages, self.clip, causal=False, dev_status=self.status)
+        o = wb.prefix_attn(self.cache, q, start, kept, self.table, self.clip_pages, self.clip, causal=False, dev_status=self.status)
+        self.seen += 1                                   # (a refused frame is not counted)
+        return o
 
 
 def band_mask(heads, blocks, width, device="cuda"):

@@ -59,3 +59,24 @@ def test_command_runs(capsys):
     cc.main(["--heads", "2", "--frames", "2", "--height", "6", "--width", "10", "--continuations", "3"])
     out = capsys.readouterr().out
     assert "frame 1: 3 continuations over 240 keys" in out
+
+
+@pytest.mark.gpu
+def test_a_refused_frame_leaves_the_layer_as_it_was():
+    heads, dim, grid, ways = 1, 64, (5, 9), 2
+    layer = cc.ClipLayer(heads, dim, grid, 2, 2, ways, page=16)
+    draw = lambda n: [torch.randn((heads, n, dim), device="cuda").bfloat16() for _ in range(3)]  # noqa: E731
+    layer.start(*draw(layer.clip), cc.band_mask(heads, 2, 1))
+    layer.step(*draw(ways * layer.frame))
+    with pytest.raises(ValueError):                               # refused by the append: queries of another head_dim
+        q, k, v = draw(ways * layer.frame)
+        layer.step(q[..., :32], k, v)
+    assert layer.seen == 1
+    layer.step(*draw(ways * layer.frame))
+    kept = layer.cache.k.clone()
+    for _ in range(2):
+        with pytest.raises(ValueError):                           # no pages left
+            layer.step(*draw(ways * layer.frame))
+        assert layer.seen == 2
+    assert torch.equal(layer.cache.k.isnan(), kept.isnan()) and torch.equal(layer.cache.k.nan_to_num(), kept.nan_to_num())
+    assert layer.status.tolist() == [0] * 4
