@@ -1,4 +1,5 @@
 """Attention over a shared prefix and each sequence's own keys, against the definition in 64 bits."""
+import copy
 import math
 
 import pytest
@@ -289,6 +290,22 @@ def test_a_start_that_decreases_spoils_no_other_sequence(name, prefix):
     assert bool(((got_lse.double().cpu() - lse).abs() <= lse_tol)[:, live].all())
     others = [t for t in range(tokens) if t not in set(live)]
     assert bool((got[:, others] == 7).all())                      # tokens of no sequence are left alone
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+def test_wide_prefix_units_dealt_whole(causal):
+    # 80 key heads of three units over six key tiles: 148 of the 240 go whole, head 49's second one begins the line
+    b = Batch(new=[300, 200, 100], own=[310, 200, 350], prefix=700, kv_heads=80, group=1, dim=64, page=64, seed=14)
+    some = [0, 48, 49, 50, 79]
+    few = copy.copy(b)
+    few.k, few.v, few.q, few.kv_heads, few.heads = b.k[:, some], b.v[:, some], b.q[some], len(some), len(some)
+    o, lse, o_tol, lse_tol = few.expected(causal)
+    b.cuda()
+    got, got_lse, status = call(b, causal)
+    assert status.tolist() == [0] * 4
+    assert bool(((got[some].double().cpu() - o).abs() <= o_tol).all())
+    assert bool(((got_lse[some].double().cpu() - lse).abs() <= lse_tol).all())
 
 
 @pytest.mark.gpu
