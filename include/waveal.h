@@ -403,7 +403,8 @@ waveal_status waveal_prefix_attn_workspace_bytes(const waveal_cache_desc* cache 
  * q, o: 16-byte aligned, strides multiples of 8 elements; the cache likewise.  q's and o's type is the cache's.
  * At most 2^30 keys in the prefix and in a row of the page table, 10^9 rows (tokens * q_heads).
  * lse: dev float [q_heads][tokens] or NULL, the natural log of the sum of exponentials; a token that sees no key has o = 0
- * and -inf.  A row whose scores hold +infinity or NaN gives NaN; values of keys that a token does not see through
+ * and -inf, and so has one whose scores are all -infinity (the quotient 0 / 0 of the definition).  A row whose scores hold +infinity or NaN gives
+ * NaN in o and lse; values of keys that a token does not see through
  * WAVEAL_PREFIX_CAUSAL must be finite all the same (they are multiplied by zero).
  * scale <= 0 means 1/sqrt(head_dim).  Scores and sums are fp32; the probabilities enter the second product in the tensors' type.
  * ws: 256-byte aligned, not shared with a call that may run at the same time; needs no clearing.  dev_status: dev int32 [4] or

@@ -309,6 +309,58 @@ def test_wide_prefix_units_dealt_whole(causal):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("new, own, prefix, group, dim", [
+    (1, 5, 0, 2, 128), (1, 40, 300, 4, 64), (3, 200, 0, 4, 128),          # few rows
+    (20, 90, 0, 4, 64), (20, 30, 500, 3, 128),                            # narrow
+    (150, 400, 0, 1, 128), (150, 200, 300, 2, 64),                        # wide
+])
+def test_infinite_and_nan_scores(new, own, prefix, group, dim):
+    # one key of each list holds +infinity in one channel: a row's score there is +infinity or -infinity by its query's sign, and with
+    # -infinity the row is as if the key were not there; one row's query is NaN
+    b = Batch(new=[new, new], own=[own, own], prefix=prefix, kv_heads=2, group=group, dim=dim, page=32, seed=15)
+    hit = [(b.table[0], 1)] + ([(b.prefix_pages, prefix // 2)] if prefix else [])      # keys that every new token of sequence 0 sees
+    for pages, key in hit:
+        b.k[int(pages[key // b.page]), :, key % b.page, 3] = math.inf
+    b.q[:, new - 1, 7] = math.nan                                 # sequence 0's last token
+    finite = copy.copy(b)
+    finite.prefix, finite.own = max(prefix - 1, 0), [own - 1, own]
+
+    def get(cache, pages, n):
+        for where, key in hit:
+            if torch.equal(pages, where):
+                x = b.get(cache, pages, n + 1)
+                return torch.cat([x[:, :key], x[:, key + 1:]], 1)
+        return b.get(cache, pages, n)
+    finite.get = get
+    o, lse, o_tol, lse_tol = finite.expected(True)
+    sees = torch.zeros((b.heads, b.tokens), dtype=torch.bool)      # tokens with a key that holds the infinity in sight
+    sees[:, :new] = True
+    if prefix:
+        sees[:] = True
+    q3 = b.q[..., 3].double()
+    nan = (sees & (q3 >= 0)) | b.q.isnan().any(-1)
+    b.cuda()
+    got, got_lse, status = call(b)
+    assert status.tolist() == [0] * 4
+    got, got_lse = got.double().cpu(), got_lse.double().cpu()
+    assert bool(got[nan].isnan().all()) and bool(got_lse[nan].isnan().all())
+    assert bool(((got - o).abs() <= o_tol)[~nan].all()) and bool(((got_lse - lse).abs() <= lse_tol)[~nan].all())
+    assert bool(nan.any()) and bool((~nan).any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new, group", [(1, 2), (20, 4), (150, 1)])
+def test_scores_that_are_all_minus_infinity_count_as_none(new, group):
+    b = Batch(new=[new], own=[new], prefix=0, group=group, dim=64, seed=16)
+    b.k[..., 2] = torch.where(b.k[..., 2].isnan(), b.k[..., 2], torch.full_like(b.k[..., 2], -math.inf))
+    b.q[..., 2] = 1.0
+    b.cuda()
+    got, lse, status = call(b)
+    assert status.tolist() == [0] * 4
+    assert bool((got == 0).all()) and bool((lse == -math.inf).all())
+
+
+@pytest.mark.gpu
 def test_a_wait_that_runs_out_leaves_the_context_usable():
     b = Batch(new=[1, 1], own=[300, 40], prefix=500, group=4, seed=11)
     o, _, o_tol, _ = b.expected(True)
