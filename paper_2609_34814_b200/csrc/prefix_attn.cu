@@ -552,7 +552,7 @@ struct TileLoader {
     __syncwarp();
     return true;
   }
-  // (after a wait gave up) leaves no copy in flight
+  // leaves no copy in flight, also where another warp gives up once this one has nothing left to load (otherwise its tiles' readers have waited for them)
   __device__ void drain(const Params& p, uint32_t full) const {
     for (int st = 0; st < kStages; ++st)
       if (armed >> st & 1) {
@@ -749,14 +749,12 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                                             lane, sbase + G::OFF_K, BAR(B_K_FULL), BAR(B_K_EMPTY), &tmK, 63);
       }
     }
-    if (*ctx.abort_smem) {
-      loader.drain(p, BAR(B_K_FULL));
-      for (int st = 0; st < 2; ++st)
-        if (q_armed >> st & 1) {
-          const long long t0 = clock64();
-          while (!mbar_try_wait(BAR(B_Q_FULL + st), q_parity >> st & 1) && clock64() - t0 < p.wait_limit / 4) {}
-        }
-    }
+    loader.drain(p, BAR(B_K_FULL));
+    for (int st = 0; st < 2; ++st)
+      if (q_armed >> st & 1) {
+        const long long t0 = clock64();
+        while (!mbar_try_wait(BAR(B_Q_FULL + st), q_parity >> st & 1) && clock64() - t0 < p.wait_limit / 4) {}
+      }
   } else if (warp == kVLoadWarp) {
     // ================================================================ V
     TileLoader<D> loader;
@@ -769,7 +767,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         ok = loader.template load<G::NVS>(ctx, p, im, im.first_key + j * kTile, j == im.tiles - 1, false, lane, sbase + G::OFF_V, BAR(B_V_FULL),
                                           BAR(B_V_EMPTY), &tmV, 64);
     }
-    if (*ctx.abort_smem) loader.drain(p, BAR(B_V_FULL));
+    loader.drain(p, BAR(B_V_FULL));
   } else if (warp < kVLoadWarp) {
     // ================================================================ products
     // Two warps issue, one S = Q K^T, the other O += P V: what they do around the products (waits, ring positions,
