@@ -442,6 +442,16 @@ def _output(name, out, like, stream):
     return out
 
 
+def _status(dev_status):
+    if dev_status is None:
+        return None
+    if dev_status.dtype is not _torch.int32 or not dev_status.is_cuda:
+        raise TypeError("dev_status must be an int32 cuda tensor")
+    if dev_status.numel() < 4 or not dev_status.is_contiguous():
+        raise ValueError("dev_status must be four contiguous words")
+    return dev_status.data_ptr()
+
+
 def _positions(positions, axes, tokens):
     if positions.dtype is not _torch.int32 or not positions.is_cuda:
         raise TypeError("positions must be an int32 cuda tensor")
@@ -545,7 +555,7 @@ def cache_append(cache: PagedCache, k, v, seq_start, kv_len, page_table, positio
     strides = _STRIDES.pack(k_st[0], k_st[1], v_st[0], v_st[1], q_st[0], q_st[1], qo_st[0], qo_st[1])
     _check(load().waveal_cache_append(cache.desc, batch, rot, strides, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, cache.k.data_ptr(),
                                       cache.v.data_ptr(), seq_start.data_ptr(), kv_len.data_ptr(), _ptr(page_table), at, freqs_ptr,
-                                      _ptr(dev_status), _stream(stream)))
+                                      _status(dev_status), _stream(stream)))
     return q_out
 
 
@@ -582,12 +592,14 @@ def prefix_attn(cache: PagedCache, q, seq_start, kv_len, page_table=None, prefix
     if lse is None:
         if return_lse:
             lse = _new(stream, lambda: q.new_empty((heads, tokens), dtype=torch.float32))
-    elif lse.dtype is not torch.float32 or lse.shape != (heads, tokens) or not lse.is_contiguous():
-        raise ValueError("lse must be a contiguous float32 [q_heads, tokens]")
+    elif lse.dtype is not torch.float32 or lse.shape != (heads, tokens) or not lse.is_cuda or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 cuda tensor [q_heads, tokens]")
     if workspace is None:
         workspace = _new(stream, lambda: q.new_empty((prefix_attn_workspace_bytes(cache, batch),), dtype=torch.uint8))
+    elif workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous uint8 cuda tensor")
     _check(load().waveal_prefix_attn(cache.desc, batch, q.data_ptr(), _PAIR.pack(q_st[0], q_st[1]), cache.k.data_ptr(), cache.v.data_ptr(),
                                      o.data_ptr(), _PAIR.pack(o_st[0], o_st[1]), _ptr(lse), seq_start.data_ptr(), kv_len.data_ptr(),
-                                     _ptr(page_table), prefix_ptr, scale, workspace.data_ptr(), workspace.numel(), _ptr(dev_status),
+                                     _ptr(page_table), prefix_ptr, scale, workspace.data_ptr(), workspace.numel(), _status(dev_status),
                                      _stream(stream)))
     return (o, lse) if return_lse else o

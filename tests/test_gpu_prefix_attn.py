@@ -397,6 +397,27 @@ def test_a_wait_that_runs_out_with_units_never_planned(shape, fill):
 
 
 @pytest.mark.gpu
+def test_tensors_the_kernels_must_not_write_to_are_refused():
+    b = Batch(new=[1, 1], own=[300, 40], prefix=500, group=4, seed=17).cuda()
+    cache = wb.PagedCache(b.k, b.v)
+    size = wb.prefix_attn_workspace_bytes(cache, wb.batch_desc(b.heads, b.tokens, b.seq_start, b.kv_len, b.table, b.prefix))
+    attend = lambda **kw: wb.prefix_attn(cache, b.q, b.seq_start, b.kv_len, b.table, b.prefix_pages, b.prefix, **kw)  # noqa: E731
+    append = lambda **kw: wb.cache_append(cache, b.k[0, :, :2], b.v[0, :, :2], b.seq_start, b.kv_len, b.table, **kw)  # noqa: E731
+    kept = b.k.clone()
+    for bad in (dict(lse=torch.empty((b.heads, b.tokens))), dict(workspace=torch.empty((size,), dtype=torch.uint8)),
+                dict(workspace=torch.empty((1,), dtype=torch.uint8, device="cuda").expand(size)),
+                dict(workspace=torch.empty((size // 4,), dtype=torch.float32, device="cuda"))):
+        with pytest.raises((TypeError, ValueError)):
+            attend(**bad)
+    for bad in (torch.zeros(4, dtype=torch.int32), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"),
+                torch.zeros(1, dtype=torch.int32, device="cuda").expand(4), torch.zeros(8, dtype=torch.int32, device="cuda")[::2]):
+        for run in (attend, append):
+            with pytest.raises((TypeError, ValueError)):
+                run(dev_status=bad)
+    assert torch.equal(b.k.view(torch.int16), kept.view(torch.int16))
+
+
+@pytest.mark.gpu
 def test_empty_calls():
     b = Batch(new=[0, 0], own=[5, 6], prefix=30, group=2).cuda()
     o, lse, status = call(b)
