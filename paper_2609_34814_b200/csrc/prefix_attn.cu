@@ -94,7 +94,7 @@ struct Parts {
   float2* ml;              // [row] {reference (log2), sum}
   int2* pieces;            // [row / group] of a unit's first row: the first and the last piece that has tiles of it (left by the CTAs that
                            // work on its first and last tile)
-  int* order;              // [0]: 1 where a start is malformed; then [1 + b]: the largest start up to b's (read_sequence); left by thread block 0
+  int4* sequences;         // [batch] {first token, new tokens, own keys}, malformed ones with 0 new tokens and starts that ascend; left by thread block 0
 };
 
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -622,7 +622,7 @@ __device__ __noinline__ void begin_out_of_order(const Params& p, Small& sm, int 
     const Sequence q = read_sequence(s, b, top, nullptr);
     mine += own_head_cost(s, q) * s.kv_heads;
     top = raise_top(s, top, q.start);
-    if (blockIdx.x == 0) p.parts.order[1 + b] = top;
+    if (blockIdx.x == 0) p.parts.sequences[b] = make_int4(top, q.n, q.len, 0);
   }
   const long long upto = scan_warp(mine, lane, [](long long a, long long b) { return a + b; });
   __syncthreads();                                   // (every warp has read the others' largest starts)
@@ -669,15 +669,17 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   bool bad_start = false;
   for (int b = b0; b < b1; ++b) {
     int bad[2] = {0, 0};
-    mine += own_head_cost(s, read_sequence(s, b, 0, bad)) * s.kv_heads;
+    const Sequence q = read_sequence(s, b, 0, bad);
+    mine += own_head_cost(s, q) * s.kv_heads;
     bad_start |= bad[0] == 50;
-    if (bad[0] && blockIdx.x == 0) report(p.dev_status, WAVEAL_ERR_BAD_MASK, bad[0], b, bad[1]);
+    if (blockIdx.x == 0) {
+      p.parts.sequences[b] = make_int4(q.start, q.n, q.len, 0);
+      if (bad[0]) report(p.dev_status, WAVEAL_ERR_BAD_MASK, bad[0], b, bad[1]);
+    }
   }
   long long upto = scan_warp(mine, lane, [](long long a, long long b) { return a + b; });
   if (lane == 31) sm.warp_sum[warp] = upto;
-  const bool in_order = !__syncthreads_or(bad_start);
-  if (threadIdx.x == 0 && blockIdx.x == 0) p.parts.order[0] = !in_order;
-  if (in_order) begin_walk<true>(s, sm, line, b0, b1, mine, upto, 0);
+  if (!__syncthreads_or(bad_start)) begin_walk<true>(s, sm, line, b0, b1, mine, upto, 0);
   else begin_out_of_order(p, sm, b0, b1);
   tc_fence_before();
   __syncthreads();
@@ -1386,11 +1388,12 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 // ------------------------------------------------------------------ parts -> output
 
 // The pieces that have tiles of a unit.  A thread block whose wait gave up has left the words of the units that it never came to as they
-// were in the workspace, and a call that reported this still ends here: what cannot be a pair of pieces is no part, and every pair
-// of pieces stands for places inside the workspace.
+// were in the workspace, and a call that reported this still ends here: whatever they hold is made a pair of pieces, and
+// every pair of pieces stands for places inside the workspace.
 __device__ __forceinline__ int2 pieces_of(const Params& p, int unit) {
   const int2 w = p.parts.pieces[unit];
-  return w.x >= 0 && w.x <= w.y && w.y < p.s.ctas ? w : make_int2(0, -1);
+  const unsigned y = min((unsigned)w.y, (unsigned)p.s.ctas - 1);
+  return make_int2((int)min((unsigned)w.x, y), (int)y);
 }
 
 // WARPS warps a row (a token's query head), with every WARPS-th part each.  The parts' references and sums are read a lane each, so that
@@ -1409,17 +1412,18 @@ __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Para
   // whose token is it (a token of no sequence is left alone)
   Sequence q = {0, 0, 0};
   if (mine) {
-    const int b = (int)((unsigned long long)token * s.batch / s.tokens);
-    const bool in_order = p.parts.order[0] == 0;
-    q = read_sequence(s, b, 0, nullptr);
-    if (!in_order || token < q.start || token >= q.start + q.n) {
-      const int* starts = in_order ? s.seq_start : p.parts.order + 1;
+    auto sequence = [&](int b) {
+      const int4 x = p.parts.sequences[b];
+      return Sequence{x.x, x.y, x.z};
+    };
+    q = sequence((int)((unsigned long long)token * s.batch / s.tokens));
+    if (token < q.start || token >= q.start + q.n) {
       int l = 0, r = s.batch - 1;
       while (l < r) {
         const int m = (l + r + 1) >> 1;
-        if (starts[m] <= token) l = m; else r = m - 1;
+        if (p.parts.sequences[m].x <= token) l = m; else r = m - 1;
       }
-      q = read_sequence(s, l, in_order ? 0 : starts[l], nullptr);
+      q = sequence(l);
     }
     mine = token >= q.start && token < q.start + q.n;
   }
@@ -1534,7 +1538,7 @@ int sm_count() {
 // pieces of the line that room is made for, whatever the device (more SMs than this are not used)
 constexpr int kMaxCtas = 192;
 
-struct Layout { size_t pieces, order, ml, o, bytes; };
+struct Layout { size_t pieces, sequences, ml, o, bytes; };
 
 Layout layout(const waveal_cache_desc* c, const waveal_batch_desc* b) {
   const int group = b->q_heads / c->kv_heads;
@@ -1542,8 +1546,8 @@ Layout layout(const waveal_cache_desc* c, const waveal_batch_desc* b) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   Layout l;
   l.pieces = 0;
-  l.order = up((size_t)b->tokens * c->kv_heads * 2 * sizeof(int2));
-  l.ml = l.order + up(((size_t)b->batch + 1) * sizeof(int));
+  l.sequences = up((size_t)b->tokens * c->kv_heads * 2 * sizeof(int2));
+  l.ml = l.sequences + up((size_t)b->batch * sizeof(int4));
   l.o = l.ml + up(rows * sizeof(float2));
   l.bytes = l.o + up(rows * c->head_dim * sizeof(float));
   return l;
@@ -1636,7 +1640,7 @@ extern "C" waveal_status waveal_prefix_attn(const waveal_cache_desc* c, const wa
   p.s.ctas = std::min(sms, kMaxCtas);
   char* w = static_cast<char*>(ws);
   p.parts.pieces = reinterpret_cast<int2*>(w + l.pieces);
-  p.parts.order = reinterpret_cast<int*>(w + l.order);
+  p.parts.sequences = reinterpret_cast<int4*>(w + l.sequences);
   p.parts.ml = reinterpret_cast<float2*>(w + l.ml);
   p.parts.o = reinterpret_cast<float*>(w + l.o);
   p.page_table = page_table, p.prefix_pages = prefix_pages;
