@@ -721,8 +721,9 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       __syncwarp();
       return true;
     };
-    for (bool more = true; ok && more;) {
-      Item next;
+    Item next;
+    bool more = true;
+    while (ok && more) {
       const unsigned who = next_units(s, p.parts, sm.walk(), next, lane);
       const int count = max(__popc(who), 1), nth = __popc(who & ((1u << lane) - 1));   // (at the end: one item without tiles)
       more = who != 0;
@@ -751,6 +752,9 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                                             lane, sbase + G::OFF_K, BAR(B_K_FULL), BAR(B_K_EMPTY), &tmK, 63);
       }
     }
+    // (a wait gave up: the rest is planned all the same.  The joining kernel reads the words that say which pieces hold a unit's parts,
+    // and the workspace need not hold anything sensible before)
+    while (!ok && more) more = next_units(s, p.parts, sm.walk(), next, lane) != 0;
     loader.drain(p, BAR(B_K_FULL));
     for (int st = 0; st < 2; ++st)
       if (q_armed >> st & 1) {
@@ -1387,15 +1391,6 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
 // ------------------------------------------------------------------ parts -> output
 
-// The pieces that have tiles of a unit.  A thread block whose wait gave up has left the words of the units that it never came to as they
-// were in the workspace, and a call that reported this still ends here: whatever they hold is made a pair of pieces, and
-// every pair of pieces stands for places inside the workspace.
-__device__ __forceinline__ int2 pieces_of(const Params& p, int unit) {
-  const int2 w = p.parts.pieces[unit];
-  const unsigned y = min((unsigned)w.y, (unsigned)p.s.ctas - 1);
-  return make_int2((int)min((unsigned)w.x, y), (int)y);
-}
-
 // WARPS warps a row (a token's query head), with every WARPS-th part each.  The parts' references and sums are read a lane each, so that
 // only one round trip stands before the loads of the parts themselves, which do not wait for each other.
 template <int D, class T, int WARPS>
@@ -1434,9 +1429,9 @@ __global__ void __launch_bounds__(128) k_join_parts(const __grid_constant__ Para
   bool written = false;
   if (mine) {
     int2 shared = {0, -1}, own = {0, -1};            // pieces
-    if (s.prefix_len) shared = pieces_of(p, h * s.tokens + token / (2 * s.tq) * 2 * s.tq);
+    if (s.prefix_len) shared = p.parts.pieces[h * s.tokens + token / (2 * s.tq) * 2 * s.tq];
     const int first = (token - q.start) / (2 * s.tq) * 2 * s.tq;
-    if ((s.causal ? q.len - q.n + min(q.n, first + 2 * s.tq) : q.len) > 0) own = pieces_of(p, (s.tokens + q.start) * s.kv_heads + h * q.n + first);
+    if ((s.causal ? q.len - q.n + min(q.n, first + 2 * s.tq) : q.len) > 0) own = p.parts.pieces[(s.tokens + q.start) * s.kv_heads + h * q.n + first];
     const int n0 = shared.y - shared.x + 1, n = n0 + own.y - own.x + 1;
     written = s.prefix_len == 0 && n == 1;
     const long long row0 = part_row(s, prefix_row(s, h, token) + g, shared.x), row1 = part_row(s, own_row(s, q, h, token - q.start) + g, own.x);
