@@ -27,14 +27,17 @@
 // O is rescaled only when a row's maximum has grown by more than 2^8.
 //
 // What bounds it (1 SM, 1.9 GHz; MMA at 64 clk for 128 x 128 x 16): few and narrow items are bound by memory: 16 / 64 / 128 rows a
-// key head over 65,536 keys of 37 heads take 204 / 211 / 222 us at a floor of 193 (6.45 TB/s).  Wide items: 3,500 to 3,900 clk a
+// key head over 65,536 keys of 37 heads take 200 / 201 / 207 us at a floor of 193 (6.45 TB/s).  Wide items: 3,500 to 3,900 clk a
 // key tile, of which the products take 2,530 (64-column products of Q K^T 47 clk instead of 32: both operands come out of
-// shared memory) and the exponentials 2,050; 1,024 rows a head over 65,536 keys 1,031 us = 1.23 PFLOP/s, 0.75 of cuBLAS's 1.65
+// shared memory) and the exponentials 2,050; 1,024 rows a head over 65,536 keys 1,085 us = 1.17 PFLOP/s, 0.71 of cuBLAS's 1.65
 // (in bursts; 65 % of it with the ends of units: 6,240 rows a head over 32,760 keys and their own, 535 us).  The softmax loop is bound by issue
 // and by how its instructions arrive: a quarter of the exponentials on the FMA pipe cost 11 %, a row of S in registers 37 % (spills),
-// exponentials first and a maximum only where the sum asks for it 3 to 5 %.  head_dim 64: 908 us for half the flops, the same
+// exponentials first and a maximum only where the sum asks for it 3 to 5 %.  head_dim 64: 863 us for half the flops, the same
 // exponentials.  A call costs ~8 us before the first tile is there (cold instructions, lengths, the first item) and ~5 us behind the
-// last one (epilogue, join): 19.6 us for three tokens over 500 keys.
+// last one (epilogue, join): 18.8 us for three tokens over 500 keys.  (Long calls in a row run under the power cap: 64 tokens over 131,072 keys
+// 164 us at 1,965 MHz and 189 us at 1,660, the same cycles.)
+// Registers: 640 threads leave 96 each, and all four variants spill (268 bytes of stores, 468 of loads a thread by -Xptxas -v).  The form with eight
+// softmax warps and more registers took 773 us for four frames, its successor with sixteen 750, today's 535.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -173,6 +176,8 @@ __device__ inline OwnUnit own_unit(const Shape& s, const Sequence& q, int i) {
   u.cost = u.tiles ? u.tiles * u.weight + unit_cost(kind) : 0;
   return u;
 }
+// (Causal units differ, and one thread adds them up: ceil(new tokens / (2 tq)) steps at the start of every CTA, one or two for decoding and drafts,
+// 3,125 for a prompt of 100,000 tokens at 8 query heads a key head.)
 __device__ inline long long own_head_cost(const Shape& s, const Sequence& q) {
   const int m = ceil_div(q.n, 2 * s.tq);
   long long c = 0;
@@ -449,6 +454,10 @@ __device__ __forceinline__ void umma4_ts(uint32_t d_tmem, uint32_t a_tmem, uint6
       : "memory");
 }
 
+// Two numbers in the tensors' type: the results, and the probabilities, because one product of 16-bit types takes both operands in the same
+// type and V is stored in this one.  (Probabilities in two terms would double the second product.)  A probability is off by half a step
+// of its own, as the result is: against 64 bits o is off by 0.0023 of its size in bf16 and 0.00029 in fp16, where probabilities in
+// fp32 give 0.0017 and 0.00021.  Their sums are taken before the rounding, in fp32.
 template <class T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;
   if constexpr (std::is_same_v<T, __half>)
@@ -466,7 +475,6 @@ enum {
   B_SUMS_READ, B_COLS, B_COLS_READ = B_COLS + 2, B_VOTE = B_COLS_READ + 2, B_PAIR = B_VOTE + 4, B_REF = B_PAIR + 8, B_FINAL = B_REF + 8, B_COUNT = B_FINAL + 2
 };
 
-// what lies behind the tiles in shared memory
 // 8 consecutive columns of this thread's lane of tensor memory
 #define WAVEAL_TMEM_LD8(taddr, v)                                                                                      \
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"                         \
@@ -489,6 +497,7 @@ __device__ __forceinline__ void st_shared_u16(uint32_t addr, uint32_t x) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"((unsigned short)x) : "memory");
 }
 
+// what lies behind the tiles in shared memory
 struct Small {
   unsigned long long bar[B_COUNT];
   Item items[kItems];
