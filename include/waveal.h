@@ -10,7 +10,9 @@
  *   positions  waveal_rope : rotary positions of queries and keys, forwards and backwards;
  *   cache      waveal_cache_append : new keys (rotated on the way) and values into a paged cache;
  *   attention  waveal_prefix_attn : a batch of queries over a prefix that all of them share and over
- *              each sequence's own keys, both in that cache.
+ *              each sequence's own keys, both in that cache;
+ *   prompts    waveal_prompt_attn : whole prompts of different lengths, each over itself, causal, grouped heads;
+ *   pages      waveal_cache_fork, waveal_cache_compact, waveal_cache_copy : who holds which page of the cache.
  *
  * Conventions for every call
  *   - "dev" pointers are device pointers on the current CUDA device, "host" pointers are
@@ -57,7 +59,8 @@ typedef enum {
   WAVEAL_ERR_WORKSPACE = 3,     /* workspace missing or too small                             */
   WAVEAL_ERR_BAD_MASK = 4,      /* device-side: index out of range / unsorted                 */
   WAVEAL_ERR_CUDA = 5,          /* a CUDA runtime/driver call failed                          */
-  WAVEAL_ERR_TIMEOUT = 6        /* device-side: a bounded wait ran out                        */
+  WAVEAL_ERR_TIMEOUT = 6,       /* device-side: a bounded wait ran out                        */
+  WAVEAL_ERR_NO_PAGES = 7       /* device-side: the pool has too few free pages               */
 } waveal_status;
 
 /* Which stages run (Section 6.5 ablation: Original, O+S1, O+S2, O+S1+S2). */
@@ -414,6 +417,101 @@ waveal_status waveal_prefix_attn(const waveal_cache_desc* cache /*host*/, const 
                                  const int64_t* o_stride /*host [2]*/, float* lse, const int32_t* seq_start,
                                  const int32_t* kv_len, const int32_t* page_table, const int32_t* prefix_pages, float scale,
                                  void* ws, size_t ws_bytes, int32_t* dev_status, void* cuda_stream);
+
+/* ---------------------------------------------------------------- whole prompts */
+
+/* Token i of a sequence sees its tokens 0 .. i only; without the flag all of them. */
+#define WAVEAL_PROMPT_CAUSAL 1
+/* As WAVEAL_PREFIX_SELFTEST_LOST_TILE. */
+#define WAVEAL_PROMPT_SELFTEST_LOST_TILE 256
+
+typedef struct waveal_prompt_desc {
+  int32_t batch, tokens;        /* sequences, tokens of the tensors (both may be 0)               */
+  int32_t q_heads, kv_heads;    /* q_heads: a multiple of kv_heads, at most 128 times as many     */
+  int32_t head_dim;             /* 64 or 128                                                      */
+  int32_t dtype;                /* WAVEAL_BF16 or WAVEAL_FP16: of q, k, v and o                   */
+  int32_t flags;                /* WAVEAL_PROMPT_*                                                */
+  int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];   /* elements: {head, token}        */
+} waveal_prompt_desc;
+
+/* Bytes of device workspace waveal_prompt_attn needs; the descriptor alone decides. */
+waveal_status waveal_prompt_attn_workspace_bytes(const waveal_prompt_desc* desc /*host*/, size_t* bytes /*host*/);
+
+/* o = softmax(scale * q K^T) V of every token over the tokens of its own sequence (query head h reads key head
+ * h / (q_heads / kv_heads)), before or beside their way into a cache.
+ * seq_start: dev int32 [batch + 1], sequence b is tokens seq_start[b] .. seq_start[b + 1] - 1 (0 <= seq_start[b] <= seq_start[b + 1] <= tokens).
+ * seq_len: dev int32 [batch] or NULL: only the first seq_len[b] of them exist (a padded batch); 0 <= seq_len[b] <= seq_start[b + 1] - seq_start[b].
+ * Both are read on the device, so a captured call follows what they hold when it is replayed.  Tokens of no sequence (in front of the first, behind
+ * the last, padding) are neither read into a result nor written.  A malformed sequence is reported in dev_status as {WAVEAL_ERR_BAD_MASK, site,
+ * sequence, value} (100: starts, 101: length) and left out.
+ * lse: dev float [q_heads][tokens] or NULL, the natural log of the sum of exponentials.  A token whose scores are all -infinity has o = 0 and -inf; a row
+ * whose scores hold +infinity or NaN gives NaN.  Keys and values that a token does not see, NaN and infinities included, never reach it.
+ * q, k, v, o: 16-byte aligned, strides multiples of 8 elements and not negative; o must not overlap the others.
+ * At most 10^9 rows (tokens * q_heads).  scale <= 0 means 1/sqrt(head_dim).  Scores, sums and the
+ * accumulated output are fp32; the probabilities enter the second product in the tensors' type.
+ * ws: 256-byte aligned, not shared with a call that may run at the same time; needs no clearing.  dev_status: dev int32 [4] or
+ * NULL, zeroed by the caller; also {WAVEAL_ERR_TIMEOUT, site, thread block, thread} when a bounded wait ran out. */
+waveal_status waveal_prompt_attn(const waveal_prompt_desc* desc /*host*/, const void* q, const void* k, const void* v, void* o, float* lse,
+                                 const int32_t* seq_start, const int32_t* seq_len, float scale, void* ws, size_t ws_bytes,
+                                 int32_t* dev_status, void* cuda_stream);
+
+/* ---------------------------------------------------------------- pages of the cache
+ *
+ * A pool is the n_pages pages of a waveal_cache_desc.  Row b of a page table names the pages of one sequence; a page may stand in
+ * several rows, and page_refs counts its holders: the rows that it stands in, and one for everything else that needs it
+ * (a shared prefix).  A page whose count is not above zero is free.  The three calls read and write all of this on the device: a step needs no
+ * answer on the host, and a captured call follows what its tensors hold.  head_dim 2 .. 512, a page of at most 2^31 - 1 elements of keys. */
+
+typedef struct waveal_fork_desc {
+  int32_t old_rows, rows;       /* of the last table, of the next one (both may be 0)             */
+  int32_t old_pages, pages;     /* entries of a row                                               */
+  int64_t old_stride, stride;   /* entries from one row to the next                               */
+} waveal_fork_desc;
+
+waveal_status waveal_cache_fork_workspace_bytes(const waveal_cache_desc* cache /*host*/, const waveal_fork_desc* fork /*host*/, size_t* bytes /*host*/);
+
+/* The next step's table.  Row b continues row parents[b] of the last one (NULL: row b; negative: a row without pages): it keeps the first
+ * keep_len[b] tokens of it and has room for max(keep_len[b], room_len[b]).  So one call lets sequences grow, cuts them back, continues
+ * one in several ways, ends some and puts the others in a new order.
+ *   old_table int32 [old_rows][old_pages], held_len int32 [old_rows]: row r holds the pages of its first held_len[r] tokens (its room, where
+ *   it had any).  All old rows let go of their pages, the new rows take theirs:
+ *     pages that the kept tokens fill are shared (their counts say by how many);
+ *     a page that they fill in part is kept by the first row that ends in it, if nobody else holds that page; every other such row gets a fresh
+ *     page with the kept tokens' keys and values copied.  So every row may append to its last page at once;
+ *     the rest are fresh pages: the free ones in ascending order, dealt out row by row (what the old rows let go is free).
+ *   table, new_refs: the result; entries behind a row's pages are -1.  Neither may lie over its old counterpart; k_cache and v_cache are written
+ *   in place, in fresh pages alone.
+ * dev_status {WAVEAL_ERR_BAD_MASK, site, row, value}: 80 parents, 81 held_len (that row then holds nothing), 82 keep_len (below 0 or above the
+ * parent's held_len), 83 room beyond `pages`; such a row of the new table is empty.  84: an entry of the last table outside the pool; it is -1 in the new one and
+ * counted nowhere.  {WAVEAL_ERR_NO_PAGES, 85, row, pages missing}: the pool is used up; entries from there on are -1. */
+waveal_status waveal_cache_fork(const waveal_cache_desc* cache /*host*/, const waveal_fork_desc* fork /*host*/, void* k_cache, void* v_cache,
+                                const int32_t* old_table, const int32_t* held_len, const int32_t* page_refs, const int32_t* parents /*or NULL*/,
+                                const int32_t* keep_len, const int32_t* room_len, int32_t* table, int32_t* new_refs, void* ws, size_t ws_bytes,
+                                int32_t* dev_status /*dev [4] or NULL*/, void* cuda_stream);
+
+typedef struct waveal_compact_desc {
+  int32_t rows, pages;          /* of the page table (0: none)                                    */
+  int32_t prefix_pages;         /* entries of a list beside it (0: none)                          */
+  int64_t old_stride, stride;
+} waveal_compact_desc;
+
+waveal_status waveal_cache_compact_workspace_bytes(const waveal_cache_desc* cache /*host*/, size_t* bytes /*host*/);
+
+/* Moves the pages in use to the lowest numbers: with n of them, the i-th one that lies at n or behind goes to the i-th free page below n, and
+ * the others stay.  Pages are copied whole; where one came from is left as it was.
+ *   place int32 [n_pages]: every page's new number, -1 for a free one; used int32 [1]: n; new_refs: the counts at their new places.
+ *   table, prefix: the entries of old_table and old_prefix by `place`, all of them; -1 for one that names a free page or none of the pool.
+ * No output may lie over its old counterpart. */
+waveal_status waveal_cache_compact(const waveal_cache_desc* cache /*host*/, const waveal_compact_desc* compact /*host*/, void* k_cache, void* v_cache,
+                                   const int32_t* page_refs, const int32_t* old_table, const int32_t* old_prefix, int32_t* new_refs, int32_t* table,
+                                   int32_t* prefix, int32_t* place, int32_t* used, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Page from_pages[i] of one cache -> page to_pages[i] of another (or the same), i < count; -1 on either side: nothing.  The caches agree in page_size,
+ * kv_heads, head_dim and dtype; strides may differ.  A page that is written must stand in to_pages once and, in one cache, not in
+ * from_pages.  dev_status {WAVEAL_ERR_BAD_MASK, 89 (from) or 90 (to), i, page}: a page outside its pool; nothing is copied for it.  No workspace. */
+waveal_status waveal_cache_copy(const waveal_cache_desc* to /*host*/, const waveal_cache_desc* from /*host*/, int32_t count, const void* from_k,
+                                const void* from_v, void* to_k, void* to_v, const int32_t* from_pages, const int32_t* to_pages,
+                                int32_t* dev_status /*dev [4] or NULL*/, void* cuda_stream);
 
 /* Number of query-block tasks the attention kernel keeps in flight on the current device
  * (SM count x CTAs per SM): the W to plan with (Section 6.1).  Returns <= 0 on failure. */

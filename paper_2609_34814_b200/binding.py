@@ -10,12 +10,12 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
-from typing import Optional
+from typing import NamedTuple, Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libwaveal.so")
 
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BAD_MASK, ERR_CUDA, ERR_TIMEOUT = range(7)
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BAD_MASK, ERR_CUDA, ERR_TIMEOUT, ERR_NO_PAGES = range(8)
 AUTO, FORCE_REORDER, FORCE_NATURAL, STAGE1_ONLY, STAGE2_ONLY = range(5)
 FLAG_SKIPPED, FLAG_SHORT_SEQ, FLAG_TOO_SPARSE, FLAG_ALREADY_LOCAL = 1, 2, 4, 8
 
@@ -23,6 +23,8 @@ EXPORTS = ["waveal_plan_desc_default", "waveal_plan_workspace_bytes", "waveal_pl
            "waveal_bitmap_to_csr", "waveal_bitmap_to_csr_noalloc", "waveal_noalloc_max_rows",
            "waveal_gather_rows", "waveal_scatter_rows", "waveal_bsattn_workspace_bytes", "waveal_bsattn_fwd",
            "waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
+           "waveal_prompt_attn_workspace_bytes", "waveal_prompt_attn", "waveal_cache_fork_workspace_bytes", "waveal_cache_fork",
+           "waveal_cache_compact_workspace_bytes", "waveal_cache_compact", "waveal_cache_copy",
            "waveal_default_wave_size", "waveal_last_launch_count", "waveal_status_string", "waveal_last_error"]
 
 
@@ -77,6 +79,22 @@ class AppendStrides(ctypes.Structure):
                 ("q_out", ctypes.c_int64 * 2)]
 
 
+class PromptDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("q_stride", ctypes.c_int64 * 2),
+                ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2)]
+
+
+class ForkDesc(ctypes.Structure):
+    _fields_ = [("old_rows", ctypes.c_int32), ("rows", ctypes.c_int32), ("old_pages", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("old_stride", ctypes.c_int64), ("stride", ctypes.c_int64)]
+
+
+class CompactDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("pages", ctypes.c_int32), ("prefix_pages", ctypes.c_int32), ("old_stride", ctypes.c_int64),
+                ("stride", ctypes.c_int64)]
+
+
 class WavealError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"waveal status {status}: {message}")
@@ -116,7 +134,15 @@ def load() -> ctypes.CDLL:
         lib.waveal_cache_append.argtypes = [P] * 17
         lib.waveal_prefix_attn_workspace_bytes.argtypes = [P, P, ctypes.POINTER(ctypes.c_size_t)]
         lib.waveal_prefix_attn.argtypes = [P] * 13 + [ctypes.c_float, P, ctypes.c_size_t, P, P]
-        for name in ["waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
+        lib.waveal_prompt_attn_workspace_bytes.argtypes = [P, ctypes.POINTER(ctypes.c_size_t)]
+        lib.waveal_prompt_attn.argtypes = [P] * 8 + [ctypes.c_float, P, ctypes.c_size_t, P, P]
+        lib.waveal_cache_fork_workspace_bytes.argtypes = [P, P, ctypes.POINTER(ctypes.c_size_t)]
+        lib.waveal_cache_fork.argtypes = [P] * 13 + [ctypes.c_size_t, P, P]
+        lib.waveal_cache_compact_workspace_bytes.argtypes = [P, ctypes.POINTER(ctypes.c_size_t)]
+        lib.waveal_cache_compact.argtypes = [P] * 13 + [ctypes.c_size_t, P]
+        lib.waveal_cache_copy.argtypes = [P, P, I32] + [P] * 8
+        for name in ["waveal_prompt_attn_workspace_bytes", "waveal_prompt_attn", "waveal_cache_fork_workspace_bytes", "waveal_cache_fork",
+                     "waveal_cache_compact_workspace_bytes", "waveal_cache_compact", "waveal_cache_copy", "waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
                      "waveal_plan_workspace_bytes", "waveal_plan_bitmap", "waveal_plan_csr", "waveal_bitmap_to_csr",
                      "waveal_gather_rows", "waveal_scatter_rows", "waveal_bsattn_workspace_bytes", "waveal_bsattn_fwd", "waveal_default_wave_size",
                      "waveal_last_launch_count"]:
@@ -603,3 +629,188 @@ def prefix_attn(cache: PagedCache, q, seq_start, kv_len, page_table=None, prefix
                                      _ptr(page_table), prefix_ptr, scale, workspace.data_ptr(), workspace.numel(), _status(dev_status),
                                      _stream(stream)))
     return (o, lse) if return_lse else o
+
+
+# ------------------------------------------------------------------ whole prompts, pages of the cache
+
+PROMPT_CAUSAL = 1
+PROMPT_SELFTEST_LOST_TILE = 256
+
+# waveal_prompt_desc, waveal_fork_desc, waveal_compact_desc as the C compiler lays them out
+_PROMPT = struct.Struct("7i4x8q")
+_FORK = struct.Struct("4i2q")
+_COMPACT = struct.Struct("3i4x2q")
+
+
+def _here(*tensors):
+    """The library works on the current device: tensors of another one are refused."""
+    dev = _torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _ints(name, t, shape):
+    """address of a contiguous int32 cuda tensor of this shape"""
+    if t.dtype is not _torch.int32 or not t.is_cuda:
+        raise TypeError(f"{name} must be an int32 cuda tensor")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {list(shape)}, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _table(name, t):
+    """(rows, pages, entries from one row to the next) of a page table"""
+    if t.dtype is not _torch.int32 or not t.is_cuda:
+        raise TypeError(f"{name} must be an int32 cuda tensor")
+    shape, st = t.shape, t.stride()
+    if len(st) != 2 or st[1] != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must be [rows, pages], a row's pages contiguous")
+    return shape[0], shape[1], st[0] if shape[0] > 1 else max(st[0], shape[1])
+
+
+def _workspace(workspace, need, like, stream):
+    if workspace is None:
+        return _new(stream, lambda: like.new_empty((need(),), dtype=_torch.uint8))
+    if workspace.dtype is not _torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous uint8 cuda tensor")
+    return workspace
+
+
+def prompt_desc(q, k, v, o, batch: int, causal: bool = True, flags: int = 0) -> bytes:
+    """The waveal_prompt_desc of a call, from its tensors."""
+    _load_torch()
+    q_st, k_st, v_st, o_st = _rows("q", q), _rows("k", k), _rows("v", v), _rows("o", o)
+    heads, tokens, dim = q.shape
+    if k.shape != v.shape or k.shape[1] != tokens or k.shape[2] != dim:
+        raise ValueError("k and v must be [kv_heads, tokens, head_dim] with q's tokens and head_dim")
+    if k.dtype is not q.dtype or v.dtype is not q.dtype:
+        raise TypeError("q, k and v must have one type")
+    return _PROMPT.pack(batch, tokens, heads, k.shape[0], dim, _dtype(q), (PROMPT_CAUSAL if causal else 0) | flags, q_st[0], q_st[1], k_st[0], k_st[1],
+                        v_st[0], v_st[1], o_st[0], o_st[1])
+
+
+def prompt_attn_workspace_bytes(desc: bytes) -> int:
+    """Bytes for prompt_attn's workspace; desc: prompt_desc of the call."""
+    n = ctypes.c_size_t(0)
+    _check(load().waveal_prompt_attn_workspace_bytes(desc, ctypes.byref(n)))
+    return n.value
+
+
+def prompt_attn(q, k, v, seq_start, seq_len=None, o=None, lse=None, return_lse: bool = False, causal: bool = True, scale: float = 0.0,
+                workspace=None, dev_status=None, flags: int = 0, stream=None):
+    """waveal_prompt_attn.  q: [q_heads, tokens, head_dim], k, v: [kv_heads, tokens, head_dim], bf16 or fp16, the tokens of all sequences one
+    after another (any strides: a [tokens, heads, head_dim] tensor is passed as x.transpose(0, 1)); seq_start int32 [batch + 1]; seq_len int32
+    [batch], where only a sequence's first tokens exist.  Every token attends to its own sequence, up to itself with causal.  Returns o (laid out
+    like q unless given), or (o, lse) with return_lse; tokens of no sequence are not written.  What the call allocates belongs to its stream."""
+    torch = _load_torch()
+    o = _output("o", o, q, stream)
+    if seq_start.dim() != 1 or seq_start.shape[0] < 1:
+        raise ValueError("seq_start must be [batch + 1]")
+    batch = seq_start.shape[0] - 1
+    start = _ints("seq_start", seq_start, (batch + 1,))
+    lens = None if seq_len is None else _ints("seq_len", seq_len, (batch,))
+    desc = prompt_desc(q, k, v, o, batch, causal, flags)
+    if lse is None:
+        if return_lse:
+            lse = _new(stream, lambda: q.new_empty(q.shape[:2], dtype=torch.float32))
+    elif lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_cuda or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 cuda tensor [q_heads, tokens]")
+    workspace = _workspace(workspace, lambda: prompt_attn_workspace_bytes(desc), q, stream)
+    _here(q, k, v, o, lse, seq_start, seq_len, workspace)
+    _check(load().waveal_prompt_attn(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), start, lens, scale,
+                                     workspace.data_ptr(), workspace.numel(), _status(dev_status), _stream(stream)))
+    return (o, lse) if return_lse else o
+
+
+def cache_fork_workspace_bytes(cache: PagedCache, fork: bytes) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().waveal_cache_fork_workspace_bytes(cache.desc, fork, ctypes.byref(n)))
+    return n.value
+
+
+def cache_fork(cache: PagedCache, page_table, held_len, page_refs, keep_len, room_len, parents=None, max_pages: Optional[int] = None,
+               table_out=None, refs_out=None, workspace=None, dev_status=None, stream=None):
+    """waveal_cache_fork: the next step's page table and counts.  page_table int32 [old rows, pages], held_len int32 [old rows]: row r holds the pages
+    of its first held_len[r] tokens; page_refs int32 [n_pages]: how many hold each page.  Row b of the new table (as many as keep_len
+    has) keeps the first keep_len[b] tokens of row parents[b] (None: row b; negative: a row without pages) and has room for room_len[b].
+    Full pages are shared, a page filled in part is copied unless the row is the only one left that holds it, fresh pages are the free ones with the
+    lowest numbers.  max_pages: entries of a new row (as many as before unless given).  Returns (page_table, page_refs): new tensors unless given."""
+    _load_torch()
+    old_rows, old_pages, old_stride = _table("page_table", page_table)
+    if keep_len.dim() != 1:
+        raise ValueError("keep_len must be [rows]")
+    rows = keep_len.shape[0]
+    held, refs = _ints("held_len", held_len, (old_rows,)), _ints("page_refs", page_refs, (cache.n_pages,))
+    keep, room = _ints("keep_len", keep_len, (rows,)), _ints("room_len", room_len, (rows,))
+    parent = None if parents is None else _ints("parents", parents, (rows,))
+    if table_out is None:
+        pages = old_pages if max_pages is None else max_pages
+        table_out = _new(stream, lambda: page_table.new_empty((rows, pages)))
+    new_rows, pages, stride = _table("table_out", table_out)
+    if new_rows != rows or max_pages is not None and pages != max_pages:
+        raise ValueError("table_out must be [rows of keep_len, max_pages]")
+    if refs_out is None:
+        refs_out = _new(stream, lambda: page_refs.new_empty((cache.n_pages,)))
+    desc = _FORK.pack(old_rows, rows, old_pages, pages, old_stride, stride)
+    workspace = _workspace(workspace, lambda: cache_fork_workspace_bytes(cache, desc), page_refs, stream)
+    _here(cache.k, cache.v, page_table, held_len, page_refs, keep_len, room_len, parents, table_out, refs_out, workspace)
+    _check(load().waveal_cache_fork(cache.desc, desc, cache.k.data_ptr(), cache.v.data_ptr(), page_table.data_ptr(), held, refs, parent, keep, room,
+                                    table_out.data_ptr(), _ints("refs_out", refs_out, (cache.n_pages,)), workspace.data_ptr(), workspace.numel(),
+                                    _status(dev_status), _stream(stream)))
+    return table_out, refs_out
+
+
+class Compacted(NamedTuple):
+    page_table: object      # [rows, pages] or None
+    prefix_pages: object    # or None
+    page_refs: object       # [n_pages]
+    place: object           # [n_pages]: every page's new number, -1 for a free one
+    used: object            # [1]: pages in use; they are the first ones now
+
+
+def cache_compact_workspace_bytes(cache: PagedCache) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().waveal_cache_compact_workspace_bytes(cache.desc, ctypes.byref(n)))
+    return n.value
+
+
+def cache_compact(cache: PagedCache, page_refs, page_table=None, prefix_pages=None, workspace=None, stream=None) -> Compacted:
+    """waveal_cache_compact: moves the pages that are in use (page_refs int32 [n_pages] above zero) to the lowest numbers and translates
+    page_table int32 [rows, pages] and the list prefix_pages, where given.  Returns new tensors (Compacted); other lists of pages are translated by
+    `place`."""
+    _load_torch()
+    refs = _ints("page_refs", page_refs, (cache.n_pages,))
+    n = cache.n_pages
+    rows = pages = old_stride = 0
+    table = prefix = None
+    if page_table is not None:
+        rows, pages, old_stride = _table("page_table", page_table)
+        table = _new(stream, lambda: page_table.new_empty((rows, pages)))
+    count = 0
+    if prefix_pages is not None:
+        count = prefix_pages.numel()
+        _ints("prefix_pages", prefix_pages, (count,))
+        prefix = _new(stream, lambda: prefix_pages.new_empty((count,)))
+    numbers = _new(stream, lambda: page_refs.new_empty((2 * n + 1,)))
+    refs_out, place, used = numbers.as_strided((n,), (1,), 0), numbers.as_strided((n,), (1,), n), numbers.as_strided((1,), (1,), 2 * n)
+    workspace = _workspace(workspace, lambda: cache_compact_workspace_bytes(cache), page_refs, stream)
+    _here(cache.k, cache.v, page_refs, page_table, prefix_pages, workspace)
+    at = numbers.data_ptr()
+    _check(load().waveal_cache_compact(cache.desc, _COMPACT.pack(rows, pages, count, old_stride, pages), cache.k.data_ptr(), cache.v.data_ptr(), refs,
+                                       _ptr(page_table), _ptr(prefix_pages), at, _ptr(table), _ptr(prefix), at + 4 * n, at + 8 * n,
+                                       workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    return Compacted(table, prefix, refs_out, place, used)
+
+
+def cache_copy(to: PagedCache, to_pages, source: PagedCache, from_pages, dev_status=None, stream=None):
+    """waveal_cache_copy: page from_pages[i] of `source` goes to page to_pages[i] of `to` (which may be the same cache); -1 on either side:
+    nothing.  int32 lists; a page that is written stands in to_pages once and, in one cache, not in from_pages."""
+    _load_torch()
+    if to.dtype is not source.dtype:
+        raise TypeError("the caches must have one type")
+    count = to_pages.numel()
+    t, f = _ints("to_pages", to_pages, (count,)), _ints("from_pages", from_pages, (count,))
+    _here(to.k, to.v, source.k, source.v, to_pages, from_pages)
+    _check(load().waveal_cache_copy(to.desc, source.desc, count, source.k.data_ptr(), source.v.data_ptr(), to.k.data_ptr(), to.v.data_ptr(), f, t,
+                                    _status(dev_status), _stream(stream)))

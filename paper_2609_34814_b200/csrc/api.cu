@@ -17,6 +17,7 @@ extern "C" const char* waveal_status_string(waveal_status s) {
     case WAVEAL_ERR_BAD_MASK: return "bad mask (device-side check)";
     case WAVEAL_ERR_CUDA: return "CUDA call failed";
     case WAVEAL_ERR_TIMEOUT: return "device-side wait timed out";
+    case WAVEAL_ERR_NO_PAGES: return "no free pages (device-side)";
   }
   return "unknown status";
 }

@@ -1,0 +1,668 @@
+// Pages of a cache's pool: the rows of a page table go on from rows of the last one (forking, growing, cutting back, ending), the pages
+// in use go to the lowest numbers of the pool, pages go from one cache to another.
+//
+// Which page goes where is decided by the pages' counts: how many rows hold each.  Sums over the pool and over the rows decide the
+// places, so the result does not depend on the order in which threads run.  A call that decides has two launches: one thread block or
+// one cluster of up to eight does the sums (its phases are separated by the cluster's own barrier; no thread waits on a flag in memory),
+// then a grid over all SMs copies what the decision says.  The first is latency (a few round trips to memory), the second
+// memory traffic: a warp has four 16-byte loads under way a lane before it stores any.
+#include <algorithm>
+#include <climits>
+#include "host_common.h"
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kCluster = 8;                          // thread blocks that decide, at most (the portable size)
+constexpr int kCopyThreads = 256, kCopyBlocks = 8;   // blocks an SM
+constexpr int kUnroll = 4;                           // vectors of a lane under way
+constexpr int kSegment = 32 * kUnroll;               // vectors of a warp's turn
+constexpr int kRun = 512;                            // table entries of a warp's turn
+
+__device__ void report(int* status, int code, int site, int where, int value) {
+  if (status && atomicCAS(status, 0, code) == 0) status[1] = site, status[2] = where, status[3] = value;
+}
+
+__device__ __forceinline__ void sync_plan() {
+  if (gridDim.x == 1) {
+    __syncthreads();
+  } else {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+  }
+}
+
+// ------------------------------------------------------------------ copying pages
+
+// One of a cache's two tensors, in vectors (of 16 bytes, or of one element where something is not aligned to that)
+struct Side { long long page, head, token; };
+struct PageShape {
+  int heads, vecs;         // vectors of a token's head
+  int shift;               // log2 of the page's tokens
+  int token_major;         // which of head and token is the inner one in the destination's memory
+  int packed;              // both sides hold a page in one piece, in the same order
+  unsigned total;          // vectors of a page (below 2^31)
+  int segments;            // warps' turns of a page
+  Side from[2], to[2];
+};
+
+// A warp's turn: vectors [segment * kSegment, ...) of the first `tokens` tokens of a page.
+template <class V>
+__device__ __forceinline__ void copy_segment(const PageShape& s, const V* from, V* to, int which, int segment, int tokens, int lane) {
+  V x[kUnroll];
+  long long at[kUnroll];
+  const unsigned first = (unsigned)segment * kSegment + lane;
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const unsigned i = first + 32 * u;
+    at[u] = -1;
+    if (i >= s.total) continue;
+    if (s.packed && tokens >> s.shift) {             // (the whole page)
+      at[u] = i;
+      x[u] = __ldg(from + i);
+      continue;
+    }
+    const unsigned row = i / (unsigned)s.vecs, col = i - row * s.vecs;
+    unsigned head, token;
+    if (s.token_major) {
+      token = row / (unsigned)s.heads, head = row - token * s.heads;
+    } else {
+      head = row >> s.shift, token = row & ((1u << s.shift) - 1);
+    }
+    if ((int)token >= tokens) continue;
+    at[u] = head * s.to[which].head + token * s.to[which].token + col;
+    x[u] = __ldg(from + head * s.from[which].head + token * s.from[which].token + col);
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u)
+    if (at[u] >= 0) to[at[u]] = x[u];
+}
+
+struct Tensors { const void* from[2]; void* to[2]; };
+
+// turn `i` of a pair of pages: its tensor and its segment
+template <class V>
+__device__ __forceinline__ void copy_turn(const PageShape& s, const Tensors& t, int from, int to, int i, int tokens, int lane) {
+  const int which = i >= s.segments, segment = i - which * s.segments;
+  copy_segment<V>(s, static_cast<const V*>(t.from[which]) + from * s.from[which].page, static_cast<V*>(t.to[which]) + to * s.to[which].page, which, segment,
+                  tokens, lane);
+}
+
+struct CopyParams {
+  PageShape shape;
+  Tensors t;
+  const int *from_pages, *to_pages;
+  int count, from_n, to_n;
+  int* dev_status;
+};
+
+template <class V>
+__global__ void __launch_bounds__(kCopyThreads) k_copy_pages(const __grid_constant__ CopyParams p) {
+  const int lane = threadIdx.x & 31;
+  const long long turns = 2ll * p.shape.segments * p.count, step = (long long)gridDim.x * (kCopyThreads / 32);
+  for (long long w = (long long)blockIdx.x * (kCopyThreads / 32) + threadIdx.x / 32; w < turns; w += step) {
+    const int pair = (int)(w / (2 * p.shape.segments)), i = (int)(w - (long long)pair * 2 * p.shape.segments);
+    const int from = p.from_pages[pair], to = p.to_pages[pair];
+    if (from == -1 || to == -1) continue;
+    if (from < 0 || from >= p.from_n || to < 0 || to >= p.to_n) {
+      if (i == 0 && lane == 0) report(p.dev_status, WAVEAL_ERR_BAD_MASK, from < 0 || from >= p.from_n ? 89 : 90, pair, from < 0 || from >= p.from_n ? from : to);
+      continue;
+    }
+    copy_turn<V>(p.shape, p.t, from, to, i, 1 << p.shape.shift, lane);
+  }
+}
+
+// ------------------------------------------------------------------ sums over a thread block
+
+// of the threads in front of this one; total: of all.  (Two barriers; shared: 33 words.)
+__device__ __forceinline__ int scan_block(int x, int* shared, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  int upto = x;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += y;
+  }
+  __syncthreads();                                   // (the words may still be read from the last call)
+  if (lane == 31) shared[warp] = upto;
+  __syncthreads();
+  int sums = shared[lane];                           // kPlanThreads / 32 == 32 warps
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int y = __shfl_up_sync(0xffffffffu, sums, d);
+    if (lane >= d) sums += y;
+  }
+  total = __shfl_sync(0xffffffffu, sums, 31);
+  const int before = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
+  return upto - x + (warp ? before : 0);
+}
+static_assert(kPlanThreads == 32 * 32, "scan_block");
+
+// this block's part of n things, begin a multiple of kPerThread
+constexpr int kPerThread = 8;                        // pages of a thread's turn: a 32-byte sector of their counts
+struct Part { int begin, end; };
+__device__ __forceinline__ Part part_of(int n) {
+  const long long each = ((long long)n + gridDim.x - 1) / gridDim.x, up = (each + kPerThread - 1) / kPerThread * kPerThread;
+  return {(int)min((long long)n, up * blockIdx.x), (int)min((long long)n, up * (blockIdx.x + 1))};
+}
+
+// ------------------------------------------------------------------ forking
+
+struct ForkParams {
+  PageShape shape;
+  Tensors t;
+  int old_rows, rows, old_pages, pages, n_pages;
+  long long old_stride, stride;
+  const int *old_table, *held, *refs, *parents, *keep, *room;
+  int *table, *new_refs;
+  // workspace
+  int* kids;               // [3][old_rows]: rows that go on from this one; the fewest and the most full pages that they keep
+  int* ends;               // [n_pages], of pages that rows end in: the first of these rows
+  int4* row;               // [rows]: parent or -1, full pages kept, pages in all, tokens in the page filled in part (bit 30: the row keeps that page)
+  int2* last;              // [rows]: the page filled in part (-1: none), where the row's fresh pages begin
+  int* fresh;              // [n_pages]: free pages in ascending order, as many as are needed
+  int* sums;               // [2][kCluster]
+  int* free_pages;         // [1]
+  int* dev_status;
+};
+constexpr int kStays = 1 << 30;
+
+__device__ __forceinline__ int held_tokens(const ForkParams& p, int r) {
+  const int n = p.held[r];
+  return n < 0 || n > (long long)p.old_pages << p.shape.shift ? 0 : n;
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_constant__ ForkParams p) {
+  __shared__ int shared[33];
+  waveal::let_next_kernel_start();
+  const int tid = blockIdx.x * kPlanThreads + threadIdx.x, threads = gridDim.x * kPlanThreads;
+  const int warp = tid / 32, warps = threads / 32, lane = threadIdx.x & 31;
+  const int shift = p.shape.shift, mask = (1 << shift) - 1;
+  int *count = p.kids, *fewest = p.kids + p.old_rows, *most = p.kids + 2 * p.old_rows;
+
+  for (int i = tid; i < p.n_pages; i += threads) p.new_refs[i] = p.refs[i];
+  for (int r = tid; r < p.old_rows; r += threads) {
+    count[r] = 0, fewest[r] = INT_MAX, most[r] = 0;
+    const int n = p.held[r];
+    if (n < 0 || n > (long long)p.old_pages << shift) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 81, r, n);
+  }
+  sync_plan();
+
+  // ---- what every row keeps
+  for (int b = tid; b < p.rows; b += threads) {
+    int parent = p.parents ? p.parents[b] : b, keep = p.keep[b], room = p.room[b];
+    if (parent >= p.old_rows) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 80, b, parent), parent = -1;
+    if (parent >= 0 && (keep < 0 || keep > held_tokens(p, parent))) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 82, b, keep), parent = -1;
+    room = max(room, keep);
+    if (parent >= 0 && room > (long long)p.pages << shift) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 83, b, room), parent = -1;
+    int4 row = {-1, 0, 0, 0};
+    int page = -1;
+    if (parent >= 0) {
+      row = {parent, keep >> shift, (int)(((long long)room + mask) >> shift), keep & mask};
+      if (row.w) {
+        page = p.old_table[parent * p.old_stride + row.y];
+        if (page < 0 || page >= p.n_pages) {
+          report(p.dev_status, WAVEAL_ERR_BAD_MASK, 84, b, page);
+          page = -1;
+        } else {
+          p.ends[page] = INT_MAX;
+        }
+      }
+      atomicAdd(count + parent, 1);
+      atomicMin(fewest + parent, row.y);
+      atomicMax(most + parent, row.y);
+    }
+    p.row[b] = row;
+    p.last[b] = {page, 0};
+  }
+  sync_plan();
+
+  // ---- counts: a page of an old row that k rows share goes from one holder to k.  (Rows of one child: no change up to what it keeps.)
+  const int old_runs = (p.old_pages + kRun - 1) / kRun, runs = (p.pages + kRun - 1) / kRun;
+  for (long long u = warp; u < (long long)p.old_rows * old_runs; u += warps) {
+    const int r = (int)(u / old_runs), run = (int)(u - (long long)r * old_runs);
+    const int kids = __ldcg(count + r), all = kids ? __ldcg(fewest + r) : 0, pages = (int)(((long long)held_tokens(p, r) + mask) >> shift);
+    for (int j = max(run * kRun, kids == 1 ? all : 0) + lane; j < min(pages, (run + 1) * kRun); j += 32) {
+      const int change = (j < all ? kids : 0) - 1, page = p.old_table[r * p.old_stride + j];
+      if (change && page >= 0 && page < p.n_pages) atomicAdd(p.new_refs + page, change);
+    }
+  }
+  for (long long u = warp; u < (long long)p.rows * runs; u += warps) {
+    const int b = (int)(u / runs), run = (int)(u - (long long)b * runs);
+    const int4 row = __ldcg(p.row + b);
+    if (row.x < 0) continue;
+    for (int j = max(run * kRun, __ldcg(fewest + row.x)) + lane; j < min(row.y, (run + 1) * kRun); j += 32) {
+      const int page = p.old_table[row.x * p.old_stride + j];
+      if (page >= 0 && page < p.n_pages) atomicAdd(p.new_refs + page, 1);
+    }
+  }
+  for (int b = tid; b < p.rows; b += threads) {
+    const int page = __ldcg(p.last + b).x;
+    if (page >= 0) atomicMin(p.ends + page, b);
+  }
+  sync_plan();
+
+  // ---- a page filled in part stays with the first row that ends in it, if nobody else holds it
+  for (int b = tid; b < p.rows; b += threads) {
+    int4 row = __ldcg(p.row + b);
+    const int page = __ldcg(p.last + b).x;
+    bool stays = row.w && page < 0;                  // (no page to copy from: the row gets -1 there)
+    if (page >= 0 && __ldcg(p.ends + page) == b && __ldcg(p.new_refs + page) <= 0) {
+      stays = true;
+      p.new_refs[page] = 1;
+    }
+    if (stays) p.row[b].w = row.w | kStays;
+    p.last[b].y = row.z - row.y - stays;             // fresh pages
+  }
+  sync_plan();
+
+  // ---- sums of the blocks' parts: free pages, fresh pages
+  const Part pages = part_of(p.n_pages), rows = part_of(p.rows);
+  int free_here = 0, need_here = 0, total;
+  for (int i = pages.begin + threadIdx.x; i < pages.end; i += kPlanThreads) free_here += __ldcg(p.new_refs + i) <= 0;
+  for (int b = rows.begin + threadIdx.x; b < rows.end; b += kPlanThreads) need_here += __ldcg(p.last + b).y;
+  scan_block(free_here, shared, total);
+  if (threadIdx.x == 0) p.sums[blockIdx.x] = total;
+  scan_block(need_here, shared, total);
+  if (threadIdx.x == 0) p.sums[kCluster + blockIdx.x] = total;
+  sync_plan();
+  int free_before = 0, need_before = 0, free_all = 0, need_all = 0;
+  for (int i = 0; i < (int)gridDim.x; ++i) {
+    const int f = __ldcg(p.sums + i), n = __ldcg(p.sums + kCluster + i);
+    if (i < (int)blockIdx.x) free_before += f, need_before += n;
+    free_all += f, need_all += n;
+  }
+  if (tid == 0) *p.free_pages = free_all;
+
+  // ---- where every row's fresh pages begin, and which pages these are
+  for (int b0 = rows.begin; b0 < rows.end; b0 += kPlanThreads) {
+    const int b = b0 + threadIdx.x, need = b < rows.end ? __ldcg(p.last + b).y : 0;
+    const int begin = need_before + scan_block(need, shared, total);
+    need_before += total;
+    if (b < rows.end) {
+      p.last[b].y = begin;
+      if (begin <= free_all && begin + need > free_all) report(p.dev_status, WAVEAL_ERR_NO_PAGES, 85, b, need_all - free_all);
+    }
+  }
+  for (int i0 = pages.begin; i0 < pages.end && free_before < need_all; i0 += kPlanThreads * kPerThread) {
+    const int i = i0 + threadIdx.x * kPerThread;
+    unsigned is_free = 0;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k)
+      if (i + k < pages.end && __ldcg(p.new_refs + i + k) <= 0) is_free |= 1u << k;
+    int at = free_before + scan_block(__popc(is_free), shared, total);
+    free_before += total;
+    for (; is_free && at < need_all; is_free &= is_free - 1, ++at) {
+      const int page = i + __ffs(is_free) - 1;
+      p.fresh[at] = page;
+      p.new_refs[page] = 1;
+    }
+  }
+}
+
+template <class V>
+__global__ void __launch_bounds__(kCopyThreads) k_fork_apply(const __grid_constant__ ForkParams p) {
+  const int lane = threadIdx.x & 31;
+  const long long warp = (long long)blockIdx.x * (kCopyThreads / 32) + threadIdx.x / 32, warps = (long long)gridDim.x * (kCopyThreads / 32);
+  const int turns = 2 * p.shape.segments;
+  waveal::wait_for_previous_kernel();
+  const int free_all = *p.free_pages;
+  // the pages that rows filled in part and do not keep
+  for (long long w = warp; w < (long long)p.rows * turns; w += warps) {
+    const int b = (int)(w / turns);
+    const int4 row = p.row[b];
+    const int2 last = p.last[b];
+    if (row.w == 0 || row.w & kStays || last.y >= free_all) continue;
+    copy_turn<V>(p.shape, p.t, last.x, p.fresh[last.y], (int)(w - (long long)b * turns), row.w, lane);
+  }
+  // the table
+  const int runs = (p.pages + kRun - 1) / kRun;
+  for (long long u = warp; u < (long long)p.rows * runs; u += warps) {
+    const int b = (int)(u / runs), run = (int)(u - (long long)b * runs);
+    const int4 row = p.row[b];
+    const int2 last = p.last[b];
+    const int stays = row.w & kStays ? 1 : 0;
+    for (int j = run * kRun + lane; j < min(p.pages, (run + 1) * kRun); j += 32) {
+      int page = -1;
+      if (j < row.y) {
+        page = p.old_table[row.x * p.old_stride + j];
+        if (page < 0 || page >= p.n_pages) {
+          report(p.dev_status, WAVEAL_ERR_BAD_MASK, 84, b, page);
+          page = -1;
+        }
+      } else if (j == row.y && stays) {
+        page = last.x;
+      } else if (j < row.z) {
+        const int i = last.y + j - row.y - stays;
+        if (i < free_all) page = p.fresh[i];
+      }
+      p.table[b * p.stride + j] = page;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ compacting
+
+struct CompactParams {
+  PageShape shape;
+  Tensors t;
+  int rows, pages, n_pages, prefix;
+  long long old_stride, stride;
+  const int *refs, *old_table, *old_prefix;
+  int *new_refs, *table, *new_prefix, *place, *used;
+  // workspace
+  int* from;               // [n_pages]: pages in use behind the first n, at the number of pages in use in front of them
+  int* to;                 // [n_pages]: free pages among the first n
+  int* sums;               // [kCluster]
+  int* first;              // [1]: pages in use among the first n: where `from` begins
+};
+
+__global__ void __launch_bounds__(kPlanThreads, 1) k_compact_plan(const __grid_constant__ CompactParams p) {
+  __shared__ int shared[33];
+  waveal::let_next_kernel_start();
+  const Part pages = part_of(p.n_pages);
+  int here = 0, total;
+  for (int i = pages.begin + threadIdx.x; i < pages.end; i += kPlanThreads) here += p.refs[i] > 0;
+  scan_block(here, shared, total);
+  if (threadIdx.x == 0) p.sums[blockIdx.x] = total;
+  sync_plan();
+  int before = 0, n = 0;
+  for (int i = 0; i < (int)gridDim.x; ++i) {
+    const int x = __ldcg(p.sums + i);
+    if (i < (int)blockIdx.x) before += x;
+    n += x;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *p.used = n;
+    if (n == p.n_pages) *p.first = n;
+  }
+  // the i-th page in use from n on goes to the i-th free page below n
+  for (int i0 = pages.begin; i0 < pages.end; i0 += kPlanThreads * kPerThread) {
+    const int i = i0 + threadIdx.x * kPerThread;
+    unsigned in_use = 0;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k)
+      if (i + k < pages.end && p.refs[i + k] > 0) in_use |= 1u << k;
+    int at = before + scan_block(__popc(in_use), shared, total);
+    before += total;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+      const int page = i + k;
+      if (page >= pages.end) break;
+      const bool u = in_use >> k & 1;
+      if (page == n) *p.first = at;
+      if (u && page >= n) p.from[at] = page;
+      if (!u && page < n) p.to[page - at] = page;
+      p.place[page] = at;                            // (for the next pass)
+      at += u;
+    }
+  }
+  sync_plan();
+  const int first = __ldcg(p.first);
+  for (int page = pages.begin + threadIdx.x; page < pages.end; page += kPlanThreads) {
+    const int count = p.refs[page];
+    int place = -1;
+    if (count > 0) {
+      place = page < n ? page : __ldcg(p.to + (__ldcg(p.place + page) - first));
+      p.new_refs[place] = count;
+    }
+    if (page >= n) p.new_refs[page] = 0;
+    p.place[page] = place;
+  }
+}
+
+template <class V>
+__global__ void __launch_bounds__(kCopyThreads) k_compact_apply(const __grid_constant__ CompactParams p) {
+  const int lane = threadIdx.x & 31;
+  const long long warp = (long long)blockIdx.x * (kCopyThreads / 32) + threadIdx.x / 32, warps = (long long)gridDim.x * (kCopyThreads / 32);
+  waveal::wait_for_previous_kernel();
+  const int first = *p.first, moves = *p.used - first, turns = 2 * p.shape.segments;
+  for (long long w = warp; w < (long long)moves * turns; w += warps) {
+    const int i = (int)(w / turns);
+    copy_turn<V>(p.shape, p.t, p.from[first + i], p.to[i], (int)(w - (long long)i * turns), 1 << p.shape.shift, lane);
+  }
+  auto moved = [&](int page) { return page >= 0 && page < p.n_pages ? p.place[page] : -1; };
+  const int runs = (p.pages + kRun - 1) / kRun;
+  for (long long u = warp; u < (long long)p.rows * runs; u += warps) {
+    const int b = (int)(u / runs), run = (int)(u - (long long)b * runs);
+    for (int j = run * kRun + lane; j < min(p.pages, (run + 1) * kRun); j += 32) p.table[b * p.stride + j] = moved(p.old_table[b * p.old_stride + j]);
+  }
+  for (long long i = warp * 32 + lane; i < p.prefix; i += warps * 32) p.new_prefix[i] = moved(p.old_prefix[i]);
+}
+
+// ------------------------------------------------------------------ host
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+waveal_status check_pool(const waveal_cache_desc* c) {
+  if (!c) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "cache is NULL");
+  if (waveal_status e = waveal::check_cache(c)) return e;
+  if (c->head_dim < 2 || c->head_dim > 512) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "head_dim %d (supported: 2 .. 512)", c->head_dim);
+  if ((long long)c->kv_heads * c->page_size * c->head_dim > INT_MAX) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^31 - 1 elements in a page");
+  return WAVEAL_OK;
+}
+
+// a cache's tensors, or two caches', as the copying kernels see them; wide: 16-byte vectors
+bool page_shape(PageShape& s, Tensors& t, const waveal_cache_desc* from, const void* from_k, const void* from_v, const waveal_cache_desc* to, void* to_k,
+                void* to_v) {
+  const int64_t *in[2] = {from->k_stride, from->v_stride}, *out[2] = {to->k_stride, to->v_stride};
+  t = {{from_k, from_v}, {to_k, to_v}};
+  bool wide = from->head_dim % 8 == 0;
+  for (int i = 0; i < 2; ++i) {
+    wide = wide && waveal::aligned(t.from[i], 16) && waveal::aligned(t.to[i], 16);
+    for (int j = 0; j < 3; ++j) wide = wide && in[i][j] % 8 == 0 && out[i][j] % 8 == 0;
+  }
+  const int64_t vec = wide ? 8 : 1, dim = from->head_dim, heads = from->kv_heads, tokens = from->page_size;
+  s.heads = from->kv_heads, s.vecs = (int)(dim / vec), s.shift = __builtin_ctz((unsigned)from->page_size);
+  s.token_major = out[0][2] > out[0][1];
+  s.packed = 1;
+  for (int i = 0; i < 2; ++i) {
+    s.from[i] = {in[i][0] / vec, in[i][1] / vec, in[i][2] / vec}, s.to[i] = {out[i][0] / vec, out[i][1] / vec, out[i][2] / vec};
+    const bool by_head = in[i][2] == dim && out[i][2] == dim && in[i][1] == dim * tokens && out[i][1] == dim * tokens;
+    const bool by_token = in[i][1] == dim && out[i][1] == dim && in[i][2] == dim * heads && out[i][2] == dim * heads;
+    if (!by_head && !by_token) s.packed = 0;
+  }
+  s.total = (unsigned)(heads * tokens * s.vecs);
+  s.segments = (int)((s.total + kSegment - 1) / kSegment);
+  return wide;
+}
+
+// blocks of a copying grid: one for every eight warps' turns, at most what the SMs hold
+unsigned copy_grid(long long turns) {
+  const long long blocks = (turns + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
+  return (unsigned)std::max(1ll, std::min(blocks, (long long)waveal::sm_count() * kCopyBlocks));
+}
+
+// thread blocks that decide: one up to 8,192 pages or as many table entries, where a barrier of the cluster costs more than it saves
+int plan_blocks(long long pages, long long entries) {
+  int n = 1;
+  while (n < kCluster && std::max(pages, entries) / 8192 >= 2 * n) n *= 2;
+  return n;
+}
+
+template <class P>
+waveal_status launch_plan(void (*kernel)(P), const P& p, int blocks, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kPlanThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)blocks, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = 1;
+  WAVEAL_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, p));
+  return WAVEAL_OK;
+}
+
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+  return x && y && x < y + b_bytes && y < x + a_bytes;
+}
+size_t table_bytes(int rows, int pages, int64_t stride) { return rows && pages ? ((size_t)(rows - 1) * stride + pages) * sizeof(int) : 0; }
+
+waveal_status check_fork(const waveal_cache_desc* c, const waveal_fork_desc* f) {
+  if (waveal_status e = check_pool(c)) return e;
+  if (!f) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "fork is NULL");
+  if (f->old_rows < 0 || f->rows < 0 || f->old_pages < 0 || f->pages < 0)
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "rows and pages must not be negative");
+  if (f->old_stride < f->old_pages || f->stride < f->pages) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "a table's stride is smaller than its pages");
+  if ((long long)f->old_rows * f->old_pages > INT_MAX || (long long)f->rows * f->pages > INT_MAX)
+    return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^31 - 1 entries in a table");
+  return WAVEAL_OK;
+}
+
+struct ForkLayout { size_t kids, ends, row, last, fresh, sums, bytes; };
+ForkLayout fork_layout(const waveal_cache_desc* c, const waveal_fork_desc* f) {
+  ForkLayout l;
+  l.sums = 0;
+  l.kids = up256((2 * kCluster + 1) * sizeof(int));
+  l.ends = l.kids + up256((size_t)f->old_rows * 3 * sizeof(int));
+  l.row = l.ends + up256((size_t)c->n_pages * sizeof(int));
+  l.last = l.row + up256((size_t)f->rows * sizeof(int4));
+  l.fresh = l.last + up256((size_t)f->rows * sizeof(int2));
+  l.bytes = l.fresh + up256((size_t)c->n_pages * sizeof(int));
+  return l;
+}
+
+struct CompactLayout { size_t from, to, sums, bytes; };
+CompactLayout compact_layout(const waveal_cache_desc* c) {
+  CompactLayout l;
+  l.sums = 0;
+  l.from = up256((kCluster + 1) * sizeof(int));
+  l.to = l.from + up256((size_t)c->n_pages * sizeof(int));
+  l.bytes = l.to + up256((size_t)c->n_pages * sizeof(int));
+  return l;
+}
+
+waveal_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (!ws || have < need) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? have : 0, need);
+  if (!waveal::aligned(ws, 256)) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  return WAVEAL_OK;
+}
+
+waveal_status check_tensors(const void* k, const void* v) {
+  if (!k || !v) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "the caches' keys and values are required");
+  if (!waveal::aligned(k, 2) || !waveal::aligned(v, 2)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "a tensor is not aligned to its element");
+  if (waveal::sm_count() <= 0) return waveal::fail(WAVEAL_ERR_CUDA, "number of SMs not available");
+  return WAVEAL_OK;
+}
+
+}  // namespace
+
+extern "C" waveal_status waveal_cache_copy(const waveal_cache_desc* to, const waveal_cache_desc* from, int32_t count, const void* from_k,
+                                           const void* from_v, void* to_k, void* to_v, const int32_t* from_pages, const int32_t* to_pages,
+                                           int32_t* dev_status, void* cuda_stream) {
+  if (waveal_status e = check_pool(to)) return e;
+  if (waveal_status e = check_pool(from)) return e;
+  if (to->page_size != from->page_size || to->kv_heads != from->kv_heads || to->head_dim != from->head_dim || to->dtype != from->dtype)
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "the caches differ in page_size, kv_heads, head_dim or dtype");
+  if (count < 0) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "count must not be negative");
+  if (count == 0) {
+    waveal::launch_counter() = 0;
+    return WAVEAL_OK;
+  }
+  if (!from_pages || !to_pages) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "from_pages and to_pages are required");
+  if (waveal_status e = check_tensors(from_k, from_v)) return e;
+  if (waveal_status e = check_tensors(to_k, to_v)) return e;
+  CopyParams p = {};
+  const bool wide = page_shape(p.shape, p.t, from, from_k, from_v, to, to_k, to_v);
+  p.from_pages = from_pages, p.to_pages = to_pages, p.count = count;
+  p.from_n = from->n_pages, p.to_n = to->n_pages, p.dev_status = dev_status;
+  const unsigned grid = copy_grid(2ll * p.shape.segments * count);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (wide) k_copy_pages<uint4><<<grid, kCopyThreads, 0, st>>>(p);
+  else k_copy_pages<unsigned short><<<grid, kCopyThreads, 0, st>>>(p);
+  WAVEAL_CUDA_OK(cudaGetLastError());
+  waveal::launch_counter() = 1;
+  return WAVEAL_OK;
+}
+
+extern "C" waveal_status waveal_cache_fork_workspace_bytes(const waveal_cache_desc* cache, const waveal_fork_desc* fork, size_t* bytes) {
+  if (!bytes) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "bytes is NULL");
+  if (waveal_status e = check_fork(cache, fork)) return e;
+  *bytes = fork_layout(cache, fork).bytes;
+  return WAVEAL_OK;
+}
+
+extern "C" waveal_status waveal_cache_fork(const waveal_cache_desc* c, const waveal_fork_desc* f, void* k_cache, void* v_cache,
+                                           const int32_t* old_table, const int32_t* held_len, const int32_t* page_refs, const int32_t* parents,
+                                           const int32_t* keep_len, const int32_t* room_len, int32_t* table, int32_t* new_refs, void* ws,
+                                           size_t ws_bytes, int32_t* dev_status, void* cuda_stream) {
+  if (waveal_status e = check_fork(c, f)) return e;
+  if (!page_refs || !new_refs || (f->old_rows && !held_len) || (f->old_rows && f->old_pages && !old_table) || (f->rows && (!keep_len || !room_len)) ||
+      (f->rows && f->pages && !table))
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "page_refs and new_refs are required, held_len and old_table with old rows, keep_len, room_len and table "
+                                                "with rows");
+  if (!parents && f->rows && f->rows != f->old_rows) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "without parents there are as many rows as before");
+  if (waveal_status e = check_tensors(k_cache, v_cache)) return e;
+  const size_t refs = (size_t)c->n_pages * sizeof(int);
+  if (overlap(page_refs, refs, new_refs, refs) ||
+      overlap(old_table, table_bytes(f->old_rows, f->old_pages, f->old_stride), table, table_bytes(f->rows, f->pages, f->stride)))
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "the new table and counts must not lie over the old ones");
+  const ForkLayout l = fork_layout(c, f);
+  if (waveal_status e = check_workspace(ws, ws_bytes, l.bytes)) return e;
+  ForkParams p = {};
+  const bool wide = page_shape(p.shape, p.t, c, k_cache, v_cache, c, k_cache, v_cache);
+  p.old_rows = f->old_rows, p.rows = f->rows, p.old_pages = f->old_pages, p.pages = f->pages, p.n_pages = c->n_pages;
+  p.old_stride = f->old_stride, p.stride = f->stride;
+  p.old_table = old_table, p.held = held_len, p.refs = page_refs, p.parents = parents, p.keep = keep_len, p.room = room_len;
+  p.table = table, p.new_refs = new_refs;
+  char* w = static_cast<char*>(ws);
+  p.sums = reinterpret_cast<int*>(w + l.sums), p.free_pages = p.sums + 2 * kCluster;
+  p.kids = reinterpret_cast<int*>(w + l.kids), p.ends = reinterpret_cast<int*>(w + l.ends);
+  p.row = reinterpret_cast<int4*>(w + l.row), p.last = reinterpret_cast<int2*>(w + l.last), p.fresh = reinterpret_cast<int*>(w + l.fresh);
+  p.dev_status = dev_status;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const long long entries = (long long)f->old_rows * f->old_pages;
+  if (waveal_status e = launch_plan(k_fork_plan, p, plan_blocks(c->n_pages, entries), st)) return e;
+  const unsigned grid = copy_grid((long long)f->rows * (2 * p.shape.segments + (f->pages + kRun - 1) / kRun));
+  if (wide) WAVEAL_CUDA_OK(waveal::launch_chained(k_fork_apply<uint4>, dim3(grid), kCopyThreads, 0, st, p));
+  else WAVEAL_CUDA_OK(waveal::launch_chained(k_fork_apply<unsigned short>, dim3(grid), kCopyThreads, 0, st, p));
+  waveal::launch_counter() = 2;
+  return WAVEAL_OK;
+}
+
+extern "C" waveal_status waveal_cache_compact_workspace_bytes(const waveal_cache_desc* cache, size_t* bytes) {
+  if (!bytes) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "bytes is NULL");
+  if (waveal_status e = check_pool(cache)) return e;
+  *bytes = compact_layout(cache).bytes;
+  return WAVEAL_OK;
+}
+
+extern "C" waveal_status waveal_cache_compact(const waveal_cache_desc* c, const waveal_compact_desc* d, void* k_cache, void* v_cache,
+                                              const int32_t* page_refs, const int32_t* old_table, const int32_t* old_prefix, int32_t* new_refs,
+                                              int32_t* table, int32_t* prefix, int32_t* place, int32_t* used, void* ws, size_t ws_bytes,
+                                              void* cuda_stream) {
+  if (waveal_status e = check_pool(c)) return e;
+  if (!d) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "compact is NULL");
+  if (d->rows < 0 || d->pages < 0 || d->prefix_pages < 0)
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "rows, pages and prefix_pages must not be negative");
+  if (d->old_stride < d->pages || d->stride < d->pages) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "a table's stride is smaller than its pages");
+  if ((long long)d->rows * d->pages > INT_MAX) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^31 - 1 entries in a table");
+  const bool has_table = d->rows && d->pages;
+  if (!page_refs || !new_refs || !place || !used || (has_table && (!old_table || !table)) || (d->prefix_pages && (!old_prefix || !prefix)))
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "page_refs, new_refs, place and used are required, both tables with rows, both lists with prefix_pages");
+  if (waveal_status e = check_tensors(k_cache, v_cache)) return e;
+  const size_t refs = (size_t)c->n_pages * sizeof(int), list = (size_t)d->prefix_pages * sizeof(int);
+  if (overlap(page_refs, refs, new_refs, refs) || overlap(old_prefix, list, prefix, list) ||
+      overlap(old_table, table_bytes(d->rows, d->pages, d->old_stride), table, table_bytes(d->rows, d->pages, d->stride)))
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "the new tables and counts must not lie over the old ones");
+  const CompactLayout l = compact_layout(c);
+  if (waveal_status e = check_workspace(ws, ws_bytes, l.bytes)) return e;
+  CompactParams p = {};
+  const bool wide = page_shape(p.shape, p.t, c, k_cache, v_cache, c, k_cache, v_cache);
+  p.rows = d->rows, p.pages = d->pages, p.n_pages = c->n_pages, p.prefix = d->prefix_pages;
+  p.old_stride = d->old_stride, p.stride = d->stride;
+  p.refs = page_refs, p.old_table = old_table, p.old_prefix = old_prefix;
+  p.new_refs = new_refs, p.table = table, p.new_prefix = prefix, p.place = place, p.used = used;
+  char* w = static_cast<char*>(ws);
+  p.sums = reinterpret_cast<int*>(w + l.sums), p.first = p.sums + kCluster;
+  p.from = reinterpret_cast<int*>(w + l.from), p.to = reinterpret_cast<int*>(w + l.to);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (waveal_status e = launch_plan(k_compact_plan, p, plan_blocks(c->n_pages, 0), st)) return e;
+  // (how many pages move is known on the device only: half of the pool at most)
+  const unsigned grid = copy_grid((long long)(c->n_pages / 2) * 2 * p.shape.segments + (long long)d->rows * ((d->pages + kRun - 1) / kRun));
+  if (wide) WAVEAL_CUDA_OK(waveal::launch_chained(k_compact_apply<uint4>, dim3(grid), kCopyThreads, 0, st, p));
+  else WAVEAL_CUDA_OK(waveal::launch_chained(k_compact_apply<unsigned short>, dim3(grid), kCopyThreads, 0, st, p));
+  waveal::launch_counter() = 2;
+  return WAVEAL_OK;
+}

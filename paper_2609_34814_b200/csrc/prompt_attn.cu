@@ -1,0 +1,894 @@
+// Attention of whole prompts: every token over its own sequence, causal or not, grouped heads, any lengths in one call.
+//
+//   o[h, t] = sum_j p_j v_j / sum_j p_j,   p_j = 2^(sl2 (q[h, t] . k_j - m)),   sl2 = scale log2(e),   j over what token t sees,
+// with m a running reference of the row (online softmax: the reference follows the row's maximum only when it has been outgrown by
+// more than 2^8, which the same reference in the sum makes exact).
+//
+// A row tile is 128 rows of S: tq = 128 / G tokens with the G query heads that share a key head, so that a key head's tiles are
+// loaded once for all of them and the causal diagonal crosses few of a tile's columns.  A thread block has two slots with a
+// row tile each and walks the key tiles of 128:
+//   slot: S = Q K^T (tensor memory) -> a thread a row: maximum, exponentials, P over the first half of S's columns -> O += P V (tensor memory)
+// One slot is in its products while the other is in its softmax.  A pair of row tiles of a sequence shares its K and V
+// tiles; the first row tile of a sequence with an odd number of them goes with that of another sequence or head (each slot
+// then has its own K and V tiles).
+//
+// Warps: 0-3 and 4-7 softmax of the slots, 8-11 epilogues, 12 items and loads, 13 and 14 the slots' products, 15 masked tiles' values.
+// S and P of a slot share their columns without a barrier: the slot's products are issued by one thread, in order.
+//
+// Values that a token must not see: their probabilities are zero, but zero times NaN is not.  Warp 15 writes zeros over what lies behind a
+// sequence's end and looks through the values of tiles that the causal mask cuts; where one is not finite, the slot's softmax warps add that tile's
+// products themselves, each row's visible keys alone.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+#include "host_common.h"
+#include "sm100.h"
+
+namespace {
+
+using namespace waveal::sm100;
+
+constexpr int kThreads = 512;
+constexpr int kLoadWarp = 12, kIssueWarp = 13, kCheckWarp = 15, kEpilogueWarp = 8;
+constexpr int kTile = 128;                           // keys of a tile, rows of a slot
+constexpr int kItems = 4;                            // between the loader and the others
+constexpr int kItemReaders = 15;                     // two issuers, the checker, eight softmax warps, four of the epilogue
+constexpr int kChecks = 8;                           // masked tiles of a slot whose verdicts are under way (more than the ring has V tiles)
+constexpr long long kTimeoutCycles = 4000000000ll;   // ~2 s at boost clock
+constexpr long long kSelfTestCycles = 4000000ll;     // ~2 ms
+constexpr float kGrowth = 8.0f;                      // log2 of how far a row's maximum may outgrow its reference
+
+template <int D> struct Geo {
+  static constexpr int SLABS = D / 64;               // 128-byte-swizzled slabs of 64 channels
+  static constexpr int SLAB_BYTES = kTile * 128;
+  static constexpr int TILE_BYTES = SLABS * SLAB_BYTES;
+  static constexpr int STAGES = D == 128 ? 5 : 10;   // of the ring of K and V tiles
+  static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE_BYTES, OFF_END = OFF_KV + STAGES * TILE_BYTES;
+  static constexpr int S_COL = 0, O_COL = 256;       // tensor memory: S (and P) 0-127, 128-255, O 256.., 384..
+};
+
+// ------------------------------------------------------------------ what there is to do
+
+// In the workspace, made by the planning kernel: the sequences by descending length (row tiles; longer ones than 1,022 row tiles in any
+// order), each with the number of row-tile pairs of the ones in front of it; those with an odd number of row tiles.
+struct Plan {
+  int4* seq;               // [batch] {first token, tokens, pairs of row tiles in front, 0}
+  int* odd;                // [batch] places in seq
+  int* head;               // [4] {pairs of all sequences, odd ones, tickets given out, sequences with tokens}
+};
+
+struct Params {
+  Plan plan;
+  const int *seq_start, *seq_len;
+  int batch, tokens, kv_heads, group, tq, causal;
+  void* o;
+  float* lse;
+  long long o_stride_h, o_stride_t;
+  int* dev_status;
+  long long wait_limit;
+  int drop_tile;
+  float sl2;               // scale * log2(e)
+};
+
+__host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+__device__ __forceinline__ void report(int* status, int code, int site, int where, int value) {
+  if (status && atomicCAS(status, 0, code) == 0) status[1] = site, status[2] = where, status[3] = value;
+}
+
+// {first token, tokens}; a malformed sequence has none
+__device__ inline int2 read_sequence(const Params& p, int b, bool tell) {
+  const int start = p.seq_start[b], end = p.seq_start[b + 1];
+  if (start < 0 || end < start || end > p.tokens) {
+    if (tell) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 100, b, start < 0 ? start : end);
+    return make_int2(0, 0);
+  }
+  int n = end - start;
+  if (p.seq_len) {
+    const int len = p.seq_len[b];
+    if (len < 0 || len > n) {
+      if (tell) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 101, b, len);
+      return make_int2(0, 0);
+    }
+    n = len;
+  }
+  return make_int2(start, n);
+}
+
+constexpr int kPlanThreads = 1024;
+
+// of the threads in front of this one; total: of all (two barriers; shared: 32 words)
+__device__ __forceinline__ int scan_block(int x, int* shared, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  int upto = x;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += y;
+  }
+  __syncthreads();
+  if (lane == 31) shared[warp] = upto;
+  __syncthreads();
+  int sums = shared[lane];
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int y = __shfl_up_sync(0xffffffffu, sums, d);
+    if (lane >= d) sums += y;
+  }
+  total = __shfl_sync(0xffffffffu, sums, 31);
+  const int before = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
+  return upto - x + (warp ? before : 0);
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 1) k_prompt_plan(const __grid_constant__ Params p) {
+  __shared__ int count[kPlanThreads], shared[32];
+  waveal::let_next_kernel_start();
+  count[threadIdx.x] = 0;
+  __syncthreads();
+  // bucket 0: the longest; the last one: no tokens
+  auto bucket = [&](int n) { return kPlanThreads - 1 - min(ceil_div(n, p.tq), kPlanThreads - 1); };
+  for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) atomicAdd(&count[bucket(read_sequence(p, b, true).y)], 1);
+  __syncthreads();
+  int total;
+  const int mine = count[threadIdx.x], first = scan_block(mine, shared, total);
+  __syncthreads();
+  count[threadIdx.x] = first;
+  if (threadIdx.x == kPlanThreads - 1) p.plan.head[3] = first;
+  __syncthreads();
+  for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) {
+    const int2 q = read_sequence(p, b, false);
+    p.plan.seq[atomicAdd(&count[bucket(q.y)], 1)] = make_int4(q.x, q.y, 0, 0);
+  }
+  __syncthreads();
+  int pairs = 0, odds = 0;
+  for (int r0 = 0; r0 < p.batch; r0 += kPlanThreads) {
+    const int r = r0 + threadIdx.x, tiles = r < p.batch ? ceil_div(p.plan.seq[r].y, p.tq) : 0;
+    const int at = pairs + scan_block(tiles / 2, shared, total);
+    if (r < p.batch) p.plan.seq[r].z = at;
+    pairs += total;
+    const int odd = odds + scan_block(tiles & 1, shared, total);
+    if (tiles & 1) p.plan.odd[odd] = r;
+    odds += total;
+  }
+  if (threadIdx.x == 0) p.plan.head[0] = pairs, p.plan.head[1] = odds, p.plan.head[2] = 0;
+}
+
+// A slot's part of an item: a row tile of a sequence and key head.
+struct Slot {
+  int tiles;               // of keys; 0: nothing
+  int masked;              // the first of them that a mask cuts
+  int head;                // key head
+  int token, n;            // first token, tokens
+  int key, keys;           // first token of the sequence; how many of its tokens any row sees
+  int sees;                // how many the first token sees (causal: every token one more)
+  int len;                 // tokens of the sequence
+};
+struct Item {
+  int end;                 // nothing left
+  int tiles;               // the larger of the slots'
+  int shared;              // both slots walk the same K and V tiles
+  int first_masked;        // of both slots
+  Slot slot[2];
+};
+
+__device__ inline Slot make_slot(const Params& p, const int4& q, int head, int tile) {
+  Slot s;
+  const int first = tile * p.tq;
+  s.head = head;
+  s.n = min(p.tq, q.y - first);
+  s.token = q.x + first;
+  s.key = q.x, s.len = q.y;
+  s.keys = p.causal ? first + s.n : q.y;
+  s.sees = p.causal ? first + 1 : q.y;
+  s.tiles = ceil_div(s.keys, kTile);
+  s.masked = s.sees / kTile;
+  return s;
+}
+
+// Item number `ticket` (a whole warp calls it): pairs of row tiles first, sequence by sequence, the ones with most keys first, all key heads of
+// a place after each other; then the single row tiles, two by two.
+__device__ inline bool make_item(const Params& p, int pairs, int odds, int sequences, long long ticket, Item& im, int lane) {
+  const long long wide = (long long)pairs * p.kv_heads, singles = (long long)odds * p.kv_heads;
+  im.end = 0;
+  if (ticket < wide) {
+    const int u = (int)(ticket / p.kv_heads), h = (int)(ticket - (long long)u * p.kv_heads);
+    // the last sequence that begins at u or in front of it: every step cuts the range to a 32nd
+    int lo = 0, hi = sequences;
+    while (hi - lo > 1) {
+      const int step = ceil_div(hi - lo, 32), at = lo + lane * step;
+      const bool in = at < hi && __ldcg(p.plan.seq + at).z <= u;
+      const int last = 31 - __clz(__ballot_sync(0xffffffffu, in));
+      hi = min(hi, lo + (last + 1) * step);
+      lo += last * step;
+    }
+    const int4 q = __ldcg(p.plan.seq + lo);
+    const int tiles = ceil_div(q.y, p.tq), tile = tiles - 2 * (u - q.z) - 2;
+    im.shared = 1;
+    im.slot[0] = make_slot(p, q, h, tile);
+    im.slot[1] = make_slot(p, q, h, tile + 1);
+  } else {
+    const long long i = 2 * (ticket - wide);
+    if (i >= singles) return false;
+    im.shared = 0;
+    im.slot[1].tiles = 0;
+    for (int s = 0; s < 2 && i + s < singles; ++s) {
+      const int u = (int)((i + s) / p.kv_heads), h = (int)(i + s - (long long)u * p.kv_heads);
+      im.slot[s] = make_slot(p, __ldcg(p.plan.seq + __ldcg(p.plan.odd + u)), h, 0);
+    }
+  }
+  im.tiles = max(im.slot[0].tiles, im.slot[1].tiles);
+  im.first_masked = im.slot[1].tiles ? min(im.slot[0].masked, im.slot[1].masked) : im.slot[0].masked;
+  return true;
+}
+
+// ------------------------------------------------------------------ kernel
+
+struct Ctx {
+  volatile int* abort_smem;
+  int* dev_status;
+  long long limit;
+};
+
+// bounded wait; false = gave up (this CTA is leaving)
+__device__ __forceinline__ bool wait_slow(const Ctx& c, uint32_t bar, uint32_t parity, int site) {
+  const long long t0 = clock64();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (*c.abort_smem) return false;
+    if (clock64() - t0 > c.limit) {
+      *c.abort_smem = 1;
+      report(c.dev_status, WAVEAL_ERR_TIMEOUT, site, blockIdx.x, threadIdx.x);
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ bool warp_wait(const Ctx& c, uint32_t bar, uint32_t parity, int site) {
+  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) || wait_slow(c, bar, parity, site));
+}
+
+// Two numbers in the tensors' type: the results, and the probabilities, because one product of 16-bit types takes both operands in the
+// same type and V is stored in this one.  Either is off by half a step of its own; the sums are taken before the rounding, in fp32.
+template <class T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if constexpr (std::is_same_v<T, __half>)
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <class T> __device__ __forceinline__ float2 unpack2(uint32_t x) {
+  if constexpr (std::is_same_v<T, __half>) {
+    return __half22float2(*reinterpret_cast<__half2*>(&x));
+  } else {
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+  }
+}
+// two 16-bit numbers: is one of them infinite or NaN (all bits of its exponent set)
+template <class T> __device__ __forceinline__ bool not_finite2(uint32_t x) {
+  constexpr uint32_t m = std::is_same_v<T, __half> ? 0x7c00u : 0x7f80u;
+  return (x & m) == m || (x & m << 16) == m << 16;
+}
+
+enum {
+  B_ITEM_FULL = 0, B_ITEM_EMPTY = B_ITEM_FULL + kItems, B_Q_FULL = B_ITEM_EMPTY + kItems, B_Q_EMPTY = B_Q_FULL + 2,
+  B_S_FULL = B_Q_EMPTY + 2, B_P_FIRST = B_S_FULL + 2, B_P_LAST = B_P_FIRST + 2, B_O_FULL = B_P_LAST + 2, B_O_EMPTY = B_O_FULL + 2,
+  B_SUMS = B_O_EMPTY + 2, B_CHECK = B_SUMS + 2, B_FINAL = B_CHECK + 2 * kChecks, B_KV_FULL = B_FINAL + 2
+};
+template <int D> constexpr int kBars = B_KV_FULL + 2 * Geo<D>::STAGES;
+
+// what lies behind the tiles in shared memory
+template <int D> struct Small {
+  unsigned long long bar[kBars<D>];
+  Item items[kItems];
+  float2 sums[2][kTile];                             // [slot][row]: sum and reference, from the softmax to the epilogue
+  int verdict[2][kChecks];                           // not every value of the slot's masked tile is finite
+  uint32_t tmem;
+  int abort;
+};
+
+// the ring of K and V tiles as one of its users walks it
+template <int D> struct Ring {
+  uint32_t stage = 0, phase = 0;
+  __device__ void next() {
+    if (++stage == (uint32_t)Geo<D>::STAGES) stage = 0, phase ^= 1;
+  }
+};
+
+// A masked tile some of whose values are not finite: the row's sum over the keys that it sees, added to its accumulator (first: written).
+// P is read back from tensor memory, as the products would take it.
+template <int D, class T>
+__device__ __forceinline__ void add_visible(uint32_t p_addr, uint32_t o_addr, uint32_t v_smem, int visible, int first) {
+  using G = Geo<D>;
+#pragma unroll 1
+  for (int c = 0; c < D; c += 8) {
+    float acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < kTile; k += 2) {
+      uint32_t pk;
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(pk) : "r"(p_addr + k / 2) : "memory");
+      asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(pk)::"memory");
+      const float2 pr = unpack2<T>(pk);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int key = k + x;
+        // (128-byte swizzle: 16-byte chunk i of row r lies at chunk i ^ (r & 7))
+        const uint32_t a = v_smem + c / 64 * G::SLAB_BYTES + key * 128 + ((c % 64 / 8) ^ (key & 7)) * 16;
+        uint32_t w[4];
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
+        if (key < visible) {
+          const float pv = x ? pr.y : pr.x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 v = unpack2<T>(w[i]);
+            acc[2 * i] += pv * v.x, acc[2 * i + 1] += pv * v.y;
+          }
+        }
+      }
+    }
+    uint32_t o[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]) : "r"(o_addr + c) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(o[0]), "+r"(o[1]), "+r"(o[2]), "+r"(o[3]), "+r"(o[4]), "+r"(o[5]), "+r"(o[6]), "+r"(o[7])::"memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(first ? acc[i] : __uint_as_float(o[i]) + acc[i]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(o_addr + c) : "memory");
+  }
+  tc_wait_st();
+}
+
+// O of this thread's row times `scale`
+template <int D> __device__ __forceinline__ void rescale(uint32_t o_addr, float scale) {
+#pragma unroll 1
+  for (int c = 0; c < D; c += 16) {
+    uint32_t v[16];
+    WAVEAL_TMEM_LD16(o_addr + c, v, 0);
+    WAVEAL_TMEM_WAIT_LD16(v, 0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * scale);
+    WAVEAL_TMEM_ST16(o_addr + c, v, 0);
+  }
+  tc_wait_st();
+}
+
+template <int D, class T>
+__global__ void __launch_bounds__(kThreads, 1)
+k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+              const __grid_constant__ Params p) {
+  using G = Geo<D>;
+  constexpr int B_KV_EMPTY = B_KV_FULL + G::STAGES;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const uint32_t sbase = smem_u32(smem);
+  Small<D>& sm = *reinterpret_cast<Small<D>*>(smem + G::OFF_END);
+  const uint32_t bars = smem_u32(sm.bar);
+  auto BAR = [&](int i) { return bars + 8 * i; };
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&sm.tmem), 512);
+    tmem_relinquish();
+  } else if (warp == 2) {
+    for (int i = lane; i < kBars<D>; i += 32) {
+      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps4 = (i >= B_P_FIRST && i < B_O_FULL) || (i >= B_O_EMPTY && i < B_CHECK);
+      mbar_init(BAR(i), item ? kItemReaders : warps4 ? 4 : i >= B_KV_EMPTY ? 3 : 1);
+    }
+    if (lane == 0) sm.abort = 0;
+    fence_mbar_init();
+  } else if (warp == 3 && lane == 0) {
+    prefetch_tmap(&tmQ), prefetch_tmap(&tmK), prefetch_tmap(&tmV);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+  const Ctx ctx = {&sm.abort, p.dev_status, p.wait_limit};
+  bool ok = true;
+
+  // the next item, for everyone but the loader: false when there is none or a wait gave up
+  uint32_t item_no = 0;
+  const Item* im;
+  auto next_item = [&] {
+    const uint32_t at = item_no % kItems;
+    if (!warp_wait(ctx, BAR(B_ITEM_FULL + at), item_no / kItems & 1, 110)) return ok = false;
+    im = &sm.items[at];
+    return !im->end;
+  };
+  auto item_done = [&] {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(BAR(B_ITEM_EMPTY + item_no % kItems));
+    ++item_no;
+  };
+
+  if (warp >= kLoadWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp == kLoadWarp) {
+      // ================================================================ items, Q, K, V
+      Ring<D> ring;
+      uint32_t loaded = 0, armed = 0, parity = 0, q_it[2] = {0, 0}, q_armed = 0;
+      auto load_tile = [&](const CUtensorMap* tm, const Slot& s, int j, bool drop) {
+        if (loaded >= (uint32_t)G::STAGES && !(ok = warp_wait(ctx, BAR(B_KV_EMPTY + ring.stage), ring.phase ^ 1, 111))) return;
+        ++loaded;
+        if (!drop) {
+          if (lane == 0) {
+            mbar_expect_tx(BAR(B_KV_FULL + ring.stage), G::TILE_BYTES);
+#pragma unroll
+            for (int i = 0; i < G::SLABS; ++i)
+              tma_load_3d(sbase + G::OFF_KV + ring.stage * G::TILE_BYTES + i * G::SLAB_BYTES, tm, i * 64, s.head, s.key + j * kTile, BAR(B_KV_FULL + ring.stage));
+          }
+          armed |= 1u << ring.stage, parity = (parity & ~(1u << ring.stage)) | ring.phase << ring.stage;
+        }
+        __syncwarp();
+        ring.next();
+      };
+      auto load_q = [&](const Slot& s, int x) {
+        if (s.tiles == 0) return;
+        if (q_it[x] && !(ok = warp_wait(ctx, BAR(B_Q_EMPTY + x), (q_it[x] & 1) ^ 1, 112))) return;
+        ++q_it[x];
+        q_armed |= 1u << x;
+        if (lane == 0) {
+          mbar_expect_tx(BAR(B_Q_FULL + x), p.tq * p.group * 128 * G::SLABS);
+#pragma unroll
+          for (int i = 0; i < G::SLABS; ++i)
+            tma_load_3d(sbase + G::OFF_Q + x * G::TILE_BYTES + i * G::SLAB_BYTES, &tmQ, i * 64, s.head * p.group, s.token, BAR(B_Q_FULL + x));
+        }
+        __syncwarp();
+      };
+      waveal::wait_for_previous_kernel();
+      const int pairs = __ldcg(p.plan.head), odds = __ldcg(p.plan.head + 1), sequences = __ldcg(p.plan.head + 3);
+      long long ticket = blockIdx.x;
+      bool more = true;
+      while (ok && more) {
+        const uint32_t at = item_no % kItems;
+        if (item_no >= kItems && !(ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + at), (item_no / kItems & 1) ^ 1, 113))) break;
+        Item next;
+        more = make_item(p, pairs, odds, sequences, ticket, next, lane);
+        int asked = 0;
+        if (lane == 0) {
+          next.end = !more;
+          sm.items[at] = next;
+          mbar_arrive(BAR(B_ITEM_FULL + at));
+          if (more) asked = atomicAdd(p.plan.head + 2, 1);     // (used when this item's tiles have been asked for)
+        }
+        __syncwarp();
+        ++item_no;
+        if (!more) break;
+        for (int j = 0; ok && j < next.tiles; ++j) {
+          if (j == 0) load_q(next.slot[0], 0);
+          const bool drop = p.drop_tile && blockIdx.x == 0 && loaded == 0;
+          for (int x = 0; ok && x < 2; ++x) {
+            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_tile(&tmK, next.slot[next.shared ? 1 : x], j, drop);
+            if (ok && x == 0 && j == 0) load_q(next.slot[1], 1);
+          }
+          for (int x = 0; ok && x < 2; ++x)
+            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_tile(&tmV, next.slot[next.shared ? 1 : x], j, false);
+        }
+        ticket = (long long)gridDim.x + __shfl_sync(0xffffffffu, asked, 0);
+      }
+      // leaves no copy in flight, also where another warp has given up
+      for (int st = 0; st < G::STAGES + 2; ++st) {
+        const bool is_q = st >= G::STAGES;
+        if (!((is_q ? q_armed >> (st - G::STAGES) : armed >> st) & 1)) continue;
+        const uint32_t bar = is_q ? BAR(B_Q_FULL + st - G::STAGES) : BAR(B_KV_FULL + st), ph = is_q ? (q_it[st - G::STAGES] & 1) ^ 1 : parity >> st & 1;
+        const long long t0 = clock64();
+        while (!mbar_try_wait(bar, ph) && clock64() - t0 < p.wait_limit / 4) {}
+      }
+    } else if (warp < kCheckWarp) {
+      // ================================================================ products of a slot
+      // (operands of the products come from shuffles, so that the compiler knows them to be the same in all lanes)
+      constexpr uint32_t kTypeBits = (1u << 7) | (1u << 10), kType = std::is_same_v<T, __half> ? 0u : kTypeBits;
+      constexpr uint32_t kQK = (make_idesc(128, 128, false) & ~kTypeBits) | kType, kPV = (make_idesc(128, D, true) & ~kTypeBits) | kType;
+      const int x = warp - kIssueWarp;
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), s_col = tm + G::S_COL + x * kTile, o_col = tm + G::O_COL + x * kTile;
+      const uint64_t q_desc = make_desc(sbase + G::OFF_Q + x * G::TILE_BYTES, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_KV, 16, 1024);
+      const uint64_t v_desc0 = make_desc(sbase + G::OFF_KV, G::SLAB_BYTES, 1024);
+      Ring<D> ring;
+      uint32_t items = 0, p_no = 0, checks = 0;
+      while (ok && next_item()) {
+        const int tiles = __shfl_sync(0xffffffffu, im->slot[x].tiles, 0), all = __shfl_sync(0xffffffffu, im->tiles, 0), shared = __shfl_sync(0xffffffffu, im->shared, 0);
+        const int other = __shfl_sync(0xffffffffu, im->slot[x ^ 1].tiles, 0), keys = __shfl_sync(0xffffffffu, im->slot[x].keys, 0);
+        const int masked = __shfl_sync(0xffffffffu, im->slot[x].masked, 0);
+        item_done();
+        // the other slot's tile: this warp lets it go when it is there
+        auto pass = [&] {
+          if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 114))) return;
+          if (lane == 0) mbar_arrive(BAR(B_KV_EMPTY + ring.stage));
+          ring.next();
+        };
+        for (int j = 0; ok && j < all; ++j) {
+          const bool mine = j < tiles;
+          if (!shared && x == 1 && j < other) pass();
+          if (ok && mine) {
+            if (j == 0 && !(ok = warp_wait(ctx, BAR(B_Q_FULL + x), items & 1, 115))) break;
+            if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 116))) break;
+            tc_fence_after();
+            const uint64_t kd = k_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
+#pragma unroll
+            for (int slab = 0; slab < G::SLABS; ++slab)
+              umma4_ss(s_col, q_desc + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kQK, slab > 0);
+            tc_commit(BAR(B_S_FULL + x));
+            tc_commit(BAR(B_KV_EMPTY + ring.stage));
+            if (j == tiles - 1) tc_commit(BAR(B_Q_EMPTY + x));
+            ring.next();
+          } else if (ok && shared) {
+            pass();
+          }
+          if (ok && !shared && x == 0 && j < other) pass();
+          // ---- V
+          if (ok && !shared && x == 1 && j < other) pass();
+          if (ok && mine) {
+            const int groups = (min(kTile, keys - j * kTile) + 15) / 16;
+            if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 117))) break;
+            if (j == 0 && items && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items & 1) ^ 1, 118))) break;
+            int skip = 0;
+            if (j >= masked) {
+              if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + checks % kChecks), checks / kChecks & 1, 119))) break;
+              skip = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&sm.verdict[x][checks % kChecks]), 0);
+              ++checks;
+            }
+            const uint64_t vd = v_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              if (!(ok = warp_wait(ctx, BAR((half ? B_P_LAST : B_P_FIRST) + x), p_no & 1, 120))) break;
+              tc_fence_after();
+              const int here = skip ? 0 : groups - 4 * half;
+              const uint32_t a = s_col + half * 32;
+              const uint64_t v = vd + (uint64_t)(half * 64 * 128 >> 4);
+              if (here >= 4) {
+                umma4_ts(o_col, a, v, kPV, j > 0 || half > 0);
+              } else {
+#pragma unroll 1
+                for (int c = 0; c < here; ++c) umma_bf16_ts(o_col, a + c * 8, v + (uint64_t)(c * 16 * 128 >> 4), kPV, j > 0 || half > 0 || c > 0);
+              }
+            }
+            if (!ok) break;
+            ++p_no;
+            tc_commit(BAR(B_KV_EMPTY + ring.stage));
+            if (j == tiles - 1) tc_commit(BAR(B_O_FULL + x));
+            ring.next();
+          } else if (ok && shared) {
+            pass();
+          }
+          if (ok && !shared && x == 0 && j < other) pass();
+        }
+        if (tiles) ++items;
+      }
+      // no product is still running when tensor memory is given back
+      tc_commit(BAR(B_FINAL + x));
+      __syncwarp();
+      const long long t0 = clock64();
+      while (!mbar_try_wait(BAR(B_FINAL + x), 0) && clock64() - t0 < p.wait_limit / 4) {}
+    } else {
+      // ================================================================ values of masked tiles
+      Ring<D> ring;
+      uint32_t checks[2] = {0, 0};
+      while (ok && next_item()) {
+        const Item it = *im;
+        item_done();
+        auto step = [&](bool is_v, int x, int j) {
+          if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 121))) return;
+          const bool cut[2] = {is_v && (it.shared || x == 0) && j < it.slot[0].tiles && j >= it.slot[0].masked,
+                               is_v && (it.shared || x == 1) && j < it.slot[1].tiles && j >= it.slot[1].masked};
+          if (cut[0] || cut[1]) {
+            const uint32_t v = sbase + G::OFF_KV + ring.stage * G::TILE_BYTES;
+            const int len = it.slot[x].len - j * kTile;     // rows of the tile that are the sequence's
+            bool bad = false;
+            if (p.causal) {
+              for (int i = lane; i < min(len, kTile) * 8; i += 32) {
+#pragma unroll
+                for (int slab = 0; slab < G::SLABS; ++slab) {
+                  uint32_t w[4];
+                  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + slab * G::SLAB_BYTES + i * 16));
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) bad |= not_finite2<T>(w[k]);
+                }
+              }
+            }
+            if (len < kTile) {
+#pragma unroll
+              for (int slab = 0; slab < G::SLABS; ++slab)
+                for (int i = len * 8 + lane; i < kTile * 8; i += 32) st_shared_v4(v + slab * G::SLAB_BYTES + i * 16, 0, 0, 0, 0);
+              fence_proxy_async();
+            }
+            const int verdict = __any_sync(0xffffffffu, bad);
+            __syncwarp();
+            if (lane == 0) {
+#pragma unroll
+              for (int s = 0; s < 2; ++s)
+                if (cut[s]) {
+                  sm.verdict[s][checks[s] % kChecks] = verdict;
+                  mbar_arrive(BAR(B_CHECK + s * kChecks + checks[s] % kChecks));
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) checks[s] += cut[s];
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR(B_KV_EMPTY + ring.stage));
+          ring.next();
+        };
+        for (int j = 0; ok && j < it.tiles; ++j)
+          for (int k = 0; ok && k < 4; ++k) {
+            const int x = k & 1;
+            if (it.shared ? x == 0 : j < it.slot[x].tiles) step(k >= 2, it.shared ? 1 : x, j);
+          }
+      }
+    }
+  } else if (warp >= kEpilogueWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    // ================================================================ epilogues
+    const int quad = warp & 3, r = quad * 32 + lane, tok = r / p.group, g = r - tok * p.group;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    uint32_t items[2] = {0, 0};
+    while (ok && next_item()) {
+      for (int x = 0; ok && x < 2; ++x) {
+        const Slot s = im->slot[x];
+        if (s.tiles == 0) continue;
+        if (!(ok = warp_wait(ctx, BAR(B_SUMS + x), items[x] & 1, 122))) break;
+        if (!(ok = warp_wait(ctx, BAR(B_O_FULL + x), items[x] & 1, 123))) break;
+        ++items[x];
+        tc_fence_after();
+        const float2 lm = sm.sums[x][r];
+        const bool live = tok < s.n;
+        const int head = s.head * p.group + g, token = s.token + tok;
+        const float inv = lm.x == 0.f ? 0.f : 1.0f / lm.x;
+        T* o = static_cast<T*>(p.o) + head * p.o_stride_h + token * p.o_stride_t;
+        const uint32_t o_addr = tmem + lanes + G::O_COL + x * kTile;
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          uint32_t v[32], w[16];
+          WAVEAL_TMEM_LD32(o_addr + c, v, 0);
+          WAVEAL_TMEM_WAIT_LD32(v, 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            // (a row without a sum: O may be 0 times something)
+            const float a = __uint_as_float(v[2 * i]), b = __uint_as_float(v[2 * i + 1]);
+            w[i] = lm.x == 0.f ? 0u : pack2<T>(a * inv, b * inv);
+          }
+          if (live) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(o + c + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+          }
+        }
+        if (live && p.lse) p.lse[(long long)head * p.tokens + token] = lm.x == 0.f ? -INFINITY : (lm.y * p.sl2 + log2f(lm.x)) * 0.69314718055994531f;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + x));
+      }
+      if (ok) item_done();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    // ================================================================ softmax: a thread a row
+    const int x = warp / 4, quad = warp & 3, r = quad * 32 + lane, tok = r / p.group;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + G::S_COL + x * kTile, o_addr = tmem + lanes + G::O_COL + x * kTile;
+    const float sl2 = p.sl2;
+    uint32_t s_no = 0, items = 0, checks = 0, v_at = 0;    // v_at: place in the ring where the item's tiles begin
+    while (ok && next_item()) {
+      const Slot s = im->slot[x];
+      const int all = im->tiles, shared = im->shared, other = im->slot[x ^ 1].tiles;
+      item_done();
+      // where a tile's values are in the ring (asked for in the rare case that they are added here)
+      const uint32_t begin = v_at;
+      auto v_stage = [&](int j) {
+        const int before = shared ? 2 * j : 2 * j + 2 * min(j, other), mine = shared ? 1 : 1 + (j < other ? (x ? 2 : 1) : 0);
+        return (begin + before + mine) % G::STAGES;
+      };
+      v_at = (begin + (shared ? 2 * all : 2 * (s.tiles + other))) % G::STAGES;
+      if (s.tiles == 0) continue;
+      const bool live = tok < s.n;
+      const int sees = min(p.causal ? s.sees + tok : s.keys, s.keys);
+      float ref = -INFINITY, sum = 0.f;
+#pragma unroll 1
+      for (int j = 0; j < s.tiles; ++j) {
+        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + x), s_no & 1, 124))) break;
+        ++s_no;
+        tc_fence_after();
+        uint32_t v[128];
+        WAVEAL_TMEM_LD32(s_addr, v, 0);
+        WAVEAL_TMEM_LD32(s_addr + 32, v, 32);
+        WAVEAL_TMEM_LD32(s_addr + 64, v, 64);
+        WAVEAL_TMEM_LD32(s_addr + 96, v, 96);
+        WAVEAL_TMEM_WAIT_LD32(v, 0);
+        WAVEAL_TMEM_WAIT_LD32(v, 32);
+        WAVEAL_TMEM_WAIT_LD32(v, 64);
+        WAVEAL_TMEM_WAIT_LD32(v, 96);
+        if (j >= s.masked) {
+          const int visible = sees - j * kTile;
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (i >= visible) v[i] = 0xff800000u;
+        }
+        float m4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m4[i] = __uint_as_float(v[i]);
+#pragma unroll
+        for (int i = 4; i < 124; i += 8) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) m4[k] = fmax3(m4[k], __uint_as_float(v[i + 2 * k]), __uint_as_float(v[i + 2 * k + 1]));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m4[i] = fmaxf(m4[i], __uint_as_float(v[124 + i]));
+        const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        if (j == 0) {
+          ref = top;
+        } else {
+          const bool grown = live && (top - ref) * sl2 > kGrowth;
+          if (__any_sync(0xffffffffu, grown)) {
+            // (S of this tile is there, so the last tile's P V, issued before it, is done)
+            const float scale = grown ? ex2((ref - top) * sl2) : 1.0f;
+            if (grown) ref = top;
+            sum *= scale;
+            rescale<D>(o_addr, scale);
+          }
+        }
+        const float minus = ref == -INFINITY ? 0.f : -ref * sl2;
+        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t w[32];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const int c = half * 64 + 2 * i;
+            float a, b, d, e;
+            ffma2(a, b, __uint_as_float(v[c]), __uint_as_float(v[c + 1]), sl2, sl2, minus, minus);
+            ffma2(d, e, __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]), sl2, sl2, minus, minus);
+            a = ex2(a), b = ex2(b), d = ex2(d), e = ex2(e);
+            fadd2(s0, s1, s0, s1, a, b);
+            fadd2(s2, s3, s2, s3, d, e);
+            w[i] = pack2<T>(a, b), w[i + 1] = pack2<T>(d, e);
+          }
+          WAVEAL_TMEM_ST32(s_addr + half * 32, w, 0);
+          tc_wait_st();
+          if (half && j >= s.masked) {
+            if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + checks % kChecks), checks / kChecks & 1, 125))) break;
+            if (*reinterpret_cast<volatile int*>(&sm.verdict[x][checks % kChecks])) {
+              if (j == 0 && items && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items & 1) ^ 1, 127))) break;
+              tc_fence_after();
+              add_visible<D, T>(s_addr, o_addr, sbase + G::OFF_KV + v_stage(j) * G::TILE_BYTES, sees - j * kTile, j == 0);
+            }
+            ++checks;
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR((half ? B_P_LAST : B_P_FIRST) + x));
+        }
+        if (!ok) break;
+        sum += (s0 + s1) + (s2 + s3);
+      }
+      if (!ok) break;
+      // (the epilogue has read the last item's)
+      if (items && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items & 1) ^ 1, 126))) break;
+      ++items;
+      sm.sums[x][r] = make_float2(sum, ref);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(B_SUMS + x));
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// ------------------------------------------------------------------ host
+
+// [tokens][heads][channels] in boxes of 64 channels
+waveal_status make_map(CUtensorMap* tm, const waveal_prompt_desc* d, const void* base, int heads, const int64_t* stride, int box_heads, int box_tokens,
+                       const char* what) {
+  const auto enc = waveal::tensor_map_encoder();
+  if (!enc) return waveal::fail(WAVEAL_ERR_CUDA, "cuTensorMapEncodeTiled entry point not available");
+  const cuuint64_t dims[3] = {(cuuint64_t)d->head_dim, (cuuint64_t)heads, (cuuint64_t)d->tokens};
+  const cuuint64_t bytes[2] = {(cuuint64_t)stride[0] * 2, (cuuint64_t)stride[1] * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens}, one[3] = {1, 1, 1};
+  const CUresult r = enc(tm, d->dtype == WAVEAL_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base),
+                         dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return waveal::fail(WAVEAL_ERR_CUDA, "tensor map for %s rejected (CUresult %d)", what, (int)r);
+  return WAVEAL_OK;
+}
+
+struct Layout { size_t seq, odd, bytes; };
+Layout layout(const waveal_prompt_desc* d) {
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  Layout l;
+  l.seq = 256;
+  l.odd = l.seq + up((size_t)d->batch * sizeof(int4));
+  l.bytes = l.odd + up((size_t)d->batch * sizeof(int));
+  return l;
+}
+
+waveal_status check(const waveal_prompt_desc* d) {
+  if (!d) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "desc is NULL");
+  if (d->batch < 0 || d->tokens < 0) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "batch and tokens must not be negative");
+  if (d->dtype != WAVEAL_BF16 && d->dtype != WAVEAL_FP16) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "dtype %d (WAVEAL_BF16 or WAVEAL_FP16)", d->dtype);
+  if (d->head_dim != 64 && d->head_dim != 128) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", d->head_dim);
+  if (d->kv_heads <= 0 || d->q_heads <= 0 || d->q_heads % d->kv_heads || d->q_heads / d->kv_heads > kTile)
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q_heads %d: a multiple of kv_heads (%d), at most %d times as many", d->q_heads, d->kv_heads, kTile);
+  if (d->flags & ~(WAVEAL_PROMPT_CAUSAL | WAVEAL_PROMPT_SELFTEST_LOST_TILE)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "unknown flags 0x%x", d->flags);
+  if ((long long)d->tokens * d->q_heads > 1000000000ll) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 10^9 rows (tokens * q_heads)");
+  const int64_t* strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
+  for (const int64_t* s : strides)
+    for (int i = 0; i < 2; ++i)
+      if (s[i] % 8 || s[i] < 0) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "strides must be multiples of 8 elements (16 bytes) and not negative");
+  return WAVEAL_OK;
+}
+
+template <int D, class T>
+waveal_status launch(const CUtensorMap* tm, const Params& p, unsigned grid, cudaStream_t st) {
+  constexpr size_t smem = Geo<D>::OFF_END + sizeof(Small<D>);
+  static_assert(smem <= 232448, "shared memory of an SM");
+  static bool set[64] = {};
+  int dev = 0;
+  WAVEAL_CUDA_OK(cudaGetDevice(&dev));
+  if (dev >= 64 || !set[dev]) {
+    WAVEAL_CUDA_OK(cudaFuncSetAttribute(k_prompt_attn<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (dev < 64) set[dev] = true;
+  }
+  k_prompt_plan<<<1, kPlanThreads, 0, st>>>(p);
+  WAVEAL_CUDA_OK(cudaGetLastError());
+  WAVEAL_CUDA_OK(waveal::launch_chained(k_prompt_attn<D, T>, dim3(grid), kThreads, smem, st, tm[0], tm[1], tm[2], p));
+  waveal::launch_counter() = 2;
+  return WAVEAL_OK;
+}
+
+}  // namespace
+
+extern "C" waveal_status waveal_prompt_attn_workspace_bytes(const waveal_prompt_desc* desc, size_t* bytes) {
+  if (!bytes) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "bytes is NULL");
+  if (waveal_status e = check(desc)) return e;
+  *bytes = layout(desc).bytes;
+  return WAVEAL_OK;
+}
+
+extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const void* q, const void* k, const void* v, void* o, float* lse,
+                                            const int32_t* seq_start, const int32_t* seq_len, float scale, void* ws, size_t ws_bytes,
+                                            int32_t* dev_status, void* cuda_stream) {
+  if (waveal_status e = check(d)) return e;
+  if (d->tokens == 0 || d->batch == 0) {
+    waveal::launch_counter() = 0;
+    return WAVEAL_OK;
+  }
+  if (!q || !k || !v || !o || !seq_start) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q, k, v, o and seq_start are required");
+  if (!waveal::aligned(q, 16) || !waveal::aligned(k, 16) || !waveal::aligned(v, 16) || !waveal::aligned(o, 16))
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q, k, v and o must be 16-byte aligned");
+  const Layout l = layout(d);
+  if (!ws || ws_bytes < l.bytes) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, l.bytes);
+  if (!waveal::aligned(ws, 256)) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const int sms = waveal::sm_count();
+  if (sms <= 0) return waveal::fail(WAVEAL_ERR_CUDA, "number of SMs not available");
+
+  Params p = {};
+  p.batch = d->batch, p.tokens = d->tokens, p.kv_heads = d->kv_heads, p.group = d->q_heads / d->kv_heads, p.tq = kTile / p.group;
+  p.causal = d->flags & WAVEAL_PROMPT_CAUSAL ? 1 : 0;
+  char* w = static_cast<char*>(ws);
+  p.plan.head = reinterpret_cast<int*>(w);
+  p.plan.seq = reinterpret_cast<int4*>(w + l.seq);
+  p.plan.odd = reinterpret_cast<int*>(w + l.odd);
+  p.seq_start = seq_start, p.seq_len = seq_len;
+  p.o = o, p.lse = lse, p.o_stride_h = d->o_stride[0], p.o_stride_t = d->o_stride[1];
+  p.dev_status = dev_status;
+  p.drop_tile = d->flags & WAVEAL_PROMPT_SELFTEST_LOST_TILE ? 1 : 0;
+  p.wait_limit = p.drop_tile ? kSelfTestCycles : kTimeoutCycles;
+  p.sl2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)d->head_dim)) * 1.4426950408889634f;
+
+  CUtensorMap tm[3];
+  if (waveal_status e = make_map(&tm[0], d, q, d->q_heads, d->q_stride, p.group, p.tq, "q")) return e;
+  if (waveal_status e = make_map(&tm[1], d, k, d->kv_heads, d->k_stride, 1, kTile, "k")) return e;
+  if (waveal_status e = make_map(&tm[2], d, v, d->kv_heads, d->v_stride, 1, kTile, "v")) return e;
+  // a thread block an SM, and no more than there can be items: pairs of row tiles and single ones, of every key head
+  const long long most = ((long long)d->tokens / (2 * p.tq) + d->batch) * d->kv_heads;
+  const unsigned grid = (unsigned)std::min((long long)sms, std::max(1ll, most));
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (d->dtype == WAVEAL_FP16) return d->head_dim == 128 ? launch<128, __half>(tm, p, grid, st) : launch<64, __half>(tm, p, grid, st);
+  return d->head_dim == 128 ? launch<128, __nv_bfloat16>(tm, p, grid, st) : launch<64, __nv_bfloat16>(tm, p, grid, st);
+}
