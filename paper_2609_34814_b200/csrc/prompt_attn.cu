@@ -7,13 +7,13 @@
 // A row tile is 128 rows of S: tq = 128 / G tokens with the G query heads that share a key head, so that a key head's tiles are
 // loaded once for all of them and the causal diagonal crosses few of a tile's columns.  A thread block has two slots with a
 // row tile each and walks the key tiles of 128:
-//   slot: S = Q K^T (tensor memory) -> a thread a row: maximum, exponentials, P over the first half of S's columns -> O += P V (tensor memory)
+//   slot: S = Q K^T (tensor memory) -> maximum, exponentials, P over S's columns -> O += P V (tensor memory)
 // One slot is in its products while the other is in its softmax.  A pair of row tiles of a sequence shares its K and V
 // tiles; the first row tile of a sequence with an odd number of them goes with that of another sequence or head (each slot
 // then has its own K and V tiles).
 //
-// Warps: 0-3 and 4-7 softmax of the slots, 8-11 epilogues, 12 items and loads, 13 and 14 the slots' products, 15 masked tiles' values.
-// S and P of a slot share their columns without a barrier: the slot's products are issued by one thread, in order.
+// Warps: 0-7 and 8-15 softmax and epilogue of the slots (two threads a row, 64 keys of a tile each: a warp by itself issues an instruction in
+// four clocks, so that four of them a scheduler are needed), 16 items and loads, 17 and 18 products, 19 masked tiles' values.
 //
 // Values that a token must not see: their probabilities are zero, but zero times NaN is not.  Warp 15 writes zeros over what lies behind a
 // sequence's end and looks through the values of tiles that the causal mask cuts; where one is not finite, the slot's softmax warps add that tile's
@@ -22,6 +22,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 #include "host_common.h"
@@ -31,22 +32,26 @@ namespace {
 
 using namespace waveal::sm100;
 
-constexpr int kThreads = 512;
-constexpr int kLoadWarp = 12, kIssueWarp = 13, kCheckWarp = 15, kEpilogueWarp = 8;
+constexpr int kThreads = 640;
+constexpr int kLoadWarp = 16, kScoreWarp = 17, kCheckWarp = 19;
 constexpr int kTile = 128;                           // keys of a tile, rows of a slot
 constexpr int kItems = 4;                            // between the loader and the others
-constexpr int kItemReaders = 15;                     // two issuers, the checker, eight softmax warps, four of the epilogue
+constexpr int kItemReaders = 19;                     // two issuers, the checker, sixteen softmax warps
+constexpr int kParts = 2;                            // of a tile: P goes to the products 32 keys of each half at a time
 constexpr int kChecks = 8;                           // masked tiles of a slot whose verdicts are under way (more than the ring has V tiles)
 constexpr long long kTimeoutCycles = 4000000000ll;   // ~2 s at boost clock
 constexpr long long kSelfTestCycles = 4000000ll;     // ~2 ms
 constexpr float kGrowth = 8.0f;                      // log2 of how far a row's maximum may outgrow its reference
+// Most row tiles need only one reference: that of their first tile of keys.  Nothing is lost while no number overflows: P of bf16, the sums and O
+// have the range of fp32, P of fp16 has 2^16.  The sum of a tile's probabilities tells: all its terms are positive, so none of them is larger.
+template <class T> constexpr float kSumLimit = std::is_same_v<T, __half> ? 0x1p15f : 0x1p60f;
 
 template <int D> struct Geo {
   static constexpr int SLABS = D / 64;               // 128-byte-swizzled slabs of 64 channels
   static constexpr int SLAB_BYTES = kTile * 128;
   static constexpr int TILE_BYTES = SLABS * SLAB_BYTES;
-  static constexpr int STAGES = D == 128 ? 5 : 10;   // of the ring of K and V tiles
-  static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE_BYTES, OFF_END = OFF_KV + STAGES * TILE_BYTES;
+  static constexpr int NKS = D == 128 ? 2 : 4, NVS = NKS;   // stages of the rings of K and V tiles
+  static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NKS * TILE_BYTES, OFF_END = OFF_V + NVS * TILE_BYTES;
   static constexpr int S_COL = 0, O_COL = 256;       // tensor memory: S (and P) 0-127, 128-255, O 256.., 384..
 };
 
@@ -57,6 +62,7 @@ template <int D> struct Geo {
 struct Plan {
   int4* seq;               // [batch] {first token, tokens, pairs of row tiles in front, 0}
   int* odd;                // [batch] places in seq
+  int* again;              // [2 * tickets]: chains of row tiles that are computed again (2 * ticket + slot, each with the one before it)
   int* head;               // [4] {pairs of all sequences, odd ones, tickets given out, sequences with tokens}
 };
 
@@ -75,7 +81,7 @@ struct Params {
 
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-__device__ __forceinline__ void report(int* status, int code, int site, int where, int value) {
+__device__ __noinline__ void report(int* status, int code, int site, int where, int value) {
   if (status && atomicCAS(status, 0, code) == 0) status[1] = site, status[2] = where, status[3] = value;
 }
 
@@ -167,10 +173,11 @@ struct Slot {
   int len;                 // tokens of the sequence
 };
 struct Item {
-  int end;                 // nothing left
+  int end;                 // 1: nothing left; 2: everyone says when all items before this one are done
+  int ticket;
+  int safe;                // maxima of every tile
   int tiles;               // the larger of the slots'
   int shared;              // both slots walk the same K and V tiles
-  int first_masked;        // of both slots
   Slot slot[2];
 };
 
@@ -190,11 +197,11 @@ __device__ inline Slot make_slot(const Params& p, const int4& q, int head, int t
 
 // Item number `ticket` (a whole warp calls it): pairs of row tiles first, sequence by sequence, the ones with most keys first, all key heads of
 // a place after each other; then the single row tiles, two by two.
-__device__ inline bool make_item(const Params& p, int pairs, int odds, int sequences, long long ticket, Item& im, int lane) {
+__device__ inline bool make_item(const Params& p, int pairs, int odds, int sequences, int ticket, Item& im, int lane) {
   const long long wide = (long long)pairs * p.kv_heads, singles = (long long)odds * p.kv_heads;
-  im.end = 0;
+  im.end = 0, im.safe = 0, im.ticket = ticket;
   if (ticket < wide) {
-    const int u = (int)(ticket / p.kv_heads), h = (int)(ticket - (long long)u * p.kv_heads);
+    const int u = ticket / p.kv_heads, h = ticket - u * p.kv_heads;
     // the last sequence that begins at u or in front of it: every step cuts the range to a 32nd
     int lo = 0, hi = sequences;
     while (hi - lo > 1) {
@@ -220,7 +227,6 @@ __device__ inline bool make_item(const Params& p, int pairs, int odds, int seque
     }
   }
   im.tiles = max(im.slot[0].tiles, im.slot[1].tiles);
-  im.first_masked = im.slot[1].tiles ? min(im.slot[0].masked, im.slot[1].masked) : im.slot[0].masked;
   return true;
 }
 
@@ -233,7 +239,7 @@ struct Ctx {
 };
 
 // bounded wait; false = gave up (this CTA is leaving)
-__device__ __forceinline__ bool wait_slow(const Ctx& c, uint32_t bar, uint32_t parity, int site) {
+__device__ __noinline__ bool wait_slow(const Ctx& c, uint32_t bar, uint32_t parity, int site) {
   const long long t0 = clock64();
   for (;;) {
 #pragma unroll 1
@@ -276,33 +282,34 @@ template <class T> __device__ __forceinline__ bool not_finite2(uint32_t x) {
 
 enum {
   B_ITEM_FULL = 0, B_ITEM_EMPTY = B_ITEM_FULL + kItems, B_Q_FULL = B_ITEM_EMPTY + kItems, B_Q_EMPTY = B_Q_FULL + 2,
-  B_S_FULL = B_Q_EMPTY + 2, B_P_FIRST = B_S_FULL + 2, B_P_LAST = B_P_FIRST + 2, B_O_FULL = B_P_LAST + 2, B_O_EMPTY = B_O_FULL + 2,
-  B_SUMS = B_O_EMPTY + 2, B_CHECK = B_SUMS + 2, B_FINAL = B_CHECK + 2 * kChecks, B_KV_FULL = B_FINAL + 2
+  B_S_FULL = B_Q_EMPTY + 2, B_P = B_S_FULL + 2, B_O_FULL = B_P + 2 * kParts, B_O_EMPTY = B_O_FULL + 2,
+  B_PV_DONE = B_O_EMPTY + 2, B_PAIR = B_PV_DONE + 2, B_CHECK = B_PAIR + 8, B_FINAL = B_CHECK + 2 * kChecks, B_DONE = B_FINAL + 2, B_K_FULL
 };
-template <int D> constexpr int kBars = B_KV_FULL + 2 * Geo<D>::STAGES;
+template <int D> constexpr int kBars = B_K_FULL + 2 * (Geo<D>::NKS + Geo<D>::NVS);
 
 // what lies behind the tiles in shared memory
 template <int D> struct Small {
   unsigned long long bar[kBars<D>];
   Item items[kItems];
-  float2 sums[2][kTile];                             // [slot][row]: sum and reference, from the softmax to the epilogue
+  float pair[2][2][2][kTile];                        // [slot][turn][half][row]: maxima and sums, from a row's one thread to its other
   int verdict[2][kChecks];                           // not every value of the slot's masked tile is finite
   uint32_t tmem;
   int abort;
+  int again, last_again[2];                          // row tiles to be computed again: the last one of the chain; of each slot
 };
 
-// the ring of K and V tiles as one of its users walks it
-template <int D> struct Ring {
+// a ring of tiles as one of its users walks it
+template <int STAGES> struct Ring {
   uint32_t stage = 0, phase = 0;
   __device__ void next() {
-    if (++stage == (uint32_t)Geo<D>::STAGES) stage = 0, phase ^= 1;
+    if (++stage == (uint32_t)STAGES) stage = 0, phase ^= 1;
   }
 };
 
 // A masked tile some of whose values are not finite: the row's sum over the keys that it sees, added to its accumulator (first: written).
 // P is read back from tensor memory, as the products would take it.
 template <int D, class T>
-__device__ __forceinline__ void add_visible(uint32_t p_addr, uint32_t o_addr, uint32_t v_smem, int visible, int first) {
+__device__ __noinline__ void add_visible(uint32_t p_addr, uint32_t o_addr, uint32_t v_smem, int visible, int first) {
   using G = Geo<D>;
 #pragma unroll 1
   for (int c = 0; c < D; c += 8) {
@@ -312,7 +319,7 @@ __device__ __forceinline__ void add_visible(uint32_t p_addr, uint32_t o_addr, ui
 #pragma unroll 1
     for (int k = 0; k < kTile; k += 2) {
       uint32_t pk;
-      asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(pk) : "r"(p_addr + k / 2) : "memory");
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(pk) : "r"(p_addr + k / 64 * 64 + k % 64 / 2) : "memory");
       asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(pk)::"memory");
       const float2 pr = unpack2<T>(pk);
 #pragma unroll
@@ -345,8 +352,19 @@ __device__ __forceinline__ void add_visible(uint32_t p_addr, uint32_t o_addr, ui
   tc_wait_st();
 }
 
+// two products with A in tensor memory, 8 columns further, and B 16 keys further
+__device__ __forceinline__ void umma2_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .b32 rx, a;\n\t.reg .pred e, p, t;\n\t.reg .b64 b;\n\t"
+      "elect.sync rx|e, 0xFFFFFFFF;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, %3, %3;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "add.u32 a, %1, 8;\n\tadd.s64 b, %2, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
 // O of this thread's row times `scale`
-template <int D> __device__ __forceinline__ void rescale(uint32_t o_addr, float scale) {
+template <int D> __device__ __noinline__ void rescale(uint32_t o_addr, float scale) {
 #pragma unroll 1
   for (int c = 0; c < D; c += 16) {
     uint32_t v[16];
@@ -364,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               const __grid_constant__ Params p) {
   using G = Geo<D>;
-  constexpr int B_KV_EMPTY = B_KV_FULL + G::STAGES;
+  constexpr int B_K_EMPTY = B_K_FULL + G::NKS, B_V_FULL = B_K_EMPTY + G::NKS, B_V_EMPTY = B_V_FULL + G::NVS;
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem);
   Small<D>& sm = *reinterpret_cast<Small<D>*>(smem + G::OFF_END);
@@ -377,10 +395,10 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     tmem_relinquish();
   } else if (warp == 2) {
     for (int i = lane; i < kBars<D>; i += 32) {
-      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps4 = (i >= B_P_FIRST && i < B_O_FULL) || (i >= B_O_EMPTY && i < B_CHECK);
-      mbar_init(BAR(i), item ? kItemReaders : warps4 ? 4 : i >= B_KV_EMPTY ? 3 : 1);
+      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps8 = (i >= B_P && i < B_O_FULL) || (i >= B_O_EMPTY && i < B_PV_DONE);
+      mbar_init(BAR(i), item ? kItemReaders : i == B_DONE ? 16 : warps8 ? 8 : i >= B_V_EMPTY || (i >= B_PAIR && i < B_CHECK) ? 2 : 1);
     }
-    if (lane == 0) sm.abort = 0;
+    if (lane == 0) sm.abort = 0, sm.again = sm.last_again[0] = sm.last_again[1] = -1;
     fence_mbar_init();
   } else if (warp == 3 && lane == 0) {
     prefetch_tmap(&tmQ), prefetch_tmap(&tmK), prefetch_tmap(&tmV);
@@ -399,7 +417,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const uint32_t at = item_no % kItems;
     if (!warp_wait(ctx, BAR(B_ITEM_FULL + at), item_no / kItems & 1, 110)) return ok = false;
     im = &sm.items[at];
-    return !im->end;
+    return im->end != 1;
   };
   auto item_done = [&] {
     __syncwarp();
@@ -408,31 +426,33 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   };
 
   if (warp >= kLoadWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == kLoadWarp) {
       // ================================================================ items, Q, K, V
-      Ring<D> ring;
-      uint32_t loaded = 0, armed = 0, parity = 0, q_it[2] = {0, 0}, q_armed = 0;
-      auto load_tile = [&](const CUtensorMap* tm, const Slot& s, int j, bool drop) {
-        if (loaded >= (uint32_t)G::STAGES && !(ok = warp_wait(ctx, BAR(B_KV_EMPTY + ring.stage), ring.phase ^ 1, 111))) return;
-        ++loaded;
-        if (!drop) {
-          if (lane == 0) {
-            mbar_expect_tx(BAR(B_KV_FULL + ring.stage), G::TILE_BYTES);
+      Ring<G::NKS> k_ring;
+      Ring<G::NVS> v_ring;
+      uint32_t k_no = 0, v_no = 0, q_it[2] = {0, 0};
+      auto load_tile = [&](const CUtensorMap* tm, const Slot& s, int j, uint32_t smem_at, uint32_t full) {
+        if (lane == 0) {
+          mbar_expect_tx(full, G::TILE_BYTES);
 #pragma unroll
-            for (int i = 0; i < G::SLABS; ++i)
-              tma_load_3d(sbase + G::OFF_KV + ring.stage * G::TILE_BYTES + i * G::SLAB_BYTES, tm, i * 64, s.head, s.key + j * kTile, BAR(B_KV_FULL + ring.stage));
-          }
-          armed |= 1u << ring.stage, parity = (parity & ~(1u << ring.stage)) | ring.phase << ring.stage;
+          for (int i = 0; i < G::SLABS; ++i) tma_load_3d(smem_at + i * G::SLAB_BYTES, tm, i * 64, s.head, s.key + j * kTile, full);
         }
         __syncwarp();
-        ring.next();
+      };
+      auto load_k = [&](const Slot& s, int j) {
+        if (k_no >= (uint32_t)G::NKS && !(ok = warp_wait(ctx, BAR(B_K_EMPTY + k_ring.stage), k_ring.phase ^ 1, 111))) return;
+        if (!(p.drop_tile && blockIdx.x == 0 && k_no == 0)) load_tile(&tmK, s, j, sbase + G::OFF_K + k_ring.stage * G::TILE_BYTES, BAR(B_K_FULL + k_ring.stage));
+        ++k_no, k_ring.next();
+      };
+      auto load_v = [&](const Slot& s, int j) {
+        if (v_no >= (uint32_t)G::NVS && !(ok = warp_wait(ctx, BAR(B_V_EMPTY + v_ring.stage), v_ring.phase ^ 1, 128))) return;
+        load_tile(&tmV, s, j, sbase + G::OFF_V + v_ring.stage * G::TILE_BYTES, BAR(B_V_FULL + v_ring.stage));
+        ++v_no, v_ring.next();
       };
       auto load_q = [&](const Slot& s, int x) {
         if (s.tiles == 0) return;
         if (q_it[x] && !(ok = warp_wait(ctx, BAR(B_Q_EMPTY + x), (q_it[x] & 1) ^ 1, 112))) return;
         ++q_it[x];
-        q_armed |= 1u << x;
         if (lane == 0) {
           mbar_expect_tx(BAR(B_Q_FULL + x), p.tq * p.group * 128 * G::SLABS);
 #pragma unroll
@@ -443,141 +463,184 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       };
       waveal::wait_for_previous_kernel();
       const int pairs = __ldcg(p.plan.head), odds = __ldcg(p.plan.head + 1), sequences = __ldcg(p.plan.head + 3);
-      long long ticket = blockIdx.x;
-      bool more = true;
-      while (ok && more) {
+      auto publish = [&](const Item& next) {
         const uint32_t at = item_no % kItems;
-        if (item_no >= kItems && !(ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + at), (item_no / kItems & 1) ^ 1, 113))) break;
-        Item next;
-        more = make_item(p, pairs, odds, sequences, ticket, next, lane);
-        int asked = 0;
+        if (item_no >= kItems && !(ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + at), (item_no / kItems & 1) ^ 1, 113))) return;
         if (lane == 0) {
-          next.end = !more;
           sm.items[at] = next;
           mbar_arrive(BAR(B_ITEM_FULL + at));
-          if (more) asked = atomicAdd(p.plan.head + 2, 1);     // (used when this item's tiles have been asked for)
         }
         __syncwarp();
         ++item_no;
-        if (!more) break;
         for (int j = 0; ok && j < next.tiles; ++j) {
           if (j == 0) load_q(next.slot[0], 0);
-          const bool drop = p.drop_tile && blockIdx.x == 0 && loaded == 0;
           for (int x = 0; ok && x < 2; ++x) {
-            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_tile(&tmK, next.slot[next.shared ? 1 : x], j, drop);
+            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_k(next.slot[next.shared ? 1 : x], j);
             if (ok && x == 0 && j == 0) load_q(next.slot[1], 1);
           }
           for (int x = 0; ok && x < 2; ++x)
-            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_tile(&tmV, next.slot[next.shared ? 1 : x], j, false);
+            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_v(next.slot[next.shared ? 1 : x], j);
         }
+      };
+      Item next;
+      long long ticket = blockIdx.x;
+      const long long tickets = (long long)pairs * p.kv_heads + ((long long)odds * p.kv_heads + 1) / 2;
+      while (ok && ticket < tickets) {
+        int asked = 0;
+        if (lane == 0) asked = atomicAdd(p.plan.head + 2, 1);    // (used when this item's tiles have been asked for)
+        make_item(p, pairs, odds, sequences, (int)ticket, next, lane);
+        publish(next);
         ticket = (long long)gridDim.x + __shfl_sync(0xffffffffu, asked, 0);
       }
-      // leaves no copy in flight, also where another warp has given up
-      for (int st = 0; st < G::STAGES + 2; ++st) {
-        const bool is_q = st >= G::STAGES;
-        if (!((is_q ? q_armed >> (st - G::STAGES) : armed >> st) & 1)) continue;
-        const uint32_t bar = is_q ? BAR(B_Q_FULL + st - G::STAGES) : BAR(B_KV_FULL + st), ph = is_q ? (q_it[st - G::STAGES] & 1) ^ 1 : parity >> st & 1;
+      // row tiles to be computed again, once everyone has said which
+      next.tiles = next.slot[0].tiles = next.slot[1].tiles = 0, next.shared = 0;
+      next.end = 2;
+      if (ok) publish(next);
+      if (ok && (ok = warp_wait(ctx, BAR(B_DONE), 0, 129))) {
+        for (int id = *reinterpret_cast<volatile int*>(&sm.again); ok && id >= 0; id = p.plan.again[id]) {
+          make_item(p, pairs, odds, sequences, id / 2, next, lane);
+          next.shared = 0, next.safe = 1;
+          next.tiles = next.slot[id & 1].tiles;
+          next.slot[(id & 1) ^ 1].tiles = 0;
+          publish(next);
+        }
+        next.end = 1, next.tiles = 0;
+        if (ok) publish(next);
+      }
+      // leaves no copy in flight, also where another warp has given up: the last one into each stage
+      auto landed = [&](uint32_t bar, uint32_t ph) {
         const long long t0 = clock64();
         while (!mbar_try_wait(bar, ph) && clock64() - t0 < p.wait_limit / 4) {}
+      };
+      for (uint32_t i = 0; i < (uint32_t)G::NKS && i < k_no; ++i) {
+        const uint32_t n = k_no - 1 - i;
+        if (!(p.drop_tile && blockIdx.x == 0 && n == 0)) landed(BAR(B_K_FULL + n % G::NKS), n / G::NKS & 1);
       }
+      for (uint32_t i = 0; i < (uint32_t)G::NVS && i < v_no; ++i) landed(BAR(B_V_FULL + (v_no - 1 - i) % G::NVS), (v_no - 1 - i) / G::NVS & 1);
+      for (int x = 0; x < 2; ++x)
+        if (q_it[x]) landed(BAR(B_Q_FULL + x), (q_it[x] & 1) ^ 1);
     } else if (warp < kCheckWarp) {
-      // ================================================================ products of a slot
+      // ================================================================ products
+      // Two warps issue, one S = Q K^T, the other O += P V, each for both slots in turn: what they do around the products (waits, ring
+      // positions) is a chain of 250 clk and more for each group of them, and four products (256 clk) are all that the tensor pipe has queued.
+      // (Measured on 512 pairs of row tiles over 32,760 keys, clk a pair and key tile without any softmax: one warp 3,810.  A warp a slot: the slots'
+      // products mix, both come out late, and both softmaxes then run at the same time, with no product beside them.)
       // (operands of the products come from shuffles, so that the compiler knows them to be the same in all lanes)
       constexpr uint32_t kTypeBits = (1u << 7) | (1u << 10), kType = std::is_same_v<T, __half> ? 0u : kTypeBits;
       constexpr uint32_t kQK = (make_idesc(128, 128, false) & ~kTypeBits) | kType, kPV = (make_idesc(128, D, true) & ~kTypeBits) | kType;
-      const int x = warp - kIssueWarp;
-      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), s_col = tm + G::S_COL + x * kTile, o_col = tm + G::O_COL + x * kTile;
-      const uint64_t q_desc = make_desc(sbase + G::OFF_Q + x * G::TILE_BYTES, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_KV, 16, 1024);
-      const uint64_t v_desc0 = make_desc(sbase + G::OFF_KV, G::SLAB_BYTES, 1024);
-      Ring<D> ring;
-      uint32_t items = 0, p_no = 0, checks = 0;
-      while (ok && next_item()) {
-        const int tiles = __shfl_sync(0xffffffffu, im->slot[x].tiles, 0), all = __shfl_sync(0xffffffffu, im->tiles, 0), shared = __shfl_sync(0xffffffffu, im->shared, 0);
-        const int other = __shfl_sync(0xffffffffu, im->slot[x ^ 1].tiles, 0), keys = __shfl_sync(0xffffffffu, im->slot[x].keys, 0);
-        const int masked = __shfl_sync(0xffffffffu, im->slot[x].masked, 0);
-        item_done();
-        // the other slot's tile: this warp lets it go when it is there
-        auto pass = [&] {
-          if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 114))) return;
-          if (lane == 0) mbar_arrive(BAR(B_KV_EMPTY + ring.stage));
-          ring.next();
-        };
-        for (int j = 0; ok && j < all; ++j) {
-          const bool mine = j < tiles;
-          if (!shared && x == 1 && j < other) pass();
-          if (ok && mine) {
-            if (j == 0 && !(ok = warp_wait(ctx, BAR(B_Q_FULL + x), items & 1, 115))) break;
-            if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 116))) break;
-            tc_fence_after();
-            const uint64_t kd = k_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      if (warp == kScoreWarp) {
+        const uint64_t q_desc = make_desc(sbase + G::OFF_Q, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_K, 16, 1024);
+        Ring<G::NKS> ring;
+        uint32_t items[2] = {0, 0}, done[2] = {0, 0};
+        while (ok && next_item()) {
+          const int tiles0 = __shfl_sync(0xffffffffu, im->slot[0].tiles, 0), tiles1 = __shfl_sync(0xffffffffu, im->slot[1].tiles, 0);
+          const int all = __shfl_sync(0xffffffffu, im->tiles, 0), shared = __shfl_sync(0xffffffffu, im->shared, 0);
+          item_done();
+          for (int j = 0; ok && j < all; ++j) {
 #pragma unroll
-            for (int slab = 0; slab < G::SLABS; ++slab)
-              umma4_ss(s_col, q_desc + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kQK, slab > 0);
-            tc_commit(BAR(B_S_FULL + x));
-            tc_commit(BAR(B_KV_EMPTY + ring.stage));
-            if (j == tiles - 1) tc_commit(BAR(B_Q_EMPTY + x));
-            ring.next();
-          } else if (ok && shared) {
-            pass();
-          }
-          if (ok && !shared && x == 0 && j < other) pass();
-          // ---- V
-          if (ok && !shared && x == 1 && j < other) pass();
-          if (ok && mine) {
-            const int groups = (min(kTile, keys - j * kTile) + 15) / 16;
-            if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 117))) break;
-            if (j == 0 && items && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items & 1) ^ 1, 118))) break;
-            int skip = 0;
-            if (j >= masked) {
-              if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + checks % kChecks), checks / kChecks & 1, 119))) break;
-              skip = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&sm.verdict[x][checks % kChecks]), 0);
-              ++checks;
-            }
-            const uint64_t vd = v_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              if (!(ok = warp_wait(ctx, BAR((half ? B_P_LAST : B_P_FIRST) + x), p_no & 1, 120))) break;
+            for (int x = 0; x < 2; ++x) {
+              const int tiles = x ? tiles1 : tiles0;
+              if (!ok || j >= tiles) continue;
+              if (!(ok = warp_wait(ctx, BAR(B_K_FULL + ring.stage), ring.phase, 116))) continue;
+              if (j == 0 && !(ok = warp_wait(ctx, BAR(B_Q_FULL + x), items[x] & 1, 115))) continue;
+              const uint64_t qd = q_desc + (uint64_t)(x * (G::TILE_BYTES >> 4)), kd = k_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
+              // (S lies over the last tile's P: its P V is over)
+              if (done[x] && !(ok = warp_wait(ctx, BAR(B_PV_DONE + x), (done[x] & 1) ^ 1, 114))) continue;
+              ++done[x];
               tc_fence_after();
-              const int here = skip ? 0 : groups - 4 * half;
-              const uint32_t a = s_col + half * 32;
-              const uint64_t v = vd + (uint64_t)(half * 64 * 128 >> 4);
-              if (here >= 4) {
-                umma4_ts(o_col, a, v, kPV, j > 0 || half > 0);
-              } else {
-#pragma unroll 1
-                for (int c = 0; c < here; ++c) umma_bf16_ts(o_col, a + c * 8, v + (uint64_t)(c * 16 * 128 >> 4), kPV, j > 0 || half > 0 || c > 0);
+#pragma unroll
+              for (int slab = 0; slab < G::SLABS; ++slab)
+                umma4_ss(tm + G::S_COL + x * kTile, qd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kQK, slab > 0);
+              tc_commit(BAR(B_S_FULL + x));
+              if (!shared || x) {
+                tc_commit(BAR(B_K_EMPTY + ring.stage));
+                ring.next();
               }
+              if (j == tiles - 1) tc_commit(BAR(B_Q_EMPTY + x));
             }
-            if (!ok) break;
-            ++p_no;
-            tc_commit(BAR(B_KV_EMPTY + ring.stage));
-            if (j == tiles - 1) tc_commit(BAR(B_O_FULL + x));
-            ring.next();
-          } else if (ok && shared) {
-            pass();
           }
-          if (ok && !shared && x == 0 && j < other) pass();
+          items[0] += tiles0 > 0, items[1] += tiles1 > 0;
         }
-        if (tiles) ++items;
+      } else {
+        const uint64_t v_desc0 = make_desc(sbase + G::OFF_V, G::SLAB_BYTES, 1024);
+        Ring<G::NVS> ring;
+        uint32_t items[2] = {0, 0}, p_no[2] = {0, 0}, checks[2] = {0, 0};
+        while (ok && next_item()) {
+          int tiles[2], keys[2], masked[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            tiles[x] = __shfl_sync(0xffffffffu, im->slot[x].tiles, 0);
+            keys[x] = __shfl_sync(0xffffffffu, im->slot[x].keys, 0);
+            masked[x] = __shfl_sync(0xffffffffu, im->safe ? im->slot[x].masked : INT_MAX, 0);
+          }
+          const int all = __shfl_sync(0xffffffffu, im->tiles, 0), shared = __shfl_sync(0xffffffffu, im->shared, 0);
+          item_done();
+          for (int j = 0; ok && j < all; ++j) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              if (!ok || j >= tiles[x]) continue;
+              if (!(ok = warp_wait(ctx, BAR(B_V_FULL + ring.stage), ring.phase, 117))) continue;
+              if (j == 0 && items[x] && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items[x] & 1) ^ 1, 118))) continue;
+              const uint32_t o_col = tm + G::O_COL + x * kTile, s_col = tm + G::S_COL + x * kTile;
+              const uint64_t vd = v_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
+              int groups = min(kTile / 16, (keys[x] - j * kTile + 15) / 16);   // of 16 keys that some row sees
+              if (j >= masked[x]) {
+                const uint32_t c = checks[x] % kChecks;
+                if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + c), checks[x] / kChecks & 1, 119))) continue;
+                if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&sm.verdict[x][c]), 0)) groups = 0;
+                ++checks[x];
+              }
+              if (!(ok = warp_wait(ctx, BAR(B_P + x * kParts), p_no[x] & 1, 120))) continue;
+              tc_fence_after();
+              // (P of keys 64 on lies 64 columns further: group c of 16 keys at column c / 4 * 64 + c % 4 * 8)
+              auto group = [&](int c) {
+                if (c < groups) umma_bf16_ts(o_col, s_col + c / 4 * 64 + c % 4 * 8, vd + (uint64_t)(c * 128), kPV, j > 0 || c > 0);
+              };
+              if (groups == 8) {
+                umma2_ts(o_col, s_col, vd, kPV, j > 0);
+                umma2_ts(o_col, s_col + 64, vd + 4 * 128, kPV, 1);
+              } else {
+                group(0), group(1), group(4), group(5);
+              }
+              if (!(ok = warp_wait(ctx, BAR(B_P + x * kParts + 1), p_no[x] & 1, 120))) continue;
+              ++p_no[x];
+              tc_fence_after();
+              if (groups == 8) {
+                umma2_ts(o_col, s_col + 16, vd + 2 * 128, kPV, 1);
+                umma2_ts(o_col, s_col + 80, vd + 6 * 128, kPV, 1);
+              } else {
+                group(2), group(3), group(6), group(7);
+              }
+              tc_commit(BAR(B_PV_DONE + x));
+              if (!shared || x) {
+                tc_commit(BAR(B_V_EMPTY + ring.stage));
+                ring.next();
+              }
+              if (j == tiles[x] - 1) tc_commit(BAR(B_O_FULL + x));
+            }
+          }
+          items[0] += tiles[0] > 0, items[1] += tiles[1] > 0;
+        }
       }
       // no product is still running when tensor memory is given back
-      tc_commit(BAR(B_FINAL + x));
+      tc_commit(BAR(B_FINAL + warp - kScoreWarp));
       __syncwarp();
       const long long t0 = clock64();
-      while (!mbar_try_wait(BAR(B_FINAL + x), 0) && clock64() - t0 < p.wait_limit / 4) {}
+      while (!mbar_try_wait(BAR(B_FINAL + warp - kScoreWarp), 0) && clock64() - t0 < p.wait_limit / 4) {}
     } else {
       // ================================================================ values of masked tiles
-      Ring<D> ring;
+      Ring<G::NVS> ring;
       uint32_t checks[2] = {0, 0};
       while (ok && next_item()) {
         const Item it = *im;
         item_done();
-        auto step = [&](bool is_v, int x, int j) {
-          if (!(ok = warp_wait(ctx, BAR(B_KV_FULL + ring.stage), ring.phase, 121))) return;
-          const bool cut[2] = {is_v && (it.shared || x == 0) && j < it.slot[0].tiles && j >= it.slot[0].masked,
-                               is_v && (it.shared || x == 1) && j < it.slot[1].tiles && j >= it.slot[1].masked};
+        auto step = [&](int x, int j) {
+          if (!(ok = warp_wait(ctx, BAR(B_V_FULL + ring.stage), ring.phase, 121))) return;
+          const bool cut[2] = {it.safe && (it.shared || x == 0) && j < it.slot[0].tiles && j >= it.slot[0].masked,
+                               it.safe && (it.shared || x == 1) && j < it.slot[1].tiles && j >= it.slot[1].masked};
           if (cut[0] || cut[1]) {
-            const uint32_t v = sbase + G::OFF_KV + ring.stage * G::TILE_BYTES;
+            const uint32_t v = sbase + G::OFF_V + ring.stage * G::TILE_BYTES;
             const int len = it.slot[x].len - j * kTile;     // rows of the tile that are the sequence's
             bool bad = false;
             if (p.causal) {
@@ -611,166 +674,182 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             for (int s = 0; s < 2; ++s) checks[s] += cut[s];
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(B_KV_EMPTY + ring.stage));
+          if (lane == 0) mbar_arrive(BAR(B_V_EMPTY + ring.stage));
           ring.next();
         };
         for (int j = 0; ok && j < it.tiles; ++j)
-          for (int k = 0; ok && k < 4; ++k) {
-            const int x = k & 1;
-            if (it.shared ? x == 0 : j < it.slot[x].tiles) step(k >= 2, it.shared ? 1 : x, j);
-          }
+          for (int x = 0; ok && x < 2; ++x)
+            if (it.shared ? x == 0 : j < it.slot[x].tiles) step(it.shared ? 1 : x, j);
       }
-    }
-  } else if (warp >= kEpilogueWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    // ================================================================ epilogues
-    const int quad = warp & 3, r = quad * 32 + lane, tok = r / p.group, g = r - tok * p.group;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    uint32_t items[2] = {0, 0};
-    while (ok && next_item()) {
-      for (int x = 0; ok && x < 2; ++x) {
-        const Slot s = im->slot[x];
-        if (s.tiles == 0) continue;
-        if (!(ok = warp_wait(ctx, BAR(B_SUMS + x), items[x] & 1, 122))) break;
-        if (!(ok = warp_wait(ctx, BAR(B_O_FULL + x), items[x] & 1, 123))) break;
-        ++items[x];
-        tc_fence_after();
-        const float2 lm = sm.sums[x][r];
-        const bool live = tok < s.n;
-        const int head = s.head * p.group + g, token = s.token + tok;
-        const float inv = lm.x == 0.f ? 0.f : 1.0f / lm.x;
-        T* o = static_cast<T*>(p.o) + head * p.o_stride_h + token * p.o_stride_t;
-        const uint32_t o_addr = tmem + lanes + G::O_COL + x * kTile;
-#pragma unroll
-        for (int c = 0; c < D; c += 32) {
-          uint32_t v[32], w[16];
-          WAVEAL_TMEM_LD32(o_addr + c, v, 0);
-          WAVEAL_TMEM_WAIT_LD32(v, 0);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            // (a row without a sum: O may be 0 times something)
-            const float a = __uint_as_float(v[2 * i]), b = __uint_as_float(v[2 * i + 1]);
-            w[i] = lm.x == 0.f ? 0u : pack2<T>(a * inv, b * inv);
-          }
-          if (live) {
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(o + c + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-          }
-        }
-        if (live && p.lse) p.lse[(long long)head * p.tokens + token] = lm.x == 0.f ? -INFINITY : (lm.y * p.sl2 + log2f(lm.x)) * 0.69314718055994531f;
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + x));
-      }
-      if (ok) item_done();
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-    // ================================================================ softmax: a thread a row
-    const int x = warp / 4, quad = warp & 3, r = quad * 32 + lane, tok = r / p.group;
+    // ================================================================ softmax, epilogue
+    const int x = warp / 8, half = warp / 4 & 1, quad = warp & 3, r = quad * 32 + lane, tok = r / p.group;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + G::S_COL + x * kTile, o_addr = tmem + lanes + G::O_COL + x * kTile;
+    const uint32_t s_addr = tmem + lanes + G::S_COL + x * kTile, h_addr = s_addr + half * 64, o_addr = tmem + lanes + G::O_COL + x * kTile + half * (D / 2);
     const float sl2 = p.sl2;
-    uint32_t s_no = 0, items = 0, checks = 0, v_at = 0;    // v_at: place in the ring where the item's tiles begin
+    uint32_t s_no = 0, items = 0, checks = 0, pairs = 0, v_at = 0;   // v_at: place in the ring where the item's values begin
+    // what the row's other thread has
+    auto give = [&](float mine) {
+      sm.pair[x][pairs & 1][half][r] = mine;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(B_PAIR + x * 4 + quad));
+    };
+    auto take = [&](float& other) {
+      if (!(ok = warp_wait(ctx, BAR(B_PAIR + x * 4 + quad), pairs & 1, 122))) return;
+      other = sm.pair[x][pairs & 1][half ^ 1][r];
+      ++pairs;
+    };
     while (ok && next_item()) {
       const Slot s = im->slot[x];
-      const int all = im->tiles, shared = im->shared, other = im->slot[x ^ 1].tiles;
+      const int all = im->tiles, shared = im->shared, other = im->slot[x ^ 1].tiles, safe = im->safe, id = 2 * im->ticket + x;
+      const bool said = im->end == 2;
       item_done();
+      if (said && lane == 0) mbar_arrive(BAR(B_DONE));
       // where a tile's values are in the ring (asked for in the rare case that they are added here)
       const uint32_t begin = v_at;
-      auto v_stage = [&](int j) {
-        const int before = shared ? 2 * j : 2 * j + 2 * min(j, other), mine = shared ? 1 : 1 + (j < other ? (x ? 2 : 1) : 0);
-        return (begin + before + mine) % G::STAGES;
-      };
-      v_at = (begin + (shared ? 2 * all : 2 * (s.tiles + other))) % G::STAGES;
+      auto v_stage = [&](int j) { return (begin + j + (shared ? 0 : min(j, other) + (x && j < other))) % G::NVS; };
+      v_at = (begin + (shared ? all : s.tiles + other)) % G::NVS;
       if (s.tiles == 0) continue;
       const bool live = tok < s.n;
-      const int sees = min(p.causal ? s.sees + tok : s.keys, s.keys);
+      const int sees = min(p.causal ? s.sees + tok : s.keys, s.keys) - half * 64;
       float ref = -INFINITY, sum = 0.f;
+      bool over = false;
 #pragma unroll 1
       for (int j = 0; j < s.tiles; ++j) {
         if (!(ok = warp_wait(ctx, BAR(B_S_FULL + x), s_no & 1, 124))) break;
         ++s_no;
         tc_fence_after();
-        uint32_t v[128];
-        WAVEAL_TMEM_LD32(s_addr, v, 0);
-        WAVEAL_TMEM_LD32(s_addr + 32, v, 32);
-        WAVEAL_TMEM_LD32(s_addr + 64, v, 64);
-        WAVEAL_TMEM_LD32(s_addr + 96, v, 96);
-        WAVEAL_TMEM_WAIT_LD32(v, 0);
-        WAVEAL_TMEM_WAIT_LD32(v, 32);
-        WAVEAL_TMEM_WAIT_LD32(v, 64);
-        WAVEAL_TMEM_WAIT_LD32(v, 96);
-        if (j >= s.masked) {
-          const int visible = sees - j * kTile;
+        const bool cut = j >= s.masked;
+        const int chunks = min(2, (s.keys - j * kTile - half * 64 + 31) / 32);   // of this thread's 64 keys (what is behind the last key is not used)
+        uint32_t u[32], w[16];
+        if (cut) {
+          // scores that the row does not see, 16 columns at a time from the first that some row does not see.  (Code that runs once or twice an
+          // item is short: each 128 bytes of it come from beyond the instruction caches.)
+          const int visible = sees - j * kTile, from = max(0, s.sees - j * kTile - half * 64) / 16 * 16;
+#pragma unroll 1
+          for (int c = from; c < 32 * chunks; c += 16) {
+            uint32_t t[16];
+            WAVEAL_TMEM_LD16(h_addr + c, t, 0);
+            WAVEAL_TMEM_WAIT_LD16(t, 0);
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i >= visible) v[i] = 0xff800000u;
+            for (int i = 0; i < 16; ++i)
+              if (i >= visible - c) t[i] = 0xff800000u;
+            WAVEAL_TMEM_ST16(h_addr + c, t, 0);
+          }
+          tc_wait_st();
         }
-        float m4[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m4[i] = __uint_as_float(v[i]);
-#pragma unroll
-        for (int i = 4; i < 124; i += 8) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) m4[k] = fmax3(m4[k], __uint_as_float(v[i + 2 * k]), __uint_as_float(v[i + 2 * k + 1]));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m4[i] = fmaxf(m4[i], __uint_as_float(v[124 + i]));
-        const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        if (j == 0) {
-          ref = top;
-        } else {
-          const bool grown = live && (top - ref) * sl2 > kGrowth;
-          if (__any_sync(0xffffffffu, grown)) {
-            // (S of this tile is there, so the last tile's P V, issued before it, is done)
-            const float scale = grown ? ex2((ref - top) * sl2) : 1.0f;
-            if (grown) ref = top;
-            sum *= scale;
-            rescale<D>(o_addr, scale);
+        if (j == 0 || safe) {
+          float top = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < chunks; ++c) {
+            WAVEAL_TMEM_LD32(h_addr + 32 * c, u, 0);
+            WAVEAL_TMEM_WAIT_LD32(u, 0);
+            top = fmaxf(top, row_max32(u));
+          }
+                  give(top);
+          float top2;
+          take(top2);
+          if (!ok) break;
+          top = fmaxf(top, top2);
+          if (j == 0) {
+            ref = top;
+          } else {
+            const bool grown = live && (top - ref) * sl2 > kGrowth;
+            if (__any_sync(0xffffffffu, grown)) {
+              // (S of this tile is there, so the last tile's P V is done)
+              const float scale = grown ? ex2((ref - top) * sl2) : 1.0f;
+              if (grown) ref = top;
+              sum *= scale;
+              rescale<D / 2>(o_addr, scale);
+            }
           }
         }
         const float minus = ref == -INFINITY ? 0.f : -ref * sl2;
         float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+        auto release = [&](int part) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR(B_P + x * kParts + part));
+        };
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c) {
+          WAVEAL_TMEM_LD32(h_addr + 32 * c, u, 0);
+          WAVEAL_TMEM_WAIT_LD32(u, 0);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t w[32];
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const int c = half * 64 + 2 * i;
+          for (int i = 0; i < 16; i += 2) {
             float a, b, d, e;
-            ffma2(a, b, __uint_as_float(v[c]), __uint_as_float(v[c + 1]), sl2, sl2, minus, minus);
-            ffma2(d, e, __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]), sl2, sl2, minus, minus);
+            ffma2(a, b, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), sl2, sl2, minus, minus);
+            ffma2(d, e, __uint_as_float(u[2 * i + 2]), __uint_as_float(u[2 * i + 3]), sl2, sl2, minus, minus);
             a = ex2(a), b = ex2(b), d = ex2(d), e = ex2(e);
             fadd2(s0, s1, s0, s1, a, b);
             fadd2(s2, s3, s2, s3, d, e);
             w[i] = pack2<T>(a, b), w[i + 1] = pack2<T>(d, e);
           }
-          WAVEAL_TMEM_ST32(s_addr + half * 32, w, 0);
+          WAVEAL_TMEM_ST16(h_addr + 16 * c, w, 0);
           tc_wait_st();
-          if (half && j >= s.masked) {
-            if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + checks % kChecks), checks / kChecks & 1, 125))) break;
-            if (*reinterpret_cast<volatile int*>(&sm.verdict[x][checks % kChecks])) {
+          if (c == 0) release(0);
+        }
+        if (chunks <= 0) release(0);
+        if (cut && safe) {
+          if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + checks % kChecks), checks / kChecks & 1, 125))) break;
+          if (*reinterpret_cast<volatile int*>(&sm.verdict[x][checks % kChecks])) {
+            // the row's first thread adds for both, when both have written P
+            tc_fence_before();
+            float none;
+            give(0.f);
+            take(none);
+            if (!ok) break;
+            if (half == 0) {
               if (j == 0 && items && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items & 1) ^ 1, 127))) break;
               tc_fence_after();
-              add_visible<D, T>(s_addr, o_addr, sbase + G::OFF_KV + v_stage(j) * G::TILE_BYTES, sees - j * kTile, j == 0);
+              add_visible<D, T>(s_addr, o_addr, sbase + G::OFF_V + v_stage(j) * G::TILE_BYTES, sees - j * kTile, j == 0);
             }
-            ++checks;
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(BAR((half ? B_P_LAST : B_P_FIRST) + x));
+          ++checks;
         }
-        if (!ok) break;
-        sum += (s0 + s1) + (s2 + s3);
+        release(1);
+        s0 = (s0 + s1) + (s2 + s3);
+        over |= !(s0 < kSumLimit<T>);
+        sum += s0;
       }
       if (!ok) break;
-      // (the epilogue has read the last item's)
-      if (items && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items & 1) ^ 1, 126))) break;
+      give(sum);
+      float sum2;
+      take(sum2);
+      if (!ok || !(ok = warp_wait(ctx, BAR(B_O_FULL + x), items & 1, 123))) break;
       ++items;
-      sm.sums[x][r] = make_float2(sum, ref);
+      tc_fence_after();
+      sum += sum2;
+      const int head = s.head * p.group + r - tok * p.group, token = s.token + tok;
+      const float inv = sum == 0.f ? 0.f : __fdividef(1.0f, sum);
+      T* o = static_cast<T*>(p.o) + head * p.o_stride_h + token * p.o_stride_t + half * (D / 2);
+      float none0 = 0.f, none1 = 0.f;                // zero, NaN where something in O is not finite
+#pragma unroll 1
+      for (int c = 0; c < D / 2; c += 16) {
+        uint32_t u[16], w[8];
+        WAVEAL_TMEM_LD16(o_addr + c, u, 0);
+        WAVEAL_TMEM_WAIT_LD16(u, 0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float a, b;
+          ffma2(none0, none1, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), 0.f, 0.f, none0, none1);
+          ffma2(a, b, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), inv, inv, 0.f, 0.f);
+          w[i] = sum == 0.f ? 0u : pack2<T>(a, b);   // (O may be 0 times something)
+        }
+        if (live) {
+          *reinterpret_cast<uint4*>(o + c) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(o + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+      }
+      if (live && p.lse && half == 0) p.lse[(long long)head * p.tokens + token] = sum == 0.f ? -INFINITY : (ref * sl2 + __log2f(sum)) * 0.69314718055994531f;
+      // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
+      const bool bad = over || (ref == -INFINITY && s.tiles > 1) || !(none0 + none1 == 0.f);
+      tc_fence_before();
+      // (the slot's eight warps are never more than an item apart)
+      if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.last_again[x], id) != id) p.plan.again[id] = atomicExch(&sm.again, id);
       __syncwarp();
-      if (lane == 0) mbar_arrive(BAR(B_SUMS + x));
+      if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + x));
     }
   }
 
@@ -797,13 +876,20 @@ waveal_status make_map(CUtensorMap* tm, const waveal_prompt_desc* d, const void*
   return WAVEAL_OK;
 }
 
-struct Layout { size_t seq, odd, bytes; };
+// tickets that there can be: pairs of row tiles and single ones, two by two, of every key head
+long long most_tickets(const waveal_prompt_desc* d) {
+  const long long tq = kTile / (d->q_heads / d->kv_heads);
+  return (d->tokens / (2 * tq) + d->batch) * d->kv_heads + 1;
+}
+
+struct Layout { size_t seq, odd, again, bytes; };
 Layout layout(const waveal_prompt_desc* d) {
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   Layout l;
   l.seq = 256;
   l.odd = l.seq + up((size_t)d->batch * sizeof(int4));
-  l.bytes = l.odd + up((size_t)d->batch * sizeof(int));
+  l.again = l.odd + up((size_t)d->batch * sizeof(int));
+  l.bytes = l.again + up((size_t)most_tickets(d) * 2 * sizeof(int));
   return l;
 }
 
@@ -815,6 +901,7 @@ waveal_status check(const waveal_prompt_desc* d) {
   if (d->kv_heads <= 0 || d->q_heads <= 0 || d->q_heads % d->kv_heads || d->q_heads / d->kv_heads > kTile)
     return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q_heads %d: a multiple of kv_heads (%d), at most %d times as many", d->q_heads, d->kv_heads, kTile);
   if (d->flags & ~(WAVEAL_PROMPT_CAUSAL | WAVEAL_PROMPT_SELFTEST_LOST_TILE)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "unknown flags 0x%x", d->flags);
+  if (most_tickets(d) > 1000000000ll) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 10^9 row tiles (of every sequence and key head)");
   if ((long long)d->tokens * d->q_heads > 1000000000ll) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 10^9 rows (tokens * q_heads)");
   const int64_t* strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
   for (const int64_t* s : strides)
@@ -874,6 +961,7 @@ extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const v
   p.plan.head = reinterpret_cast<int*>(w);
   p.plan.seq = reinterpret_cast<int4*>(w + l.seq);
   p.plan.odd = reinterpret_cast<int*>(w + l.odd);
+  p.plan.again = reinterpret_cast<int*>(w + l.again);
   p.seq_start = seq_start, p.seq_len = seq_len;
   p.o = o, p.lse = lse, p.o_stride_h = d->o_stride[0], p.o_stride_t = d->o_stride[1];
   p.dev_status = dev_status;
@@ -885,9 +973,7 @@ extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const v
   if (waveal_status e = make_map(&tm[0], d, q, d->q_heads, d->q_stride, p.group, p.tq, "q")) return e;
   if (waveal_status e = make_map(&tm[1], d, k, d->kv_heads, d->k_stride, 1, kTile, "k")) return e;
   if (waveal_status e = make_map(&tm[2], d, v, d->kv_heads, d->v_stride, 1, kTile, "v")) return e;
-  // a thread block an SM, and no more than there can be items: pairs of row tiles and single ones, of every key head
-  const long long most = ((long long)d->tokens / (2 * p.tq) + d->batch) * d->kv_heads;
-  const unsigned grid = (unsigned)std::min((long long)sms, std::max(1ll, most));
+  const unsigned grid = (unsigned)std::min((long long)sms, most_tickets(d));   // a thread block an SM
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (d->dtype == WAVEAL_FP16) return d->head_dim == 128 ? launch<128, __half>(tm, p, grid, st) : launch<64, __half>(tm, p, grid, st);
   return d->head_dim == 128 ? launch<128, __nv_bfloat16>(tm, p, grid, st) : launch<64, __nv_bfloat16>(tm, p, grid, st);
