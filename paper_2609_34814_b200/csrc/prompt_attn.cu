@@ -75,7 +75,7 @@ struct Params {
   long long o_stride_h, o_stride_t;
   int* dev_status;
   long long wait_limit;
-  int drop_tile;
+  int drop_tile, wide_o;   // wide_o: o in 32-byte pieces
   float sl2;               // scale * log2(e)
 };
 
@@ -171,6 +171,7 @@ struct Slot {
   int key, keys;           // first token of the sequence; how many of its tokens any row sees
   int sees;                // how many the first token sees (causal: every token one more)
   int len;                 // tokens of the sequence
+  long long o;             // the first token and query head in o
 };
 struct Item {
   int end;                 // 1: nothing left; 2: everyone says when all items before this one are done
@@ -192,6 +193,7 @@ __device__ inline Slot make_slot(const Params& p, const int4& q, int head, int t
   s.sees = p.causal ? first + 1 : q.y;
   s.tiles = ceil_div(s.keys, kTile);
   s.masked = s.sees / kTile;
+  s.o = (long long)head * p.group * p.o_stride_h + (long long)s.token * p.o_stride_t;
   return s;
 }
 
@@ -287,11 +289,16 @@ enum {
 };
 template <int D> constexpr int kBars = B_K_FULL + 2 * (Geo<D>::NKS + Geo<D>::NVS);
 
+// Where P of 16 keys lies among the columns of the slot's S: keys 0-31 at 48, 32-63 at 32, 64 on at 64.  It covers scores that its own threads have
+// read (the second half of keys 0-63 first); columns 0-31 keep theirs, which all threads take the reference from.
+__device__ __forceinline__ int p_column(int group) { return group < 4 ? 32 + (group ^ 2) * 8 : 32 + group * 8; }
+
 // what lies behind the tiles in shared memory
 template <int D> struct Small {
   unsigned long long bar[kBars<D>];
   Item items[kItems];
-  float pair[2][2][2][kTile];                        // [slot][turn][half][row]: maxima and sums, from a row's one thread to its other
+  float pair[2][2][2][kTile];                        // [slot][turn][half][row]: maxima, from a row's one thread to its other
+  float sums[2][2][2][kTile];                        // [slot][turn][half][row] (a warp may be an item ahead of the row's other one)
   int verdict[2][kChecks];                           // not every value of the slot's masked tile is finite
   uint32_t tmem;
   int abort;
@@ -319,7 +326,7 @@ __device__ __noinline__ void add_visible(uint32_t p_addr, uint32_t o_addr, uint3
 #pragma unroll 1
     for (int k = 0; k < kTile; k += 2) {
       uint32_t pk;
-      asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(pk) : "r"(p_addr + k / 64 * 64 + k % 64 / 2) : "memory");
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(pk) : "r"(p_addr + p_column(k / 16) + k % 16 / 2) : "memory");
       asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(pk)::"memory");
       const float2 pr = unpack2<T>(pk);
 #pragma unroll
@@ -592,25 +599,20 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 ++checks[x];
               }
               if (!(ok = warp_wait(ctx, BAR(B_P + x * kParts), p_no[x] & 1, 120))) continue;
-              tc_fence_after();
-              // (P of keys 64 on lies 64 columns further: group c of 16 keys at column c / 4 * 64 + c % 4 * 8)
-              auto group = [&](int c) {
-                if (c < groups) umma_bf16_ts(o_col, s_col + c / 4 * 64 + c % 4 * 8, vd + (uint64_t)(c * 128), kPV, j > 0 || c > 0);
-              };
               if (groups == 8) {
-                umma2_ts(o_col, s_col, vd, kPV, j > 0);
+                tc_fence_after();
+                umma2_ts(o_col, s_col + 32, vd + 2 * 128, kPV, j > 0);
                 umma2_ts(o_col, s_col + 64, vd + 4 * 128, kPV, 1);
-              } else {
-                group(0), group(1), group(4), group(5);
               }
               if (!(ok = warp_wait(ctx, BAR(B_P + x * kParts + 1), p_no[x] & 1, 120))) continue;
               ++p_no[x];
               tc_fence_after();
               if (groups == 8) {
-                umma2_ts(o_col, s_col + 16, vd + 2 * 128, kPV, 1);
+                umma2_ts(o_col, s_col + 48, vd, kPV, 1);
                 umma2_ts(o_col, s_col + 80, vd + 6 * 128, kPV, 1);
               } else {
-                group(2), group(3), group(6), group(7);
+#pragma unroll 1
+                for (int c = 0; c < groups; ++c) umma_bf16_ts(o_col, s_col + p_column(c), vd + (uint64_t)(c * 128), kPV, j > 0 || c > 0);
               }
               tc_commit(BAR(B_PV_DONE + x));
               if (!shared || x) {
@@ -688,6 +690,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const uint32_t s_addr = tmem + lanes + G::S_COL + x * kTile, h_addr = s_addr + half * 64, o_addr = tmem + lanes + G::O_COL + x * kTile + half * (D / 2);
     const float sl2 = p.sl2;
+    const int g = r - tok * p.group;
+    T* const o0 = static_cast<T*>(p.o) + g * p.o_stride_h + tok * p.o_stride_t + half * (D / 2);
     uint32_t s_no = 0, items = 0, checks = 0, pairs = 0, v_at = 0;   // v_at: place in the ring where the item's values begin
     // what the row's other thread has
     auto give = [&](float mine) {
@@ -700,17 +704,28 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       other = sm.pair[x][pairs & 1][half ^ 1][r];
       ++pairs;
     };
-    while (ok && next_item()) {
-      const Slot s = im->slot[x];
-      const int all = im->tiles, shared = im->shared, other = im->slot[x ^ 1].tiles, safe = im->safe, id = 2 * im->ticket + x;
-      const bool said = im->end == 2;
+    // this item's part of the slot; read while the last item's products end
+    Slot s;
+    int all, shared, other, safe, id, said;
+    bool more;
+    auto read_item = [&] {
+      more = next_item();
+      if (!more) return;
+      s = im->slot[x];
+      all = im->tiles, shared = im->shared, other = im->slot[x ^ 1].tiles, safe = im->safe, id = 2 * im->ticket + x, said = im->end == 2;
       item_done();
-      if (said && lane == 0) mbar_arrive(BAR(B_DONE));
+    };
+    read_item();
+    while (ok && more) {
       // where a tile's values are in the ring (asked for in the rare case that they are added here)
       const uint32_t begin = v_at;
-      auto v_stage = [&](int j) { return (begin + j + (shared ? 0 : min(j, other) + (x && j < other))) % G::NVS; };
       v_at = (begin + (shared ? all : s.tiles + other)) % G::NVS;
-      if (s.tiles == 0) continue;
+      if (s.tiles == 0) {
+        if (said && lane == 0) mbar_arrive(BAR(B_DONE));
+        read_item();
+        continue;
+      }
+      auto v_stage = [&](int j) { return (begin + j + (shared ? 0 : min(j, other) + (x && j < other))) % G::NVS; };
       const bool live = tok < s.n;
       const int sees = min(p.causal ? s.sees + tok : s.keys, s.keys) - half * 64;
       float ref = -INFINITY, sum = 0.f;
@@ -739,7 +754,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           }
           tc_wait_st();
         }
-        if (j == 0 || safe) {
+        if (safe) {
           float top = -INFINITY;
 #pragma unroll 1
           for (int c = 0; c < chunks; ++c) {
@@ -747,7 +762,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             WAVEAL_TMEM_WAIT_LD32(u, 0);
             top = fmaxf(top, row_max32(u));
           }
-                  give(top);
+          give(top);
           float top2;
           take(top2);
           if (!ok) break;
@@ -764,6 +779,15 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               rescale<D / 2>(o_addr, scale);
             }
           }
+        } else if (j == 0) {
+          // the largest of the first 16 scores: both threads of a row find the same
+          uint32_t t[16];
+          WAVEAL_TMEM_LD16(s_addr, t, 0);
+          WAVEAL_TMEM_WAIT_LD16(t, 0);
+          const int visible = sees + half * 64;
+          ref = __uint_as_float(t[0]);
+#pragma unroll
+          for (int i = 1; i < 16; ++i) ref = fmaxf(ref, i < visible ? __uint_as_float(t[i]) : -INFINITY);
         }
         const float minus = ref == -INFINITY ? 0.f : -ref * sl2;
         float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
@@ -773,7 +797,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           if (lane == 0) mbar_arrive(BAR(B_P + x * kParts + part));
         };
 #pragma unroll 1
-        for (int c = 0; c < chunks; ++c) {
+        for (int n = 0; n < chunks; ++n) {
+          const int c = half ? n : chunks - 1 - n;
           WAVEAL_TMEM_LD32(h_addr + 32 * c, u, 0);
           WAVEAL_TMEM_WAIT_LD32(u, 0);
 #pragma unroll
@@ -786,9 +811,9 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             fadd2(s2, s3, s2, s3, d, e);
             w[i] = pack2<T>(a, b), w[i + 1] = pack2<T>(d, e);
           }
-          WAVEAL_TMEM_ST16(h_addr + 16 * c, w, 0);
+          WAVEAL_TMEM_ST16(s_addr + p_column(4 * half + 2 * c), w, 0);
           tc_wait_st();
-          if (c == 0) release(0);
+          if (n == 0) release(0);
         }
         if (chunks <= 0) release(0);
         if (cut && safe) {
@@ -808,22 +833,25 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           }
           ++checks;
         }
-        release(1);
         s0 = (s0 + s1) + (s2 + s3);
         over |= !(s0 < kSumLimit<T>);
         sum += s0;
+        if (j == s.tiles - 1) sm.sums[x][items & 1][half][r] = sum;       // (read once the products of this tile are done)
+        release(1);
       }
       if (!ok) break;
-      give(sum);
-      float sum2;
-      take(sum2);
-      if (!ok || !(ok = warp_wait(ctx, BAR(B_O_FULL + x), items & 1, 123))) break;
-      ++items;
+      T* const o = o0 + s.o;
+      float* const lse = live && p.lse && half == 0 ? p.lse + (long long)(s.head * p.group + g) * p.tokens + s.token + tok : nullptr;
+      bool bad = over || (ref == -INFINITY && s.tiles > 1);
+      const bool again = live && !safe;
+      const int this_id = id;
+      const uint32_t o_phase = items & 1;
+      read_item();
+      if (!ok || !(ok = warp_wait(ctx, BAR(B_O_FULL + x), o_phase, 123))) break;
       tc_fence_after();
-      sum += sum2;
-      const int head = s.head * p.group + r - tok * p.group, token = s.token + tok;
+      sum += sm.sums[x][items & 1][half ^ 1][r];
+      ++items;
       const float inv = sum == 0.f ? 0.f : __fdividef(1.0f, sum);
-      T* o = static_cast<T*>(p.o) + head * p.o_stride_h + token * p.o_stride_t + half * (D / 2);
       float none0 = 0.f, none1 = 0.f;                // zero, NaN where something in O is not finite
 #pragma unroll 1
       for (int c = 0; c < D / 2; c += 16) {
@@ -837,17 +865,23 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           ffma2(a, b, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), inv, inv, 0.f, 0.f);
           w[i] = sum == 0.f ? 0u : pack2<T>(a, b);   // (O may be 0 times something)
         }
+        // (a warp's rows lie far apart: every store is 32 lines to the memory pipe, so the fewer the better)
         if (live) {
-          *reinterpret_cast<uint4*>(o + c) = make_uint4(w[0], w[1], w[2], w[3]);
-          *reinterpret_cast<uint4*>(o + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+          if (p.wide_o) {
+            st_global_v8(o + c, w);
+          } else {
+            *reinterpret_cast<uint4*>(o + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(o + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+          }
         }
       }
-      if (live && p.lse && half == 0) p.lse[(long long)head * p.tokens + token] = sum == 0.f ? -INFINITY : (ref * sl2 + __log2f(sum)) * 0.69314718055994531f;
+      if (lse) *lse = sum == 0.f ? -INFINITY : (ref * sl2 + __log2f(sum)) * 0.69314718055994531f;
       // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
-      const bool bad = over || (ref == -INFINITY && s.tiles > 1) || !(none0 + none1 == 0.f);
+      bad |= !(none0 + none1 == 0.f);
       tc_fence_before();
       // (the slot's eight warps are never more than an item apart)
-      if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.last_again[x], id) != id) p.plan.again[id] = atomicExch(&sm.again, id);
+      if (__any_sync(0xffffffffu, bad && again) && lane == 0 && atomicExch(&sm.last_again[x], this_id) != this_id)
+        p.plan.again[this_id] = atomicExch(&sm.again, this_id);
       __syncwarp();
       if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + x));
     }
@@ -964,6 +998,7 @@ extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const v
   p.plan.again = reinterpret_cast<int*>(w + l.again);
   p.seq_start = seq_start, p.seq_len = seq_len;
   p.o = o, p.lse = lse, p.o_stride_h = d->o_stride[0], p.o_stride_t = d->o_stride[1];
+  p.wide_o = waveal::aligned(o, 32) && d->o_stride[0] % 16 == 0 && d->o_stride[1] % 16 == 0;
   p.dev_status = dev_status;
   p.drop_tile = d->flags & WAVEAL_PROMPT_SELFTEST_LOST_TILE ? 1 : 0;
   p.wait_limit = p.drop_tile ? kSelfTestCycles : kTimeoutCycles;

@@ -152,12 +152,12 @@ def test_scores_that_grow(dtype):
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("dim, heads, kv_heads", [(128, 2, 2), (64, 2, 2), (128, 16, 2)])
 def test_values_that_a_token_does_not_see(what, dim, heads, kv_heads):
-    """Tokens in front of a bad value or key have the results they have without it (the very bits where it is a key; a bad value's tile
-    is added in another order, which fp32 sums of 128 numbers see in their last bits: within the definition's tolerance)."""
+    """Tokens in front of a bad value or key have the results they have without it, within the definition's tolerance: the row tiles that meet
+    it are computed again, with another reference and their sums in another order."""
     n = 700
     q, k, v = tensors(2 * n, heads, kv_heads, dim, BF, seed=6)
     clean, clean_lse = check(q, k, v, [0, n, 2 * n])
-    want, _, tol, _ = expected(q, k, v, [0, n], [n, n], True)
+    want, want_lse, tol, lse_tol = expected(q, k, v, [0, n], [n, n], True)
     for at in (0, 5, 100, 127, 128, 300, n - 1):
         for t in (k, v):
             bad = t.clone()
@@ -166,11 +166,10 @@ def test_values_that_a_token_does_not_see(what, dim, heads, kv_heads):
                 bad[:, at, 1:] = t[:, at, 1:]                          # one channel: the score is + or - infinity
             o, lse, status = run(q, bad if t is k else k, bad if t is v else v, [0, n, 2 * n])
             assert status == [0, 0, 0, 0]
-            assert torch.equal(lse[:, :at], clean_lse[:, :at])
-            assert torch.equal(o[:, :at], clean[:, :at]) if t is k else ((o.double() - want).abs() <= tol)[:, :at].all()
+            assert ((lse.double() - want_lse).abs() <= lse_tol)[:, :at].all() and ((o.double() - want).abs() <= tol)[:, :at].all()
             assert torch.equal(o[:, n:], clean[:, n:]) and torch.equal(lse[:, n:], clean_lse[:, n:])      # the other sequence
             if t is v:
-                assert torch.equal(lse, clean_lse)
+                assert ((lse.double() - want_lse).abs() <= lse_tol).all()
                 assert (o[:, at:n].isnan() if math.isnan(what) else o[:, at:n] == what).all()
             elif math.isnan(what):
                 assert o[:, at:n].isnan().all() and lse[:, at:n].isnan().all()
