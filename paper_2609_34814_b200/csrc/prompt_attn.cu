@@ -5,19 +5,18 @@
 // more than 2^8, which the same reference in the sum makes exact).
 //
 // A row tile is 128 rows of S: tq = 128 / G tokens with the G query heads that share a key head, so that a key head's tiles are
-// loaded once for all of them and the causal diagonal crosses few of a tile's columns.  A thread block has two slots with a
-// row tile each and walks the key tiles of 128:
-//   slot: S = Q K^T (tensor memory) -> maximum, exponentials, P over S's columns -> O += P V (tensor memory)
-// One slot is in its products while the other is in its softmax.  A pair of row tiles of a sequence shares its K and V
-// tiles; the first row tile of a sequence with an odd number of them goes with that of another sequence or head (each slot
-// then has its own K and V tiles).
+// loaded once for all of them and the causal diagonal crosses few of a tile's columns.  A thread block takes row tiles one after another,
+// and their key tiles of 128 as one stream:
+//   S = Q K^T (one of three buffers in tensor memory) -> exponentials, P over S's columns -> O += P V (tensor memory).
+// Two teams of eight warps take the tiles of the stream in turn, also across row tiles: one row tile's end (its last products, its
+// results on their way out) runs beside the next one's first tiles.
 //
-// Warps: 0-7 and 8-15 softmax and epilogue of the slots (two threads a row, 64 keys of a tile each: a warp by itself issues an instruction in
-// four clocks, so that four of them a scheduler are needed), 16 items and loads, 17 and 18 products, 19 masked tiles' values.
+// Warps: 0-7 and 8-15 the teams (two threads a row, 64 keys of a tile each: a warp by itself issues an instruction in four clocks, so
+// that four of them a scheduler are needed), 16 items, Q and K, 17 and 18 products, 19 V.
 //
-// Values that a token must not see: their probabilities are zero, but zero times NaN is not.  Warp 15 writes zeros over what lies behind a
-// sequence's end and looks through the values of tiles that the causal mask cuts; where one is not finite, the slot's softmax warps add that tile's
-// products themselves, each row's visible keys alone.
+// Values that a token must not see: their probabilities are zero, but zero times NaN is not.  A row tile whose results are not finite is computed
+// again: then warp 19 writes zeros over what lies behind a sequence's end and looks through the values of tiles that the causal mask cuts; where one is
+// not finite, the softmax warps add that tile's products themselves, each row's visible keys alone.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -33,12 +32,12 @@ namespace {
 using namespace waveal::sm100;
 
 constexpr int kThreads = 640;
-constexpr int kLoadWarp = 16, kScoreWarp = 17, kCheckWarp = 19;
-constexpr int kTile = 128;                           // keys of a tile, rows of a slot
-constexpr int kItems = 4;                            // between the loader and the others
-constexpr int kItemReaders = 19;                     // two issuers, the checker, sixteen softmax warps
+constexpr int kLoadWarp = 16, kScoreWarp = 17, kProductWarp = 18;
+constexpr int kTile = 128;                           // keys of a tile, rows of a row tile
+constexpr int kItems = 4;                            // row tiles under way: their descriptions, references and sums
+constexpr int kItemReaders = 19;                     // two issuers, the V loader, sixteen softmax warps
 constexpr int kParts = 2;                            // of a tile: P goes to the products 32 keys of each half at a time
-constexpr int kChecks = 8;                           // masked tiles of a slot whose verdicts are under way (more than the ring has V tiles)
+constexpr int kChecks = 8;                           // masked tiles whose verdicts are under way (more than the ring has V tiles)
 constexpr long long kTimeoutCycles = 4000000000ll;   // ~2 s at boost clock
 constexpr long long kSelfTestCycles = 4000000ll;     // ~2 ms
 constexpr float kGrowth = 8.0f;                      // log2 of how far a row's maximum may outgrow its reference
@@ -52,18 +51,18 @@ template <int D> struct Geo {
   static constexpr int TILE_BYTES = SLABS * SLAB_BYTES;
   static constexpr int NKS = D == 128 ? 2 : 4, NVS = NKS;   // stages of the rings of K and V tiles
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NKS * TILE_BYTES, OFF_END = OFF_V + NVS * TILE_BYTES;
-  static constexpr int S_COL = 0, O_COL = 256;       // tensor memory: S (and P) 0-127, 128-255, O 256.., 384..
+  static constexpr int S_COL = 0, O_COL = 384;       // tensor memory: S (and P) 0-127, 128-255, 256-383, O 384..
+  static constexpr int OS = D == 128 ? 1 : 2;        // accumulators: at head_dim 64 two row tiles have one each
 };
 
 // ------------------------------------------------------------------ what there is to do
 
 // In the workspace, made by the planning kernel: the sequences by descending length (row tiles; longer ones than 1,022 row tiles in any
-// order), each with the number of row-tile pairs of the ones in front of it; those with an odd number of row tiles.
+// order), each with the number of row tiles of the ones in front of it.
 struct Plan {
-  int4* seq;               // [batch] {first token, tokens, pairs of row tiles in front, 0}
-  int* odd;                // [batch] places in seq
-  int* again;              // [2 * tickets]: chains of row tiles that are computed again (2 * ticket + slot, each with the one before it)
-  int* head;               // [4] {pairs of all sequences, odd ones, tickets given out, sequences with tokens}
+  int4* seq;               // [batch] {first token, tokens, row tiles in front, 0}
+  int* again;              // [tickets]: chains of row tiles that are computed again (each with the one before it)
+  int* head;               // [4] {row tiles of all sequences, tickets given out, sequences with tokens, 0}
 };
 
 struct Params {
@@ -139,32 +138,32 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_prompt_plan(const __grid_co
   for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) atomicAdd(&count[bucket(read_sequence(p, b, true).y)], 1);
   __syncthreads();
   int total;
-  const int mine = count[threadIdx.x], first = scan_block(mine, shared, total);
+  const int first = scan_block(count[threadIdx.x], shared, total);
   __syncthreads();
   count[threadIdx.x] = first;
-  if (threadIdx.x == kPlanThreads - 1) p.plan.head[3] = first;
+  if (threadIdx.x == kPlanThreads - 1) p.plan.head[2] = first;
   __syncthreads();
   for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) {
     const int2 q = read_sequence(p, b, false);
     p.plan.seq[atomicAdd(&count[bucket(q.y)], 1)] = make_int4(q.x, q.y, 0, 0);
   }
   __syncthreads();
-  int pairs = 0, odds = 0;
+  int tiles = 0;
   for (int r0 = 0; r0 < p.batch; r0 += kPlanThreads) {
-    const int r = r0 + threadIdx.x, tiles = r < p.batch ? ceil_div(p.plan.seq[r].y, p.tq) : 0;
-    const int at = pairs + scan_block(tiles / 2, shared, total);
+    const int r = r0 + threadIdx.x, mine = r < p.batch ? ceil_div(p.plan.seq[r].y, p.tq) : 0;
+    const int at = tiles + scan_block(mine, shared, total);
     if (r < p.batch) p.plan.seq[r].z = at;
-    pairs += total;
-    const int odd = odds + scan_block(tiles & 1, shared, total);
-    if (tiles & 1) p.plan.odd[odd] = r;
-    odds += total;
+    tiles += total;
   }
-  if (threadIdx.x == 0) p.plan.head[0] = pairs, p.plan.head[1] = odds, p.plan.head[2] = 0;
+  if (threadIdx.x == 0) p.plan.head[0] = tiles, p.plan.head[1] = 0;
 }
 
-// A slot's part of an item: a row tile of a sequence and key head.
-struct Slot {
-  int tiles;               // of keys; 0: nothing
+// A row tile of a sequence and key head.
+struct Item {
+  int end;                 // 1: nothing left; 2: everyone says when all items before this one are done
+  int ticket;
+  int safe;                // maxima of every tile, all of them by one team
+  int tiles;               // of keys
   int masked;              // the first of them that a mask cuts
   int head;                // key head
   int token, n;            // first token, tokens
@@ -173,63 +172,31 @@ struct Slot {
   int len;                 // tokens of the sequence
   long long o;             // the first token and query head in o
 };
-struct Item {
-  int end;                 // 1: nothing left; 2: everyone says when all items before this one are done
-  int ticket;
-  int safe;                // maxima of every tile
-  int tiles;               // the larger of the slots'
-  int shared;              // both slots walk the same K and V tiles
-  Slot slot[2];
-};
 
-__device__ inline Slot make_slot(const Params& p, const int4& q, int head, int tile) {
-  Slot s;
-  const int first = tile * p.tq;
-  s.head = head;
-  s.n = min(p.tq, q.y - first);
-  s.token = q.x + first;
-  s.key = q.x, s.len = q.y;
-  s.keys = p.causal ? first + s.n : q.y;
-  s.sees = p.causal ? first + 1 : q.y;
-  s.tiles = ceil_div(s.keys, kTile);
-  s.masked = s.sees / kTile;
-  s.o = (long long)head * p.group * p.o_stride_h + (long long)s.token * p.o_stride_t;
-  return s;
-}
-
-// Item number `ticket` (a whole warp calls it): pairs of row tiles first, sequence by sequence, the ones with most keys first, all key heads of
-// a place after each other; then the single row tiles, two by two.
-__device__ inline bool make_item(const Params& p, int pairs, int odds, int sequences, int ticket, Item& im, int lane) {
-  const long long wide = (long long)pairs * p.kv_heads, singles = (long long)odds * p.kv_heads;
+// Row tile number `ticket` (a whole warp calls it): sequence by sequence, the ones with most keys first, all key heads of a place after each other.
+__device__ inline void make_item(const Params& p, int sequences, int ticket, Item& im, int lane) {
+  const int u = ticket / p.kv_heads;
   im.end = 0, im.safe = 0, im.ticket = ticket;
-  if (ticket < wide) {
-    const int u = ticket / p.kv_heads, h = ticket - u * p.kv_heads;
-    // the last sequence that begins at u or in front of it: every step cuts the range to a 32nd
-    int lo = 0, hi = sequences;
-    while (hi - lo > 1) {
-      const int step = ceil_div(hi - lo, 32), at = lo + lane * step;
-      const bool in = at < hi && __ldcg(p.plan.seq + at).z <= u;
-      const int last = 31 - __clz(__ballot_sync(0xffffffffu, in));
-      hi = min(hi, lo + (last + 1) * step);
-      lo += last * step;
-    }
-    const int4 q = __ldcg(p.plan.seq + lo);
-    const int tiles = ceil_div(q.y, p.tq), tile = tiles - 2 * (u - q.z) - 2;
-    im.shared = 1;
-    im.slot[0] = make_slot(p, q, h, tile);
-    im.slot[1] = make_slot(p, q, h, tile + 1);
-  } else {
-    const long long i = 2 * (ticket - wide);
-    if (i >= singles) return false;
-    im.shared = 0;
-    im.slot[1].tiles = 0;
-    for (int s = 0; s < 2 && i + s < singles; ++s) {
-      const int u = (int)((i + s) / p.kv_heads), h = (int)(i + s - (long long)u * p.kv_heads);
-      im.slot[s] = make_slot(p, __ldcg(p.plan.seq + __ldcg(p.plan.odd + u)), h, 0);
-    }
+  im.head = ticket - u * p.kv_heads;
+  // the last sequence that begins at u or in front of it: every step cuts the range to a 32nd
+  int lo = 0, hi = sequences;
+  while (hi - lo > 1) {
+    const int step = ceil_div(hi - lo, 32), at = lo + lane * step;
+    const bool in = at < hi && __ldcg(p.plan.seq + at).z <= u;
+    const int last = 31 - __clz(__ballot_sync(0xffffffffu, in));
+    hi = min(hi, lo + (last + 1) * step);
+    lo += last * step;
   }
-  im.tiles = max(im.slot[0].tiles, im.slot[1].tiles);
-  return true;
+  const int4 q = __ldcg(p.plan.seq + lo);
+  const int first = (ceil_div(q.y, p.tq) - 1 - (u - q.z)) * p.tq;
+  im.n = min(p.tq, q.y - first);
+  im.token = q.x + first;
+  im.key = q.x, im.len = q.y;
+  im.keys = p.causal ? first + im.n : q.y;
+  im.sees = p.causal ? first + 1 : q.y;
+  im.tiles = ceil_div(im.keys, kTile);
+  im.masked = im.sees / kTile;
+  im.o = (long long)im.head * p.group * p.o_stride_h + (long long)im.token * p.o_stride_t;
 }
 
 // ------------------------------------------------------------------ kernel
@@ -282,14 +249,17 @@ template <class T> __device__ __forceinline__ bool not_finite2(uint32_t x) {
   return (x & m) == m || (x & m << 16) == m << 16;
 }
 
+constexpr int kBuffers = 3;                          // of S
 enum {
   B_ITEM_FULL = 0, B_ITEM_EMPTY = B_ITEM_FULL + kItems, B_Q_FULL = B_ITEM_EMPTY + kItems, B_Q_EMPTY = B_Q_FULL + 2,
-  B_S_FULL = B_Q_EMPTY + 2, B_P = B_S_FULL + 2, B_O_FULL = B_P + 2 * kParts, B_O_EMPTY = B_O_FULL + 2,
-  B_PV_DONE = B_O_EMPTY + 2, B_PAIR = B_PV_DONE + 2, B_CHECK = B_PAIR + 8, B_FINAL = B_CHECK + 2 * kChecks, B_DONE = B_FINAL + 2, B_K_FULL
+  B_S_FULL = B_Q_EMPTY + 2,                          // twice as many as buffers: a barrier's phases are waited for by one team, in turn
+  B_S_FREE = B_S_FULL + 2 * kBuffers, B_P = B_S_FREE + kBuffers, B_O_EMPTY = B_P + kParts * kBuffers, B_O_FULL = B_O_EMPTY + 2,
+  B_REF = B_O_FULL + 2 * 2, B_PV_DONE = B_REF + kItems, B_PAIR = B_PV_DONE + 2, B_CHECK = B_PAIR + 8, B_FINAL = B_CHECK + 2 * kChecks, B_DONE = B_FINAL + 2,
+  B_K_FULL
 };
 template <int D> constexpr int kBars = B_K_FULL + 2 * (Geo<D>::NKS + Geo<D>::NVS);
 
-// Where P of 16 keys lies among the columns of the slot's S: keys 0-31 at 48, 32-63 at 32, 64 on at 64.  It covers scores that its own threads have
+// Where P of 16 keys lies among the columns of its S: keys 0-31 at 48, 32-63 at 32, 64 on at 64.  It covers scores that its own threads have
 // read (the second half of keys 0-63 first); columns 0-31 keep theirs, which all threads take the reference from.
 __device__ __forceinline__ int p_column(int group) { return group < 4 ? 32 + (group ^ 2) * 8 : 32 + group * 8; }
 
@@ -297,12 +267,13 @@ __device__ __forceinline__ int p_column(int group) { return group < 4 ? 32 + (gr
 template <int D> struct Small {
   unsigned long long bar[kBars<D>];
   Item items[kItems];
-  float pair[2][2][2][kTile];                        // [slot][turn][half][row]: maxima, from a row's one thread to its other
-  float sums[2][2][2][kTile];                        // [slot][turn][half][row] (a warp may be an item ahead of the row's other one)
-  int verdict[2][kChecks];                           // not every value of the slot's masked tile is finite
+  float ref[kItems][kTile];                          // of the rows, from the team of the first tile
+  float sums[kItems][2][2][kTile];                   // [item][team][half][row]
+  float pair[2][2][2][kTile];                        // [team][turn][half][row]: maxima, from a row's one thread to its other
+  int verdict[2][kChecks];                           // not every value of the team's masked tile is finite
   uint32_t tmem;
   int abort;
-  int again, last_again[2];                          // row tiles to be computed again: the last one of the chain; of each slot
+  int again, last_again[2];                          // row tiles to be computed again: the last one of the chain; of each team
 };
 
 // a ring of tiles as one of its users walks it
@@ -402,8 +373,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     tmem_relinquish();
   } else if (warp == 2) {
     for (int i = lane; i < kBars<D>; i += 32) {
-      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps8 = (i >= B_P && i < B_O_FULL) || (i >= B_O_EMPTY && i < B_PV_DONE);
-      mbar_init(BAR(i), item ? kItemReaders : i == B_DONE ? 16 : warps8 ? 8 : i >= B_V_EMPTY || (i >= B_PAIR && i < B_CHECK) ? 2 : 1);
+      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps8 = i >= B_P && i < B_O_FULL;
+      mbar_init(BAR(i), item ? kItemReaders : i == B_DONE ? 16 : warps8 ? 8 : i >= B_REF && i < B_PV_DONE ? 4 : i >= B_PAIR && i < B_CHECK ? 2 : 1);
     }
     if (lane == 0) sm.abort = 0, sm.again = sm.last_again[0] = sm.last_again[1] = -1;
     fence_mbar_init();
@@ -433,43 +404,14 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   };
 
   if (warp >= kLoadWarp) {
+    auto landed = [&](uint32_t bar, uint32_t ph) {   // (no copy is left in flight, also where another warp has given up)
+      const long long t0 = clock64();
+      while (!mbar_try_wait(bar, ph) && clock64() - t0 < p.wait_limit / 4) {}
+    };
     if (warp == kLoadWarp) {
-      // ================================================================ items, Q, K, V
-      Ring<G::NKS> k_ring;
-      Ring<G::NVS> v_ring;
-      uint32_t k_no = 0, v_no = 0, q_it[2] = {0, 0};
-      auto load_tile = [&](const CUtensorMap* tm, const Slot& s, int j, uint32_t smem_at, uint32_t full) {
-        if (lane == 0) {
-          mbar_expect_tx(full, G::TILE_BYTES);
-#pragma unroll
-          for (int i = 0; i < G::SLABS; ++i) tma_load_3d(smem_at + i * G::SLAB_BYTES, tm, i * 64, s.head, s.key + j * kTile, full);
-        }
-        __syncwarp();
-      };
-      auto load_k = [&](const Slot& s, int j) {
-        if (k_no >= (uint32_t)G::NKS && !(ok = warp_wait(ctx, BAR(B_K_EMPTY + k_ring.stage), k_ring.phase ^ 1, 111))) return;
-        if (!(p.drop_tile && blockIdx.x == 0 && k_no == 0)) load_tile(&tmK, s, j, sbase + G::OFF_K + k_ring.stage * G::TILE_BYTES, BAR(B_K_FULL + k_ring.stage));
-        ++k_no, k_ring.next();
-      };
-      auto load_v = [&](const Slot& s, int j) {
-        if (v_no >= (uint32_t)G::NVS && !(ok = warp_wait(ctx, BAR(B_V_EMPTY + v_ring.stage), v_ring.phase ^ 1, 128))) return;
-        load_tile(&tmV, s, j, sbase + G::OFF_V + v_ring.stage * G::TILE_BYTES, BAR(B_V_FULL + v_ring.stage));
-        ++v_no, v_ring.next();
-      };
-      auto load_q = [&](const Slot& s, int x) {
-        if (s.tiles == 0) return;
-        if (q_it[x] && !(ok = warp_wait(ctx, BAR(B_Q_EMPTY + x), (q_it[x] & 1) ^ 1, 112))) return;
-        ++q_it[x];
-        if (lane == 0) {
-          mbar_expect_tx(BAR(B_Q_FULL + x), p.tq * p.group * 128 * G::SLABS);
-#pragma unroll
-          for (int i = 0; i < G::SLABS; ++i)
-            tma_load_3d(sbase + G::OFF_Q + x * G::TILE_BYTES + i * G::SLAB_BYTES, &tmQ, i * 64, s.head * p.group, s.token, BAR(B_Q_FULL + x));
-        }
-        __syncwarp();
-      };
-      waveal::wait_for_previous_kernel();
-      const int pairs = __ldcg(p.plan.head), odds = __ldcg(p.plan.head + 1), sequences = __ldcg(p.plan.head + 3);
+      // ================================================================ items, Q, K
+      Ring<G::NKS> ring;
+      uint32_t k_no = 0, q_no = 0;
       auto publish = [&](const Item& next) {
         const uint32_t at = item_no % kItems;
         if (item_no >= kItems && !(ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + at), (item_no / kItems & 1) ^ 1, 113))) return;
@@ -479,171 +421,173 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         }
         __syncwarp();
         ++item_no;
-        for (int j = 0; ok && j < next.tiles; ++j) {
-          if (j == 0) load_q(next.slot[0], 0);
-          for (int x = 0; ok && x < 2; ++x) {
-            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_k(next.slot[next.shared ? 1 : x], j);
-            if (ok && x == 0 && j == 0) load_q(next.slot[1], 1);
+        if (next.tiles == 0) return;
+        const uint32_t qb = q_no & 1, q_full = BAR(B_Q_FULL + qb);
+        if (q_no >= 2 && !(ok = warp_wait(ctx, BAR(B_Q_EMPTY + qb), (q_no >> 1 & 1) ^ 1, 112))) return;
+        ++q_no;
+        if (lane == 0) {
+          mbar_expect_tx(q_full, p.tq * p.group * 128 * G::SLABS);
+#pragma unroll
+          for (int i = 0; i < G::SLABS; ++i)
+            tma_load_3d(sbase + G::OFF_Q + qb * G::TILE_BYTES + i * G::SLAB_BYTES, &tmQ, i * 64, next.head * p.group, next.token, q_full);
+        }
+        __syncwarp();
+        for (int j = 0; j < next.tiles; ++j) {
+          if (k_no >= (uint32_t)G::NKS && !(ok = warp_wait(ctx, BAR(B_K_EMPTY + ring.stage), ring.phase ^ 1, 111))) return;
+          if (lane == 0 && !(p.drop_tile && blockIdx.x == 0 && k_no == 0)) {
+            mbar_expect_tx(BAR(B_K_FULL + ring.stage), G::TILE_BYTES);
+#pragma unroll
+            for (int i = 0; i < G::SLABS; ++i)
+              tma_load_3d(sbase + G::OFF_K + ring.stage * G::TILE_BYTES + i * G::SLAB_BYTES, &tmK, i * 64, next.head, next.key + j * kTile, BAR(B_K_FULL + ring.stage));
           }
-          for (int x = 0; ok && x < 2; ++x)
-            if (next.shared ? x == 0 : j < next.slot[x].tiles) load_v(next.slot[next.shared ? 1 : x], j);
+          __syncwarp();
+          ++k_no, ring.next();
         }
       };
+      waveal::wait_for_previous_kernel();
+      const long long tickets = (long long)__ldcg(p.plan.head) * p.kv_heads;
+      const int sequences = __ldcg(p.plan.head + 2);
       Item next;
       long long ticket = blockIdx.x;
-      const long long tickets = (long long)pairs * p.kv_heads + ((long long)odds * p.kv_heads + 1) / 2;
       while (ok && ticket < tickets) {
         int asked = 0;
-        if (lane == 0) asked = atomicAdd(p.plan.head + 2, 1);    // (used when this item's tiles have been asked for)
-        make_item(p, pairs, odds, sequences, (int)ticket, next, lane);
+        if (lane == 0) asked = atomicAdd(p.plan.head + 1, 1);    // (used when this item's tiles have been asked for)
+        make_item(p, sequences, (int)ticket, next, lane);
         publish(next);
         ticket = (long long)gridDim.x + __shfl_sync(0xffffffffu, asked, 0);
       }
       // row tiles to be computed again, once everyone has said which
-      next.tiles = next.slot[0].tiles = next.slot[1].tiles = 0, next.shared = 0;
-      next.end = 2;
+      next.end = 2, next.tiles = 0;
       if (ok) publish(next);
       if (ok && (ok = warp_wait(ctx, BAR(B_DONE), 0, 129))) {
         for (int id = *reinterpret_cast<volatile int*>(&sm.again); ok && id >= 0; id = p.plan.again[id]) {
-          make_item(p, pairs, odds, sequences, id / 2, next, lane);
-          next.shared = 0, next.safe = 1;
-          next.tiles = next.slot[id & 1].tiles;
-          next.slot[(id & 1) ^ 1].tiles = 0;
+          make_item(p, sequences, id, next, lane);
+          next.safe = 1;
           publish(next);
         }
         next.end = 1, next.tiles = 0;
         if (ok) publish(next);
       }
-      // leaves no copy in flight, also where another warp has given up: the last one into each stage
-      auto landed = [&](uint32_t bar, uint32_t ph) {
-        const long long t0 = clock64();
-        while (!mbar_try_wait(bar, ph) && clock64() - t0 < p.wait_limit / 4) {}
-      };
       for (uint32_t i = 0; i < (uint32_t)G::NKS && i < k_no; ++i) {
         const uint32_t n = k_no - 1 - i;
         if (!(p.drop_tile && blockIdx.x == 0 && n == 0)) landed(BAR(B_K_FULL + n % G::NKS), n / G::NKS & 1);
       }
-      for (uint32_t i = 0; i < (uint32_t)G::NVS && i < v_no; ++i) landed(BAR(B_V_FULL + (v_no - 1 - i) % G::NVS), (v_no - 1 - i) / G::NVS & 1);
-      for (int x = 0; x < 2; ++x)
-        if (q_it[x]) landed(BAR(B_Q_FULL + x), (q_it[x] & 1) ^ 1);
-    } else if (warp < kCheckWarp) {
+      for (uint32_t i = 0; i < 2 && i < q_no; ++i) landed(BAR(B_Q_FULL + (q_no - 1 - i & 1)), (q_no - 1 - i) >> 1 & 1);
+    } else if (warp <= kProductWarp) {
       // ================================================================ products
-      // Two warps issue, one S = Q K^T, the other O += P V, each for both slots in turn: what they do around the products (waits, ring
-      // positions) is a chain of 250 clk and more for each group of them, and four products (256 clk) are all that the tensor pipe has queued.
-      // (Measured on 512 pairs of row tiles over 32,760 keys, clk a pair and key tile without any softmax: one warp 3,810.  A warp a slot: the slots'
-      // products mix, both come out late, and both softmaxes then run at the same time, with no product beside them.)
+      // Two warps issue, one S = Q K^T, the other O += P V: what they do around the products (waits, ring positions) is a chain of 250 clk
+      // and more for each group of them, and four products (256 clk) are all that the tensor pipe has queued.
       // (operands of the products come from shuffles, so that the compiler knows them to be the same in all lanes)
       constexpr uint32_t kTypeBits = (1u << 7) | (1u << 10), kType = std::is_same_v<T, __half> ? 0u : kTypeBits;
       constexpr uint32_t kQK = (make_idesc(128, 128, false) & ~kTypeBits) | kType, kPV = (make_idesc(128, D, true) & ~kTypeBits) | kType;
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      uint32_t b = 0, g2 = 0;                        // the tile's buffer, its number's last bit
+      uint32_t uses = 0;                             // bits: how often each buffer has been used, modulo 2
       if (warp == kScoreWarp) {
-        const uint64_t q_desc = make_desc(sbase + G::OFF_Q, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_K, 16, 1024);
+        const uint64_t q_desc0 = make_desc(sbase + G::OFF_Q, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_K, 16, 1024);
         Ring<G::NKS> ring;
-        uint32_t items[2] = {0, 0}, done[2] = {0, 0};
+        uint32_t items = 0, used = 0;
         while (ok && next_item()) {
-          const int tiles0 = __shfl_sync(0xffffffffu, im->slot[0].tiles, 0), tiles1 = __shfl_sync(0xffffffffu, im->slot[1].tiles, 0);
-          const int all = __shfl_sync(0xffffffffu, im->tiles, 0), shared = __shfl_sync(0xffffffffu, im->shared, 0);
+          const int tiles = __shfl_sync(0xffffffffu, im->tiles, 0), safe = __shfl_sync(0xffffffffu, im->safe, 0);
           item_done();
-          for (int j = 0; ok && j < all; ++j) {
+          if (tiles == 0) continue;
+          if (!(ok = warp_wait(ctx, BAR(B_Q_FULL + (items & 1)), items >> 1 & 1, 115))) break;
+          const uint64_t qd = q_desc0 + (uint64_t)((items & 1) * (G::TILE_BYTES >> 4));
+          for (int j = 0; j < tiles; ++j) {
+            if (!(ok = warp_wait(ctx, BAR(B_K_FULL + ring.stage), ring.phase, 116))) break;
+            const uint64_t kd = k_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
+            const uint32_t s_col = tm + G::S_COL + b * kTile;
+            // (S lies over an earlier tile's P: its P V is over)
+            if ((used >> b & 1) && !(ok = warp_wait(ctx, BAR(B_S_FREE + b), (uses >> b & 1) ^ 1, 114))) break;
+            used |= 1u << b, uses ^= 1u << b;
+            tc_fence_after();
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int tiles = x ? tiles1 : tiles0;
-              if (!ok || j >= tiles) continue;
-              if (!(ok = warp_wait(ctx, BAR(B_K_FULL + ring.stage), ring.phase, 116))) continue;
-              if (j == 0 && !(ok = warp_wait(ctx, BAR(B_Q_FULL + x), items[x] & 1, 115))) continue;
-              const uint64_t qd = q_desc + (uint64_t)(x * (G::TILE_BYTES >> 4)), kd = k_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
-              // (S lies over the last tile's P: its P V is over)
-              if (done[x] && !(ok = warp_wait(ctx, BAR(B_PV_DONE + x), (done[x] & 1) ^ 1, 114))) continue;
-              ++done[x];
-              tc_fence_after();
-#pragma unroll
-              for (int slab = 0; slab < G::SLABS; ++slab)
-                umma4_ss(tm + G::S_COL + x * kTile, qd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kQK, slab > 0);
-              tc_commit(BAR(B_S_FULL + x));
-              if (!shared || x) {
-                tc_commit(BAR(B_K_EMPTY + ring.stage));
-                ring.next();
-              }
-              if (j == tiles - 1) tc_commit(BAR(B_Q_EMPTY + x));
-            }
+            for (int slab = 0; slab < G::SLABS; ++slab)
+              umma4_ss(s_col, qd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kd + (uint64_t)(slab * G::SLAB_BYTES >> 4), kQK, slab > 0);
+            tc_commit(BAR(B_S_FULL + 2 * b + g2));
+            tc_commit(BAR(B_K_EMPTY + ring.stage));
+            ring.next();
+            b = b == kBuffers - 1 ? 0 : b + 1;
+            if (safe) b = b == kBuffers - 1 ? 0 : b + 1;
+            else g2 ^= 1;
           }
-          items[0] += tiles0 > 0, items[1] += tiles1 > 0;
+          tc_commit(BAR(B_Q_EMPTY + (items & 1)));
+          ++items;
         }
       } else {
         const uint64_t v_desc0 = make_desc(sbase + G::OFF_V, G::SLAB_BYTES, 1024);
         Ring<G::NVS> ring;
-        uint32_t items[2] = {0, 0}, p_no[2] = {0, 0}, checks[2] = {0, 0};
+        uint32_t items = 0, checks[2] = {0, 0};
         while (ok && next_item()) {
-          int tiles[2], keys[2], masked[2];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            tiles[x] = __shfl_sync(0xffffffffu, im->slot[x].tiles, 0);
-            keys[x] = __shfl_sync(0xffffffffu, im->slot[x].keys, 0);
-            masked[x] = __shfl_sync(0xffffffffu, im->safe ? im->slot[x].masked : INT_MAX, 0);
-          }
-          const int all = __shfl_sync(0xffffffffu, im->tiles, 0), shared = __shfl_sync(0xffffffffu, im->shared, 0);
+          const int tiles = __shfl_sync(0xffffffffu, im->tiles, 0), safe = __shfl_sync(0xffffffffu, im->safe, 0);
+          const int keys = __shfl_sync(0xffffffffu, im->keys, 0), masked = __shfl_sync(0xffffffffu, safe ? im->masked : INT_MAX, 0);
           item_done();
-          for (int j = 0; ok && j < all; ++j) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              if (!ok || j >= tiles[x]) continue;
-              if (!(ok = warp_wait(ctx, BAR(B_V_FULL + ring.stage), ring.phase, 117))) continue;
-              if (j == 0 && items[x] && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items[x] & 1) ^ 1, 118))) continue;
-              const uint32_t o_col = tm + G::O_COL + x * kTile, s_col = tm + G::S_COL + x * kTile;
-              const uint64_t vd = v_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
-              int groups = min(kTile / 16, (keys[x] - j * kTile + 15) / 16);   // of 16 keys that some row sees
-              if (j >= masked[x]) {
-                const uint32_t c = checks[x] % kChecks;
-                if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + c), checks[x] / kChecks & 1, 119))) continue;
-                if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&sm.verdict[x][c]), 0)) groups = 0;
-                ++checks[x];
-              }
-              if (!(ok = warp_wait(ctx, BAR(B_P + x * kParts), p_no[x] & 1, 120))) continue;
-              if (groups == 8) {
-                tc_fence_after();
-                umma2_ts(o_col, s_col + 32, vd + 2 * 128, kPV, j > 0);
-                umma2_ts(o_col, s_col + 64, vd + 4 * 128, kPV, 1);
-              }
-              if (!(ok = warp_wait(ctx, BAR(B_P + x * kParts + 1), p_no[x] & 1, 120))) continue;
-              ++p_no[x];
-              tc_fence_after();
-              if (groups == 8) {
-                umma2_ts(o_col, s_col + 48, vd, kPV, 1);
-                umma2_ts(o_col, s_col + 80, vd + 6 * 128, kPV, 1);
-              } else {
-#pragma unroll 1
-                for (int c = 0; c < groups; ++c) umma_bf16_ts(o_col, s_col + p_column(c), vd + (uint64_t)(c * 128), kPV, j > 0 || c > 0);
-              }
-              tc_commit(BAR(B_PV_DONE + x));
-              if (!shared || x) {
-                tc_commit(BAR(B_V_EMPTY + ring.stage));
-                ring.next();
-              }
-              if (j == tiles[x] - 1) tc_commit(BAR(B_O_FULL + x));
+          if (tiles == 0) continue;
+          const uint32_t ob = items % G::OS, o_col = tm + G::O_COL + ob * D;
+          for (int j = 0; j < tiles; ++j) {
+            if (!(ok = warp_wait(ctx, BAR(B_V_FULL + ring.stage), ring.phase, 117))) break;
+            if (j == 0 && items >= G::OS && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + ob), (items / G::OS & 1) ^ 1, 118))) break;
+            const uint32_t s_col = tm + G::S_COL + b * kTile;
+            const uint64_t vd = v_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
+            int groups = min(kTile / 16, (keys - j * kTile + 15) / 16);   // of 16 keys that some row sees
+            if (j >= masked) {
+              const uint32_t c = checks[g2] % kChecks;
+              if (!(ok = warp_wait(ctx, BAR(B_CHECK + g2 * kChecks + c), checks[g2] / kChecks & 1, 119))) break;
+              if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&sm.verdict[g2][c]), 0)) groups = 0;
+              ++checks[g2];
             }
+            if (!(ok = warp_wait(ctx, BAR(B_P + b * kParts), uses >> b & 1, 120))) break;
+            if (groups == 8) {
+              tc_fence_after();
+              umma2_ts(o_col, s_col + 32, vd + 2 * 128, kPV, j > 0);
+              umma2_ts(o_col, s_col + 64, vd + 4 * 128, kPV, 1);
+            }
+            if (!(ok = warp_wait(ctx, BAR(B_P + b * kParts + 1), uses >> b & 1, 120))) break;
+            uses ^= 1u << b;
+            tc_fence_after();
+            if (groups == 8) {
+              umma2_ts(o_col, s_col + 48, vd, kPV, 1);
+              umma2_ts(o_col, s_col + 80, vd + 6 * 128, kPV, 1);
+            } else {
+#pragma unroll 1
+              for (int c = 0; c < groups; ++c) umma_bf16_ts(o_col, s_col + p_column(c), vd + (uint64_t)(c * 128), kPV, j > 0 || c > 0);
+            }
+            tc_commit(BAR(B_S_FREE + b));
+            tc_commit(BAR(B_V_EMPTY + ring.stage));
+            if (safe) tc_commit(BAR(B_PV_DONE + g2));
+            if (j == tiles - 1) tc_commit(BAR(B_O_FULL + 2 * ob + g2));
+            ring.next();
+            b = b == kBuffers - 1 ? 0 : b + 1;
+            if (safe) b = b == kBuffers - 1 ? 0 : b + 1;
+            else g2 ^= 1;
           }
-          items[0] += tiles[0] > 0, items[1] += tiles[1] > 0;
+          ++items;
         }
       }
       // no product is still running when tensor memory is given back
       tc_commit(BAR(B_FINAL + warp - kScoreWarp));
       __syncwarp();
-      const long long t0 = clock64();
-      while (!mbar_try_wait(BAR(B_FINAL + warp - kScoreWarp), 0) && clock64() - t0 < p.wait_limit / 4) {}
+      landed(BAR(B_FINAL + warp - kScoreWarp), 0);
     } else {
-      // ================================================================ values of masked tiles
+      // ================================================================ V
       Ring<G::NVS> ring;
-      uint32_t checks[2] = {0, 0};
+      uint32_t v_no = 0, g2 = 0, checks[2] = {0, 0};
       while (ok && next_item()) {
         const Item it = *im;
         item_done();
-        auto step = [&](int x, int j) {
-          if (!(ok = warp_wait(ctx, BAR(B_V_FULL + ring.stage), ring.phase, 121))) return;
-          const bool cut[2] = {it.safe && (it.shared || x == 0) && j < it.slot[0].tiles && j >= it.slot[0].masked,
-                               it.safe && (it.shared || x == 1) && j < it.slot[1].tiles && j >= it.slot[1].masked};
-          if (cut[0] || cut[1]) {
-            const uint32_t v = sbase + G::OFF_V + ring.stage * G::TILE_BYTES;
-            const int len = it.slot[x].len - j * kTile;     // rows of the tile that are the sequence's
+        for (int j = 0; j < it.tiles; ++j) {
+          const uint32_t full = BAR(B_V_FULL + ring.stage), v = sbase + G::OFF_V + ring.stage * G::TILE_BYTES;
+          if (v_no >= (uint32_t)G::NVS && !(ok = warp_wait(ctx, BAR(B_V_EMPTY + ring.stage), ring.phase ^ 1, 128))) break;
+          if (lane == 0) {
+            mbar_expect_tx(full, G::TILE_BYTES);
+#pragma unroll
+            for (int i = 0; i < G::SLABS; ++i) tma_load_3d(v + i * G::SLAB_BYTES, &tmV, i * 64, it.head, it.key + j * kTile, full);
+          }
+          __syncwarp();
+          ++v_no;
+          if (it.safe && j >= it.masked) {
+            if (!(ok = warp_wait(ctx, full, ring.phase, 121))) break;
+            const int len = it.len - j * kTile;      // rows of the tile that are the sequence's
             bool bad = false;
             if (p.causal) {
               for (int i = lane; i < min(len, kTile) * 8; i += 32) {
@@ -665,83 +609,64 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const int verdict = __any_sync(0xffffffffu, bad);
             __syncwarp();
             if (lane == 0) {
-#pragma unroll
-              for (int s = 0; s < 2; ++s)
-                if (cut[s]) {
-                  sm.verdict[s][checks[s] % kChecks] = verdict;
-                  mbar_arrive(BAR(B_CHECK + s * kChecks + checks[s] % kChecks));
-                }
+              sm.verdict[g2][checks[g2] % kChecks] = verdict;
+              mbar_arrive(BAR(B_CHECK + g2 * kChecks + checks[g2] % kChecks));
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) checks[s] += cut[s];
+            __syncwarp();
+            ++checks[g2];
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(B_V_EMPTY + ring.stage));
           ring.next();
-        };
-        for (int j = 0; ok && j < it.tiles; ++j)
-          for (int x = 0; ok && x < 2; ++x)
-            if (it.shared ? x == 0 : j < it.slot[x].tiles) step(it.shared ? 1 : x, j);
+          if (!it.safe) g2 ^= 1;
+        }
       }
+      for (uint32_t i = 0; i < (uint32_t)G::NVS && i < v_no; ++i) landed(BAR(B_V_FULL + (v_no - 1 - i) % G::NVS), (v_no - 1 - i) / G::NVS & 1);
     }
   } else {
     // ================================================================ softmax, epilogue
-    const int x = warp / 8, half = warp / 4 & 1, quad = warp & 3, r = quad * 32 + lane, tok = r / p.group;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + G::S_COL + x * kTile, h_addr = s_addr + half * 64, o_addr = tmem + lanes + G::O_COL + x * kTile + half * (D / 2);
+    const uint32_t team = warp / 8;
+    const int half = warp / 4 & 1, quad = warp & 3, r = quad * 32 + lane, tok = r / p.group, g = r - tok * p.group;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16, tm = tmem + lanes;
     const float sl2 = p.sl2;
-    const int g = r - tok * p.group;
     T* const o0 = static_cast<T*>(p.o) + g * p.o_stride_h + tok * p.o_stride_t + half * (D / 2);
-    uint32_t s_no = 0, items = 0, checks = 0, pairs = 0, v_at = 0;   // v_at: place in the ring where the item's values begin
+    uint32_t b = 0, g2 = 0;                          // buffer and number (its last bit) of the item's first tile
+    uint32_t s_ph = 0, ends = 0;                     // bits: phases of this team's barriers of the buffers, of the accumulators
+    uint32_t items = 0, pairs = 0, checks = 0, done = 0, v_no = 0;
     // what the row's other thread has
-    auto give = [&](float mine) {
-      sm.pair[x][pairs & 1][half][r] = mine;
+    auto exchange = [&](float mine) {
+      sm.pair[team][pairs & 1][half][r] = mine;
       __syncwarp();
-      if (lane == 0) mbar_arrive(BAR(B_PAIR + x * 4 + quad));
+      if (lane == 0) mbar_arrive(BAR(B_PAIR + team * 4 + quad));
+      ok = warp_wait(ctx, BAR(B_PAIR + team * 4 + quad), pairs & 1, 122);
+      return sm.pair[team][pairs++ & 1][half ^ 1][r];
     };
-    auto take = [&](float& other) {
-      if (!(ok = warp_wait(ctx, BAR(B_PAIR + x * 4 + quad), pairs & 1, 122))) return;
-      other = sm.pair[x][pairs & 1][half ^ 1][r];
-      ++pairs;
-    };
-    // this item's part of the slot; read while the last item's products end
-    Slot s;
-    int all, shared, other, safe, id, said;
-    bool more;
-    auto read_item = [&] {
-      more = next_item();
-      if (!more) return;
-      s = im->slot[x];
-      all = im->tiles, shared = im->shared, other = im->slot[x ^ 1].tiles, safe = im->safe, id = 2 * im->ticket + x, said = im->end == 2;
-      item_done();
-    };
-    read_item();
-    while (ok && more) {
-      // where a tile's values are in the ring (asked for in the rare case that they are added here)
-      const uint32_t begin = v_at;
-      v_at = (begin + (shared ? all : s.tiles + other)) % G::NVS;
-      if (s.tiles == 0) {
-        if (said && lane == 0) mbar_arrive(BAR(B_DONE));
-        read_item();
+    while (ok && next_item()) {
+      const int tiles = im->tiles, safe = im->safe;
+      if (tiles == 0) {
+        if (im->end == 2 && lane == 0) mbar_arrive(BAR(B_DONE));
+        item_done();
         continue;
       }
-      auto v_stage = [&](int j) { return (begin + j + (shared ? 0 : min(j, other) + (x && j < other))) % G::NVS; };
-      const bool live = tok < s.n;
-      const int sees = min(p.causal ? s.sees + tok : s.keys, s.keys) - half * 64;
+      const uint32_t at = item_no % kItems, step = safe ? 2 : 1, last_team = safe ? g2 : (g2 + tiles - 1) & 1;
+      const int keys = im->keys, first_sees = im->sees, masked = im->masked;
+      const bool live = tok < im->n;
+      const int sees = min(p.causal ? first_sees + tok : keys, keys) - half * 64;
       float ref = -INFINITY, sum = 0.f;
       bool over = false;
+      const int j0 = g2 == team ? 0 : safe ? tiles : 1;
+      uint32_t buf = (b + j0 * step) % kBuffers;
 #pragma unroll 1
-      for (int j = 0; j < s.tiles; ++j) {
-        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + x), s_no & 1, 124))) break;
-        ++s_no;
+      for (int j = j0; j < tiles; j += 3 - step) {
+        const uint32_t s_addr = tm + G::S_COL + buf * kTile, h_addr = s_addr + half * 64;
+        if (!(ok = warp_wait(ctx, BAR(B_S_FULL + 2 * buf + team), s_ph >> buf & 1, 124))) break;
+        s_ph ^= 1u << buf;
         tc_fence_after();
-        const bool cut = j >= s.masked;
-        const int chunks = min(2, (s.keys - j * kTile - half * 64 + 31) / 32);   // of this thread's 64 keys (what is behind the last key is not used)
+        const bool cut = j >= masked;
+        const int chunks = cut ? min(2, (keys - j * kTile - half * 64 + 31) / 32) : 2;   // of this thread's 64 keys (what is behind the last key is not used)
         uint32_t u[32], w[16];
         if (cut) {
           // scores that the row does not see, 16 columns at a time from the first that some row does not see.  (Code that runs once or twice an
           // item is short: each 128 bytes of it come from beyond the instruction caches.)
-          const int visible = sees - j * kTile, from = max(0, s.sees - j * kTile - half * 64) / 16 * 16;
+          const int visible = sees - j * kTile, from = max(0, first_sees - j * kTile - half * 64) / 16 * 16;
 #pragma unroll 1
           for (int c = from; c < 32 * chunks; c += 16) {
             uint32_t t[16];
@@ -762,21 +687,19 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             WAVEAL_TMEM_WAIT_LD32(u, 0);
             top = fmaxf(top, row_max32(u));
           }
-          give(top);
-          float top2;
-          take(top2);
+          top = fmaxf(top, exchange(top));
           if (!ok) break;
-          top = fmaxf(top, top2);
           if (j == 0) {
             ref = top;
           } else {
+            if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + team), done++ & 1, 130))) break;   // of the last tile
+            tc_fence_after();
             const bool grown = live && (top - ref) * sl2 > kGrowth;
             if (__any_sync(0xffffffffu, grown)) {
-              // (S of this tile is there, so the last tile's P V is done)
               const float scale = grown ? ex2((ref - top) * sl2) : 1.0f;
               if (grown) ref = top;
               sum *= scale;
-              rescale<D / 2>(o_addr, scale);
+              rescale<D / 2>(tm + G::O_COL + items % G::OS * D + half * (D / 2), scale);
             }
           }
         } else if (j == 0) {
@@ -788,13 +711,21 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           ref = __uint_as_float(t[0]);
 #pragma unroll
           for (int i = 1; i < 16; ++i) ref = fmaxf(ref, i < visible ? __uint_as_float(t[i]) : -INFINITY);
+          if (half == 0) {
+            sm.ref[at][r] = ref;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(B_REF + at));
+          }
+        } else if (j == 1) {
+          if (!(ok = warp_wait(ctx, BAR(B_REF + at), item_no / kItems & 1, 131))) break;
+          ref = sm.ref[at][r];
         }
         const float minus = ref == -INFINITY ? 0.f : -ref * sl2;
         float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
         auto release = [&](int part) {
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(B_P + x * kParts + part));
+          if (lane == 0) mbar_arrive(BAR(B_P + buf * kParts + part));
         };
 #pragma unroll 1
         for (int n = 0; n < chunks; ++n) {
@@ -817,18 +748,16 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         }
         if (chunks <= 0) release(0);
         if (cut && safe) {
-          if (!(ok = warp_wait(ctx, BAR(B_CHECK + x * kChecks + checks % kChecks), checks / kChecks & 1, 125))) break;
-          if (*reinterpret_cast<volatile int*>(&sm.verdict[x][checks % kChecks])) {
+          if (!(ok = warp_wait(ctx, BAR(B_CHECK + team * kChecks + checks % kChecks), checks / kChecks & 1, 125))) break;
+          if (*reinterpret_cast<volatile int*>(&sm.verdict[team][checks % kChecks])) {
             // the row's first thread adds for both, when both have written P
             tc_fence_before();
-            float none;
-            give(0.f);
-            take(none);
+            exchange(0.f);
             if (!ok) break;
             if (half == 0) {
-              if (j == 0 && items && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + x), (items & 1) ^ 1, 127))) break;
+              if (j == 0 && items >= G::OS && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + items % G::OS), (items / G::OS & 1) ^ 1, 127))) break;
               tc_fence_after();
-              add_visible<D, T>(s_addr, o_addr, sbase + G::OFF_V + v_stage(j) * G::TILE_BYTES, sees - j * kTile, j == 0);
+              add_visible<D, T>(s_addr, tm + G::O_COL + items % G::OS * D, sbase + G::OFF_V + (v_no + j) % G::NVS * G::TILE_BYTES, sees - j * kTile, j == 0);
             }
           }
           ++checks;
@@ -836,54 +765,62 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         s0 = (s0 + s1) + (s2 + s3);
         over |= !(s0 < kSumLimit<T>);
         sum += s0;
-        if (j == s.tiles - 1) sm.sums[x][items & 1][half][r] = sum;       // (read once the products of this tile are done)
+        // (read once the products of the last tile are done; infinite where something overflowed)
+        if (j + 3 - (int)step >= tiles) sm.sums[at][team][half][r] = over && !safe ? INFINITY : sum;
         release(1);
+        buf = buf == 0 ? kBuffers - 1 : buf - 1;     // two on
       }
       if (!ok) break;
-      T* const o = o0 + s.o;
-      float* const lse = live && p.lse && half == 0 ? p.lse + (long long)(s.head * p.group + g) * p.tokens + s.token + tok : nullptr;
-      bool bad = over || (ref == -INFINITY && s.tiles > 1);
-      const bool again = live && !safe;
-      const int this_id = id;
-      const uint32_t o_phase = items & 1;
-      read_item();
-      if (!ok || !(ok = warp_wait(ctx, BAR(B_O_FULL + x), o_phase, 123))) break;
-      tc_fence_after();
-      sum += sm.sums[x][items & 1][half ^ 1][r];
-      ++items;
-      const float inv = sum == 0.f ? 0.f : __fdividef(1.0f, sum);
-      float none0 = 0.f, none1 = 0.f;                // zero, NaN where something in O is not finite
+      if (last_team == team) {
+        T* const o = o0 + im->o;
+        float* const lse = live && p.lse && half == 0 ? p.lse + (long long)(im->head * p.group + g) * p.tokens + im->token + tok : nullptr;
+        const int ticket = im->ticket;
+        const uint32_t ob = items % G::OS, o_addr = tm + G::O_COL + ob * D + half * (D / 2);
+        if (!(ok = warp_wait(ctx, BAR(B_O_FULL + 2 * ob + team), ends >> ob & 1, 123))) break;
+        ends ^= 1u << ob;
+        tc_fence_after();
+        sum += sm.sums[at][team][half ^ 1][r];
+        if (!safe && tiles > 1) sum += sm.sums[at][team ^ 1][0][r] + sm.sums[at][team ^ 1][1][r];
+        const float inv = sum == 0.f ? 0.f : __fdividef(1.0f, sum);
+        float none0 = 0.f, none1 = 0.f;              // zero, NaN where something in O is not finite
 #pragma unroll 1
-      for (int c = 0; c < D / 2; c += 16) {
-        uint32_t u[16], w[8];
-        WAVEAL_TMEM_LD16(o_addr + c, u, 0);
-        WAVEAL_TMEM_WAIT_LD16(u, 0);
+        for (int c = 0; c < D / 2; c += 16) {
+          uint32_t u[16], w[8];
+          WAVEAL_TMEM_LD16(o_addr + c, u, 0);
+          WAVEAL_TMEM_WAIT_LD16(u, 0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float a, b;
-          ffma2(none0, none1, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), 0.f, 0.f, none0, none1);
-          ffma2(a, b, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), inv, inv, 0.f, 0.f);
-          w[i] = sum == 0.f ? 0u : pack2<T>(a, b);   // (O may be 0 times something)
-        }
-        // (a warp's rows lie far apart: every store is 32 lines to the memory pipe, so the fewer the better)
-        if (live) {
-          if (p.wide_o) {
-            st_global_v8(o + c, w);
-          } else {
-            *reinterpret_cast<uint4*>(o + c) = make_uint4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint4*>(o + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+          for (int i = 0; i < 8; ++i) {
+            float x, y;
+            ffma2(none0, none1, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), 0.f, 0.f, none0, none1);
+            ffma2(x, y, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), inv, inv, 0.f, 0.f);
+            w[i] = sum == 0.f ? 0u : pack2<T>(x, y);   // (O may be 0 times something)
+          }
+          // (a warp's rows lie far apart: every store is 32 lines to the memory pipe, so the fewer the better)
+          if (live) {
+            if (p.wide_o) {
+              st_global_v8(o + c, w);
+            } else {
+              *reinterpret_cast<uint4*>(o + c) = make_uint4(w[0], w[1], w[2], w[3]);
+              *reinterpret_cast<uint4*>(o + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+            }
           }
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + ob));
+        if (lse) *lse = sum == 0.f ? -INFINITY : (ref * sl2 + __log2f(sum)) * 0.69314718055994531f;
+        // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
+        const bool bad = over || !(sum < INFINITY) || (ref == -INFINITY && tiles > 1) || !(none0 + none1 == 0.f);
+        // (the team's eight warps are never more than an item apart)
+        if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.last_again[team], ticket) != ticket)
+          p.plan.again[ticket] = atomicExch(&sm.again, ticket);
+        __syncwarp();
       }
-      if (lse) *lse = sum == 0.f ? -INFINITY : (ref * sl2 + __log2f(sum)) * 0.69314718055994531f;
-      // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
-      bad |= !(none0 + none1 == 0.f);
-      tc_fence_before();
-      // (the slot's eight warps are never more than an item apart)
-      if (__any_sync(0xffffffffu, bad && again) && lane == 0 && atomicExch(&sm.last_again[x], this_id) != this_id)
-        p.plan.again[this_id] = atomicExch(&sm.again, this_id);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + x));
+      item_done();
+      b = (b + tiles * step) % kBuffers;
+      if (!safe) g2 = (g2 + tiles) & 1;
+      v_no += tiles;
+      ++items;
     }
   }
 
@@ -910,20 +847,19 @@ waveal_status make_map(CUtensorMap* tm, const waveal_prompt_desc* d, const void*
   return WAVEAL_OK;
 }
 
-// tickets that there can be: pairs of row tiles and single ones, two by two, of every key head
+// row tiles of all key heads that there can be
 long long most_tickets(const waveal_prompt_desc* d) {
   const long long tq = kTile / (d->q_heads / d->kv_heads);
-  return (d->tokens / (2 * tq) + d->batch) * d->kv_heads + 1;
+  return (d->tokens / tq + d->batch) * d->kv_heads;
 }
 
-struct Layout { size_t seq, odd, again, bytes; };
+struct Layout { size_t seq, again, bytes; };
 Layout layout(const waveal_prompt_desc* d) {
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   Layout l;
   l.seq = 256;
-  l.odd = l.seq + up((size_t)d->batch * sizeof(int4));
-  l.again = l.odd + up((size_t)d->batch * sizeof(int));
-  l.bytes = l.again + up((size_t)most_tickets(d) * 2 * sizeof(int));
+  l.again = l.seq + up((size_t)d->batch * sizeof(int4));
+  l.bytes = l.again + up((size_t)most_tickets(d) * sizeof(int));
   return l;
 }
 
@@ -994,7 +930,6 @@ extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const v
   char* w = static_cast<char*>(ws);
   p.plan.head = reinterpret_cast<int*>(w);
   p.plan.seq = reinterpret_cast<int4*>(w + l.seq);
-  p.plan.odd = reinterpret_cast<int*>(w + l.odd);
   p.plan.again = reinterpret_cast<int*>(w + l.again);
   p.seq_start = seq_start, p.seq_len = seq_len;
   p.o = o, p.lse = lse, p.o_stride_h = d->o_stride[0], p.o_stride_t = d->o_stride[1];
