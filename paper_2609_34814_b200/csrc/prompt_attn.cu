@@ -554,7 +554,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             }
             tc_commit(BAR(B_S_FREE + b));
             tc_commit(BAR(B_V_EMPTY + ring.stage));
-            if (safe) tc_commit(BAR(B_PV_DONE + g2));
+            if (safe && j < tiles - 1) tc_commit(BAR(B_PV_DONE + g2));   // (waited for in front of the next tile)
             if (j == tiles - 1) tc_commit(BAR(B_O_FULL + 2 * ob + g2));
             ring.next();
             b = b == kBuffers - 1 ? 0 : b + 1;

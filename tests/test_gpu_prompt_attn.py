@@ -149,6 +149,15 @@ def test_scores_that_grow(dtype):
     check(q, k, v, [0, 700, 1500], causal=False, scale=0.3)
 
 
+@pytest.mark.parametrize("dtype, dim", [(BF, 128), (HF, 64)])
+def test_every_row_tile_is_computed_again(dtype, dim):
+    """Scores that rise by hundreds of bits along the sequence: several row tiles of every thread block overflow."""
+    q, k, v = tensors(3500, 32, 4, dim, dtype, seed=13, q_scale=0.1)
+    q[..., 0], k[..., 0] = 8.0, (torch.arange(3500, device="cuda") / 5.0).to(dtype)
+    check(q, k, v, [0, 1700, 3500], scale=0.125)
+    check(q, k, v, [0, 1700, 3500], causal=False, scale=0.125)
+
+
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("dim, heads, kv_heads", [(128, 2, 2), (64, 2, 2), (128, 16, 2)])
 def test_values_that_a_token_does_not_see(what, dim, heads, kv_heads):
