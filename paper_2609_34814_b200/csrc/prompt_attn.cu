@@ -12,7 +12,7 @@
 // results on their way out) runs beside the next one's first tiles.
 //
 // Warps: 0-7 and 8-15 the teams (two threads a row, 64 keys of a tile each: a warp by itself issues an instruction in four clocks, so
-// that four of them a scheduler are needed), 16 items, Q and K, 17 and 18 products, 19 V.
+// that four of them a scheduler are needed), 16 items, Q and K, 17 and 18 products, 19 V, 20-23 results.
 //
 // Values that a token must not see: their probabilities are zero, but zero times NaN is not.  A row tile whose results are not finite is computed
 // again: then warp 19 writes zeros over what lies behind a sequence's end and looks through the values of tiles that the causal mask cuts; where one is
@@ -31,11 +31,11 @@ namespace {
 
 using namespace waveal::sm100;
 
-constexpr int kThreads = 640;
-constexpr int kLoadWarp = 16, kScoreWarp = 17, kProductWarp = 18;
+constexpr int kThreads = 768;
+constexpr int kLoadWarp = 16, kScoreWarp = 17, kProductWarp = 18, kValueWarp = 19;
 constexpr int kTile = 128;                           // keys of a tile, rows of a row tile
 constexpr int kItems = 4;                            // row tiles under way: their descriptions, references and sums
-constexpr int kItemReaders = 19;                     // two issuers, the V loader, sixteen softmax warps
+constexpr int kItemReaders = 23;                     // two issuers, the V loader, sixteen softmax warps, four for the results
 constexpr int kParts = 2;                            // of a tile: P goes to the products 32 keys of each half at a time
 constexpr int kChecks = 8;                           // masked tiles whose verdicts are under way (more than the ring has V tiles)
 constexpr long long kTimeoutCycles = 4000000000ll;   // ~2 s at boost clock
@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_prompt_plan(const __grid_co
   __syncthreads();
   // bucket 0: the longest; the last one: no tokens
   auto bucket = [&](int n) { return kPlanThreads - 1 - min(ceil_div(n, p.tq), kPlanThreads - 1); };
+#pragma unroll 1
   for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) atomicAdd(&count[bucket(read_sequence(p, b, true).y)], 1);
   __syncthreads();
   int total;
@@ -143,12 +144,14 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_prompt_plan(const __grid_co
   count[threadIdx.x] = first;
   if (threadIdx.x == kPlanThreads - 1) p.plan.head[2] = first;
   __syncthreads();
+#pragma unroll 1
   for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) {
     const int2 q = read_sequence(p, b, false);
     p.plan.seq[atomicAdd(&count[bucket(q.y)], 1)] = make_int4(q.x, q.y, 0, 0);
   }
   __syncthreads();
   int tiles = 0;
+#pragma unroll 1
   for (int r0 = 0; r0 < p.batch; r0 += kPlanThreads) {
     const int r = r0 + threadIdx.x, mine = r < p.batch ? ceil_div(p.plan.seq[r].y, p.tq) : 0;
     const int at = tiles + scan_block(mine, shared, total);
@@ -164,6 +167,7 @@ struct Item {
   int ticket;
   int safe;                // maxima of every tile, all of them by one team
   int tiles;               // of keys
+  int teams;               // bits: who has any of them
   int masked;              // the first of them that a mask cuts
   int head;                // key head
   int token, n;            // first token, tokens
@@ -180,6 +184,7 @@ __device__ inline void make_item(const Params& p, int sequences, int ticket, Ite
   im.head = ticket - u * p.kv_heads;
   // the last sequence that begins at u or in front of it: every step cuts the range to a 32nd
   int lo = 0, hi = sequences;
+#pragma unroll 1
   while (hi - lo > 1) {
     const int step = ceil_div(hi - lo, 32), at = lo + lane * step;
     const bool in = at < hi && __ldcg(p.plan.seq + at).z <= u;
@@ -223,7 +228,8 @@ __device__ __noinline__ bool wait_slow(const Ctx& c, uint32_t bar, uint32_t pari
   }
 }
 __device__ __forceinline__ bool warp_wait(const Ctx& c, uint32_t bar, uint32_t parity, int site) {
-  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) || wait_slow(c, bar, parity, site));
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, wait_slow(c, bar, parity, site));
 }
 
 // Two numbers in the tensors' type: the results, and the probabilities, because one product of 16-bit types takes both operands in the
@@ -254,7 +260,7 @@ enum {
   B_ITEM_FULL = 0, B_ITEM_EMPTY = B_ITEM_FULL + kItems, B_Q_FULL = B_ITEM_EMPTY + kItems, B_Q_EMPTY = B_Q_FULL + 2,
   B_S_FULL = B_Q_EMPTY + 2,                          // twice as many as buffers: a barrier's phases are waited for by one team, in turn
   B_S_FREE = B_S_FULL + 2 * kBuffers, B_P = B_S_FREE + kBuffers, B_O_EMPTY = B_P + kParts * kBuffers, B_O_FULL = B_O_EMPTY + 2,
-  B_REF = B_O_FULL + 2 * 2, B_PV_DONE = B_REF + kItems, B_PAIR = B_PV_DONE + 2, B_CHECK = B_PAIR + 8, B_FINAL = B_CHECK + 2 * kChecks, B_DONE = B_FINAL + 2,
+  B_REF = B_O_FULL + 2, B_PV_DONE = B_REF + kItems, B_PAIR = B_PV_DONE + 2, B_CHECK = B_PAIR + 8, B_FINAL = B_CHECK + 2 * kChecks, B_DONE = B_FINAL + 2,
   B_K_FULL
 };
 template <int D> constexpr int kBars = B_K_FULL + 2 * (Geo<D>::NKS + Geo<D>::NVS);
@@ -273,7 +279,7 @@ template <int D> struct Small {
   int verdict[2][kChecks];                           // not every value of the team's masked tile is finite
   uint32_t tmem;
   int abort;
-  int again, last_again[2];                          // row tiles to be computed again: the last one of the chain; of each team
+  int again, last_again;                             // row tiles to be computed again: the last one of the chain (of a warp)
 };
 
 // a ring of tiles as one of its users walks it
@@ -372,11 +378,12 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     tmem_alloc(smem_u32(&sm.tmem), 512);
     tmem_relinquish();
   } else if (warp == 2) {
+#pragma unroll 1
     for (int i = lane; i < kBars<D>; i += 32) {
-      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps8 = i >= B_P && i < B_O_FULL;
-      mbar_init(BAR(i), item ? kItemReaders : i == B_DONE ? 16 : warps8 ? 8 : i >= B_REF && i < B_PV_DONE ? 4 : i >= B_PAIR && i < B_CHECK ? 2 : 1);
+      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps8 = i >= B_P && i < B_O_EMPTY;
+      mbar_init(BAR(i), item ? kItemReaders : i == B_DONE ? 20 : warps8 ? 8 : (i >= B_REF && i < B_PV_DONE) || (i >= B_O_EMPTY && i < B_O_FULL) ? 4 : i >= B_PAIR && i < B_CHECK ? 2 : 1);
     }
-    if (lane == 0) sm.abort = 0, sm.again = sm.last_again[0] = sm.last_again[1] = -1;
+    if (lane == 0) sm.abort = 0, sm.again = sm.last_again = -1;
     fence_mbar_init();
   } else if (warp == 3 && lane == 0) {
     prefetch_tmap(&tmQ), prefetch_tmap(&tmK), prefetch_tmap(&tmV);
@@ -406,34 +413,57 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (warp >= kLoadWarp) {
     auto landed = [&](uint32_t bar, uint32_t ph) {   // (no copy is left in flight, also where another warp has given up)
       const long long t0 = clock64();
+#pragma unroll 1
       while (!mbar_try_wait(bar, ph) && clock64() - t0 < p.wait_limit / 4) {}
     };
     if (warp == kLoadWarp) {
       // ================================================================ items, Q, K
       Ring<G::NKS> ring;
       uint32_t k_no = 0, q_no = 0;
-      auto publish = [&](const Item& next) {
+      waveal::wait_for_previous_kernel();
+      const long long tickets = (long long)__ldcg(p.plan.head) * p.kv_heads;
+      const int sequences = __ldcg(p.plan.head + 2);
+      // first every row tile, then a word to say that these were all, then those that are to be computed again, then the end
+      int id = blockIdx.x < tickets ? (int)blockIdx.x : -1;
+      bool again = false;
+      uint32_t g2 = 0;                               // team of the next tile
+      Item next;
+      next.tiles = 0, next.end = 0;
+#pragma unroll 1
+      while (ok && next.end != 1) {
+        int asked = 0;
+        if (id >= 0) {
+          if (lane == 0 && !again) asked = atomicAdd(p.plan.head + 1, 1);   // (used when this item's tiles have been asked for)
+          make_item(p, sequences, id, next, lane);
+          next.safe = again;
+          next.teams = next.tiles > 1 && !again ? 3 : 1 << g2;
+          if (!again) g2 = (g2 + next.tiles) & 1;
+        } else {
+          next.end = again ? 1 : 2, next.tiles = 0;
+        }
         const uint32_t at = item_no % kItems;
-        if (item_no >= kItems && !(ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + at), (item_no / kItems & 1) ^ 1, 113))) return;
+        if (item_no >= kItems && !(ok = warp_wait(ctx, BAR(B_ITEM_EMPTY + at), (item_no / kItems & 1) ^ 1, 113))) break;
         if (lane == 0) {
           sm.items[at] = next;
           mbar_arrive(BAR(B_ITEM_FULL + at));
         }
         __syncwarp();
         ++item_no;
-        if (next.tiles == 0) return;
-        const uint32_t qb = q_no & 1, q_full = BAR(B_Q_FULL + qb);
-        if (q_no >= 2 && !(ok = warp_wait(ctx, BAR(B_Q_EMPTY + qb), (q_no >> 1 & 1) ^ 1, 112))) return;
-        ++q_no;
-        if (lane == 0) {
-          mbar_expect_tx(q_full, p.tq * p.group * 128 * G::SLABS);
+        if (next.tiles) {
+          const uint32_t qb = q_no % 2, q_full = BAR(B_Q_FULL + qb);
+          if (q_no >= 2 && !(ok = warp_wait(ctx, BAR(B_Q_EMPTY + qb), (q_no / 2 & 1) ^ 1, 112))) break;
+          ++q_no;
+          if (lane == 0) {
+            mbar_expect_tx(q_full, p.tq * p.group * 128 * G::SLABS);
 #pragma unroll
-          for (int i = 0; i < G::SLABS; ++i)
-            tma_load_3d(sbase + G::OFF_Q + qb * G::TILE_BYTES + i * G::SLAB_BYTES, &tmQ, i * 64, next.head * p.group, next.token, q_full);
+            for (int i = 0; i < G::SLABS; ++i)
+              tma_load_3d(sbase + G::OFF_Q + qb * G::TILE_BYTES + i * G::SLAB_BYTES, &tmQ, i * 64, next.head * p.group, next.token, q_full);
+          }
+          __syncwarp();
         }
-        __syncwarp();
+#pragma unroll 1
         for (int j = 0; j < next.tiles; ++j) {
-          if (k_no >= (uint32_t)G::NKS && !(ok = warp_wait(ctx, BAR(B_K_EMPTY + ring.stage), ring.phase ^ 1, 111))) return;
+          if (k_no >= (uint32_t)G::NKS && !(ok = warp_wait(ctx, BAR(B_K_EMPTY + ring.stage), ring.phase ^ 1, 111))) break;
           if (lane == 0 && !(p.drop_tile && blockIdx.x == 0 && k_no == 0)) {
             mbar_expect_tx(BAR(B_K_FULL + ring.stage), G::TILE_BYTES);
 #pragma unroll
@@ -443,35 +473,21 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           __syncwarp();
           ++k_no, ring.next();
         }
-      };
-      waveal::wait_for_previous_kernel();
-      const long long tickets = (long long)__ldcg(p.plan.head) * p.kv_heads;
-      const int sequences = __ldcg(p.plan.head + 2);
-      Item next;
-      long long ticket = blockIdx.x;
-      while (ok && ticket < tickets) {
-        int asked = 0;
-        if (lane == 0) asked = atomicAdd(p.plan.head + 1, 1);    // (used when this item's tiles have been asked for)
-        make_item(p, sequences, (int)ticket, next, lane);
-        publish(next);
-        ticket = (long long)gridDim.x + __shfl_sync(0xffffffffu, asked, 0);
-      }
-      // row tiles to be computed again, once everyone has said which
-      next.end = 2, next.tiles = 0;
-      if (ok) publish(next);
-      if (ok && (ok = warp_wait(ctx, BAR(B_DONE), 0, 129))) {
-        for (int id = *reinterpret_cast<volatile int*>(&sm.again); ok && id >= 0; id = p.plan.again[id]) {
-          make_item(p, sequences, id, next, lane);
-          next.safe = 1;
-          publish(next);
+        if (next.end == 2) {
+          if (!(ok = warp_wait(ctx, BAR(B_DONE), 0, 129))) break;
+          again = true;
+          id = *reinterpret_cast<volatile int*>(&sm.again);
+        } else if (id >= 0) {
+          const long long ticket = (long long)gridDim.x + __shfl_sync(0xffffffffu, asked, 0);
+          id = again ? p.plan.again[id] : ticket < tickets ? (int)ticket : -1;
         }
-        next.end = 1, next.tiles = 0;
-        if (ok) publish(next);
       }
+#pragma unroll 1
       for (uint32_t i = 0; i < (uint32_t)G::NKS && i < k_no; ++i) {
         const uint32_t n = k_no - 1 - i;
         if (!(p.drop_tile && blockIdx.x == 0 && n == 0)) landed(BAR(B_K_FULL + n % G::NKS), n / G::NKS & 1);
       }
+#pragma unroll 1
       for (uint32_t i = 0; i < 2 && i < q_no; ++i) landed(BAR(B_Q_FULL + (q_no - 1 - i & 1)), (q_no - 1 - i) >> 1 & 1);
     } else if (warp <= kProductWarp) {
       // ================================================================ products
@@ -487,12 +503,14 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const uint64_t q_desc0 = make_desc(sbase + G::OFF_Q, 16, 1024), k_desc0 = make_desc(sbase + G::OFF_K, 16, 1024);
         Ring<G::NKS> ring;
         uint32_t items = 0, used = 0;
+#pragma unroll 1
         while (ok && next_item()) {
           const int tiles = __shfl_sync(0xffffffffu, im->tiles, 0), safe = __shfl_sync(0xffffffffu, im->safe, 0);
           item_done();
           if (tiles == 0) continue;
           if (!(ok = warp_wait(ctx, BAR(B_Q_FULL + (items & 1)), items >> 1 & 1, 115))) break;
           const uint64_t qd = q_desc0 + (uint64_t)((items & 1) * (G::TILE_BYTES >> 4));
+#pragma unroll 1
           for (int j = 0; j < tiles; ++j) {
             if (!(ok = warp_wait(ctx, BAR(B_K_FULL + ring.stage), ring.phase, 116))) break;
             const uint64_t kd = k_desc0 + (uint64_t)(ring.stage * (G::TILE_BYTES >> 4));
@@ -518,12 +536,14 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const uint64_t v_desc0 = make_desc(sbase + G::OFF_V, G::SLAB_BYTES, 1024);
         Ring<G::NVS> ring;
         uint32_t items = 0, checks[2] = {0, 0};
+#pragma unroll 1
         while (ok && next_item()) {
           const int tiles = __shfl_sync(0xffffffffu, im->tiles, 0), safe = __shfl_sync(0xffffffffu, im->safe, 0);
           const int keys = __shfl_sync(0xffffffffu, im->keys, 0), masked = __shfl_sync(0xffffffffu, safe ? im->masked : INT_MAX, 0);
           item_done();
           if (tiles == 0) continue;
           const uint32_t ob = items % G::OS, o_col = tm + G::O_COL + ob * D;
+#pragma unroll 1
           for (int j = 0; j < tiles; ++j) {
             if (!(ok = warp_wait(ctx, BAR(B_V_FULL + ring.stage), ring.phase, 117))) break;
             if (j == 0 && items >= G::OS && !(ok = warp_wait(ctx, BAR(B_O_EMPTY + ob), (items / G::OS & 1) ^ 1, 118))) break;
@@ -555,7 +575,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             tc_commit(BAR(B_S_FREE + b));
             tc_commit(BAR(B_V_EMPTY + ring.stage));
             if (safe && j < tiles - 1) tc_commit(BAR(B_PV_DONE + g2));   // (waited for in front of the next tile)
-            if (j == tiles - 1) tc_commit(BAR(B_O_FULL + 2 * ob + g2));
+            if (j == tiles - 1) tc_commit(BAR(B_O_FULL + ob));
             ring.next();
             b = b == kBuffers - 1 ? 0 : b + 1;
             if (safe) b = b == kBuffers - 1 ? 0 : b + 1;
@@ -568,13 +588,15 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       tc_commit(BAR(B_FINAL + warp - kScoreWarp));
       __syncwarp();
       landed(BAR(B_FINAL + warp - kScoreWarp), 0);
-    } else {
+    } else if (warp == kValueWarp) {
       // ================================================================ V
       Ring<G::NVS> ring;
       uint32_t v_no = 0, g2 = 0, checks[2] = {0, 0};
+#pragma unroll 1
       while (ok && next_item()) {
         const Item it = *im;
         item_done();
+#pragma unroll 1
         for (int j = 0; j < it.tiles; ++j) {
           const uint32_t full = BAR(B_V_FULL + ring.stage), v = sbase + G::OFF_V + ring.stage * G::TILE_BYTES;
           if (v_no >= (uint32_t)G::NVS && !(ok = warp_wait(ctx, BAR(B_V_EMPTY + ring.stage), ring.phase ^ 1, 128))) break;
@@ -590,6 +612,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const int len = it.len - j * kTile;      // rows of the tile that are the sequence's
             bool bad = false;
             if (p.causal) {
+#pragma unroll 1
               for (int i = lane; i < min(len, kTile) * 8; i += 32) {
 #pragma unroll
                 for (int slab = 0; slab < G::SLABS; ++slab) {
@@ -603,6 +626,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             if (len < kTile) {
 #pragma unroll
               for (int slab = 0; slab < G::SLABS; ++slab)
+#pragma unroll 1
                 for (int i = len * 8 + lane; i < kTile * 8; i += 32) st_shared_v4(v + slab * G::SLAB_BYTES + i * 16, 0, 0, 0, 0);
               fence_proxy_async();
             }
@@ -619,17 +643,81 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           if (!it.safe) g2 ^= 1;
         }
       }
+#pragma unroll 1
       for (uint32_t i = 0; i < (uint32_t)G::NVS && i < v_no; ++i) landed(BAR(B_V_FULL + (v_no - 1 - i) % G::NVS), (v_no - 1 - i) / G::NVS & 1);
+    } else {
+      // ================================================================ results: a thread a row
+      const int quad = warp & 3, r = quad * 32 + lane, tok = r / p.group, g = r - tok * p.group;
+      T* const o0 = static_cast<T*>(p.o) + g * p.o_stride_h + tok * p.o_stride_t;
+      uint32_t items = 0;
+#pragma unroll 1
+      while (ok && next_item()) {
+        const int tiles = im->tiles, safe = im->safe, ticket = im->ticket;
+        if (tiles == 0) {
+          if (im->end == 2 && lane == 0) mbar_arrive(BAR(B_DONE));
+          item_done();
+          continue;
+        }
+        const uint32_t at = item_no % kItems, ob = items % G::OS, o_addr = tmem + ((uint32_t)(quad * 32) << 16) + G::O_COL + ob * D;
+        const bool live = tok < im->n;
+        T* const o = o0 + im->o;
+        float* const lse = live && p.lse ? p.lse + (long long)(im->head * p.group + g) * p.tokens + im->token + tok : nullptr;
+        if (!(ok = warp_wait(ctx, BAR(B_O_FULL + ob), items / G::OS & 1, 123))) break;
+        ++items;
+        tc_fence_after();
+        // (of each team and half; safe: one team alone, by the number of the items' tiles in front; one tile: its team alone)
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (im->teams >> i & 1) sum += sm.sums[at][i][0][r] + sm.sums[at][i][1][r];
+        const float ref = sm.ref[at][r], inv = sum == 0.f ? 0.f : __fdividef(1.0f, sum);
+        float none0 = 0.f, none1 = 0.f;              // zero, NaN where something in O is not finite
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t u[32], w[16];
+          WAVEAL_TMEM_LD32(o_addr + c, u, 0);
+          WAVEAL_TMEM_WAIT_LD32(u, 0);
+          if (c == D - 32) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + ob));
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float x, y;
+            ffma2(none0, none1, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), 0.f, 0.f, none0, none1);
+            ffma2(x, y, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), inv, inv, 0.f, 0.f);
+            w[i] = sum == 0.f ? 0u : pack2<T>(x, y);   // (O may be 0 times something)
+          }
+          // (a warp's rows lie far apart: every store is 32 lines to the memory pipe, so the fewer the better)
+          if (live) {
+            if (p.wide_o) {
+              st_global_v8(o + c, w);
+              st_global_v8(o + c + 16, w + 8);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(o + c + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+            }
+          }
+        }
+        if (lse) *lse = sum == 0.f ? -INFINITY : (ref * p.sl2 + __log2f(sum)) * 0.69314718055994531f;
+        // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
+        const bool bad = !(sum < INFINITY) || (ref == -INFINITY && tiles > 1) || !(none0 + none1 == 0.f);
+        // (the four warps are never more than an item apart)
+        if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.last_again, ticket) != ticket)
+          p.plan.again[ticket] = atomicExch(&sm.again, ticket);
+        __syncwarp();
+        item_done();
+      }
     }
   } else {
-    // ================================================================ softmax, epilogue
+    // ================================================================ softmax
     const uint32_t team = warp / 8;
-    const int half = warp / 4 & 1, quad = warp & 3, r = quad * 32 + lane, tok = r / p.group, g = r - tok * p.group;
+    const int half = warp / 4 & 1, quad = warp & 3, r = quad * 32 + lane, tok = r / p.group;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16, tm = tmem + lanes;
     const float sl2 = p.sl2;
-    T* const o0 = static_cast<T*>(p.o) + g * p.o_stride_h + tok * p.o_stride_t + half * (D / 2);
     uint32_t b = 0, g2 = 0;                          // buffer and number (its last bit) of the item's first tile
-    uint32_t s_ph = 0, ends = 0;                     // bits: phases of this team's barriers of the buffers, of the accumulators
+    uint32_t s_ph = 0;                               // bits: phases of this team's barriers of the buffers
     uint32_t items = 0, pairs = 0, checks = 0, done = 0, v_no = 0;
     // what the row's other thread has
     auto exchange = [&](float mine) {
@@ -639,6 +727,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       ok = warp_wait(ctx, BAR(B_PAIR + team * 4 + quad), pairs & 1, 122);
       return sm.pair[team][pairs++ & 1][half ^ 1][r];
     };
+#pragma unroll 1
     while (ok && next_item()) {
       const int tiles = im->tiles, safe = im->safe;
       if (tiles == 0) {
@@ -646,7 +735,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         item_done();
         continue;
       }
-      const uint32_t at = item_no % kItems, step = safe ? 2 : 1, last_team = safe ? g2 : (g2 + tiles - 1) & 1;
+      const uint32_t at = item_no % kItems, step = safe ? 2 : 1;
       const int keys = im->keys, first_sees = im->sees, masked = im->masked;
       const bool live = tok < im->n;
       const int sees = min(p.causal ? first_sees + tok : keys, keys) - half * 64;
@@ -767,55 +856,11 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         sum += s0;
         // (read once the products of the last tile are done; infinite where something overflowed)
         if (j + 3 - (int)step >= tiles) sm.sums[at][team][half][r] = over && !safe ? INFINITY : sum;
+        if (safe && j == tiles - 1 && half == 0) sm.ref[at][r] = ref;
         release(1);
         buf = buf == 0 ? kBuffers - 1 : buf - 1;     // two on
       }
       if (!ok) break;
-      if (last_team == team) {
-        T* const o = o0 + im->o;
-        float* const lse = live && p.lse && half == 0 ? p.lse + (long long)(im->head * p.group + g) * p.tokens + im->token + tok : nullptr;
-        const int ticket = im->ticket;
-        const uint32_t ob = items % G::OS, o_addr = tm + G::O_COL + ob * D + half * (D / 2);
-        if (!(ok = warp_wait(ctx, BAR(B_O_FULL + 2 * ob + team), ends >> ob & 1, 123))) break;
-        ends ^= 1u << ob;
-        tc_fence_after();
-        sum += sm.sums[at][team][half ^ 1][r];
-        if (!safe && tiles > 1) sum += sm.sums[at][team ^ 1][0][r] + sm.sums[at][team ^ 1][1][r];
-        const float inv = sum == 0.f ? 0.f : __fdividef(1.0f, sum);
-        float none0 = 0.f, none1 = 0.f;              // zero, NaN where something in O is not finite
-#pragma unroll 1
-        for (int c = 0; c < D / 2; c += 16) {
-          uint32_t u[16], w[8];
-          WAVEAL_TMEM_LD16(o_addr + c, u, 0);
-          WAVEAL_TMEM_WAIT_LD16(u, 0);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float x, y;
-            ffma2(none0, none1, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), 0.f, 0.f, none0, none1);
-            ffma2(x, y, __uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), inv, inv, 0.f, 0.f);
-            w[i] = sum == 0.f ? 0u : pack2<T>(x, y);   // (O may be 0 times something)
-          }
-          // (a warp's rows lie far apart: every store is 32 lines to the memory pipe, so the fewer the better)
-          if (live) {
-            if (p.wide_o) {
-              st_global_v8(o + c, w);
-            } else {
-              *reinterpret_cast<uint4*>(o + c) = make_uint4(w[0], w[1], w[2], w[3]);
-              *reinterpret_cast<uint4*>(o + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-            }
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(B_O_EMPTY + ob));
-        if (lse) *lse = sum == 0.f ? -INFINITY : (ref * sl2 + __log2f(sum)) * 0.69314718055994531f;
-        // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
-        const bool bad = over || !(sum < INFINITY) || (ref == -INFINITY && tiles > 1) || !(none0 + none1 == 0.f);
-        // (the team's eight warps are never more than an item apart)
-        if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.last_again[team], ticket) != ticket)
-          p.plan.again[ticket] = atomicExch(&sm.again, ticket);
-        __syncwarp();
-      }
       item_done();
       b = (b + tiles * step) % kBuffers;
       if (!safe) g2 = (g2 + tiles) & 1;
@@ -874,7 +919,9 @@ waveal_status check(const waveal_prompt_desc* d) {
   if (most_tickets(d) > 1000000000ll) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 10^9 row tiles (of every sequence and key head)");
   if ((long long)d->tokens * d->q_heads > 1000000000ll) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 10^9 rows (tokens * q_heads)");
   const int64_t* strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
+#pragma unroll 1
   for (const int64_t* s : strides)
+#pragma unroll 1
     for (int i = 0; i < 2; ++i)
       if (s[i] % 8 || s[i] < 0) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "strides must be multiples of 8 elements (16 bytes) and not negative");
   return WAVEAL_OK;
