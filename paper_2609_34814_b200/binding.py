@@ -650,6 +650,32 @@ def _here(*tensors):
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
 
 
+_bytes = {}
+
+
+def _workspace_bytes(query, *descs):
+    """What a size query answers for these descriptors, which alone decide it; the last ones asked for are kept."""
+    n = _bytes.get(descs)
+    if n is None:
+        n = query(*descs)
+        if len(_bytes) >= 256:
+            _bytes.clear()
+        _bytes[descs] = n
+    return n
+
+
+def _block(like, sizes, stream):
+    """A new tensor of int32 words with room for pieces of these many words, and where each begins (256 bytes apart at least): one
+    allocation instead of one a piece, which took longer than the call itself.  The caller's views keep it alive."""
+    at, total = [], 0
+    for n in sizes:
+        at.append(total)
+        total += (n + 63) // 64 * 64
+    if stream is None:
+        return like.new_empty((total,), dtype=_torch.int32), at
+    return _new(stream, lambda: like.new_empty((total,), dtype=_torch.int32)), at
+
+
 def _ints(name, t, shape):
     """address of a contiguous int32 cuda tensor of this shape"""
     if t.dtype is not _torch.int32 or not t.is_cuda:
@@ -669,12 +695,9 @@ def _table(name, t):
     return shape[0], shape[1], st[0] if shape[0] > 1 else max(st[0], shape[1])
 
 
-def _workspace(workspace, need, like, stream):
-    if workspace is None:
-        return _new(stream, lambda: like.new_empty((need(),), dtype=_torch.uint8))
+def _check_workspace(workspace):
     if workspace.dtype is not _torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous uint8 cuda tensor")
-    return workspace
 
 
 def prompt_desc(q, k, v, o, batch: int, causal: bool = True, flags: int = 0) -> bytes:
@@ -711,21 +734,31 @@ def prompt_attn(q, k, v, seq_start, seq_len=None, o=None, lse=None, return_lse: 
     start = _ints("seq_start", seq_start, (batch + 1,))
     lens = None if seq_len is None else _ints("seq_len", seq_len, (batch,))
     desc = prompt_desc(q, k, v, o, batch, causal, flags)
-    if lse is None:
-        if return_lse:
-            lse = _new(stream, lambda: q.new_empty(q.shape[:2], dtype=torch.float32))
-    elif lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_cuda or not lse.is_contiguous():
+    heads, tokens = q.shape[0], q.shape[1]
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (heads, tokens) or not lse.is_cuda or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 cuda tensor [q_heads, tokens]")
-    workspace = _workspace(workspace, lambda: prompt_attn_workspace_bytes(desc), q, stream)
+    new_lse = lse is None and return_lse
+    if workspace is None:
+        size = _workspace_bytes(prompt_attn_workspace_bytes, desc)
+        block, at = _block(q, (size // 4, heads * tokens if new_lse else 0), stream)
+        ws_ptr = block.data_ptr()
+        if new_lse:
+            lse = block.view(torch.float32).as_strided((heads, tokens), (tokens, 1), at[1])
+    else:
+        _check_workspace(workspace)
+        ws_ptr, size = workspace.data_ptr(), workspace.numel()
+        if new_lse:
+            lse = _new(stream, lambda: q.new_empty((heads, tokens), dtype=torch.float32))
     _here(q, k, v, o, lse, seq_start, seq_len, workspace)
-    _check(load().waveal_prompt_attn(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), start, lens, scale,
-                                     workspace.data_ptr(), workspace.numel(), _status(dev_status), _stream(stream)))
+    _check(load().waveal_prompt_attn(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), start, lens, scale, ws_ptr, size,
+                                     _status(dev_status), _stream(stream)))
     return (o, lse) if return_lse else o
 
 
-def cache_fork_workspace_bytes(cache: PagedCache, fork: bytes) -> int:
+def cache_fork_workspace_bytes(cache_desc: bytes, fork: bytes) -> int:
+    """Bytes for cache_fork's workspace: PagedCache.desc and the packed waveal_fork_desc."""
     n = ctypes.c_size_t(0)
-    _check(load().waveal_cache_fork_workspace_bytes(cache.desc, fork, ctypes.byref(n)))
+    _check(load().waveal_cache_fork_workspace_bytes(cache_desc, fork, ctypes.byref(n)))
     return n.value
 
 
@@ -744,20 +777,32 @@ def cache_fork(cache: PagedCache, page_table, held_len, page_refs, keep_len, roo
     held, refs = _ints("held_len", held_len, (old_rows,)), _ints("page_refs", page_refs, (cache.n_pages,))
     keep, room = _ints("keep_len", keep_len, (rows,)), _ints("room_len", room_len, (rows,))
     parent = None if parents is None else _ints("parents", parents, (rows,))
-    if table_out is None:
-        pages = old_pages if max_pages is None else max_pages
-        table_out = _new(stream, lambda: page_table.new_empty((rows, pages)))
-    new_rows, pages, stride = _table("table_out", table_out)
-    if new_rows != rows or max_pages is not None and pages != max_pages:
-        raise ValueError("table_out must be [rows of keep_len, max_pages]")
-    if refs_out is None:
-        refs_out = _new(stream, lambda: page_refs.new_empty((cache.n_pages,)))
+    pages, n = old_pages if max_pages is None else max_pages, cache.n_pages
+    stride = pages
+    if table_out is not None:
+        new_rows, pages, stride = _table("table_out", table_out)
+        if new_rows != rows or max_pages is not None and pages != max_pages:
+            raise ValueError("table_out must be [rows of keep_len, max_pages]")
     desc = _FORK.pack(old_rows, rows, old_pages, pages, old_stride, stride)
-    workspace = _workspace(workspace, lambda: cache_fork_workspace_bytes(cache, desc), page_refs, stream)
+    size = _workspace_bytes(cache_fork_workspace_bytes, cache.desc, desc)
+    # what is not given, in one piece
+    block, at = _block(page_refs, (0 if table_out is not None else rows * pages, 0 if refs_out is not None else n,
+                                   0 if workspace is not None else size // 4), stream)
+    base = block.data_ptr()
+    if table_out is None:
+        table_out = block.as_strided((rows, pages), (pages, 1), 0)
+    if refs_out is None:
+        refs_out, refs_ptr = block.as_strided((n,), (1,), at[1]), base + 4 * at[1]
+    else:
+        refs_ptr = _ints("refs_out", refs_out, (n,))
+    if workspace is None:
+        ws_ptr = base + 4 * at[2]
+    else:
+        _check_workspace(workspace)
+        ws_ptr, size = workspace.data_ptr(), workspace.numel()
     _here(cache.k, cache.v, page_table, held_len, page_refs, keep_len, room_len, parents, table_out, refs_out, workspace)
     _check(load().waveal_cache_fork(cache.desc, desc, cache.k.data_ptr(), cache.v.data_ptr(), page_table.data_ptr(), held, refs, parent, keep, room,
-                                    table_out.data_ptr(), _ints("refs_out", refs_out, (cache.n_pages,)), workspace.data_ptr(), workspace.numel(),
-                                    _status(dev_status), _stream(stream)))
+                                    table_out.data_ptr(), refs_ptr, ws_ptr, size, _status(dev_status), _stream(stream)))
     return table_out, refs_out
 
 
@@ -769,9 +814,10 @@ class Compacted(NamedTuple):
     used: object            # [1]: pages in use; they are the first ones now
 
 
-def cache_compact_workspace_bytes(cache: PagedCache) -> int:
+def cache_compact_workspace_bytes(cache_desc: bytes) -> int:
+    """Bytes for cache_compact's workspace: PagedCache.desc."""
     n = ctypes.c_size_t(0)
-    _check(load().waveal_cache_compact_workspace_bytes(cache.desc, ctypes.byref(n)))
+    _check(load().waveal_cache_compact_workspace_bytes(cache_desc, ctypes.byref(n)))
     return n.value
 
 
@@ -782,24 +828,30 @@ def cache_compact(cache: PagedCache, page_refs, page_table=None, prefix_pages=No
     _load_torch()
     refs = _ints("page_refs", page_refs, (cache.n_pages,))
     n = cache.n_pages
-    rows = pages = old_stride = 0
-    table = prefix = None
+    rows = pages = old_stride = count = 0
+    table = prefix = table_ptr = prefix_ptr = None
     if page_table is not None:
         rows, pages, old_stride = _table("page_table", page_table)
-        table = _new(stream, lambda: page_table.new_empty((rows, pages)))
-    count = 0
     if prefix_pages is not None:
         count = prefix_pages.numel()
         _ints("prefix_pages", prefix_pages, (count,))
-        prefix = _new(stream, lambda: prefix_pages.new_empty((count,)))
-    numbers = _new(stream, lambda: page_refs.new_empty((2 * n + 1,)))
-    refs_out, place, used = numbers.as_strided((n,), (1,), 0), numbers.as_strided((n,), (1,), n), numbers.as_strided((1,), (1,), 2 * n)
-    workspace = _workspace(workspace, lambda: cache_compact_workspace_bytes(cache), page_refs, stream)
+    size = _workspace_bytes(cache_compact_workspace_bytes, cache.desc)
+    block, at = _block(page_refs, (rows * pages, count, n, n, 1, 0 if workspace is not None else size // 4), stream)
+    base = block.data_ptr()
+    if page_table is not None:
+        table, table_ptr = block.as_strided((rows, pages), (pages, 1), 0), base
+    if prefix_pages is not None:
+        prefix, prefix_ptr = block.as_strided((count,), (1,), at[1]), base + 4 * at[1]
+    refs_out, place, used = block.as_strided((n,), (1,), at[2]), block.as_strided((n,), (1,), at[3]), block.as_strided((1,), (1,), at[4])
+    if workspace is None:
+        ws_ptr = base + 4 * at[5]
+    else:
+        _check_workspace(workspace)
+        ws_ptr, size = workspace.data_ptr(), workspace.numel()
     _here(cache.k, cache.v, page_refs, page_table, prefix_pages, workspace)
-    at = numbers.data_ptr()
     _check(load().waveal_cache_compact(cache.desc, _COMPACT.pack(rows, pages, count, old_stride, pages), cache.k.data_ptr(), cache.v.data_ptr(), refs,
-                                       _ptr(page_table), _ptr(prefix_pages), at, _ptr(table), _ptr(prefix), at + 4 * n, at + 8 * n,
-                                       workspace.data_ptr(), workspace.numel(), _stream(stream)))
+                                       _ptr(page_table), _ptr(prefix_pages), base + 4 * at[2], table_ptr, prefix_ptr, base + 4 * at[3], base + 4 * at[4],
+                                       ws_ptr, size, _stream(stream)))
     return Compacted(table, prefix, refs_out, place, used)
 
 

@@ -3,7 +3,7 @@
 //
 // Which page goes where is decided by the pages' counts: how many rows hold each.  Sums over the pool and over the rows decide the
 // places, so the result does not depend on the order in which threads run.  A call that decides has two launches: one thread block or
-// one cluster of up to eight does the sums (its phases are separated by the cluster's own barrier; no thread waits on a flag in memory),
+// one cluster of up to sixteen does the sums (its phases are separated by the cluster's own barrier; no thread waits on a flag in memory),
 // then a grid over all SMs copies what the decision says.  The first is latency (a few round trips to memory), the second
 // memory traffic: a warp has four 16-byte loads under way a lane before it stores any.
 #include <algorithm>
@@ -13,7 +13,7 @@
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kCluster = 8;                          // thread blocks that decide, at most (the portable size)
+constexpr int kCluster = 16;                         // thread blocks that decide, at most (what this GPU allows)
 constexpr int kCopyThreads = 256, kCopyBlocks = 8;   // blocks an SM
 constexpr int kUnroll = 4;                           // vectors of a lane under way
 constexpr int kSegment = 32 * kUnroll;               // vectors of a warp's turn
@@ -99,6 +99,7 @@ template <class V>
 __global__ void __launch_bounds__(kCopyThreads) k_copy_pages(const __grid_constant__ CopyParams p) {
   const int lane = threadIdx.x & 31;
   const long long turns = 2ll * p.shape.segments * p.count, step = (long long)gridDim.x * (kCopyThreads / 32);
+#pragma unroll 1
   for (long long w = (long long)blockIdx.x * (kCopyThreads / 32) + threadIdx.x / 32; w < turns; w += step) {
     const int pair = (int)(w / (2 * p.shape.segments)), i = (int)(w - (long long)pair * 2 * p.shape.segments);
     const int from = p.from_pages[pair], to = p.to_pages[pair];
@@ -137,6 +138,32 @@ __device__ __forceinline__ int scan_block(int x, int* shared, int& total) {
 }
 static_assert(kPlanThreads == 32 * 32, "scan_block");
 
+// The counts of a pool, sixteen bytes at a time where they are aligned to that: eight thread blocks read them all, so what a thread has under
+// way at once decides (1.3 MB of counts took 10 us a pass one by one).
+__device__ __forceinline__ bool by_four(const void* a, const void* b) {
+  return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15) == 0;
+}
+__device__ __forceinline__ void copy_counts(int* to, const int* from, int n, int tid, int threads) {
+  int done = 0;
+  if (by_four(to, from)) {
+    done = n / 4 * 4;
+#pragma unroll 4
+    for (int i = tid; i < n / 4; i += threads) reinterpret_cast<int4*>(to)[i] = __ldg(reinterpret_cast<const int4*>(from) + i);
+  }
+#pragma unroll 1
+  for (int i = done + tid; i < n; i += threads) to[i] = __ldg(from + i);
+}
+// eight counts from i on (those from `end` on: `none`)
+__device__ __forceinline__ void load_counts(const int* counts, int i, int end, bool four, int none, int (&v)[8]) {
+  if (four && i + 8 <= end) {
+    const int4 a = __ldcg(reinterpret_cast<const int4*>(counts + i)), b = __ldcg(reinterpret_cast<const int4*>(counts + i + 4));
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = i + k < end ? __ldcg(counts + i + k) : none;
+  }
+}
+
 // this block's part of n things, begin a multiple of kPerThread
 constexpr int kPerThread = 8;                        // pages of a thread's turn: a 32-byte sector of their counts
 struct Part { int begin, end; };
@@ -172,14 +199,15 @@ __device__ __forceinline__ int held_tokens(const ForkParams& p, int r) {
 }
 
 __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_constant__ ForkParams p) {
-  __shared__ int shared[33];
+  __shared__ int shared[33], list[kPlanThreads * kPerThread];
   waveal::let_next_kernel_start();
   const int tid = blockIdx.x * kPlanThreads + threadIdx.x, threads = gridDim.x * kPlanThreads;
   const int warp = tid / 32, warps = threads / 32, lane = threadIdx.x & 31;
   const int shift = p.shape.shift, mask = (1 << shift) - 1;
   int *count = p.kids, *fewest = p.kids + p.old_rows, *most = p.kids + 2 * p.old_rows;
 
-  for (int i = tid; i < p.n_pages; i += threads) p.new_refs[i] = p.refs[i];
+  copy_counts(p.new_refs, p.refs, p.n_pages, tid, threads);
+#pragma unroll 1
   for (int r = tid; r < p.old_rows; r += threads) {
     count[r] = 0, fewest[r] = INT_MAX, most[r] = 0;
     const int n = p.held[r];
@@ -188,6 +216,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
   sync_plan();
 
   // ---- what every row keeps
+#pragma unroll 1
   for (int b = tid; b < p.rows; b += threads) {
     int parent = p.parents ? p.parents[b] : b, keep = p.keep[b], room = p.room[b];
     if (parent >= p.old_rows) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 80, b, parent), parent = -1;
@@ -218,23 +247,28 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
 
   // ---- counts: a page of an old row that k rows share goes from one holder to k.  (Rows of one child: no change up to what it keeps.)
   const int old_runs = (p.old_pages + kRun - 1) / kRun, runs = (p.pages + kRun - 1) / kRun;
+#pragma unroll 1
   for (long long u = warp; u < (long long)p.old_rows * old_runs; u += warps) {
     const int r = (int)(u / old_runs), run = (int)(u - (long long)r * old_runs);
     const int kids = __ldcg(count + r), all = kids ? __ldcg(fewest + r) : 0, pages = (int)(((long long)held_tokens(p, r) + mask) >> shift);
+#pragma unroll 4
     for (int j = max(run * kRun, kids == 1 ? all : 0) + lane; j < min(pages, (run + 1) * kRun); j += 32) {
       const int change = (j < all ? kids : 0) - 1, page = p.old_table[r * p.old_stride + j];
       if (change && page >= 0 && page < p.n_pages) atomicAdd(p.new_refs + page, change);
     }
   }
+#pragma unroll 1
   for (long long u = warp; u < (long long)p.rows * runs; u += warps) {
     const int b = (int)(u / runs), run = (int)(u - (long long)b * runs);
     const int4 row = __ldcg(p.row + b);
     if (row.x < 0) continue;
+#pragma unroll 4
     for (int j = max(run * kRun, __ldcg(fewest + row.x)) + lane; j < min(row.y, (run + 1) * kRun); j += 32) {
       const int page = p.old_table[row.x * p.old_stride + j];
       if (page >= 0 && page < p.n_pages) atomicAdd(p.new_refs + page, 1);
     }
   }
+#pragma unroll 1
   for (int b = tid; b < p.rows; b += threads) {
     const int page = __ldcg(p.last + b).x;
     if (page >= 0) atomicMin(p.ends + page, b);
@@ -242,6 +276,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
   sync_plan();
 
   // ---- a page filled in part stays with the first row that ends in it, if nobody else holds it
+#pragma unroll 1
   for (int b = tid; b < p.rows; b += threads) {
     int4 row = __ldcg(p.row + b);
     const int page = __ldcg(p.last + b).x;
@@ -258,7 +293,15 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
   // ---- sums of the blocks' parts: free pages, fresh pages
   const Part pages = part_of(p.n_pages), rows = part_of(p.rows);
   int free_here = 0, need_here = 0, total;
-  for (int i = pages.begin + threadIdx.x; i < pages.end; i += kPlanThreads) free_here += __ldcg(p.new_refs + i) <= 0;
+  const bool four = by_four(p.new_refs, p.new_refs);
+#pragma unroll 2
+  for (int i = pages.begin + threadIdx.x * kPerThread; i < pages.end; i += kPlanThreads * kPerThread) {
+    int v[kPerThread];
+    load_counts(p.new_refs, i, pages.end, four, 1, v);
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) free_here += v[k] <= 0;
+  }
+#pragma unroll 1
   for (int b = rows.begin + threadIdx.x; b < rows.end; b += kPlanThreads) need_here += __ldcg(p.last + b).y;
   scan_block(free_here, shared, total);
   if (threadIdx.x == 0) p.sums[blockIdx.x] = total;
@@ -266,14 +309,16 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
   if (threadIdx.x == 0) p.sums[kCluster + blockIdx.x] = total;
   sync_plan();
   int free_before = 0, need_before = 0, free_all = 0, need_all = 0;
-  for (int i = 0; i < (int)gridDim.x; ++i) {
-    const int f = __ldcg(p.sums + i), n = __ldcg(p.sums + kCluster + i);
+#pragma unroll
+  for (int i = 0; i < kCluster; ++i) {
+    const int f = i < (int)gridDim.x ? __ldcg(p.sums + i) : 0, n = i < (int)gridDim.x ? __ldcg(p.sums + kCluster + i) : 0;
     if (i < (int)blockIdx.x) free_before += f, need_before += n;
     free_all += f, need_all += n;
   }
   if (tid == 0) *p.free_pages = free_all;
 
   // ---- where every row's fresh pages begin, and which pages these are
+#pragma unroll 1
   for (int b0 = rows.begin; b0 < rows.end; b0 += kPlanThreads) {
     const int b = b0 + threadIdx.x, need = b < rows.end ? __ldcg(p.last + b).y : 0;
     const int begin = need_before + scan_block(need, shared, total);
@@ -283,19 +328,37 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
       if (begin <= free_all && begin + need > free_all) report(p.dev_status, WAVEAL_ERR_NO_PAGES, 85, b, need_all - free_all);
     }
   }
+#pragma unroll 1
   for (int i0 = pages.begin; i0 < pages.end && free_before < need_all; i0 += kPlanThreads * kPerThread) {
     const int i = i0 + threadIdx.x * kPerThread;
+    int v[kPerThread];
+    load_counts(p.new_refs, min(i, pages.end), pages.end, four, 1, v);
     unsigned is_free = 0;
 #pragma unroll
+    for (int k = 0; k < kPerThread; ++k) is_free |= (unsigned)(v[k] <= 0) << k;
+    // (the list goes through shared memory, the counts back eight at once: a store whose lanes lie apart costs as many as there are lanes)
+    int at = scan_block(__popc(is_free), shared, total);
+    const int take = min(total, need_all - free_before);
+#pragma unroll
     for (int k = 0; k < kPerThread; ++k)
-      if (i + k < pages.end && __ldcg(p.new_refs + i + k) <= 0) is_free |= 1u << k;
-    int at = free_before + scan_block(__popc(is_free), shared, total);
-    free_before += total;
-    for (; is_free && at < need_all; is_free &= is_free - 1, ++at) {
-      const int page = i + __ffs(is_free) - 1;
-      p.fresh[at] = page;
-      p.new_refs[page] = 1;
+      if (is_free >> k & 1) {
+        if (at < take) list[at] = i + k, v[k] = 1;
+        ++at;
+      }
+    if (is_free) {
+      if (four && i + kPerThread <= pages.end) {
+        int4* to = reinterpret_cast<int4*>(p.new_refs + i);
+        to[0] = make_int4(v[0], v[1], v[2], v[3]), to[1] = make_int4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k)
+          if (i + k < pages.end) p.new_refs[i + k] = v[k];
+      }
     }
+    __syncthreads();
+#pragma unroll 1
+    for (int k = threadIdx.x; k < take; k += kPlanThreads) p.fresh[free_before + k] = list[k];
+    free_before += total;
   }
 }
 
@@ -307,6 +370,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(const __grid_consta
   waveal::wait_for_previous_kernel();
   const int free_all = *p.free_pages;
   // the pages that rows filled in part and do not keep
+#pragma unroll 1
   for (long long w = warp; w < (long long)p.rows * turns; w += warps) {
     const int b = (int)(w / turns);
     const int4 row = p.row[b];
@@ -316,26 +380,33 @@ __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(const __grid_consta
   }
   // the table
   const int runs = (p.pages + kRun - 1) / kRun;
+#pragma unroll 1
   for (long long u = warp; u < (long long)p.rows * runs; u += warps) {
     const int b = (int)(u / runs), run = (int)(u - (long long)b * runs);
     const int4 row = p.row[b];
     const int2 last = p.last[b];
-    const int stays = row.w & kStays ? 1 : 0;
-    for (int j = run * kRun + lane; j < min(p.pages, (run + 1) * kRun); j += 32) {
-      int page = -1;
-      if (j < row.y) {
-        page = p.old_table[row.x * p.old_stride + j];
-        if (page < 0 || page >= p.n_pages) {
-          report(p.dev_status, WAVEAL_ERR_BAD_MASK, 84, b, page);
-          page = -1;
-        }
-      } else if (j == row.y && stays) {
-        page = last.x;
-      } else if (j < row.z) {
-        const int i = last.y + j - row.y - stays;
-        if (i < free_all) page = p.fresh[i];
+    const int stays = row.w & kStays ? 1 : 0, end = min(p.pages, (run + 1) * kRun);
+    // (four entries of a lane at once: they come from the last table or from the list of fresh pages)
+#pragma unroll 1
+    for (int j0 = run * kRun + lane; j0 < end; j0 += 4 * 32) {
+      int page[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = j0 + 32 * k, i = last.y + j - row.y - stays;
+        const bool old = j < row.y, fresh = !old && j < row.z && !(j == row.y && stays) && i < free_all;
+        page[k] = j == row.y && stays ? last.x : -1;
+        if (j < end && (old || fresh)) page[k] = old ? p.old_table[row.x * p.old_stride + j] : p.fresh[i];
       }
-      p.table[b * p.stride + j] = page;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = j0 + 32 * k;
+        if (j >= end) continue;
+        if (j < row.y && (page[k] < 0 || page[k] >= p.n_pages)) {
+          report(p.dev_status, WAVEAL_ERR_BAD_MASK, 84, b, page[k]);
+          page[k] = -1;
+        }
+        p.table[b * p.stride + j] = page[k];
+      }
     }
   }
 }
@@ -361,13 +432,21 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_compact_plan(const __grid_c
   waveal::let_next_kernel_start();
   const Part pages = part_of(p.n_pages);
   int here = 0, total;
-  for (int i = pages.begin + threadIdx.x; i < pages.end; i += kPlanThreads) here += p.refs[i] > 0;
+  const bool four = by_four(p.refs, p.refs);
+#pragma unroll 2
+  for (int i = pages.begin + threadIdx.x * kPerThread; i < pages.end; i += kPlanThreads * kPerThread) {
+    int v[kPerThread];
+    load_counts(p.refs, i, pages.end, four, 0, v);
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) here += v[k] > 0;
+  }
   scan_block(here, shared, total);
   if (threadIdx.x == 0) p.sums[blockIdx.x] = total;
   sync_plan();
   int before = 0, n = 0;
-  for (int i = 0; i < (int)gridDim.x; ++i) {
-    const int x = __ldcg(p.sums + i);
+#pragma unroll
+  for (int i = 0; i < kCluster; ++i) {
+    const int x = i < (int)gridDim.x ? __ldcg(p.sums + i) : 0;
     if (i < (int)blockIdx.x) before += x;
     n += x;
   }
@@ -376,12 +455,14 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_compact_plan(const __grid_c
     if (n == p.n_pages) *p.first = n;
   }
   // the i-th page in use from n on goes to the i-th free page below n
+#pragma unroll 1
   for (int i0 = pages.begin; i0 < pages.end; i0 += kPlanThreads * kPerThread) {
     const int i = i0 + threadIdx.x * kPerThread;
+    int v[kPerThread];
+    load_counts(p.refs, min(i, pages.end), pages.end, four, 0, v);
     unsigned in_use = 0;
 #pragma unroll
-    for (int k = 0; k < kPerThread; ++k)
-      if (i + k < pages.end && p.refs[i + k] > 0) in_use |= 1u << k;
+    for (int k = 0; k < kPerThread; ++k) in_use |= (unsigned)(v[k] > 0) << k;
     int at = before + scan_block(__popc(in_use), shared, total);
     before += total;
 #pragma unroll
@@ -398,6 +479,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_compact_plan(const __grid_c
   }
   sync_plan();
   const int first = __ldcg(p.first);
+#pragma unroll 1
   for (int page = pages.begin + threadIdx.x; page < pages.end; page += kPlanThreads) {
     const int count = p.refs[page];
     int place = -1;
@@ -416,16 +498,20 @@ __global__ void __launch_bounds__(kCopyThreads) k_compact_apply(const __grid_con
   const long long warp = (long long)blockIdx.x * (kCopyThreads / 32) + threadIdx.x / 32, warps = (long long)gridDim.x * (kCopyThreads / 32);
   waveal::wait_for_previous_kernel();
   const int first = *p.first, moves = *p.used - first, turns = 2 * p.shape.segments;
+#pragma unroll 1
   for (long long w = warp; w < (long long)moves * turns; w += warps) {
     const int i = (int)(w / turns);
     copy_turn<V>(p.shape, p.t, p.from[first + i], p.to[i], (int)(w - (long long)i * turns), 1 << p.shape.shift, lane);
   }
   auto moved = [&](int page) { return page >= 0 && page < p.n_pages ? p.place[page] : -1; };
   const int runs = (p.pages + kRun - 1) / kRun;
+#pragma unroll 1
   for (long long u = warp; u < (long long)p.rows * runs; u += warps) {
     const int b = (int)(u / runs), run = (int)(u - (long long)b * runs);
+#pragma unroll 4
     for (int j = run * kRun + lane; j < min(p.pages, (run + 1) * kRun); j += 32) p.table[b * p.stride + j] = moved(p.old_table[b * p.old_stride + j]);
   }
+#pragma unroll 1
   for (long long i = warp * 32 + lane; i < p.prefix; i += warps * 32) p.new_prefix[i] = moved(p.old_prefix[i]);
 }
 
@@ -481,6 +567,13 @@ int plan_blocks(long long pages, long long entries) {
 
 template <class P>
 waveal_status launch_plan(void (*kernel)(P), const P& p, int blocks, cudaStream_t st) {
+  static bool set[64] = {};                          // (one for each kernel: more than eight blocks a cluster have to be asked for)
+  int dev = 0;
+  WAVEAL_CUDA_OK(cudaGetDevice(&dev));
+  if (blocks > 8 && (dev >= 64 || !set[dev])) {
+    WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (dev < 64) set[dev] = true;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kPlanThreads);
