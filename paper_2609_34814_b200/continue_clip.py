@@ -1,11 +1,11 @@
 """One attention layer of a model that continues a clip in several ways: the calls of this library as they follow each other.
 
-  python -m paper_2609_34814_b200.continue_clip [--heads 8] [--frames 6] [--new-frames 2] [--continuations 4]
+  python -m paper_2609_34814_b200.continue_clip [--heads 8] [--frames 6] [--new-frames 2] [--continuations 4] [--choose]
 
 The clip so far goes through the block-sparse attention in its planned order, on queries and keys rotated by frame, height and
 width, and its keys and values into the paged cache, once.  Every continuation then adds frame after frame: the frame's keys are rotated
 on their way into the continuation's own pages, the queries beside them, and all continuations attend to the shared clip and to their
-own frames in one call.  A model would put its projections and its other layers around this; here the queries, keys and values are drawn.
+own frames in one call.  Between frames the better continuations may go on in several ways and the others end (choose).  A model would put its projections and its other layers around this; here the queries, keys and values are drawn.
 """
 from __future__ import annotations
 
@@ -30,6 +30,7 @@ class ClipLayer:
         self.cache = wb.PagedCache(*(torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)))
         pages = torch.arange(shape[0], dtype=torch.int32, device=device)
         self.clip_pages, self.table = pages[:shared], pages[shared:].view(continuations, own)
+        self.refs = torch.ones_like(pages)               # holders of every page
         pairs = head_dim // 2
         self.axis_pairs = [pairs - 2 * (pairs // 3), pairs // 3, pairs // 3]
         self.freqs = torch.cat([wb.rope_freqs(2 * n, device=device)[0] for n in self.axis_pairs])
@@ -76,6 +77,19 @@ class ClipLayer:
         return o
 
 
+    def choose(self, parents):
+        """Continuation b goes on from what is now continuation parents[b]: several from the same one, as many in all as there were or fewer.
+        They share the pages that their common frames fill; a page filled in part is copied."""
+        parents = torch.as_tensor(parents, dtype=torch.int32, device=self.device)
+        rows = parents.shape[0]
+        if rows > self.continuations:
+            raise ValueError("there is room for as many continuations as before")
+        tokens = lambda n, frames: torch.full((n,), frames * self.frame, dtype=torch.int32, device=self.device)  # noqa: E731
+        self.table, self.refs = wb.cache_fork(self.cache, self.table, tokens(self.continuations, self.new_frames), self.refs, tokens(rows, self.seen),
+                                              tokens(rows, self.new_frames), parents=parents, dev_status=self.status)
+        self.continuations = rows
+
+
 def band_mask(heads, blocks, width, device="cuda"):
     """bitmap of a band of blocks around the diagonal and the first block for all"""
     i = torch.arange(blocks)
@@ -91,6 +105,7 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     for name, value in (("heads", 8), ("head-dim", 128), ("height", 30), ("width", 52), ("frames", 6), ("new-frames", 2), ("continuations", 4)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--choose", action="store_true", help="after a frame the better half of the continuations goes on twice (by drawn scores)")
     a = ap.parse_args(argv)
     layer = ClipLayer(a.heads, a.head_dim, (a.height, a.width), a.frames, a.new_frames, a.continuations)
     g = torch.Generator(device="cuda").manual_seed(0)
@@ -108,6 +123,10 @@ def main(argv=None):
         flops = 4 * a.heads * a.head_dim * q.shape[1] * keys
         print(f"frame {f}: {a.continuations} continuations over {keys} keys, {begin.elapsed_time(end) * 1e3:.0f} us "
               f"({flops / begin.elapsed_time(end) / 1e9:.0f} TFLOP/s, append included), mean |o| {o.float().abs().mean().item():.4f}")
+        if a.choose and f + 1 < a.new_frames:
+            best = torch.rand((a.continuations,), generator=g, device="cuda").argsort(descending=True)[:(a.continuations + 1) // 2]
+            layer.choose(best.repeat(2)[:a.continuations])
+            print(f"frame {f}: continuations {best.tolist()} go on")
     code = layer.status.tolist()
     if code[0]:
         raise SystemExit(f"device status {code}")

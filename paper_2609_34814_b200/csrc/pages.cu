@@ -635,8 +635,12 @@ waveal_status check_workspace(const void* ws, size_t have, size_t need) {
 waveal_status check_tensors(const void* k, const void* v) {
   if (!k || !v) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "the caches' keys and values are required");
   if (!waveal::aligned(k, 2) || !waveal::aligned(v, 2)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "a tensor is not aligned to its element");
-  if (waveal::sm_count() <= 0) return waveal::fail(WAVEAL_ERR_CUDA, "number of SMs not available");
   return WAVEAL_OK;
+}
+
+// (behind all other checks)
+waveal_status check_device() {
+  return waveal::sm_count() > 0 ? WAVEAL_OK : waveal::fail(WAVEAL_ERR_CUDA, "number of SMs not available");
 }
 
 }  // namespace
@@ -656,6 +660,7 @@ extern "C" waveal_status waveal_cache_copy(const waveal_cache_desc* to, const wa
   if (!from_pages || !to_pages) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "from_pages and to_pages are required");
   if (waveal_status e = check_tensors(from_k, from_v)) return e;
   if (waveal_status e = check_tensors(to_k, to_v)) return e;
+  if (waveal_status e = check_device()) return e;
   CopyParams p = {};
   const bool wide = page_shape(p.shape, p.t, from, from_k, from_v, to, to_k, to_v);
   p.from_pages = from_pages, p.to_pages = to_pages, p.count = count;
@@ -693,6 +698,7 @@ extern "C" waveal_status waveal_cache_fork(const waveal_cache_desc* c, const wav
     return waveal::fail(WAVEAL_ERR_INVALID_ARG, "the new table and counts must not lie over the old ones");
   const ForkLayout l = fork_layout(c, f);
   if (waveal_status e = check_workspace(ws, ws_bytes, l.bytes)) return e;
+  if (waveal_status e = check_device()) return e;
   ForkParams p = {};
   const bool wide = page_shape(p.shape, p.t, c, k_cache, v_cache, c, k_cache, v_cache);
   p.old_rows = f->old_rows, p.rows = f->rows, p.old_pages = f->old_pages, p.pages = f->pages, p.n_pages = c->n_pages;
@@ -741,6 +747,7 @@ extern "C" waveal_status waveal_cache_compact(const waveal_cache_desc* c, const 
     return waveal::fail(WAVEAL_ERR_INVALID_ARG, "the new tables and counts must not lie over the old ones");
   const CompactLayout l = compact_layout(c);
   if (waveal_status e = check_workspace(ws, ws_bytes, l.bytes)) return e;
+  if (waveal_status e = check_device()) return e;
   CompactParams p = {};
   const bool wide = page_shape(p.shape, p.t, c, k_cache, v_cache, c, k_cache, v_cache);
   p.rows = d->rows, p.pages = d->pages, p.n_pages = c->n_pages, p.prefix = d->prefix_pages;
