@@ -36,14 +36,13 @@ constexpr int kLoadWarp = 16, kScoreWarp = 17, kProductWarp = 18, kValueWarp = 1
 constexpr int kTile = 128;                           // keys of a tile, rows of a row tile
 constexpr int kItems = 4;                            // row tiles under way: their descriptions, references and sums
 constexpr int kItemReaders = 23;                     // two issuers, the V loader, sixteen softmax warps, four for the results
-constexpr int kParts = 2;                            // of a tile: P goes to the products 32 keys of each half at a time
 constexpr int kChecks = 8;                           // masked tiles whose verdicts are under way (more than the ring has V tiles)
 constexpr long long kTimeoutCycles = 4000000000ll;   // ~2 s at boost clock
 constexpr long long kSelfTestCycles = 4000000ll;     // ~2 ms
 constexpr float kGrowth = 8.0f;                      // log2 of how far a row's maximum may outgrow its reference
 // Most row tiles need only one reference: that of their first tile of keys.  Nothing is lost while no number overflows: P of bf16, the sums and O
-// have the range of fp32, P of fp16 has 2^16.  The sum of a tile's probabilities tells: all its terms are positive, so none of them is larger.
-template <class T> constexpr float kSumLimit = std::is_same_v<T, __half> ? 0x1p15f : 0x1p60f;
+// have the range of fp32, P of fp16 has 2^16.  What overflows shows in the results: an element of O is not finite, or a sum beyond what divides well.
+constexpr float kSumLimit = 0x1p100f;
 
 template <int D> struct Geo {
   static constexpr int SLABS = D / 64;               // 128-byte-swizzled slabs of 64 channels
@@ -259,7 +258,7 @@ constexpr int kBuffers = 3;                          // of S
 enum {
   B_ITEM_FULL = 0, B_ITEM_EMPTY = B_ITEM_FULL + kItems, B_Q_FULL = B_ITEM_EMPTY + kItems, B_Q_EMPTY = B_Q_FULL + 2,
   B_S_FULL = B_Q_EMPTY + 2,                          // twice as many as buffers: a barrier's phases are waited for by one team, in turn
-  B_S_FREE = B_S_FULL + 2 * kBuffers, B_P = B_S_FREE + kBuffers, B_O_EMPTY = B_P + kParts * kBuffers, B_O_FULL = B_O_EMPTY + 2,
+  B_S_FREE = B_S_FULL + 2 * kBuffers, B_P = B_S_FREE + kBuffers, B_O_EMPTY = B_P + kBuffers, B_O_FULL = B_O_EMPTY + 2,
   B_REF = B_O_FULL + 2, B_PV_DONE = B_REF + kItems, B_PAIR = B_PV_DONE + 2, B_CHECK = B_PAIR + 8, B_FINAL = B_CHECK + 2 * kChecks, B_DONE = B_FINAL + 2,
   B_K_FULL
 };
@@ -556,18 +555,13 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&sm.verdict[g2][c]), 0)) groups = 0;
               ++checks[g2];
             }
-            if (!(ok = warp_wait(ctx, BAR(B_P + b * kParts), uses >> b & 1, 120))) break;
-            if (groups == 8) {
-              tc_fence_after();
-              umma2_ts(o_col, s_col + 32, vd + 2 * 128, kPV, j > 0);
-              umma2_ts(o_col, s_col + 64, vd + 4 * 128, kPV, 1);
-            }
-            if (!(ok = warp_wait(ctx, BAR(B_P + b * kParts + 1), uses >> b & 1, 120))) break;
+            if (!(ok = warp_wait(ctx, BAR(B_P + b), uses >> b & 1, 120))) break;
             uses ^= 1u << b;
             tc_fence_after();
             if (groups == 8) {
-              umma2_ts(o_col, s_col + 48, vd, kPV, 1);
-              umma2_ts(o_col, s_col + 80, vd + 6 * 128, kPV, 1);
+              umma2_ts(o_col, s_col + 48, vd, kPV, j > 0);
+              umma2_ts(o_col, s_col + 32, vd + 2 * 128, kPV, 1);
+              umma4_ts(o_col, s_col + 64, vd + 4 * 128, kPV, 1);
             } else {
 #pragma unroll 1
               for (int c = 0; c < groups; ++c) umma_bf16_ts(o_col, s_col + p_column(c), vd + (uint64_t)(c * 128), kPV, j > 0 || c > 0);
@@ -702,7 +696,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         }
         if (lse) *lse = sum == 0.f ? -INFINITY : (ref * p.sl2 + __log2f(sum)) * 0.69314718055994531f;
         // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
-        const bool bad = !(sum < INFINITY) || (ref == -INFINITY && tiles > 1) || !(none0 + none1 == 0.f);
+        const bool bad = !(sum < kSumLimit) || (ref == -INFINITY && tiles > 1) || !(none0 + none1 == 0.f);
         // (the four warps are never more than an item apart)
         if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.last_again, ticket) != ticket)
           p.plan.again[ticket] = atomicExch(&sm.again, ticket);
@@ -739,8 +733,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       const int keys = im->keys, first_sees = im->sees, masked = im->masked;
       const bool live = tok < im->n;
       const int sees = min(p.causal ? first_sees + tok : keys, keys) - half * 64;
-      float ref = -INFINITY, sum = 0.f;
-      bool over = false;
+      float ref = -INFINITY, minus = 0.f, s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+      const int plain = safe ? tiles : 2;            // from this tile on there is nothing to do but the exponentials, up to the first that a mask cuts
       const int j0 = g2 == team ? 0 : safe ? tiles : 1;
       uint32_t buf = (b + j0 * step) % kBuffers;
 #pragma unroll 1
@@ -749,10 +743,12 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         if (!(ok = warp_wait(ctx, BAR(B_S_FULL + 2 * buf + team), s_ph >> buf & 1, 124))) break;
         s_ph ^= 1u << buf;
         tc_fence_after();
-        const bool cut = j >= masked;
-        const int chunks = cut ? min(2, (keys - j * kTile - half * 64 + 31) / 32) : 2;   // of this thread's 64 keys (what is behind the last key is not used)
+        int chunks = 2;                              // of this thread's 64 keys
         uint32_t u[32], w[16];
+        const bool cut = j >= masked;
+        if (j < plain || cut) {
         if (cut) {
+          chunks = min(2, (keys - j * kTile - half * 64 + 31) / 32);   // (what is behind the last key is not used)
           // scores that the row does not see, 16 columns at a time from the first that some row does not see.  (Code that runs once or twice an
           // item is short: each 128 bytes of it come from beyond the instruction caches.)
           const int visible = sees - j * kTile, from = max(0, first_sees - j * kTile - half * 64) / 16 * 16;
@@ -787,7 +783,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             if (__any_sync(0xffffffffu, grown)) {
               const float scale = grown ? ex2((ref - top) * sl2) : 1.0f;
               if (grown) ref = top;
-              sum *= scale;
+              s0 *= scale, s1 *= scale, s2 *= scale, s3 *= scale;
               rescale<D / 2>(tm + G::O_COL + items % G::OS * D + half * (D / 2), scale);
             }
           }
@@ -809,13 +805,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           if (!(ok = warp_wait(ctx, BAR(B_REF + at), item_no / kItems & 1, 131))) break;
           ref = sm.ref[at][r];
         }
-        const float minus = ref == -INFINITY ? 0.f : -ref * sl2;
-        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-        auto release = [&](int part) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(B_P + buf * kParts + part));
-        };
+        minus = ref == -INFINITY ? 0.f : -ref * sl2;
+        }
 #pragma unroll 1
         for (int n = 0; n < chunks; ++n) {
           const int c = half ? n : chunks - 1 - n;
@@ -832,10 +823,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             w[i] = pack2<T>(a, b), w[i + 1] = pack2<T>(d, e);
           }
           WAVEAL_TMEM_ST16(s_addr + p_column(4 * half + 2 * c), w, 0);
-          tc_wait_st();
-          if (n == 0) release(0);
         }
-        if (chunks <= 0) release(0);
+        tc_wait_st();
         if (cut && safe) {
           if (!(ok = warp_wait(ctx, BAR(B_CHECK + team * kChecks + checks % kChecks), checks / kChecks & 1, 125))) break;
           if (*reinterpret_cast<volatile int*>(&sm.verdict[team][checks % kChecks])) {
@@ -851,13 +840,14 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           }
           ++checks;
         }
-        s0 = (s0 + s1) + (s2 + s3);
-        over |= !(s0 < kSumLimit<T>);
-        sum += s0;
-        // (read once the products of the last tile are done; infinite where something overflowed)
-        if (j + 3 - (int)step >= tiles) sm.sums[at][team][half][r] = over && !safe ? INFINITY : sum;
-        if (safe && j == tiles - 1 && half == 0) sm.ref[at][r] = ref;
-        release(1);
+        // (read once the products of the last tile are done)
+        if (j + 3 - (int)step >= tiles) {
+          sm.sums[at][team][half][r] = (s0 + s1) + (s2 + s3);
+          if (safe && half == 0) sm.ref[at][r] = ref;
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_P + buf));
         buf = buf == 0 ? kBuffers - 1 : buf - 1;     // two on
       }
       if (!ok) break;
