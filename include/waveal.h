@@ -443,11 +443,15 @@ waveal_status waveal_prompt_attn_workspace_bytes(const waveal_prompt_desc* desc 
  * seq_len: dev int32 [batch] or NULL: only the first seq_len[b] of them exist (a padded batch); 0 <= seq_len[b] <= seq_start[b + 1] - seq_start[b].
  * Both are read on the device, so a captured call follows what they hold when it is replayed.  Tokens of no sequence (in front of the first, behind
  * the last, padding) are neither read into a result nor written.  A malformed sequence is reported in dev_status as {WAVEAL_ERR_BAD_MASK, site,
- * sequence, value} (100: starts, 101: length) and left out.
+ * sequence, value} (100: starts, 101: length) and left out, after 100 also every sequence that begins in front of an earlier start (as far as that is
+ * within 0 .. tokens): no two sequences claim the same token.
  * lse: dev float [q_heads][tokens] or NULL, the natural log of the sum of exponentials.  A token whose scores are all -infinity has o = 0 and -inf; a row
  * whose scores hold +infinity or NaN gives NaN.  Keys and values that a token does not see, NaN and infinities included, never reach it.
- * q, k, v, o: 16-byte aligned, strides multiples of 8 elements and not negative; o must not overlap the others.
- * At most 10^9 rows (tokens * q_heads).  scale <= 0 means 1/sqrt(head_dim).  Scores, sums and the
+ * (128 rows some of whose results are not finite, or whose scores rise by 2^15 (fp16) or 2^100 (bf16) times their first ones' exponentials, are
+ * computed a second time in a slower way.)
+ * q, k, v, o: 16-byte aligned, strides multiples of 8 elements and not negative (that of a dimension with one entry: anything); o must not overlap the
+ * others.  At most 2^25 tokens, 10^9 rows (tokens * q_heads) and 10^9 row tiles ((tokens / (128 / group) + batch) * kv_heads, with group = q_heads
+ * / kv_heads).  scale <= 0 means 1/sqrt(head_dim).  Scores, sums and the
  * accumulated output are fp32; the probabilities enter the second product in the tensors' type.
  * ws: 256-byte aligned, not shared with a call that may run at the same time; needs no clearing.  dev_status: dev int32 [4] or
  * NULL, zeroed by the caller; also {WAVEAL_ERR_TIMEOUT, site, thread block, thread} when a bounded wait ran out. */
@@ -472,7 +476,7 @@ waveal_status waveal_cache_fork_workspace_bytes(const waveal_cache_desc* cache /
 
 /* The next step's table.  Row b continues row parents[b] of the last one (NULL: row b; negative: a row without pages): it keeps the first
  * keep_len[b] tokens of it and has room for max(keep_len[b], room_len[b]).  So one call lets sequences grow, cuts them back, continues
- * one in several ways, ends some and puts the others in a new order.
+ * one in several ways, ends some, puts the others in a new order, and begins new ones (keep_len 0 of any row).
  *   old_table int32 [old_rows][old_pages], held_len int32 [old_rows]: row r holds the pages of its first held_len[r] tokens (its room, where
  *   it had any).  All old rows let go of their pages, the new rows take theirs:
  *     pages that the kept tokens fill are shared (their counts say by how many);

@@ -142,7 +142,8 @@ def load() -> ctypes.CDLL:
         lib.waveal_cache_compact.argtypes = [P] * 13 + [ctypes.c_size_t, P]
         lib.waveal_cache_copy.argtypes = [P, P, I32] + [P] * 8
         for name in ["waveal_prompt_attn_workspace_bytes", "waveal_prompt_attn", "waveal_cache_fork_workspace_bytes", "waveal_cache_fork",
-                     "waveal_cache_compact_workspace_bytes", "waveal_cache_compact", "waveal_cache_copy", "waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
+                     "waveal_cache_compact_workspace_bytes", "waveal_cache_compact", "waveal_cache_copy",
+                     "waveal_rope_freqs", "waveal_rope", "waveal_cache_append", "waveal_prefix_attn_workspace_bytes", "waveal_prefix_attn",
                      "waveal_plan_workspace_bytes", "waveal_plan_bitmap", "waveal_plan_csr", "waveal_bitmap_to_csr",
                      "waveal_gather_rows", "waveal_scatter_rows", "waveal_bsattn_workspace_bytes", "waveal_bsattn_fwd", "waveal_default_wave_size",
                      "waveal_last_launch_count"]:
@@ -749,7 +750,7 @@ def prompt_attn(q, k, v, seq_start, seq_len=None, o=None, lse=None, return_lse: 
         ws_ptr, size = workspace.data_ptr(), workspace.numel()
         if new_lse:
             lse = _new(stream, lambda: q.new_empty((heads, tokens), dtype=torch.float32))
-    _here(q, k, v, o, lse, seq_start, seq_len, workspace)
+    _here(q, k, v, o, lse, seq_start, seq_len, workspace, dev_status)
     _check(load().waveal_prompt_attn(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), start, lens, scale, ws_ptr, size,
                                      _status(dev_status), _stream(stream)))
     return (o, lse) if return_lse else o
@@ -800,7 +801,7 @@ def cache_fork(cache: PagedCache, page_table, held_len, page_refs, keep_len, roo
     else:
         _check_workspace(workspace)
         ws_ptr, size = workspace.data_ptr(), workspace.numel()
-    _here(cache.k, cache.v, page_table, held_len, page_refs, keep_len, room_len, parents, table_out, refs_out, workspace)
+    _here(cache.k, cache.v, page_table, held_len, page_refs, keep_len, room_len, parents, table_out, refs_out, workspace, dev_status)
     _check(load().waveal_cache_fork(cache.desc, desc, cache.k.data_ptr(), cache.v.data_ptr(), page_table.data_ptr(), held, refs, parent, keep, room,
                                     table_out.data_ptr(), refs_ptr, ws_ptr, size, _status(dev_status), _stream(stream)))
     return table_out, refs_out
@@ -863,6 +864,6 @@ def cache_copy(to: PagedCache, to_pages, source: PagedCache, from_pages, dev_sta
         raise TypeError("the caches must have one type")
     count = to_pages.numel()
     t, f = _ints("to_pages", to_pages, (count,)), _ints("from_pages", from_pages, (count,))
-    _here(to.k, to.v, source.k, source.v, to_pages, from_pages)
+    _here(to.k, to.v, source.k, source.v, to_pages, from_pages, dev_status)
     _check(load().waveal_cache_copy(to.desc, source.desc, count, source.k.data_ptr(), source.v.data_ptr(), to.k.data_ptr(), to.v.data_ptr(), f, t,
                                     _status(dev_status), _stream(stream)))

@@ -83,12 +83,12 @@ __device__ __noinline__ void report(int* status, int code, int site, int where, 
   if (status && atomicCAS(status, 0, code) == 0) status[1] = site, status[2] = where, status[3] = value;
 }
 
-// {first token, tokens}; a malformed sequence has none
+// {first token, tokens}; none of a malformed sequence (-1: its starts are)
 __device__ inline int2 read_sequence(const Params& p, int b, bool tell) {
   const int start = p.seq_start[b], end = p.seq_start[b + 1];
   if (start < 0 || end < start || end > p.tokens) {
     if (tell) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 100, b, start < 0 ? start : end);
-    return make_int2(0, 0);
+    return make_int2(0, -1);
   }
   int n = end - start;
   if (p.seq_len) {
@@ -128,16 +128,55 @@ __device__ __forceinline__ int scan_block(int x, int* shared, int& total) {
 }
 
 __global__ void __launch_bounds__(kPlanThreads, 1) k_prompt_plan(const __grid_constant__ Params p) {
-  __shared__ int count[kPlanThreads], shared[32];
+  __shared__ int count[kPlanThreads], shared[32], malformed;
   waveal::let_next_kernel_start();
   count[threadIdx.x] = 0;
+  if (threadIdx.x == 0) malformed = 0;
   __syncthreads();
   // bucket 0: the longest; the last one: no tokens
   auto bucket = [&](int n) { return kPlanThreads - 1 - min(ceil_div(n, p.tq), kPlanThreads - 1); };
 #pragma unroll 1
-  for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) atomicAdd(&count[bucket(read_sequence(p, b, true).y)], 1);
+  for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) {
+    const int n = read_sequence(p, b, true).y;
+    if (n < 0) malformed = 1;
+    atomicAdd(&count[bucket(max(n, 0))], 1);
+  }
   __syncthreads();
   int total;
+  const bool some_left_out = malformed;
+  if (some_left_out) {
+    // Starts that go back would let sequences claim the same tokens, and make more row tiles than the workspace has places for: a
+    // sequence that begins in front of an earlier start has no tokens either (said in the places of the chains, of which there are more than sequences).
+    int top = -1;
+#pragma unroll 1
+    for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+      const int b = b0 + threadIdx.x, start = b < p.batch ? p.seq_start[b] : -1;
+      __syncthreads();
+      count[threadIdx.x] = start > p.tokens ? -1 : start;
+      __syncthreads();
+#pragma unroll 1
+      for (int d = 1; d < kPlanThreads; d *= 2) {
+        const int y = threadIdx.x >= d ? count[threadIdx.x - d] : -1;
+        __syncthreads();
+        count[threadIdx.x] = max(count[threadIdx.x], y);
+        __syncthreads();
+      }
+      if (b < p.batch) p.plan.again[b] = max(top, count[threadIdx.x]) > start;
+      top = max(top, count[kPlanThreads - 1]);
+    }
+    __syncthreads();
+    count[threadIdx.x] = 0;
+    __syncthreads();
+  }
+  auto sequence = [&](int b) {
+    const int2 q = read_sequence(p, b, false);
+    return q.y <= 0 || (some_left_out && p.plan.again[b]) ? make_int2(0, 0) : q;
+  };
+  if (some_left_out) {
+#pragma unroll 1
+    for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) atomicAdd(&count[bucket(sequence(b).y)], 1);
+    __syncthreads();
+  }
   const int first = scan_block(count[threadIdx.x], shared, total);
   __syncthreads();
   count[threadIdx.x] = first;
@@ -145,7 +184,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_prompt_plan(const __grid_co
   __syncthreads();
 #pragma unroll 1
   for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) {
-    const int2 q = read_sequence(p, b, false);
+    const int2 q = sequence(b);
     p.plan.seq[atomicAdd(&count[bucket(q.y)], 1)] = make_int4(q.x, q.y, 0, 0);
   }
   __syncthreads();
@@ -278,7 +317,8 @@ template <int D> struct Small {
   int verdict[2][kChecks];                           // not every value of the team's masked tile is finite
   uint32_t tmem;
   int abort;
-  int again, last_again;                             // row tiles to be computed again: the last one of the chain (of a warp)
+  int again;                                         // row tiles to be computed again: the last one of the chain
+  int chained[kItems];                               // the row tile that a warp of the results has put into the chain from here, so that no other does
 };
 
 // a ring of tiles as one of its users walks it
@@ -382,7 +422,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps8 = i >= B_P && i < B_O_EMPTY;
       mbar_init(BAR(i), item ? kItemReaders : i == B_DONE ? 20 : warps8 ? 8 : (i >= B_REF && i < B_PV_DONE) || (i >= B_O_EMPTY && i < B_O_FULL) ? 4 : i >= B_PAIR && i < B_CHECK ? 2 : 1);
     }
-    if (lane == 0) sm.abort = 0, sm.again = sm.last_again = -1;
+    if (lane == 0) sm.abort = 0, sm.again = -1;
+    if (lane < kItems) sm.chained[lane] = -1;
     fence_mbar_init();
   } else if (warp == 3 && lane == 0) {
     prefetch_tmap(&tmQ), prefetch_tmap(&tmK), prefetch_tmap(&tmV);
@@ -478,7 +519,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           id = *reinterpret_cast<volatile int*>(&sm.again);
         } else if (id >= 0) {
           const long long ticket = (long long)gridDim.x + __shfl_sync(0xffffffffu, asked, 0);
-          id = again ? p.plan.again[id] : ticket < tickets ? (int)ticket : -1;
+          id = again ? __ldcg(p.plan.again + id) : ticket < tickets ? (int)ticket : -1;
         }
       }
 #pragma unroll 1
@@ -696,9 +737,9 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         }
         if (lse) *lse = sum == 0.f ? -INFINITY : (ref * p.sl2 + __log2f(sum)) * 0.69314718055994531f;
         // O outgrew fp32 (V is very large), or met a value that the row does not see: neither happens in the other way
-        const bool bad = !(sum < kSumLimit) || (ref == -INFINITY && tiles > 1) || !(none0 + none1 == 0.f);
-        // (the four warps are never more than an item apart)
-        if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.last_again, ticket) != ticket)
+        const bool bad = !(sum < kSumLimit) || ref == -INFINITY || !(none0 + none1 == 0.f);
+        // (once: the four warps may be several items apart, so every item's place has its own mark)
+        if (__any_sync(0xffffffffu, bad && live && !safe) && lane == 0 && atomicExch(&sm.chained[at], ticket) != ticket)
           p.plan.again[ticket] = atomicExch(&sm.again, ticket);
         __syncwarp();
         item_done();
@@ -747,65 +788,65 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         uint32_t u[32], w[16];
         const bool cut = j >= masked;
         if (j < plain || cut) {
-        if (cut) {
-          chunks = min(2, (keys - j * kTile - half * 64 + 31) / 32);   // (what is behind the last key is not used)
-          // scores that the row does not see, 16 columns at a time from the first that some row does not see.  (Code that runs once or twice an
-          // item is short: each 128 bytes of it come from beyond the instruction caches.)
-          const int visible = sees - j * kTile, from = max(0, first_sees - j * kTile - half * 64) / 16 * 16;
+          if (cut) {
+            chunks = min(2, (keys - j * kTile - half * 64 + 31) / 32);   // (what is behind the last key is not used)
+            // scores that the row does not see, 16 columns at a time from the first that some row does not see.  (Code that runs once or twice an
+            // item is short: each 128 bytes of it come from beyond the instruction caches.)
+            const int visible = sees - j * kTile, from = max(0, first_sees - j * kTile - half * 64) / 16 * 16;
 #pragma unroll 1
-          for (int c = from; c < 32 * chunks; c += 16) {
-            uint32_t t[16];
-            WAVEAL_TMEM_LD16(h_addr + c, t, 0);
-            WAVEAL_TMEM_WAIT_LD16(t, 0);
+            for (int c = from; c < 32 * chunks; c += 16) {
+              uint32_t t[16];
+              WAVEAL_TMEM_LD16(h_addr + c, t, 0);
+              WAVEAL_TMEM_WAIT_LD16(t, 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (i >= visible - c) t[i] = 0xff800000u;
-            WAVEAL_TMEM_ST16(h_addr + c, t, 0);
-          }
-          tc_wait_st();
-        }
-        if (safe) {
-          float top = -INFINITY;
-#pragma unroll 1
-          for (int c = 0; c < chunks; ++c) {
-            WAVEAL_TMEM_LD32(h_addr + 32 * c, u, 0);
-            WAVEAL_TMEM_WAIT_LD32(u, 0);
-            top = fmaxf(top, row_max32(u));
-          }
-          top = fmaxf(top, exchange(top));
-          if (!ok) break;
-          if (j == 0) {
-            ref = top;
-          } else {
-            if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + team), done++ & 1, 130))) break;   // of the last tile
-            tc_fence_after();
-            const bool grown = live && (top - ref) * sl2 > kGrowth;
-            if (__any_sync(0xffffffffu, grown)) {
-              const float scale = grown ? ex2((ref - top) * sl2) : 1.0f;
-              if (grown) ref = top;
-              s0 *= scale, s1 *= scale, s2 *= scale, s3 *= scale;
-              rescale<D / 2>(tm + G::O_COL + items % G::OS * D + half * (D / 2), scale);
+              for (int i = 0; i < 16; ++i)
+                if (i >= visible - c) t[i] = 0xff800000u;
+              WAVEAL_TMEM_ST16(h_addr + c, t, 0);
             }
+            tc_wait_st();
           }
-        } else if (j == 0) {
-          // the largest of the first 16 scores: both threads of a row find the same
-          uint32_t t[16];
-          WAVEAL_TMEM_LD16(s_addr, t, 0);
-          WAVEAL_TMEM_WAIT_LD16(t, 0);
-          const int visible = sees + half * 64;
-          ref = __uint_as_float(t[0]);
+          if (safe) {
+            float top = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+              WAVEAL_TMEM_LD32(h_addr + 32 * c, u, 0);
+              WAVEAL_TMEM_WAIT_LD32(u, 0);
+              top = fmaxf(top, row_max32(u));
+            }
+            top = fmaxf(top, exchange(top));
+            if (!ok) break;
+            if (j == 0) {
+              ref = top;
+            } else {
+              if (!(ok = warp_wait(ctx, BAR(B_PV_DONE + team), done++ & 1, 130))) break;   // of the last tile
+              tc_fence_after();
+              const bool grown = live && (top - ref) * sl2 > kGrowth;
+              if (__any_sync(0xffffffffu, grown)) {
+                const float scale = grown ? ex2((ref - top) * sl2) : 1.0f;
+                if (grown) ref = top;
+                s0 *= scale, s1 *= scale, s2 *= scale, s3 *= scale;
+                rescale<D / 2>(tm + G::O_COL + items % G::OS * D + half * (D / 2), scale);
+              }
+            }
+          } else if (j == 0) {
+            // the largest of the first 16 scores: both threads of a row find the same
+            uint32_t t[16];
+            WAVEAL_TMEM_LD16(s_addr, t, 0);
+            WAVEAL_TMEM_WAIT_LD16(t, 0);
+            const int visible = sees + half * 64;
+            ref = __uint_as_float(t[0]);
 #pragma unroll
-          for (int i = 1; i < 16; ++i) ref = fmaxf(ref, i < visible ? __uint_as_float(t[i]) : -INFINITY);
-          if (half == 0) {
-            sm.ref[at][r] = ref;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(BAR(B_REF + at));
+            for (int i = 1; i < 16; ++i) ref = fmaxf(ref, i < visible ? __uint_as_float(t[i]) : -INFINITY);
+            if (half == 0) {
+              sm.ref[at][r] = ref;
+              __syncwarp();
+              if (lane == 0) mbar_arrive(BAR(B_REF + at));
+            }
+          } else if (j == 1) {
+            if (!(ok = warp_wait(ctx, BAR(B_REF + at), item_no / kItems & 1, 131))) break;
+            ref = sm.ref[at][r];
           }
-        } else if (j == 1) {
-          if (!(ok = warp_wait(ctx, BAR(B_REF + at), item_no / kItems & 1, 131))) break;
-          ref = sm.ref[at][r];
-        }
-        minus = ref == -INFINITY ? 0.f : -ref * sl2;
+          minus = ref == -INFINITY ? 0.f : -ref * sl2;
         }
 #pragma unroll 1
         for (int n = 0; n < chunks; ++n) {
@@ -867,13 +908,17 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
 // ------------------------------------------------------------------ host
 
+// A dimension with one entry: its stride says nothing.
+bool one_entry(const waveal_prompt_desc* d, int heads, int dim) { return (dim ? d->tokens : heads) <= 1; }
+
 // [tokens][heads][channels] in boxes of 64 channels
 waveal_status make_map(CUtensorMap* tm, const waveal_prompt_desc* d, const void* base, int heads, const int64_t* stride, int box_heads, int box_tokens,
                        const char* what) {
   const auto enc = waveal::tensor_map_encoder();
   if (!enc) return waveal::fail(WAVEAL_ERR_CUDA, "cuTensorMapEncodeTiled entry point not available");
   const cuuint64_t dims[3] = {(cuuint64_t)d->head_dim, (cuuint64_t)heads, (cuuint64_t)d->tokens};
-  const cuuint64_t bytes[2] = {(cuuint64_t)stride[0] * 2, (cuuint64_t)stride[1] * 2};
+  cuuint64_t bytes[2];
+  for (int i = 0; i < 2; ++i) bytes[i] = (cuuint64_t)(one_entry(d, heads, i) ? d->head_dim : stride[i]) * 2;
   const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens}, one[3] = {1, 1, 1};
   const CUresult r = enc(tm, d->dtype == WAVEAL_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base),
                          dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -908,12 +953,12 @@ waveal_status check(const waveal_prompt_desc* d) {
   if (d->flags & ~(WAVEAL_PROMPT_CAUSAL | WAVEAL_PROMPT_SELFTEST_LOST_TILE)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "unknown flags 0x%x", d->flags);
   if (most_tickets(d) > 1000000000ll) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 10^9 row tiles (of every sequence and key head)");
   if ((long long)d->tokens * d->q_heads > 1000000000ll) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 10^9 rows (tokens * q_heads)");
+  // (one item takes all keys of its sequence: every wait for its end stays far below the limit)
+  if (d->tokens > 1 << 25) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^25 tokens");
   const int64_t* strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
-#pragma unroll 1
-  for (const int64_t* s : strides)
-#pragma unroll 1
+  for (int t = 0; t < 4; ++t)
     for (int i = 0; i < 2; ++i)
-      if (s[i] % 8 || s[i] < 0) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "strides must be multiples of 8 elements (16 bytes) and not negative");
+      if (!one_entry(d, t == 1 || t == 2 ? d->kv_heads : d->q_heads, i) && (strides[t][i] % 8 || strides[t][i] < 0)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "strides must be multiples of 8 elements (16 bytes) and not negative");
   return WAVEAL_OK;
 }
 
@@ -955,6 +1000,7 @@ extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const v
   if (!q || !k || !v || !o || !seq_start) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q, k, v, o and seq_start are required");
   if (!waveal::aligned(q, 16) || !waveal::aligned(k, 16) || !waveal::aligned(v, 16) || !waveal::aligned(o, 16))
     return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q, k, v and o must be 16-byte aligned");
+  if (o == q || o == k || o == v) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "o must not overlap q, k or v");
   const Layout l = layout(d);
   if (!ws || ws_bytes < l.bytes) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, l.bytes);
   if (!waveal::aligned(ws, 256)) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace must be 256-byte aligned");
@@ -970,7 +1016,8 @@ extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const v
   p.plan.again = reinterpret_cast<int*>(w + l.again);
   p.seq_start = seq_start, p.seq_len = seq_len;
   p.o = o, p.lse = lse, p.o_stride_h = d->o_stride[0], p.o_stride_t = d->o_stride[1];
-  p.wide_o = waveal::aligned(o, 32) && d->o_stride[0] % 16 == 0 && d->o_stride[1] % 16 == 0;
+  p.wide_o = waveal::aligned(o, 32);
+  for (int i = 0; i < 2; ++i) p.wide_o = p.wide_o && (one_entry(d, d->q_heads, i) || d->o_stride[i] % 16 == 0);
   p.dev_status = dev_status;
   p.drop_tile = d->flags & WAVEAL_PROMPT_SELFTEST_LOST_TILE ? 1 : 0;
   p.wait_limit = p.drop_tile ? kSelfTestCycles : kTimeoutCycles;

@@ -36,7 +36,7 @@ def prompt(lib, pointers=None, ws=0x100000, ws_bytes=1 << 40, **kw):
 
 @pytest.mark.parametrize("kw, status", [
     (dict(batch=-1), 1), (dict(tokens=-1), 1), (dict(q_heads=0), 1), (dict(kv_heads=0), 1), (dict(q_heads=7), 1), (dict(q_heads=258), 1), (dict(head_dim=96), 2),
-    (dict(head_dim=256), 2), (dict(dtype=wb.FP32), 2), (dict(dtype=-1), 2), (dict(flags=2), 1), (dict(tokens=1 << 28), 2), (dict(batch=600_000_000), 2),
+    (dict(head_dim=256), 2), (dict(dtype=wb.FP32), 2), (dict(dtype=-1), 2), (dict(flags=2), 1), (dict(tokens=1 << 28), 2), (dict(tokens=(1 << 25) + 1), 2), (dict(batch=600_000_000), 2),
     (dict(q_stride=(128, 1020)), 1), (dict(k_stride=(4, 256)), 1), (dict(v_stride=(128, -256)), 1), (dict(o_stride=(130, 1024)), 1)])
 def test_prompt_refused(lib, kw, status):
     got, d = prompt(lib, **kw)
@@ -51,6 +51,8 @@ def test_prompt_refuses_pointers_and_workspace(lib):
         assert prompt(lib, [None if i == j else p for j, p in enumerate(good)])[0] == wb.ERR_INVALID_ARG, i
     for i in range(4):
         assert prompt(lib, [p + 8 if i == j else p for j, p in enumerate(good)])[0] == wb.ERR_INVALID_ARG, i
+    for i in range(3):                                                # the results over an input
+        assert prompt(lib, [good[i] if j == 3 else p for j, p in enumerate(good)])[0] == wb.ERR_INVALID_ARG, i
     assert prompt(lib, ws=None)[0] == prompt(lib, ws_bytes=100)[0] == prompt(lib, ws=0x100010)[0] == wb.ERR_WORKSPACE
     assert lib.waveal_prompt_attn(None, *good, 0.0, 0x100000, 1 << 40, None, None) == wb.ERR_INVALID_ARG
     assert prompt(lib, [None] * 7, ws=None, tokens=0)[0] == prompt(lib, [None] * 7, ws=None, batch=0)[0] == wb.OK
@@ -58,6 +60,15 @@ def test_prompt_refuses_pointers_and_workspace(lib):
     d = prompt(lib, ws=None)[1]
     assert lib.waveal_prompt_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(n)) == wb.OK and n.value >= 2 * 16
     assert lib.waveal_prompt_attn_workspace_bytes(ctypes.byref(d), None) == wb.ERR_INVALID_ARG
+
+
+def test_the_stride_of_a_dimension_with_one_entry_is_not_looked_at(lib):
+    n = ctypes.c_size_t(0)
+    odd = dict(q_stride=(3, -5), k_stride=(1, 1), v_stride=(0, 7), o_stride=(9, 9))
+    for kw, status in ((dict(tokens=1, q_heads=1, kv_heads=1, **odd), wb.OK), (dict(tokens=1, q_heads=2, kv_heads=1, **odd), wb.ERR_INVALID_ARG),
+                       (dict(tokens=2, q_heads=1, kv_heads=1, **odd), wb.ERR_INVALID_ARG)):
+        d = prompt(lib, ws=None, **kw)[1]
+        assert lib.waveal_prompt_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(n)) == status
 
 
 def cache_desc(**kw):
