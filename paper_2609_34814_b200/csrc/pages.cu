@@ -153,14 +153,20 @@ __device__ __forceinline__ void copy_counts(int* to, const int* from, int n, int
 #pragma unroll 1
   for (int i = done + tid; i < n; i += threads) to[i] = __ldg(from + i);
 }
+// LOCAL: in shared memory
+template <bool LOCAL, class T> __device__ __forceinline__ T load_state(const T* at) {
+  if constexpr (LOCAL) return *at;
+  else return __ldcg(at);
+}
 // eight counts from i on (those from `end` on: `none`)
-__device__ __forceinline__ void load_counts(const int* counts, int i, int end, bool four, int none, int (&v)[8]) {
+template <bool LOCAL = false> __device__ __forceinline__ void load_counts(const int* counts, int i, int end, bool four, int none, int (&v)[8]) {
   if (four && i + 8 <= end) {
-    const int4 a = __ldcg(reinterpret_cast<const int4*>(counts + i)), b = __ldcg(reinterpret_cast<const int4*>(counts + i + 4));
+    const int4* at = reinterpret_cast<const int4*>(counts + i);
+    const int4 a = load_state<LOCAL>(at), b = load_state<LOCAL>(at + 1);
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = i + k < end ? __ldcg(counts + i + k) : none;
+    for (int k = 0; k < 8; ++k) v[k] = i + k < end ? load_state<LOCAL>(counts + i + k) : none;
   }
 }
 
@@ -198,18 +204,39 @@ __device__ __forceinline__ int held_tokens(const ForkParams& p, int r) {
   return n < 0 || n > (long long)p.old_pages << p.shape.shift ? 0 : n;
 }
 
+// What the phases hand on (counts, rows): LOCAL, where one thread block decides, in shared memory (eight phases read in turn what the one before has
+// written: 10.5 us of 16 rows of 63 pages instead of 12.6 through L2, 19.5 of 64 rows in beams instead of 21.6), else in the results and the workspace.
+struct ForkState {
+  int *refs, *ends, *count, *fewest, *most;
+  int4* row;
+  int2* last;
+};
+__host__ __device__ inline size_t fork_state_bytes(long long n_pages, long long old_rows, long long rows) {
+  return (size_t)(rows * (sizeof(int4) + sizeof(int2)) + (2 * ((n_pages + 3) / 4 * 4) + 3 * old_rows) * sizeof(int));
+}
+
+template <bool LOCAL>
 __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_constant__ ForkParams p) {
   __shared__ int shared[33], list[kPlanThreads * kPerThread];
+  extern __shared__ __align__(16) unsigned char local[];
+  ForkState s = {p.new_refs, p.ends, p.kids, p.kids + p.old_rows, p.kids + 2 * p.old_rows, p.row, p.last};
+  if constexpr (LOCAL) {
+    const int n = (p.n_pages + 3) / 4 * 4;
+    s.row = reinterpret_cast<int4*>(local);
+    s.refs = reinterpret_cast<int*>(s.row + p.rows);
+    s.ends = s.refs + n;
+    s.last = reinterpret_cast<int2*>(s.ends + n);
+    s.count = reinterpret_cast<int*>(s.last + p.rows), s.fewest = s.count + p.old_rows, s.most = s.fewest + p.old_rows;
+  }
   waveal::let_next_kernel_start();
   const int tid = blockIdx.x * kPlanThreads + threadIdx.x, threads = gridDim.x * kPlanThreads;
   const int warp = tid / 32, warps = threads / 32, lane = threadIdx.x & 31;
   const int shift = p.shape.shift, mask = (1 << shift) - 1;
-  int *count = p.kids, *fewest = p.kids + p.old_rows, *most = p.kids + 2 * p.old_rows;
 
-  copy_counts(p.new_refs, p.refs, p.n_pages, tid, threads);
+  copy_counts(s.refs, p.refs, p.n_pages, tid, threads);
 #pragma unroll 1
   for (int r = tid; r < p.old_rows; r += threads) {
-    count[r] = 0, fewest[r] = INT_MAX, most[r] = 0;
+    s.count[r] = 0, s.fewest[r] = INT_MAX, s.most[r] = 0;
     const int n = p.held[r];
     if (n < 0 || n > (long long)p.old_pages << shift) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 81, r, n);
   }
@@ -233,15 +260,15 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
           report(p.dev_status, WAVEAL_ERR_BAD_MASK, 84, b, page);
           page = -1;
         } else {
-          p.ends[page] = INT_MAX;
+          s.ends[page] = INT_MAX;
         }
       }
-      atomicAdd(count + parent, 1);
-      atomicMin(fewest + parent, row.y);
-      atomicMax(most + parent, row.y);
+      atomicAdd(s.count + parent, 1);
+      atomicMin(s.fewest + parent, row.y);
+      atomicMax(s.most + parent, row.y);
     }
-    p.row[b] = row;
-    p.last[b] = {page, 0};
+    s.row[b] = row;
+    s.last[b] = {page, 0};
   }
   sync_plan();
 
@@ -250,59 +277,59 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
 #pragma unroll 1
   for (long long u = warp; u < (long long)p.old_rows * old_runs; u += warps) {
     const int r = (int)(u / old_runs), run = (int)(u - (long long)r * old_runs);
-    const int kids = __ldcg(count + r), all = kids ? __ldcg(fewest + r) : 0, pages = (int)(((long long)held_tokens(p, r) + mask) >> shift);
+    const int kids = load_state<LOCAL>(s.count + r), all = kids ? load_state<LOCAL>(s.fewest + r) : 0, pages = (int)(((long long)held_tokens(p, r) + mask) >> shift);
 #pragma unroll 4
     for (int j = max(run * kRun, kids == 1 ? all : 0) + lane; j < min(pages, (run + 1) * kRun); j += 32) {
       const int change = (j < all ? kids : 0) - 1, page = p.old_table[r * p.old_stride + j];
-      if (change && page >= 0 && page < p.n_pages) atomicAdd(p.new_refs + page, change);
+      if (change && page >= 0 && page < p.n_pages) atomicAdd(s.refs + page, change);
     }
   }
 #pragma unroll 1
   for (long long u = warp; u < (long long)p.rows * runs; u += warps) {
     const int b = (int)(u / runs), run = (int)(u - (long long)b * runs);
-    const int4 row = __ldcg(p.row + b);
+    const int4 row = load_state<LOCAL>(s.row + b);
     if (row.x < 0) continue;
 #pragma unroll 4
-    for (int j = max(run * kRun, __ldcg(fewest + row.x)) + lane; j < min(row.y, (run + 1) * kRun); j += 32) {
+    for (int j = max(run * kRun, load_state<LOCAL>(s.fewest + row.x)) + lane; j < min(row.y, (run + 1) * kRun); j += 32) {
       const int page = p.old_table[row.x * p.old_stride + j];
-      if (page >= 0 && page < p.n_pages) atomicAdd(p.new_refs + page, 1);
+      if (page >= 0 && page < p.n_pages) atomicAdd(s.refs + page, 1);
     }
   }
 #pragma unroll 1
   for (int b = tid; b < p.rows; b += threads) {
-    const int page = __ldcg(p.last + b).x;
-    if (page >= 0) atomicMin(p.ends + page, b);
+    const int page = load_state<LOCAL>(s.last + b).x;
+    if (page >= 0) atomicMin(s.ends + page, b);
   }
   sync_plan();
 
   // ---- a page filled in part stays with the first row that ends in it, if nobody else holds it
 #pragma unroll 1
   for (int b = tid; b < p.rows; b += threads) {
-    int4 row = __ldcg(p.row + b);
-    const int page = __ldcg(p.last + b).x;
+    int4 row = load_state<LOCAL>(s.row + b);
+    const int page = load_state<LOCAL>(s.last + b).x;
     bool stays = row.w && page < 0;                  // (no page to copy from: the row gets -1 there)
-    if (page >= 0 && __ldcg(p.ends + page) == b && __ldcg(p.new_refs + page) <= 0) {
+    if (page >= 0 && load_state<LOCAL>(s.ends + page) == b && load_state<LOCAL>(s.refs + page) <= 0) {
       stays = true;
-      p.new_refs[page] = 1;
+      s.refs[page] = 1;
     }
-    if (stays) p.row[b].w = row.w | kStays;
-    p.last[b].y = row.z - row.y - stays;             // fresh pages
+    if (stays) s.row[b].w = row.w | kStays;
+    s.last[b].y = row.z - row.y - stays;             // fresh pages
   }
   sync_plan();
 
   // ---- sums of the blocks' parts: free pages, fresh pages
   const Part pages = part_of(p.n_pages), rows = part_of(p.rows);
   int free_here = 0, need_here = 0, total;
-  const bool four = by_four(p.new_refs, p.new_refs);
+  const bool four = LOCAL || by_four(s.refs, s.refs);
 #pragma unroll 2
   for (int i = pages.begin + threadIdx.x * kPerThread; i < pages.end; i += kPlanThreads * kPerThread) {
     int v[kPerThread];
-    load_counts(p.new_refs, i, pages.end, four, 1, v);
+    load_counts<LOCAL>(s.refs, i, pages.end, four, 1, v);
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) free_here += v[k] <= 0;
   }
 #pragma unroll 1
-  for (int b = rows.begin + threadIdx.x; b < rows.end; b += kPlanThreads) need_here += __ldcg(p.last + b).y;
+  for (int b = rows.begin + threadIdx.x; b < rows.end; b += kPlanThreads) need_here += load_state<LOCAL>(s.last + b).y;
   scan_block(free_here, shared, total);
   if (threadIdx.x == 0) p.sums[blockIdx.x] = total;
   scan_block(need_here, shared, total);
@@ -320,11 +347,11 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
   // ---- where every row's fresh pages begin, and which pages these are
 #pragma unroll 1
   for (int b0 = rows.begin; b0 < rows.end; b0 += kPlanThreads) {
-    const int b = b0 + threadIdx.x, need = b < rows.end ? __ldcg(p.last + b).y : 0;
+    const int b = b0 + threadIdx.x, need = b < rows.end ? load_state<LOCAL>(s.last + b).y : 0;
     const int begin = need_before + scan_block(need, shared, total);
     need_before += total;
     if (b < rows.end) {
-      p.last[b].y = begin;
+      s.last[b].y = begin;
       if (begin <= free_all && begin + need > free_all) report(p.dev_status, WAVEAL_ERR_NO_PAGES, 85, b, need_all - free_all);
     }
   }
@@ -332,7 +359,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
   for (int i0 = pages.begin; i0 < pages.end && free_before < need_all; i0 += kPlanThreads * kPerThread) {
     const int i = i0 + threadIdx.x * kPerThread;
     int v[kPerThread];
-    load_counts(p.new_refs, min(i, pages.end), pages.end, four, 1, v);
+    load_counts<LOCAL>(s.refs, min(i, pages.end), pages.end, four, 1, v);
     unsigned is_free = 0;
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) is_free |= (unsigned)(v[k] <= 0) << k;
@@ -347,18 +374,28 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
       }
     if (is_free) {
       if (four && i + kPerThread <= pages.end) {
-        int4* to = reinterpret_cast<int4*>(p.new_refs + i);
+        int4* to = reinterpret_cast<int4*>(s.refs + i);
         to[0] = make_int4(v[0], v[1], v[2], v[3]), to[1] = make_int4(v[4], v[5], v[6], v[7]);
       } else {
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k)
-          if (i + k < pages.end) p.new_refs[i + k] = v[k];
+          if (i + k < pages.end) s.refs[i + k] = v[k];
       }
     }
     __syncthreads();
 #pragma unroll 1
     for (int k = threadIdx.x; k < take; k += kPlanThreads) p.fresh[free_before + k] = list[k];
     free_before += total;
+  }
+  if constexpr (LOCAL) {
+    __syncthreads();
+    const bool wide = by_four(p.new_refs, p.new_refs);
+#pragma unroll 1
+    for (int i = tid; wide && i < p.n_pages / 4; i += threads) reinterpret_cast<int4*>(p.new_refs)[i] = reinterpret_cast<int4*>(s.refs)[i];
+#pragma unroll 1
+    for (int i = (wide ? p.n_pages / 4 * 4 : 0) + tid; i < p.n_pages; i += threads) p.new_refs[i] = s.refs[i];
+#pragma unroll 1
+    for (int b = tid; b < p.rows; b += threads) p.row[b] = s.row[b], p.last[b] = s.last[b];
   }
 }
 
@@ -558,25 +595,37 @@ unsigned copy_grid(long long turns) {
   return (unsigned)std::max(1ll, std::min(blocks, (long long)waveal::sm_count() * kCopyBlocks));
 }
 
-// thread blocks that decide: one up to 8,192 pages or as many table entries, where a barrier of the cluster costs more than it saves
-int plan_blocks(long long pages, long long entries) {
-  int n = 1;
-  while (n < kCluster && std::max(pages, entries) / 8192 >= 2 * n) n *= 2;
-  return n;
-}
+constexpr size_t kLocalBytes = 192 << 10;           // (beside the 32 KB and more of the kernel's own)
+
+// Thread blocks that decide about a fork: one with its state in shared memory, a cluster of eight or of sixteen, by the counts and table entries that they walk
+// through.  us of growing / forking a table of 64 rows, half of the pool in it:
+//   pages                    one           eight         sixteen
+//   1,024                    10.9 / 11.8   16.2 / 16.7   20.7 / 21.3
+//   16,384                   13.6 / 14.6   17.1 / 19.3   21.8 / 24.0
+//   32,768                   does not fit  17.6 / 22.1   21.9 / 26.5   (one, its state in L2: 18.9 / 27.5)
+//   131,072                                21.0 / 27.6   24.9 / 31.4   (35.6 / 69.5)
+//   327,680                                24.9 / 40.6   26.1 / 34.9   (64 / 151)
+// 10,000 pages, 64 rows of 1,024 entries: 17.1 / 21.7, 17.9 / 21.3, 22.4 / 26.1; 8,192 pages, 256 rows of 512: 24.8 / 44.6, 19.8 / 26.3, 23.6 / 29.4.  Two and
+// four are never more than 1 us ahead of the better neighbour.
+int fork_blocks(long long work, size_t state) { return work <= 65536 && state <= kLocalBytes ? 1 : work <= 400000 ? 8 : 16; }
+// The same for compacting, us with the copies of half of the pool's small pages: 1,024 pages 7.3 (one), 8.5 (eight), 9.8 (sixteen); 4,096 11.7, 9.4, 11.0;
+// 16,384 29.0, 13.2, 13.3; 32,768 52, 17.8, 16.7; 131,072 188, 46, 36.
+int compact_blocks(long long pages) { return pages <= 2048 ? 1 : pages <= 16384 ? 8 : 16; }
 
 template <class P>
-waveal_status launch_plan(void (*kernel)(P), const P& p, int blocks, cudaStream_t st) {
-  static bool set[64] = {};                          // (one for each kernel: more than eight blocks a cluster have to be asked for)
+waveal_status launch_plan(void (*kernel)(P), bool (&set)[64], const P& p, int blocks, size_t smem, cudaStream_t st) {
   int dev = 0;
   WAVEAL_CUDA_OK(cudaGetDevice(&dev));
-  if (blocks > 8 && (dev >= 64 || !set[dev])) {
-    WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  // more than eight blocks a cluster, and more than 48 KB, have to be asked for (set: of this kernel, by device)
+  if ((blocks > 8 || smem) && (dev >= 64 || !set[dev])) {
+    if (smem) WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLocalBytes));
+    else WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     if (dev < 64) set[dev] = true;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kPlanThreads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -712,7 +761,10 @@ extern "C" waveal_status waveal_cache_fork(const waveal_cache_desc* c, const wav
   p.dev_status = dev_status;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const long long entries = (long long)f->old_rows * f->old_pages;
-  if (waveal_status e = launch_plan(k_fork_plan, p, plan_blocks(c->n_pages, entries), st)) return e;
+  static bool set[2][64] = {};
+  const size_t state = fork_state_bytes(c->n_pages, f->old_rows, f->rows);
+  const int blocks = fork_blocks(c->n_pages + entries, state);
+  if (waveal_status e = blocks == 1 ? launch_plan(k_fork_plan<true>, set[1], p, 1, state, st) : launch_plan(k_fork_plan<false>, set[0], p, blocks, 0, st)) return e;
   const unsigned grid = copy_grid((long long)f->rows * (2 * p.shape.segments + (f->pages + kRun - 1) / kRun));
   if (wide) WAVEAL_CUDA_OK(waveal::launch_chained(k_fork_apply<uint4>, dim3(grid), kCopyThreads, 0, st, p));
   else WAVEAL_CUDA_OK(waveal::launch_chained(k_fork_apply<unsigned short>, dim3(grid), kCopyThreads, 0, st, p));
@@ -758,7 +810,8 @@ extern "C" waveal_status waveal_cache_compact(const waveal_cache_desc* c, const 
   p.sums = reinterpret_cast<int*>(w + l.sums), p.first = p.sums + kCluster;
   p.from = reinterpret_cast<int*>(w + l.from), p.to = reinterpret_cast<int*>(w + l.to);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (waveal_status e = launch_plan(k_compact_plan, p, plan_blocks(c->n_pages, 0), st)) return e;
+  static bool set[64] = {};
+  if (waveal_status e = launch_plan(k_compact_plan, set, p, compact_blocks(c->n_pages), 0, st)) return e;
   // (how many pages move is known on the device only: half of the pool at most)
   const unsigned grid = copy_grid((long long)(c->n_pages / 2) * 2 * p.shape.segments + (long long)d->rows * ((d->pages + kRun - 1) / kRun));
   if (wide) WAVEAL_CUDA_OK(waveal::launch_chained(k_compact_apply<uint4>, dim3(grid), kCopyThreads, 0, st, p));

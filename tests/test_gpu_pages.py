@@ -46,9 +46,11 @@ def wishes(pool, rows, seed, grow=50):
     (1, 0, 16, 1, {}), (1, 1, 16, 1, {}), (1, 16, 16, 3, {}), (1, 17, 16, 2, {}), (5, 100, 16, 5, {}), (5, 100, 32, 40, {}), (40, 300, 16, 3, {}),
     (7, 500, 64, 9, dict(token_major=True)), (6, 1000, 256, 30, dict(heads=5, dim=128)), (9, 300, 16, 12, dict(heads=1, dim=96, dtype=torch.float16)),
     (9, 300, 32, 12, dict(heads=3, dim=20)), (4, 200, 16, 12, dict(dim=2, heads=1)), (300, 900, 16, 350, dict(heads=1)), (1500, 60, 16, 1400, dict(heads=1, dim=8)),
-    (3, 30000, 16, 6, dict(heads=1, dim=8)), (64, 9000, 16, 64, dict(heads=1, dim=8))])
+    (3, 30000, 16, 6, dict(heads=1, dim=8)), (64, 9000, 16, 64, dict(heads=1, dim=8)), (200, 9000, 16, 210, dict(heads=1, dim=8)),
+    (600, 9000, 16, 500, dict(heads=1, dim=8)), (4, 200, 16, 12, dict(heads=1, dim=8, spare=800.0)), (4, 200, 16, 12, dict(heads=1, dim=8, spare=4000.0)),
+    (4, 200, 16, 12, dict(heads=1, dim=8, spare=15000.0)), (30, 2000, 16, 33, dict(heads=1, dim=8, spare=2.0))])
 def test_fork(rows, most, page, new_rows, kw):
-    pool = Pool(rows, most, page=page, spare=3.0 if new_rows > rows else 1.5, seed=rows + most, **kw)
+    pool = Pool(rows, most, page=page, seed=rows + most, **{"spare": 3.0 if new_rows > rows else 1.5, **kw})
     free = sum(n == 0 for n in pool.refs)
     for seed in range(3):
         parents, keep, room = wishes(pool, new_rows, seed)
@@ -194,7 +196,8 @@ def test_malformed(what, site, row, value):
 
 @pytest.mark.parametrize("rows, most, page, spare, kw", [
     (1, 1, 16, 0.0, {}), (3, 100, 16, 0.5, {}), (3, 100, 16, 20.0, {}), (40, 400, 32, 1.0, dict(token_major=True)), (9, 3000, 256, 0.7, dict(heads=3, dim=128)),
-    (20, 300, 16, 1.0, dict(heads=3, dim=20)), (500, 900, 16, 0.3, dict(heads=1, dim=8)), (300, 9000, 16, 2.0, dict(heads=1, dim=8)), (5, 100, 16, 1.0, dict(offset=1))])
+    (20, 300, 16, 1.0, dict(heads=3, dim=20)), (500, 900, 16, 0.3, dict(heads=1, dim=8)), (300, 9000, 16, 2.0, dict(heads=1, dim=8)), (5, 100, 16, 1.0, dict(offset=1)),
+    (60, 900, 16, 1.5, dict(heads=1, dim=8)), (60, 900, 16, 3.0, dict(heads=1, dim=8, offset=1)), (150, 900, 16, 5.0, dict(heads=1, dim=8, offset=1))])
 def test_compact(rows, most, page, spare, kw):
     offset = kw.get("offset", 0)
     pool = Pool(rows, most, page=page, spare=spare, seed=rows + page, **kw)
