@@ -1,18 +1,31 @@
 // Attention of whole prompts: every token over its own sequence, causal or not, grouped heads, any lengths in one call.
 //
-//   o[h, t] = sum_j p_j v_j / sum_j p_j,   p_j = 2^(sl2 (q[h, t] . k_j - m)),   sl2 = scale log2(e),   j over what token t sees,
-// with m a running reference of the row (online softmax: the reference follows the row's maximum only when it has been outgrown by
-// more than 2^8, which the same reference in the sum makes exact).
+//   o[h, t] = sum_j p_j v_j / sum_j p_j,   p_j = 2^(sl2 (q[h, t] . k_j - m)),   sl2 = scale log2(e),   j over what token t sees.
+// Any m gives the same o as long as nothing overflows or vanishes.  A row's m is the largest of its first 16 scores, so that no tile of keys
+// waits for another one's maximum; what overflows shows in the results, and such a row tile is computed again with maxima of every tile (m
+// follows when a maximum has outgrown it by more than 2^8, O and the sum are scaled).
 //
 // A row tile is 128 rows of S: tq = 128 / G tokens with the G query heads that share a key head, so that a key head's tiles are
-// loaded once for all of them and the causal diagonal crosses few of a tile's columns.  A thread block takes row tiles one after another,
-// and their key tiles of 128 as one stream:
+// loaded once for all of them and the causal diagonal crosses few of a tile's columns.  A thread block takes row tiles one after another (a ticket
+// each, the ones with most keys first), and their key tiles of 128 as one stream:
 //   S = Q K^T (one of three buffers in tensor memory) -> exponentials, P over S's columns -> O += P V (tensor memory).
 // Two teams of eight warps take the tiles of the stream in turn, also across row tiles: one row tile's end (its last products, its
 // results on their way out) runs beside the next one's first tiles.
 //
 // Warps: 0-7 and 8-15 the teams (two threads a row, 64 keys of a tile each: a warp by itself issues an instruction in four clocks, so
 // that four of them a scheduler are needed), 16 items, Q and K, 17 and 18 products, 19 V, 20-23 results.
+//
+// What bounds it: a tile of 128 x 128 at head_dim 128 is 1,024 clk of the tensor pipe and 1,024 clk of the exponentials' unit, and takes 1,370 to
+// 1,425; the rest is the way round of a buffer (products, 1,950 clk of a team's softmax, products) through three buffers, which is all that tensor
+// memory holds beside O.  32,760 causal tokens, 32 query and 8 key heads: 6.2 to 6.6 ms by the GPU (1,330 to 1,410 TFLOP/s, 80 to 85 % of the best library product),
+// 6.8 to 7.4 ms in a row of calls under the power cap.  Sixteen prompts of 20 to 2,000 tokens: 166 us; six frames of 1,560 tokens and 40 heads: 281 us (1,060
+// TFLOP/s); 150 prompts of up to 700 tokens at head_dim 64: 207 us: row tiles of one to eleven key tiles, where a team needs 2,100 to 2,700 clk for a row tile's
+// first or last tile (reference, mask, exponentials) and 700 to get to the next one, so that two teams finish a tile in 1,700.
+// The same 32,760 tokens on the way here: the row's scores in registers of one thread, 11.4 ms (its code did not fit the instruction caches: 4.2 warps
+// an issue waited for instructions); rolled loops that read S twice, 8.5; products issued by two warps, 7.9; two threads a row, 7.2; three buffers and
+// one stream, 6.8; results by warps of their own, 6.7; tiles without a mask or a first score apart, 6.55.  Without gain: polynomials for an eighth to three
+// eighths of the exponentials, waits that sleep, results through shared memory, loads of S ahead of their use in pieces of 16 columns, masks applied in
+// registers, items made by a warp of their own (a 25th: all have 72 registers then), products of a cut tile without a loop.
 //
 // Values that a token must not see: their probabilities are zero, but zero times NaN is not.  A row tile whose results are not finite is computed
 // again: then warp 19 writes zeros over what lies behind a sequence's end and looks through the values of tiles that the causal mask cuts; where one is
@@ -127,6 +140,7 @@ __device__ __forceinline__ int scan_block(int x, int* shared, int& total) {
   return upto - x + (warp ? before : 0);
 }
 
+// One thread block sorts the sequences and adds up their row tiles: latency, hidden in part behind the start of the attention kernel's blocks.
 __global__ void __launch_bounds__(kPlanThreads, 1) k_prompt_plan(const __grid_constant__ Params p) {
   __shared__ int count[kPlanThreads], shared[32], malformed;
   waveal::let_next_kernel_start();
@@ -215,22 +229,36 @@ struct Item {
   long long o;             // the first token and query head in o
 };
 
+// 32 of the planned sequences, one a lane, from number `base` on.  A thread block's tickets ascend, so that most of them fall among those that the loading
+// warp holds already: a search in memory is three loads one after the other, which cost 2,400 of an item's 5,500 clk where items are short.
+struct Window {
+  int4 seq;
+  int base;
+};
+
 // Row tile number `ticket` (a whole warp calls it): sequence by sequence, the ones with most keys first, all key heads of a place after each other.
-__device__ inline void make_item(const Params& p, int sequences, int ticket, Item& im, int lane) {
+__device__ inline void make_item(const Params& p, int sequences, int ticket, Window& win, Item& im, int lane) {
   const int u = ticket / p.kv_heads;
   im.end = 0, im.safe = 0, im.ticket = ticket;
   im.head = ticket - u * p.kv_heads;
-  // the last sequence that begins at u or in front of it: every step cuts the range to a 32nd
-  int lo = 0, hi = sequences;
+  // the last sequence that begins at u or in front of it
+  uint32_t in = __ballot_sync(0xffffffffu, win.base + lane < sequences && win.seq.z <= u);
+  if (in == 0 || (in == 0xffffffffu && win.base + 32 < sequences)) {
+    // (every step cuts the range to a 32nd)
+    int lo = 0, hi = sequences;
 #pragma unroll 1
-  while (hi - lo > 1) {
-    const int step = ceil_div(hi - lo, 32), at = lo + lane * step;
-    const bool in = at < hi && __ldcg(p.plan.seq + at).z <= u;
-    const int last = 31 - __clz(__ballot_sync(0xffffffffu, in));
-    hi = min(hi, lo + (last + 1) * step);
-    lo += last * step;
+    while (hi - lo > 1) {
+      const int step = ceil_div(hi - lo, 32), at = lo + lane * step;
+      const int last = 31 - __clz(__ballot_sync(0xffffffffu, at < hi && __ldcg(&p.plan.seq[at].z) <= u));
+      hi = min(hi, lo + (last + 1) * step);
+      lo += last * step;
+    }
+    win.base = lo;
+    win.seq = __ldcg(p.plan.seq + min(lo + lane, sequences - 1));
+    in = 1;
   }
-  const int4 q = __ldcg(p.plan.seq + lo);
+  const int from = 31 - __clz(in);
+  const int4 q = make_int4(__shfl_sync(0xffffffffu, win.seq.x, from), __shfl_sync(0xffffffffu, win.seq.y, from), __shfl_sync(0xffffffffu, win.seq.z, from), 0);
   const int first = (ceil_div(q.y, p.tq) - 1 - (u - q.z)) * p.tq;
   im.n = min(p.tq, q.y - first);
   im.token = q.x + first;
@@ -461,6 +489,8 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       Ring<G::NKS> ring;
       uint32_t k_no = 0, q_no = 0;
       waveal::wait_for_previous_kernel();
+      Window win;
+      win.base = 0, win.seq = __ldcg(p.plan.seq + min(lane, p.batch - 1));
       const long long tickets = (long long)__ldcg(p.plan.head) * p.kv_heads;
       const int sequences = __ldcg(p.plan.head + 2);
       // first every row tile, then a word to say that these were all, then those that are to be computed again, then the end
@@ -474,7 +504,7 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         int asked = 0;
         if (id >= 0) {
           if (lane == 0 && !again) asked = atomicAdd(p.plan.head + 1, 1);   // (used when this item's tiles have been asked for)
-          make_item(p, sequences, id, next, lane);
+          make_item(p, sequences, id, win, next, lane);
           next.safe = again;
           next.teams = next.tiles > 1 && !again ? 3 : 1 << g2;
           if (!again) g2 = (g2 + next.tiles) & 1;
