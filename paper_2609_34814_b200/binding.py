@@ -665,16 +665,17 @@ def _workspace_bytes(query, *descs):
     return n
 
 
-def _block(like, sizes, stream):
-    """A new tensor of int32 words with room for pieces of these many words, and where each begins (256 bytes apart at least): one
+def _block(like, sizes, stream, dtype=None):
+    """A new tensor of int32 (or other 4-byte) words with room for pieces of these many words, and where each begins (256 bytes apart at least): one
     allocation instead of one a piece, which took longer than the call itself.  The caller's views keep it alive."""
     at, total = [], 0
     for n in sizes:
         at.append(total)
         total += (n + 63) // 64 * 64
+    dtype = dtype or _torch.int32
     if stream is None:
-        return like.new_empty((total,), dtype=_torch.int32), at
-    return _new(stream, lambda: like.new_empty((total,), dtype=_torch.int32)), at
+        return like.new_empty((total,), dtype=dtype), at
+    return _new(stream, lambda: like.new_empty((total,), dtype=dtype)), at
 
 
 def _ints(name, t, shape):
@@ -741,10 +742,10 @@ def prompt_attn(q, k, v, seq_start, seq_len=None, o=None, lse=None, return_lse: 
     new_lse = lse is None and return_lse
     if workspace is None:
         size = _workspace_bytes(prompt_attn_workspace_bytes, desc)
-        block, at = _block(q, (size // 4, heads * tokens if new_lse else 0), stream)
+        block, at = _block(q, (size // 4, heads * tokens if new_lse else 0), stream, torch.float32)
         ws_ptr = block.data_ptr()
         if new_lse:
-            lse = block.view(torch.float32).as_strided((heads, tokens), (tokens, 1), at[1])
+            lse = block.as_strided((heads, tokens), (tokens, 1), at[1])
     else:
         _check_workspace(workspace)
         ws_ptr, size = workspace.data_ptr(), workspace.numel()

@@ -5,7 +5,8 @@
 The clip so far goes through the block-sparse attention in its planned order, on queries and keys rotated by frame, height and
 width, and its keys and values into the paged cache, once.  Every continuation then adds frame after frame: the frame's keys are rotated
 on their way into the continuation's own pages, the queries beside them, and all continuations attend to the shared clip and to their
-own frames in one call.  Between frames the better continuations may go on in several ways and the others end (choose).  A model would put its projections and its other layers around this; here the queries, keys and values are drawn.
+own frames in one call.  Between frames the better continuations may go on in several ways and the others end (choose).  A model would put its
+projections and its other layers around this; here the queries, keys and values are drawn.
 """
 from __future__ import annotations
 

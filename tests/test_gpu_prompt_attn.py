@@ -295,6 +295,17 @@ def test_malformed_sequences():
     assert status[:2] == [4, 100] and ((o.double() - want_o).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("lens", [[300], [1] * 32, [0, 40, 0, 0, 200, 7, 0, 129], [100] * 9])
+def test_one_launch_or_two_are_the_same(lens):
+    """Few row tiles of 32 sequences at most are planned where they are computed; 33 sequences are not."""
+    q, k, v = tensors(sum(lens), 8, 2, 64, BF, seed=18)
+    few = run(q, k, v, ends(lens))
+    assert wb.last_launch_count() == 1 and few[2] == [0, 0, 0, 0]
+    many = run(q, k, v, ends(lens + [0] * (33 - len(lens))))
+    assert wb.last_launch_count() == 2 and many[2] == [0, 0, 0, 0]
+    assert torch.equal(few[0], many[0]) and torch.equal(few[1], many[1])
+
+
 def test_captured_call_follows_the_lengths():
     q, k, v = tensors(1000, 8, 2, 128, BF, seed=11)
     start, length = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
