@@ -452,7 +452,8 @@ waveal_status waveal_prompt_attn_workspace_bytes(const waveal_prompt_desc* desc 
  * q, k, v, o: 16-byte aligned, strides multiples of 8 elements and not negative (that of a dimension with one entry: anything); o must not overlap the
  * others.  At most 2^25 tokens, 10^9 rows (tokens * q_heads) and 10^9 row tiles ((tokens / (128 / group) + batch) * kv_heads, with group = q_heads
  * / kv_heads).  scale <= 0 means 1/sqrt(head_dim).  Scores, sums and the
- * accumulated output are fp32; the probabilities enter the second product in the tensors' type.
+ * accumulated output are fp32; the probabilities, relative to one of the row's scores, enter the second product in the tensors' type
+ * (fp16: to multiples of 2^-24 below 2^-14, which adds up to 2^-25 sum |v| to a result).
  * ws: 256-byte aligned, not shared with a call that may run at the same time; needs no clearing.  dev_status: dev int32 [4] or
  * NULL, zeroed by the caller; also {WAVEAL_ERR_TIMEOUT, site, thread block, thread} when a bounded wait ran out. */
 waveal_status waveal_prompt_attn(const waveal_prompt_desc* desc /*host*/, const void* q, const void* k, const void* v, void* o, float* lse,

@@ -3,7 +3,10 @@
 What a result may be off: a score is a sum of head_dim products in fp32 and is scaled (head_dim + 2 roundings of partial sums that are at most
 |q|.|k|), its exponential is good to 2^-20, the probability is rounded to the tensors' type (half a step: UNIT) before the second product,
 whose sum is fp32, and the result is rounded once more.  So with e = (head_dim + 2) 2^-24 scale max |q|.|k| + 2^-20
-    |lse error| <= e + 2^-22 |lse|,   |o error| <= (UNIT + 2 e) sum p |v| + UNIT |o| + 2^-24."""
+    |lse error| <= e + 2^-22 |lse|,   |o error| <= (UNIT + 2 e) sum p |v| + UNIT |o| + 2^-24.
+fp16 has a smallest step, 2^-24: below 2^-14 a probability is off by up to half of that and not by UNIT of itself.  Probabilities are taken relative to a
+reference that is no more than the row's largest score, so their sum is at least 1 and |o error| is up to 2^-25 sum |v| more, over the keys that the row
+sees.  (The sum itself is taken before the rounding.)  In bf16 the smallest step is 2^-133."""
 import math
 
 import pytest
@@ -13,6 +16,7 @@ from paper_2609_34814_b200 import binding as wb
 from serving_util import UNIT
 
 pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
 
 
 def tensors(tokens, heads, kv_heads, dim, dtype, order="nhd", seed=0, q_scale=1.0, ramp=0.0):
@@ -52,6 +56,8 @@ def expected(q, k, v, starts, lens, causal, scale=None):
             e = (dim + 2) * 2.0 ** -24 * size.amax(-1) + 2.0 ** -20
             lse_tol[h, at] = e + 2.0 ** -22 * lse[h, at].abs()
             o_tol[h, at] = (w @ vh.abs()) * (unit + 2 * e)[:, None] + o[h, at].abs() * unit + 2.0 ** -24
+            if q.dtype == HF:
+                o_tol[h, at] += 2.0 ** -25 * (vh.abs().cumsum(0) if causal else vh.abs().sum(0))
     return o, lse, o_tol, lse_tol
 
 
@@ -83,9 +89,6 @@ def ends(lens, first=0):
     for n in lens:
         out.append(out[-1] + n)
     return out
-
-
-BF, HF = torch.bfloat16, torch.float16
 
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -293,6 +296,17 @@ def test_malformed_sequences():
     o, lse, status = run(q, k, v, [0, 100, 10 ** 9, 100, 300, 299, 300])
     want_o, _, tol, _ = expected(q, k, v, [0, 100], [100, 200], True)
     assert status[:2] == [4, 100] and ((o.double() - want_o).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("bits", [13, 16, 20, 23, 24, 25])
+def test_small_probabilities_of_fp16(bits):
+    """One key in front with a value near zero, a thousand behind it with probabilities of 2^-bits of it: what they add is more than that value."""
+    n = 1000
+    q, k, v = tensors(n, 2, 1, 64, HF, seed=19, q_scale=0.02)
+    q[..., 0], k[..., 0], k[:, 0, 0] = 1.0, 0.0, 8.0 * bits * math.log(2.0)
+    v[:, 0] = v[:, 0] * 2.0 ** -10
+    check(q, k, v, [0, n])
+    check(q, k, v, [0, 100, n], causal=False)
 
 
 @pytest.mark.parametrize("lens", [[300], [1] * 32, [0, 40, 0, 0, 200, 7, 0, 129], [100] * 9])
