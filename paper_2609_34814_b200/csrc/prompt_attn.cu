@@ -475,8 +475,14 @@ k_prompt_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   } else if (warp == 2) {
 #pragma unroll 1
     for (int i = lane; i < kBars<D>; i += 32) {
-      const bool item = i >= B_ITEM_EMPTY && i < B_ITEM_EMPTY + kItems, warps8 = i >= B_P && i < B_O_EMPTY;
-      mbar_init(BAR(i), item ? kItemReaders : i == B_DONE ? 20 : warps8 ? 8 : (i >= B_REF && i < B_PV_DONE) || (i >= B_O_EMPTY && i < B_O_FULL) ? 4 : i >= B_PAIR && i < B_CHECK ? 2 : 1);
+      auto within = [&](int from, int to) { return i >= from && i < to; };
+      int arrivals = 1;
+      if (within(B_ITEM_EMPTY, B_Q_FULL)) arrivals = kItemReaders;
+      else if (i == B_DONE) arrivals = 20;                                                   // softmax and results
+      else if (within(B_P, B_O_EMPTY)) arrivals = 8;                                         // a team
+      else if (within(B_REF, B_PV_DONE) || within(B_O_EMPTY, B_O_FULL)) arrivals = 4;        // half a team; results
+      else if (within(B_PAIR, B_CHECK)) arrivals = 2;                                        // the two warps of 32 rows
+      mbar_init(BAR(i), arrivals);
     }
     if (lane == 0) sm.abort = 0, sm.again = -1;
     if (lane < kItems) sm.chained[lane] = -1;
@@ -1023,7 +1029,8 @@ waveal_status check(const waveal_prompt_desc* d) {
   const int64_t* strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
   for (int t = 0; t < 4; ++t)
     for (int i = 0; i < 2; ++i)
-      if (!one_entry(d, t == 1 || t == 2 ? d->kv_heads : d->q_heads, i) && (strides[t][i] % 8 || strides[t][i] < 0)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "strides must be multiples of 8 elements (16 bytes) and not negative");
+      if (!one_entry(d, t == 1 || t == 2 ? d->kv_heads : d->q_heads, i) && (strides[t][i] % 8 || strides[t][i] < 0))
+        return waveal::fail(WAVEAL_ERR_INVALID_ARG, "strides must be multiples of 8 elements (16 bytes) and not negative");
   return WAVEAL_OK;
 }
 
