@@ -998,6 +998,33 @@ waveal_status make_map(CUtensorMap* tm, const waveal_prompt_desc* d, const void*
   return WAVEAL_OK;
 }
 
+// Does o share an element with an input of `heads` heads?  Exact where both have the same strides, so that o may lie between an input's elements (one row a
+// token for all tensors); otherwise the bytes from the first to the last element decide.
+bool meets(const waveal_prompt_desc* d, const void* o, const void* x, int heads, const int64_t* stride) {
+  using Wide = __int128;                             // (strides may be any 64-bit numbers)
+  const Wide D = d->head_dim, T = d->tokens, H = d->q_heads;
+  const Wide ot = T > 1 ? d->o_stride[1] : 0, xt = T > 1 ? stride[1] : 0;
+  const Wide oh = H > 1 ? d->o_stride[0] : heads > 1 ? stride[0] : 0, xh = heads > 1 ? stride[0] : oh;
+  const Wide apart = ((Wide) reinterpret_cast<intptr_t>(o) - (Wide) reinterpret_cast<intptr_t>(x)) / 2;   // elements (both are aligned to eight)
+  if (apart >= (heads - 1) * xh + (T - 1) * xt + D || -apart >= (H - 1) * oh + (T - 1) * ot + D) return false;
+  if (ot != xt || oh != xh) return true;
+  // two rows that are i heads and k tokens apart, 1 - heads <= i < H, -T < k < T: the fewer of them one by one (at most 2 x 31,623: 10^9 rows), the
+  // others by the two numbers that bring the rows nearest to each other
+  const bool by_head = H + heads <= 2 * T;
+  const Wide low = by_head ? 1 - (Wide)heads : 1 - T, high = by_head ? H - 1 : T - 1, step = by_head ? oh : ot;
+  const Wide other_low = by_head ? 1 - T : 1 - (Wide)heads, other_high = by_head ? T - 1 : H - 1, other = by_head ? ot : oh;
+  for (Wide i = low; i <= high; ++i) {
+    const Wide at = apart + i * step;
+    Wide k = other ? -at / other : 0;
+    if (other && k * other > -at) --k;
+    for (Wide n = k; n <= k + 1; ++n) {
+      const Wide gap = at + std::min(std::max(n, other_low), other_high) * other;
+      if (gap < D && -gap < D) return true;
+    }
+  }
+  return false;
+}
+
 // row tiles of all key heads that there can be
 long long most_tickets(const waveal_prompt_desc* d) {
   const long long tq = kTile / (d->q_heads / d->kv_heads);
@@ -1077,10 +1104,11 @@ extern "C" waveal_status waveal_prompt_attn(const waveal_prompt_desc* d, const v
   if (!q || !k || !v || !o || !seq_start) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q, k, v, o and seq_start are required");
   if (!waveal::aligned(q, 16) || !waveal::aligned(k, 16) || !waveal::aligned(v, 16) || !waveal::aligned(o, 16))
     return waveal::fail(WAVEAL_ERR_INVALID_ARG, "q, k, v and o must be 16-byte aligned");
-  if (o == q || o == k || o == v) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "o must not overlap q, k or v");
   const Layout l = layout(d);
   if (!ws || ws_bytes < l.bytes) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, l.bytes);
   if (!waveal::aligned(ws, 256)) return waveal::fail(WAVEAL_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (meets(d, o, q, d->q_heads, d->q_stride) || meets(d, o, k, d->kv_heads, d->k_stride) || meets(d, o, v, d->kv_heads, d->v_stride))
+    return waveal::fail(WAVEAL_ERR_INVALID_ARG, "o must not overlap q, k or v");
   const int sms = waveal::sm_count();
   if (sms <= 0) return waveal::fail(WAVEAL_ERR_CUDA, "number of SMs not available");
 

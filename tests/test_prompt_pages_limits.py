@@ -1,0 +1,89 @@
+"""Host-only checks of prompt attention and of the page calls: outputs over inputs, sizes whose loops would not end.  A call that is not refused
+ends where it asks for the device (ERR_CUDA), so these tests run on machines without one alone: the addresses are made up."""
+import ctypes
+import itertools
+import random
+
+import pytest
+import torch
+
+from paper_2609_34814_b200 import binding as wb
+from paper_2609_34814_b200 import build as wbuild
+
+
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="made-up addresses must not reach a device")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    wbuild.build()
+    return wb.load()
+
+
+BASE = 1 << 32
+TAKEN = wb.ERR_CUDA
+
+
+def prompt(lib, heads, kv_heads, tokens, dim, at, strides):
+    """The status of a call whose q, k, v and o lie `at` elements behind BASE."""
+    d = wb.PromptDesc(1, tokens, heads, kv_heads, dim, wb.BF16, 0, *strides)
+    q, k, v, o = (BASE + 2 * a for a in at)
+    return lib.waveal_prompt_attn(ctypes.byref(d), q, k, v, o, None, BASE - 4096, None, 0.0, BASE - (1 << 30), 1 << 29, None, None)
+
+
+@pytest.mark.parametrize("heads, kv_heads, tokens, dim", [(8, 2, 100, 128), (1, 1, 1, 64), (4, 4, 1, 64), (1, 1, 300, 64), (128, 1, 77, 64), (2, 2, 3000, 128)])
+@pytest.mark.parametrize("order", ["nhd", "hnd"])
+def test_prompt_results_beside_their_inputs(lib, heads, kv_heads, tokens, dim, order):
+    """One buffer for all four tensors, each row of a token (or head) holding q, k, v and o in turn: none of them meets another.  o moved by 8 elements
+    either way meets its neighbour, unless there is none."""
+    parts = [heads, kv_heads, kv_heads, heads]
+    if order == "nhd":
+        begin = [0] + list(itertools.accumulate(p * dim for p in parts))
+        at, strides = begin[:4], [(dim, begin[4])] * 4
+        end = begin[4]
+    else:
+        begin = [0] + list(itertools.accumulate(p * dim * tokens for p in parts))
+        at, strides = begin[:4], [(dim * tokens, dim)] * 4
+        end = begin[4]
+    assert prompt(lib, heads, kv_heads, tokens, dim, at, strides) == TAKEN
+    # into v's last head; far behind; into the next token's q (where there is one)
+    assert prompt(lib, heads, kv_heads, tokens, dim, at[:3] + [at[3] - 8], strides) == wb.ERR_INVALID_ARG
+    assert prompt(lib, heads, kv_heads, tokens, dim, at[:3] + [end * tokens], strides) == TAKEN
+    into_q = wb.ERR_INVALID_ARG if order == "nhd" and tokens > 1 else TAKEN
+    assert prompt(lib, heads, kv_heads, tokens, dim, at[:3] + [at[3] + 8], strides) == into_q
+    # o over the last row alone of each input, and just behind it
+    for i, h in enumerate((heads, kv_heads, kv_heads)):
+        last = at[i] + (h - 1) * strides[i][0] + (tokens - 1) * strides[i][1]
+        assert prompt(lib, heads, kv_heads, tokens, dim, at[:3] + [last], strides) == wb.ERR_INVALID_ARG
+
+
+def test_prompt_results_over_an_input_in_part(lib):
+    """Tensors by themselves, o beginning inside one of them."""
+    heads, kv_heads, tokens, dim = 8, 2, 100, 128
+    strides = [(dim, heads * dim), (dim, kv_heads * dim), (dim, kv_heads * dim), (dim, heads * dim)]
+    size = [heads * tokens * dim, kv_heads * tokens * dim, kv_heads * tokens * dim]
+    at = [10_000_000, 20_000_000, 30_000_000, 40_000_000]
+    assert prompt(lib, heads, kv_heads, tokens, dim, at, strides) == TAKEN
+    for i in range(3):
+        for o, status in ((at[i] + size[i] - 8, wb.ERR_INVALID_ARG), (at[i] + size[i], TAKEN), (at[i] - heads * tokens * dim + 8, wb.ERR_INVALID_ARG), (at[i] - heads * tokens * dim, TAKEN), (at[i] + 8, wb.ERR_INVALID_ARG)):
+            assert prompt(lib, heads, kv_heads, tokens, dim, at[:3] + [o], strides) == status, (i, o)
+
+
+def test_prompt_overlap_against_sets(lib):
+    """Random views of a small buffer: what is let through has no element in common, and with equal strides what is refused has one."""
+    r = random.Random(5)
+    dim, met, let = 64, 0, 0
+    for _ in range(3000):
+        heads, tokens = r.choice([(1, 1), (2, 1), (1, 5), (2, 3), (4, 3), (3, 2)])
+        kv_heads = r.choice([h for h in (1, 2, 3, 4) if heads % h == 0])
+        a, b = r.randint(8, 40) * 8, r.randint(8, 40) * 8
+        same = (a, a * heads + 8 * r.randint(0, 30)) if r.random() < 0.5 else (b * tokens + 8 * r.randint(0, 30), b)
+        strides = [same, (a, 2048), (a, 2048), same]
+        at = [r.randint(0, 100) * 8, 1_000_000, 2_000_000, r.randint(0, 300) * 8]
+
+        def elements(at, heads, stride):
+            return {at + h * stride[0] + t * stride[1] + c for h in range(heads) for t in range(tokens) for c in range(0, dim, 8)}
+        common = bool(elements(at[0], heads, same) & elements(at[3], heads, same))
+        assert prompt(lib, heads, kv_heads, tokens, dim, at, strides) == (wb.ERR_INVALID_ARG if common else TAKEN), (heads, tokens, same, at)
+        met, let = met + common, let + (not common)
+    assert met > 300 and let > 300
