@@ -466,7 +466,8 @@ waveal_status waveal_prompt_attn(const waveal_prompt_desc* desc /*host*/, const 
  * A pool is the n_pages pages of a waveal_cache_desc.  Row b of a page table names the pages of one sequence; a page may stand in
  * several rows, and page_refs counts its holders: the rows that it stands in, and one for everything else that needs it
  * (a shared prefix).  A page whose count is not above zero is free.  The three calls read and write all of this on the device: a step needs no
- * answer on the host, and a captured call follows what its tensors hold.  head_dim 2 .. 512, a page of at most 2^31 - 1 elements of keys. */
+ * answer on the host, and a captured call follows what its tensors hold.  head_dim 2 .. 512, a page of at most 2^31 - 1 elements of keys.
+ * Forking and compacting take up to 2^30 pages in the pool, 2^30 rows and 2^30 entries a row, 2^31 - 1 entries a table. */
 
 typedef struct waveal_fork_desc {
   int32_t old_rows, rows;       /* of the last table, of the next one (both may be 0)             */

@@ -564,6 +564,14 @@ waveal_status check_pool(const waveal_cache_desc* c) {
   return WAVEAL_OK;
 }
 
+// Threads walk through rows, pages of a row and pages of the pool in steps of up to 2^14 with 32-bit numbers, which must not run over.
+constexpr int kMost = 1 << 30;
+waveal_status check_counts(const waveal_cache_desc* c, int rows_a, int rows_b, int pages_a, int pages_b) {
+  if (c->n_pages > kMost || std::max(rows_a, rows_b) > kMost || std::max(pages_a, pages_b) > kMost)
+    return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^30 pages of the pool, rows of a table or entries of a row");
+  return WAVEAL_OK;
+}
+
 // a cache's tensors, or two caches', as the copying kernels see them; wide: 16-byte vectors
 bool page_shape(PageShape& s, Tensors& t, const waveal_cache_desc* from, const void* from_k, const void* from_v, const waveal_cache_desc* to, void* to_k,
                 void* to_v) {
@@ -646,6 +654,7 @@ waveal_status check_fork(const waveal_cache_desc* c, const waveal_fork_desc* f) 
   if (!f) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "fork is NULL");
   if (f->old_rows < 0 || f->rows < 0 || f->old_pages < 0 || f->pages < 0)
     return waveal::fail(WAVEAL_ERR_INVALID_ARG, "rows and pages must not be negative");
+  if (waveal_status e = check_counts(c, f->old_rows, f->rows, f->old_pages, f->pages)) return e;
   if (f->old_stride < f->old_pages || f->stride < f->pages) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "a table's stride is smaller than its pages");
   if ((long long)f->old_rows * f->old_pages > INT_MAX || (long long)f->rows * f->pages > INT_MAX)
     return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^31 - 1 entries in a table");
@@ -775,6 +784,7 @@ extern "C" waveal_status waveal_cache_fork(const waveal_cache_desc* c, const wav
 extern "C" waveal_status waveal_cache_compact_workspace_bytes(const waveal_cache_desc* cache, size_t* bytes) {
   if (!bytes) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "bytes is NULL");
   if (waveal_status e = check_pool(cache)) return e;
+  if (waveal_status e = check_counts(cache, 0, 0, 0, 0)) return e;
   *bytes = compact_layout(cache).bytes;
   return WAVEAL_OK;
 }
@@ -787,6 +797,7 @@ extern "C" waveal_status waveal_cache_compact(const waveal_cache_desc* c, const 
   if (!d) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "compact is NULL");
   if (d->rows < 0 || d->pages < 0 || d->prefix_pages < 0)
     return waveal::fail(WAVEAL_ERR_INVALID_ARG, "rows, pages and prefix_pages must not be negative");
+  if (waveal_status e = check_counts(c, d->rows, 0, d->pages, 0)) return e;
   if (d->old_stride < d->pages || d->stride < d->pages) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "a table's stride is smaller than its pages");
   if ((long long)d->rows * d->pages > INT_MAX) return waveal::fail(WAVEAL_ERR_UNSUPPORTED, "more than 2^31 - 1 entries in a table");
   const bool has_table = d->rows && d->pages;

@@ -87,3 +87,39 @@ def test_prompt_overlap_against_sets(lib):
         assert prompt(lib, heads, kv_heads, tokens, dim, at, strides) == (wb.ERR_INVALID_ARG if common else TAKEN), (heads, tokens, same, at)
         met, let = met + common, let + (not common)
     assert met > 300 and let > 300
+
+
+def pool(n_pages=10, head_dim=128):
+    return wb.CacheDesc(n_pages, 16, 2, head_dim, wb.BF16, (32 * head_dim, 16 * head_dim, head_dim), (32 * head_dim, 16 * head_dim, head_dim))
+
+
+MOST = 1 << 30
+LAST = (1 << 31) - 1
+
+
+@pytest.mark.parametrize("over", [MOST + 1, LAST - 16384, LAST])
+def test_sizes_whose_loops_would_run_over(lib, over):
+    """Loops over rows, a row's entries and the pool's pages go on in steps of up to 2^14 with 32-bit counters: from 2^31 - 2^14 on they would come back
+    negative.  Sizes up to 2^30 are taken."""
+    n = ctypes.c_size_t(0)
+    at = [BASE + (i << 34) for i in range(10)]
+    ws, room = BASE + (20 << 34), 1 << 40
+
+    def fork(cache, *sizes):
+        d = wb.ForkDesc(*sizes)
+        status = lib.waveal_cache_fork(ctypes.byref(cache), ctypes.byref(d), *at, ws, room, None, None)
+        query = lib.waveal_cache_fork_workspace_bytes(ctypes.byref(cache), ctypes.byref(d), ctypes.byref(n))
+        assert query == (wb.OK if status == TAKEN else status)
+        return status
+
+    def compact(cache, *sizes):
+        return lib.waveal_cache_compact(ctypes.byref(cache), ctypes.byref(wb.CompactDesc(*sizes)), *at, ws, room, None)
+    for n_pages, sizes in ((over, (1, 1, 1, 1, 1, 1)), (10, (over, 1, 0, 1, 0, 1)), (10, (1, over, 1, 0, 1, 0)), (10, (1, 1, over, 1, over, 1)),
+                           (10, (1, 1, 1, over, 1, over))):
+        assert fork(pool(n_pages), *sizes) == wb.ERR_UNSUPPORTED, sizes
+        assert fork(pool(min(n_pages, MOST)), *(min(x, MOST) for x in sizes)) == TAKEN, sizes
+    for n_pages, sizes in ((over, (1, 1, 1, 1, 1)), (10, (over, 0, 0, 0, 0)), (10, (1, over, 0, over, over))):
+        assert compact(pool(n_pages), *sizes) == wb.ERR_UNSUPPORTED, sizes
+        assert compact(pool(min(n_pages, MOST)), *(min(x, MOST) for x in sizes)) == TAKEN, sizes
+    assert lib.waveal_cache_compact_workspace_bytes(ctypes.byref(pool(over)), ctypes.byref(n)) == wb.ERR_UNSUPPORTED
+    assert lib.waveal_cache_compact_workspace_bytes(ctypes.byref(pool(MOST)), ctypes.byref(n)) == wb.OK
