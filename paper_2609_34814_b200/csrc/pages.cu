@@ -188,7 +188,7 @@ struct ForkParams {
   const int *old_table, *held, *refs, *parents, *keep, *room;
   int *table, *new_refs;
   // workspace
-  int* kids;               // [3][old_rows]: rows that go on from this one; the fewest and the most full pages that they keep
+  int* kids;               // [2][old_rows]: rows that go on from this one; the fewest full pages that they keep
   int* ends;               // [n_pages], of pages that rows end in: the first of these rows
   int4* row;               // [rows]: parent or -1, full pages kept, pages in all, tokens in the page filled in part (bit 30: the row keeps that page)
   int2* last;              // [rows]: the page filled in part (-1: none), where the row's fresh pages begin
@@ -207,26 +207,26 @@ __device__ __forceinline__ int held_tokens(const ForkParams& p, int r) {
 // What the phases hand on (counts, rows): LOCAL, where one thread block decides, in shared memory (eight phases read in turn what the one before has
 // written: 10.5 us of 16 rows of 63 pages instead of 12.6 through L2, 19.5 of 64 rows in beams instead of 21.6), else in the results and the workspace.
 struct ForkState {
-  int *refs, *ends, *count, *fewest, *most;
+  int *refs, *ends, *count, *fewest;
   int4* row;
   int2* last;
 };
 __host__ __device__ inline size_t fork_state_bytes(long long n_pages, long long old_rows, long long rows) {
-  return (size_t)(rows * (sizeof(int4) + sizeof(int2)) + (2 * ((n_pages + 3) / 4 * 4) + 3 * old_rows) * sizeof(int));
+  return (size_t)(rows * (sizeof(int4) + sizeof(int2)) + (2 * ((n_pages + 3) / 4 * 4) + 2 * old_rows) * sizeof(int));
 }
 
 template <bool LOCAL>
 __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_constant__ ForkParams p) {
   __shared__ int shared[33], list[kPlanThreads * kPerThread];
   extern __shared__ __align__(16) unsigned char local[];
-  ForkState s = {p.new_refs, p.ends, p.kids, p.kids + p.old_rows, p.kids + 2 * p.old_rows, p.row, p.last};
+  ForkState s = {p.new_refs, p.ends, p.kids, p.kids + p.old_rows, p.row, p.last};
   if constexpr (LOCAL) {
     const int n = (p.n_pages + 3) / 4 * 4;
     s.row = reinterpret_cast<int4*>(local);
     s.refs = reinterpret_cast<int*>(s.row + p.rows);
     s.ends = s.refs + n;
     s.last = reinterpret_cast<int2*>(s.ends + n);
-    s.count = reinterpret_cast<int*>(s.last + p.rows), s.fewest = s.count + p.old_rows, s.most = s.fewest + p.old_rows;
+    s.count = reinterpret_cast<int*>(s.last + p.rows), s.fewest = s.count + p.old_rows;
   }
   waveal::let_next_kernel_start();
   const int tid = blockIdx.x * kPlanThreads + threadIdx.x, threads = gridDim.x * kPlanThreads;
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
   copy_counts(s.refs, p.refs, p.n_pages, tid, threads);
 #pragma unroll 1
   for (int r = tid; r < p.old_rows; r += threads) {
-    s.count[r] = 0, s.fewest[r] = INT_MAX, s.most[r] = 0;
+    s.count[r] = 0, s.fewest[r] = INT_MAX;
     const int n = p.held[r];
     if (n < 0 || n > (long long)p.old_pages << shift) report(p.dev_status, WAVEAL_ERR_BAD_MASK, 81, r, n);
   }
@@ -265,7 +265,6 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_fork_plan(const __grid_cons
       }
       atomicAdd(s.count + parent, 1);
       atomicMin(s.fewest + parent, row.y);
-      atomicMax(s.most + parent, row.y);
     }
     s.row[b] = row;
     s.last[b] = {page, 0};
@@ -666,7 +665,7 @@ ForkLayout fork_layout(const waveal_cache_desc* c, const waveal_fork_desc* f) {
   ForkLayout l;
   l.sums = 0;
   l.kids = up256((2 * kCluster + 1) * sizeof(int));
-  l.ends = l.kids + up256((size_t)f->old_rows * 3 * sizeof(int));
+  l.ends = l.kids + up256((size_t)f->old_rows * 2 * sizeof(int));
   l.row = l.ends + up256((size_t)c->n_pages * sizeof(int));
   l.last = l.row + up256((size_t)f->rows * sizeof(int4));
   l.fresh = l.last + up256((size_t)f->rows * sizeof(int2));
