@@ -614,6 +614,19 @@ constexpr size_t kLocalBytes = 192 << 10;           // (beside the 32 KB and mor
 //   327,680                                24.9 / 40.6   26.1 / 34.9   (64 / 151)
 // 10,000 pages, 64 rows of 1,024 entries: 17.1 / 21.7, 17.9 / 21.3, 22.4 / 26.1; 8,192 pages, 256 rows of 512: 24.8 / 44.6, 19.8 / 26.3, 23.6 / 29.4.  Two and
 // four are never more than 1 us ahead of the better neighbour.
+// A new row's entries are walked where it keeps more than another child of its parent, so rows beyond the old ones' number count, an entry a quarter.  us where
+// every child keeps another length / all keep everything, pools of 4,096 to 20,000 pages:
+//   rows           one           eight         sixteen
+//   1 x 1,000: 64  15.4 / 13.1   22.1 / 19.3   27.9 / 25.0
+//   4 x 1,000: 128 20.9 / 14.7   22.3 / 19.5   27.6 / 25.2
+//   1 x 1,000: 256 28.5 / 17.0   27.2 / 19.9   29.5 / 24.9
+//   1 x 8,000: 64  44.0 / 21.9   39.5 / 20.9   39.0 / 25.6
+//   2 x 2,000: 500 96.1 / 31.3   61.6 / 23.8   49.4 / 27.6
+//   the same: 2,000 (not in one) 184 / 41.0    118 / 38.9
+long long fork_work(long long pool, const waveal_fork_desc* f) {
+  const long long more = std::max(0ll, (long long)f->rows - f->old_rows);
+  return pool + (long long)f->old_rows * f->old_pages + more * std::min(f->old_pages, f->pages) / 4;
+}
 int fork_blocks(long long work, size_t state) { return work <= 65536 && state <= kLocalBytes ? 1 : work <= 400000 ? 8 : 16; }
 // The same for compacting, us with the copies of half of the pool's small pages: 1,024 pages 7.3 (one), 8.5 (eight), 9.8 (sixteen); 4,096 11.7, 9.4, 11.0;
 // 16,384 29.0, 13.2, 13.3; 32,768 52, 17.8, 16.7; 131,072 188, 46, 36.
@@ -768,10 +781,9 @@ extern "C" waveal_status waveal_cache_fork(const waveal_cache_desc* c, const wav
   p.row = reinterpret_cast<int4*>(w + l.row), p.last = reinterpret_cast<int2*>(w + l.last), p.fresh = reinterpret_cast<int*>(w + l.fresh);
   p.dev_status = dev_status;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const long long entries = (long long)f->old_rows * f->old_pages;
   static bool set[2][64] = {};
   const size_t state = fork_state_bytes(c->n_pages, f->old_rows, f->rows);
-  const int blocks = fork_blocks(c->n_pages + entries, state);
+  const int blocks = fork_blocks(fork_work(c->n_pages, f), state);
   if (waveal_status e = blocks == 1 ? launch_plan(k_fork_plan<true>, set[1], p, 1, state, st) : launch_plan(k_fork_plan<false>, set[0], p, blocks, 0, st)) return e;
   const unsigned grid = copy_grid((long long)f->rows * (2 * p.shape.segments + (f->pages + kRun - 1) / kRun));
   if (wide) WAVEAL_CUDA_OK(waveal::launch_chained(k_fork_apply<uint4>, dim3(grid), kCopyThreads, 0, st, p));
