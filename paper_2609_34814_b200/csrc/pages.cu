@@ -13,7 +13,7 @@
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kCluster = 16;                         // thread blocks that decide, at most (what this GPU allows)
+constexpr int kCluster = 16;                         // thread blocks that decide, at most (the largest cluster; eight where that does not fit)
 constexpr int kCopyThreads = 256, kCopyBlocks = 8;   // blocks an SM
 constexpr int kUnroll = 4;                           // vectors of a lane under way
 constexpr int kSegment = 32 * kUnroll;               // vectors of a warp's turn
@@ -632,16 +632,13 @@ int fork_blocks(long long work, size_t state) { return work <= 65536 && state <=
 // 16,384 29.0, 13.2, 13.3; 32,768 52, 17.8, 16.7; 131,072 188, 46, 36.
 int compact_blocks(long long pages) { return pages <= 2048 ? 1 : pages <= 16384 ? 8 : 16; }
 
+// What a kernel has been given leave to on a device: nothing yet, what it asked for, clusters of eight at most.
+enum Leave : char { kUnasked = 0, kAsWanted, kEightAtMost };
+
 template <class P>
-waveal_status launch_plan(void (*kernel)(P), bool (&set)[64], const P& p, int blocks, size_t smem, cudaStream_t st) {
+waveal_status launch_plan(void (*kernel)(P), Leave (&leave)[64], const P& p, int blocks, size_t smem, cudaStream_t st) {
   int dev = 0;
   WAVEAL_CUDA_OK(cudaGetDevice(&dev));
-  // more than eight blocks a cluster, and more than 48 KB, have to be asked for (set: of this kernel, by device)
-  if ((blocks > 8 || smem) && (dev >= 64 || !set[dev])) {
-    if (smem) WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLocalBytes));
-    else WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    if (dev < 64) set[dev] = true;
-  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kPlanThreads);
@@ -651,6 +648,24 @@ waveal_status launch_plan(void (*kernel)(P), bool (&set)[64], const P& p, int bl
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)blocks, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr, cfg.numAttrs = 1;
+  // More than 48 KB have to be asked for, and more than eight blocks a cluster, which need as many SMs in one part of the GPU: where there are fewer
+  // (part of a GPU is all that the program has), eight do the same work.
+  if (blocks > 8 || smem) {
+    Leave l = dev < 64 ? leave[dev] : kUnasked;
+    if (l == kUnasked) {
+      l = kAsWanted;
+      if (smem) {
+        WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLocalBytes));
+      } else {
+        WAVEAL_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        int clusters = 0;
+        WAVEAL_CUDA_OK(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
+        if (clusters < 1) l = kEightAtMost;
+      }
+      if (dev < 64) leave[dev] = l;
+    }
+    if (l == kEightAtMost) cfg.gridDim.x = attr[0].val.clusterDim.x = 8;
+  }
   WAVEAL_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, p));
   return WAVEAL_OK;
 }
@@ -781,10 +796,10 @@ extern "C" waveal_status waveal_cache_fork(const waveal_cache_desc* c, const wav
   p.row = reinterpret_cast<int4*>(w + l.row), p.last = reinterpret_cast<int2*>(w + l.last), p.fresh = reinterpret_cast<int*>(w + l.fresh);
   p.dev_status = dev_status;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  static bool set[2][64] = {};
+  static Leave leave[2][64] = {};
   const size_t state = fork_state_bytes(c->n_pages, f->old_rows, f->rows);
   const int blocks = fork_blocks(fork_work(c->n_pages, f), state);
-  if (waveal_status e = blocks == 1 ? launch_plan(k_fork_plan<true>, set[1], p, 1, state, st) : launch_plan(k_fork_plan<false>, set[0], p, blocks, 0, st)) return e;
+  if (waveal_status e = blocks == 1 ? launch_plan(k_fork_plan<true>, leave[1], p, 1, state, st) : launch_plan(k_fork_plan<false>, leave[0], p, blocks, 0, st)) return e;
   const unsigned grid = copy_grid((long long)f->rows * (2 * p.shape.segments + (f->pages + kRun - 1) / kRun));
   if (wide) WAVEAL_CUDA_OK(waveal::launch_chained(k_fork_apply<uint4>, dim3(grid), kCopyThreads, 0, st, p));
   else WAVEAL_CUDA_OK(waveal::launch_chained(k_fork_apply<unsigned short>, dim3(grid), kCopyThreads, 0, st, p));
@@ -832,8 +847,8 @@ extern "C" waveal_status waveal_cache_compact(const waveal_cache_desc* c, const 
   p.sums = reinterpret_cast<int*>(w + l.sums), p.first = p.sums + kCluster;
   p.from = reinterpret_cast<int*>(w + l.from), p.to = reinterpret_cast<int*>(w + l.to);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  static bool set[64] = {};
-  if (waveal_status e = launch_plan(k_compact_plan, set, p, compact_blocks(c->n_pages), 0, st)) return e;
+  static Leave leave[64] = {};
+  if (waveal_status e = launch_plan(k_compact_plan, leave, p, compact_blocks(c->n_pages), 0, st)) return e;
   // (how many pages move is known on the device only: half of the pool at most)
   const unsigned grid = copy_grid((long long)(c->n_pages / 2) * 2 * p.shape.segments + (long long)d->rows * ((d->pages + kRun - 1) / kRun));
   if (wide) WAVEAL_CUDA_OK(waveal::launch_chained(k_compact_apply<uint4>, dim3(grid), kCopyThreads, 0, st, p));

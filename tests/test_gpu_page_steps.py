@@ -1,11 +1,12 @@
 """Forks and compactions as a program meets them beyond test_gpu_pages.py, against the same definitions on lists."""
+import os
 import random
+import subprocess
+import sys
 
 import pytest
-import torch
 
-from paper_2609_34814_b200 import binding as wb
-from pages_util import Pool, forked, ints, on_gpu, up
+from pages_util import Pool
 from test_gpu_pages import check
 
 pytestmark = pytest.mark.gpu
@@ -19,3 +20,32 @@ def test_few_rows_go_on_in_many_ways_of_different_lengths(old_rows, tokens, rows
     parents = [b % old_rows for b in range(rows)]
     keep = [r.randint(0, pool.held[p]) for p in parents]
     check(pool, parents, keep, [n + r.choice([0, 1, 16]) for n in keep])
+
+
+FIRST = """
+import torch
+from paper_2609_34814_b200 import binding as wb
+
+pages, rows = 400000, 512
+ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+cache = wb.PagedCache(*(torch.zeros((pages, 1, 16, 8), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+refs, table, held = torch.zeros(pages, dtype=torch.int32, device="cuda"), ints([[-1] * 4] * rows), ints([0] * rows)
+keep, room = ints([0] * rows), ints([40] * rows)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    new, counts = wb.cache_fork(cache, table, held, refs, keep, room)
+    r = wb.cache_compact(cache, counts, page_table=new)
+graph.replay()
+torch.cuda.synchronize()
+assert new.tolist() == [[3 * b, 3 * b + 1, 3 * b + 2, -1] for b in range(rows)]
+assert r.used.item() == 3 * rows and torch.equal(r.page_table, new)
+print("captured")
+"""
+
+
+def test_the_first_call_of_a_program_may_be_captured():
+    """What the largest clusters have to be asked for is asked for in that call."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "captured" in done.stdout, done.stderr[-2000:]
