@@ -665,17 +665,10 @@ def _workspace_bytes(query, *descs):
     return n
 
 
-def _block(like, sizes, stream, dtype=None):
-    """A new tensor of int32 (or other 4-byte) words with room for pieces of these many words, and where each begins (256 bytes apart at least): one
-    allocation instead of one a piece, which took longer than the call itself.  The caller's views keep it alive."""
-    at, total = [], 0
-    for n in sizes:
-        at.append(total)
-        total += (n + 63) // 64 * 64
-    dtype = dtype or _torch.int32
-    if stream is None:
-        return like.new_empty((total,), dtype=dtype), at
-    return _new(stream, lambda: like.new_empty((total,), dtype=dtype)), at
+def _new_like(like, stream, *shape):
+    """A new tensor of the type of `like`.  Every result has one of its own: who keeps or saves it keeps no other, and no workspace.  (Sizes as arguments, no
+    type: 0.9 us each; a shape and a type 1.6, a view of a common block 1.4.)"""
+    return like.new_empty(*shape) if stream is None else _new(stream, lambda: like.new_empty(*shape))
 
 
 def _ints(name, t, shape):
@@ -740,19 +733,16 @@ def prompt_attn(q, k, v, seq_start, seq_len=None, o=None, lse=None, return_lse: 
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (heads, tokens) or not lse.is_cuda or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 cuda tensor [q_heads, tokens]")
     new_lse = lse is None and return_lse
+    if new_lse:
+        lse = _new(stream, lambda: q.new_empty((heads, tokens), dtype=torch.float32))
     if workspace is None:
         size = _workspace_bytes(prompt_attn_workspace_bytes, desc)
-        block, at = _block(q, (size // 4, heads * tokens if new_lse else 0), stream, torch.float32)
-        ws_ptr = block.data_ptr()
-        if new_lse:
-            lse = block.as_strided((heads, tokens), (tokens, 1), at[1])
+        workspace = _new_like(q, stream, size // 2)
     else:
         _check_workspace(workspace)
-        ws_ptr, size = workspace.data_ptr(), workspace.numel()
-        if new_lse:
-            lse = _new(stream, lambda: q.new_empty((heads, tokens), dtype=torch.float32))
+        size = workspace.numel()
     _here(q, k, v, o, lse, seq_start, seq_len, workspace, dev_status)
-    _check(load().waveal_prompt_attn(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), start, lens, scale, ws_ptr, size,
+    _check(load().waveal_prompt_attn(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), start, lens, scale, workspace.data_ptr(), size,
                                      _status(dev_status), _stream(stream)))
     return (o, lse) if return_lse else o
 
@@ -787,24 +777,21 @@ def cache_fork(cache: PagedCache, page_table, held_len, page_refs, keep_len, roo
             raise ValueError("table_out must be [rows of keep_len, max_pages]")
     desc = _FORK.pack(old_rows, rows, old_pages, pages, old_stride, stride)
     size = _workspace_bytes(cache_fork_workspace_bytes, cache.desc, desc)
-    # what is not given, in one piece
-    block, at = _block(page_refs, (0 if table_out is not None else rows * pages, 0 if refs_out is not None else n,
-                                   0 if workspace is not None else size // 4), stream)
-    base = block.data_ptr()
     if table_out is None:
-        table_out = block.as_strided((rows, pages), (pages, 1), 0)
+        table_out = _new_like(page_refs, stream, rows, pages)
     if refs_out is None:
-        refs_out, refs_ptr = block.as_strided((n,), (1,), at[1]), base + 4 * at[1]
+        refs_out = _new_like(page_refs, stream, n)
+        refs_ptr = refs_out.data_ptr()
     else:
         refs_ptr = _ints("refs_out", refs_out, (n,))
     if workspace is None:
-        ws_ptr = base + 4 * at[2]
+        workspace = _new_like(page_refs, stream, size // 4)
     else:
         _check_workspace(workspace)
-        ws_ptr, size = workspace.data_ptr(), workspace.numel()
+        size = workspace.numel()
     _here(cache.k, cache.v, page_table, held_len, page_refs, keep_len, room_len, parents, table_out, refs_out, workspace, dev_status)
     _check(load().waveal_cache_fork(cache.desc, desc, cache.k.data_ptr(), cache.v.data_ptr(), page_table.data_ptr(), held, refs, parent, keep, room,
-                                    table_out.data_ptr(), refs_ptr, ws_ptr, size, _status(dev_status), _stream(stream)))
+                                    table_out.data_ptr(), refs_ptr, workspace.data_ptr(), size, _status(dev_status), _stream(stream)))
     return table_out, refs_out
 
 
@@ -831,29 +818,24 @@ def cache_compact(cache: PagedCache, page_refs, page_table=None, prefix_pages=No
     refs = _ints("page_refs", page_refs, (cache.n_pages,))
     n = cache.n_pages
     rows = pages = old_stride = count = 0
-    table = prefix = table_ptr = prefix_ptr = None
     if page_table is not None:
         rows, pages, old_stride = _table("page_table", page_table)
     if prefix_pages is not None:
         count = prefix_pages.numel()
         _ints("prefix_pages", prefix_pages, (count,))
     size = _workspace_bytes(cache_compact_workspace_bytes, cache.desc)
-    block, at = _block(page_refs, (rows * pages, count, n, n, 1, 0 if workspace is not None else size // 4), stream)
-    base = block.data_ptr()
-    if page_table is not None:
-        table, table_ptr = block.as_strided((rows, pages), (pages, 1), 0), base
-    if prefix_pages is not None:
-        prefix, prefix_ptr = block.as_strided((count,), (1,), at[1]), base + 4 * at[1]
-    refs_out, place, used = block.as_strided((n,), (1,), at[2]), block.as_strided((n,), (1,), at[3]), block.as_strided((1,), (1,), at[4])
+    table = None if page_table is None else _new_like(page_refs, stream, rows, pages)
+    prefix = None if prefix_pages is None else _new_like(page_refs, stream, count)
+    refs_out, place, used = _new_like(page_refs, stream, n), _new_like(page_refs, stream, n), _new_like(page_refs, stream, 1)
     if workspace is None:
-        ws_ptr = base + 4 * at[5]
+        workspace = _new_like(page_refs, stream, size // 4)
     else:
         _check_workspace(workspace)
-        ws_ptr, size = workspace.data_ptr(), workspace.numel()
+        size = workspace.numel()
     _here(cache.k, cache.v, page_refs, page_table, prefix_pages, workspace)
     _check(load().waveal_cache_compact(cache.desc, _COMPACT.pack(rows, pages, count, old_stride, pages), cache.k.data_ptr(), cache.v.data_ptr(), refs,
-                                       _ptr(page_table), _ptr(prefix_pages), base + 4 * at[2], table_ptr, prefix_ptr, base + 4 * at[3], base + 4 * at[4],
-                                       ws_ptr, size, _stream(stream)))
+                                       _ptr(page_table), _ptr(prefix_pages), refs_out.data_ptr(), _ptr(table), _ptr(prefix), place.data_ptr(),
+                                       used.data_ptr(), workspace.data_ptr(), size, _stream(stream)))
     return Compacted(table, prefix, refs_out, place, used)
 
 

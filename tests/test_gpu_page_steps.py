@@ -5,8 +5,10 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
-from pages_util import Pool
+from paper_2609_34814_b200 import binding as wb
+from pages_util import Pool, ints, on_gpu
 from test_gpu_pages import check
 
 pytestmark = pytest.mark.gpu
@@ -20,6 +22,26 @@ def test_few_rows_go_on_in_many_ways_of_different_lengths(old_rows, tokens, rows
     parents = [b % old_rows for b in range(rows)]
     keep = [r.randint(0, pool.held[p]) for p in parents]
     check(pool, parents, keep, [n + r.choice([0, 1, 16]) for n in keep])
+
+
+@pytest.mark.parametrize("stream", [False, True])
+def test_results_are_tensors_of_their_own(stream):
+    """A result that is kept or saved holds its own numbers and nothing else: no other result, no workspace."""
+    kw = dict(stream=torch.cuda.Stream()) if stream else {}
+    pool = Pool(6, 300, seed=33, spare=3.0)
+    cache, held = wb.PagedCache(on_gpu(pool.k), on_gpu(pool.v)), ints(pool.held)
+    table, refs, prefix = ints(pool.padded()), ints(pool.refs), ints(pool.prefix)
+    torch.cuda.synchronize()
+    results = [*wb.cache_fork(cache, table, held, refs, held, held, **kw)]
+    torch.cuda.synchronize()
+    results += wb.cache_compact(cache, results[1], page_table=results[0], prefix_pages=prefix, **kw)
+    x = torch.randn((2, 300, 64), device="cuda").bfloat16()
+    torch.cuda.synchronize()
+    results += wb.prompt_attn(x, x, x, ints([0, 100, 300]), return_lse=True, **kw)
+    torch.cuda.synchronize()
+    assert len({t.untyped_storage().data_ptr() for t in results}) == len(results) == 9
+    for t in results:
+        assert t.untyped_storage().nbytes() == t.numel() * t.element_size() and not t._is_view()
 
 
 FIRST = """
