@@ -490,7 +490,10 @@ waveal_status waveal_cache_fork_workspace_bytes(const waveal_cache_desc* cache /
  *   in place, in fresh pages alone.
  * dev_status {WAVEAL_ERR_BAD_MASK, site, row, value}: 80 parents, 81 held_len (that row then holds nothing), 82 keep_len (below 0 or above the
  * parent's held_len), 83 room beyond `pages`; such a row of the new table is empty.  84: an entry of the last table outside the pool; it is -1 in the new one and
- * counted nowhere.  {WAVEAL_ERR_NO_PAGES, 85, row, pages missing}: the pool is used up; entries from there on are -1. */
+ * counted nowhere.  {WAVEAL_ERR_NO_PAGES, 85, row, pages missing}: the pool is used up in that row; its entries from there
+ * on and the fresh entries of all rows behind it are -1, everything else of the new table and counts is as it would be: rows in front have their room and
+ * their copies, kept pages stay kept.  The last table is over all the same: pages that its rows have let go of may have been given out and written, so a
+ * program goes on from the new table (with fewer rows or less room), and does not call again with the old one. */
 waveal_status waveal_cache_fork(const waveal_cache_desc* cache /*host*/, const waveal_fork_desc* fork /*host*/, void* k_cache, void* v_cache,
                                 const int32_t* old_table, const int32_t* held_len, const int32_t* page_refs, const int32_t* parents /*or NULL*/,
                                 const int32_t* keep_len, const int32_t* room_len, int32_t* table, int32_t* new_refs, void* ws, size_t ws_bytes,

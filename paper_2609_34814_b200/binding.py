@@ -760,7 +760,8 @@ def cache_fork(cache: PagedCache, page_table, held_len, page_refs, keep_len, roo
     of its first held_len[r] tokens; page_refs int32 [n_pages]: how many hold each page.  Row b of the new table (as many as keep_len
     has) keeps the first keep_len[b] tokens of row parents[b] (None: row b; negative: a row without pages) and has room for room_len[b].
     Full pages are shared, a page filled in part is copied unless the row is the only one left that holds it, fresh pages are the free ones with the
-    lowest numbers.  max_pages: entries of a new row (as many as before unless given).  Returns (page_table, page_refs): new tensors unless given."""
+    lowest numbers.  max_pages: entries of a new row (as many as before unless given).  Returns (page_table, page_refs): new tensors unless given.
+    Where the pool runs out (ERR_NO_PAGES in dev_status) entries are -1; the old table is over then too, as its pages may have been written."""
     _load_torch()
     old_rows, old_pages, old_stride = _table("page_table", page_table)
     if keep_len.dim() != 1:

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2609_34814_b200 import binding as wb
-from pages_util import Pool, ints, on_gpu
+from pages_util import Pool, forked, ints, on_gpu
 from test_gpu_pages import check
 
 pytestmark = pytest.mark.gpu
@@ -42,6 +42,36 @@ def test_results_are_tensors_of_their_own(stream):
     assert len({t.untyped_storage().data_ptr() for t in results}) == len(results) == 9
     for t in results:
         assert t.untyped_storage().nbytes() == t.numel() * t.element_size() and not t._is_view()
+
+
+def test_what_a_fork_that_runs_out_of_pages_leaves():
+    """Rows in front of the first that is short have everything, pages written may be such as ended rows have let go of, and the new table goes on."""
+    pool = Pool(4, 40, page=16, spare=0.0, seed=34, shared=0.0, outside=0.0)
+    pool.held = [40, 20, 16, 8]
+    pool.table, pool.wide = [[5, 2, 7], [0, 9], [4], [1]], 3
+    pool.n_pages = 10
+    pool.refs = [1, 1, 1, 0, 1, 1, 0, 1, 0, 1]
+    shape = (10,) + tuple(pool.k.shape[1:])
+    pool.k, pool.v = (torch.randn(shape).bfloat16() for _ in range(2))
+    k, v = on_gpu(pool.k), on_gpu(pool.v)
+    cache, status = wb.PagedCache(k, v), ints([0] * 4)
+    # rows 1 and 3 end, row 0 goes on in four ways with copies of page 7: pages 0, 1, 3, 6, 8, 9 are free
+    parents, keep, room = [0, 0, 2, 0, 0, 2], [40, 40, 16, 40, 40, 16], [49, 49, 16, 48, 64, 40]
+    table, refs = wb.cache_fork(cache, ints(pool.padded()), ints(pool.held), ints(pool.refs), ints(keep), ints(room), parents=ints(parents), max_pages=5,
+                                dev_status=status)
+    rows, counts, copies = forked(pool.table, pool.held, pool.refs, keep, room, parents, 16)
+    assert table.tolist() == [r + [-1] * (5 - len(r)) for r in rows] and refs.tolist() == counts
+    assert table.tolist() == [[5, 2, 7, 0, -1], [5, 2, 1, 3, -1], [4, -1, -1, -1, -1], [5, 2, 6, -1, -1], [5, 2, 8, 9, -1], [4, -1, -1, -1, -1]]
+    assert status.tolist() == [wb.ERR_NO_PAGES, 85, 5, 2]
+    want_k, want_v = pool.k.clone(), pool.v.clone()
+    for a, b, n in copies:
+        want_k[b, :, :n], want_v[b, :, :n] = pool.k[a, :, :n], pool.v[a, :, :n]
+    assert torch.equal(k.cpu(), want_k) and torch.equal(v.cpu(), want_v)
+    assert {b for _, b, _ in copies} == {1, 6, 8} and not torch.equal(k[1].cpu(), pool.k[1])     # page 1 was row 3's
+    # without the last row, and nobody short
+    status.zero_()
+    table, refs = wb.cache_fork(cache, table, ints([49, 49, 16, 48, 64, 16]), refs, ints([49, 16, 48]), ints([49, 16, 60]), parents=ints([0, 2, 3]), dev_status=status)
+    assert status.tolist() == [0] * 4 and table.tolist() == [[5, 2, 7, 0, -1], [4, -1, -1, -1, -1], [5, 2, 6, 1, -1]]
 
 
 FIRST = """
