@@ -998,30 +998,49 @@ waveal_status make_map(CUtensorMap* tm, const waveal_prompt_desc* d, const void*
   return WAVEAL_OK;
 }
 
+using Wide = __int128;                               // (strides may be any 64-bit numbers)
+
+// Does any of low .. high steps bring a row at `at` onto one at 0, both `dim` elements long?  (The distance falls and then rises.)
+bool lands(Wide at, Wide step, Wide low, Wide high, Wide dim) {
+  if (low > high) return false;
+  Wide n = step ? -at / step : low;
+  if (step && n * step > -at) --n;
+  for (const Wide k : {n, n + 1}) {
+    const Wide gap = at + std::min(std::max(k, low), high) * step;
+    if (gap < dim && -gap < dim) return true;
+  }
+  return false;
+}
+
 // Does o share an element with an input of `heads` heads?  Exact where both have the same strides, so that o may lie between an input's elements (one row a
 // token for all tensors); otherwise the bytes from the first to the last element decide.
 bool meets(const waveal_prompt_desc* d, const void* o, const void* x, int heads, const int64_t* stride) {
-  using Wide = __int128;                             // (strides may be any 64-bit numbers)
   const Wide D = d->head_dim, T = d->tokens, H = d->q_heads;
   const Wide ot = T > 1 ? d->o_stride[1] : 0, xt = T > 1 ? stride[1] : 0;
   const Wide oh = H > 1 ? d->o_stride[0] : heads > 1 ? stride[0] : 0, xh = heads > 1 ? stride[0] : oh;
   const Wide apart = ((Wide) reinterpret_cast<intptr_t>(o) - (Wide) reinterpret_cast<intptr_t>(x)) / 2;   // elements (both are aligned to eight)
   if (apart >= (heads - 1) * xh + (T - 1) * xt + D || -apart >= (H - 1) * oh + (T - 1) * ot + D) return false;
   if (ot != xt || oh != xh) return true;
-  // two rows that are i heads and k tokens apart, 1 - heads <= i < H, -T < k < T: the fewer of them one by one (at most 2 x 31,623: 10^9 rows), the
-  // others by the two numbers that bring the rows nearest to each other
-  const bool by_head = H + heads <= 2 * T;
-  const Wide low = by_head ? 1 - (Wide)heads : 1 - T, high = by_head ? H - 1 : T - 1, step = by_head ? oh : ot;
-  const Wide other_low = by_head ? 1 - T : 1 - (Wide)heads, other_high = by_head ? T - 1 : H - 1, other = by_head ? ot : oh;
-  for (Wide i = low; i <= high; ++i) {
-    const Wide at = apart + i * step;
-    Wide k = other ? -at / other : 0;
-    if (other && k * other > -at) --k;
-    for (Wide n = k; n <= k + 1; ++n) {
-      const Wide gap = at + std::min(std::max(n, other_low), other_high) * other;
-      if (gap < D && -gap < D) return true;
-    }
+  // two rows that are i heads and k tokens apart, 1 - heads <= i < H, -T < k < T: the fewer of them one by one (at most 2 x 31,623: 10^9 rows)
+  if (H + heads <= 2 * T) {
+    for (Wide i = 1 - heads; i < H; ++i)
+      if (lands(apart + i * oh, ot, 1 - T, T - 1, D)) return true;
+  } else {
+    for (Wide k = 1 - T; k < T; ++k)
+      if (lands(apart + k * ot, oh, 1 - heads, H - 1, D)) return true;
   }
+  return false;
+}
+
+// Do two of o's own rows share an element?
+bool folds(const waveal_prompt_desc* d) {
+  const Wide D = d->head_dim;
+  Wide n = d->q_heads, step = n > 1 ? d->o_stride[0] : 0, more = d->tokens, far = more > 1 ? d->o_stride[1] : 0;
+  if (more <= 1 || (n > 1 && far < step)) std::swap(n, more), std::swap(step, far);
+  if ((n <= 1 || step >= D) && (more <= 1 || far >= (n - 1) * step + D)) return false;   // one dimension inside the other's steps
+  if (n > more) std::swap(n, more), std::swap(step, far);
+  for (Wide i = 0; i < n; ++i)
+    if (lands(i * step, far, i ? 1 - more : 1, more - 1, D)) return true;
   return false;
 }
 
@@ -1058,6 +1077,7 @@ waveal_status check(const waveal_prompt_desc* d) {
     for (int i = 0; i < 2; ++i)
       if (!one_entry(d, t == 1 || t == 2 ? d->kv_heads : d->q_heads, i) && (strides[t][i] % 8 || strides[t][i] < 0))
         return waveal::fail(WAVEAL_ERR_INVALID_ARG, "strides must be multiples of 8 elements (16 bytes) and not negative");
+  if (d->tokens && folds(d)) return waveal::fail(WAVEAL_ERR_INVALID_ARG, "o's strides let its rows overlap each other");
   return WAVEAL_OK;
 }
 

@@ -123,3 +123,23 @@ def test_sizes_whose_loops_would_run_over(lib, over):
         assert compact(pool(min(n_pages, MOST)), *(min(x, MOST) for x in sizes)) == TAKEN, sizes
     assert lib.waveal_cache_compact_workspace_bytes(ctypes.byref(pool(over)), ctypes.byref(n)) == wb.ERR_UNSUPPORTED
     assert lib.waveal_cache_compact_workspace_bytes(ctypes.byref(pool(MOST)), ctypes.byref(n)) == wb.OK
+
+
+def test_prompt_results_over_each_other(lib):
+    """Strides of o by which two of its rows have an element in common are refused, all others taken."""
+    r, met, let = random.Random(6), 0, 0
+    for _ in range(4000):
+        heads, tokens, dim = r.randint(1, 6), r.randint(1, 6), r.choice([64, 128])
+        stride = [r.choice([0, 8, dim - 8, dim, dim + 8, r.randint(0, 100) * 8, dim * r.randint(1, 6)]) for _ in range(2)]
+        rows = sorted(h * stride[0] + t * stride[1] for h in range(heads) for t in range(tokens))
+        common = any(b - a < dim for a, b in zip(rows, rows[1:]))
+        strides = [(dim, heads * dim), (dim, dim), (dim, dim), stride]
+        d = wb.PromptDesc(1, tokens, heads, 1, dim, wb.BF16, 0, *map(tuple, strides))
+        n = ctypes.c_size_t(0)
+        assert lib.waveal_prompt_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(n)) == (wb.ERR_INVALID_ARG if common else wb.OK), (heads, tokens, dim, stride)
+        met, let = met + common, let + (not common)
+    assert met > 500 and let > 500
+    # the largest: 10^9 rows, heads and tokens as many (a token's heads reach 30,999 * 128 + 128 = 31,000 * 128 elements far)
+    for stride, status in (((128, 128 * 31000 + 8), wb.OK), ((128, 128 * 31000 - 8), wb.ERR_INVALID_ARG), ((136, 128 * 31000 + 8), wb.ERR_INVALID_ARG), ((1 << 40, 128), wb.OK), ((128, 1 << 40), wb.OK), ((0, 1 << 62), wb.ERR_INVALID_ARG)):
+        d = wb.PromptDesc(1, 31000, 31000, 31000, 128, wb.BF16, 0, (128, 128), (128, 128), (128, 128), stride)
+        assert lib.waveal_prompt_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(ctypes.c_size_t(0))) == status, stride
