@@ -447,8 +447,9 @@ waveal_status waveal_prompt_attn_workspace_bytes(const waveal_prompt_desc* desc 
  * within 0 .. tokens): no two sequences claim the same token.
  * lse: dev float [q_heads][tokens] or NULL, the natural log of the sum of exponentials.  A token whose scores are all -infinity has o = 0 and -inf; a row
  * whose scores hold +infinity or NaN gives NaN.  Keys and values that a token does not see, NaN and infinities included, never reach it.
+ * A value that is infinite gives an infinity, or NaN where its probability rounds to zero in the tensors' type.
  * (128 rows some of whose results are not finite, or whose scores' exponentials exceed 2^16 (fp16) or 2^100 (bf16) times those of their first 16, are
- * computed a second time in a slower way.)
+ * computed a second time in a slower way, behind all others: a call with many of them takes two to three times as long.)
  * q, k, v, o: 16-byte aligned, strides multiples of 8 elements and not negative (that of a dimension with one entry: anything); o must overlap neither the others nor
  * itself, which is checked (it may lie between the elements of one that has the same strides, as in a buffer with one row a token for all of
  * them).  At most 2^25 tokens, 10^9 rows (tokens * q_heads) and 10^9 row tiles ((tokens / (128 / group) + batch) * kv_heads, with group = q_heads

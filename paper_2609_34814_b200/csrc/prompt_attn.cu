@@ -16,11 +16,13 @@
 // that four of them a scheduler are needed), 16 items, Q and K, 17 and 18 products, 19 V, 20-23 results.
 //
 // What bounds it: a tile of 128 x 128 at head_dim 128 is 1,024 clk of the tensor pipe and 1,024 clk of the exponentials' unit, and takes 1,370 to
-// 1,425; the rest is the way round of a buffer (products, 1,950 clk of a team's softmax, products) through three buffers, which is all that tensor
-// memory holds beside O.  32,760 causal tokens, 32 query and 8 key heads: 6.2 to 6.6 ms by the GPU (1,330 to 1,410 TFLOP/s, 80 to 85 % of the best library product),
-// 6.8 to 7.4 ms in a row of calls under the power cap.  Sixteen prompts of 20 to 2,000 tokens: 166 us; six frames of 1,560 tokens and 40 heads: 281 us (1,060
-// TFLOP/s); 150 prompts of up to 700 tokens at head_dim 64: 207 us: row tiles of one to eleven key tiles, where a team needs 2,100 to 2,700 clk for a row tile's
-// first or last tile (reference, mask, exponentials) and 700 to get to the next one, so that two teams finish a tile in 1,700.
+// 1,450; the rest is the way round of a buffer (products, 1,950 clk of a team's softmax, products) through three buffers, which is all that tensor
+// memory holds beside O.  In a row of calls, under the power cap, with the SM clock that was sampled meanwhile / in the first 4 ms after a pause:
+//   32,760 causal tokens, 32 query and 8 key heads          7.4 ms at 1,387 MHz / 6.2 to 6.6     1,180 TFLOP/s: 86 % of a library product kept up, 71 % of its burst
+//   16 prompts of 20 to 2,000 tokens, the same heads        195 us at 1,470 MHz / 169            11,400 clk a row tile of 5.8 key tiles: 3,000 beside the loop's pace
+//   6 frames of 1,560 tokens, 40 heads, not causal          328 us at 1,432 MHz / 287            910 TFLOP/s; 13 key tiles whose last one has 24 keys, 22 turns of row tiles
+//   150 prompts of up to 700 tokens, head_dim 64, fp16      228 us at 1,687 MHz / 196            4,700 clk a row tile of 2.4 key tiles
+// Short row tiles: a team needs 2,100 to 2,700 clk for a row tile's first or last tile (reference, mask, exponentials) and 700 to get to the next one.
 // The same 32,760 tokens on the way here: the row's scores in registers of one thread, 11.4 ms (its code did not fit the instruction caches: 4.2 warps
 // an issue waited for instructions); rolled loops that read S twice, 8.5; products issued by two warps, 7.9; two threads a row, 7.2; three buffers and
 // one stream, 6.8; results by warps of their own, 6.7; tiles without a mask or a first score apart, 6.55.  Without gain: polynomials for an eighth to three

@@ -148,3 +148,19 @@ def test_one_buffer_for_inputs_and_results(order):
             wb.prompt_attn(x, y, z, start, o=buf[sum(parts[:3]) - early:sum(parts) - early])
         assert e.value.status == wb.ERR_INVALID_ARG
     assert torch.equal(buf, before)
+
+
+@pytest.mark.parametrize("dim, dtype, bits", [(64, HF, 10), (64, HF, 40), (128, BF, 40), (128, BF, 300)])
+def test_an_infinite_value_with_a_small_probability(dim, dtype, bits):
+    """2^-bits of the largest one: the rows that see it have an infinity there, or NaN where the probability rounds to zero; nothing else changes."""
+    n = 400
+    q, k, v = tensors(n, 4, 2, dim, dtype, seed=26, q_scale=0.02)
+    q[..., 0], k[..., 0], k[:, 0, 0] = 8.0, 0.0, bits * math.log(2.0) * math.sqrt(dim) / 8.0
+    want, want_lse, tol, lse_tol = expected(q, k, v, [0], [n], True)
+    v[:, 150, 3] = math.inf
+    o, lse, status = run(q, k, v, [0, n])
+    assert status == [0, 0, 0, 0]
+    seen = o[:, 150:, 3]
+    assert ((seen == math.inf) | seen.isnan()).all() and ((seen == math.inf).all() if bits == 10 else True)
+    o[:, 150:, 3] = want[:, 150:, 3].to(dtype)
+    compare(o, lse, want, want_lse, tol, lse_tol)
