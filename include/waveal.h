@@ -451,8 +451,8 @@ waveal_status waveal_prompt_attn_workspace_bytes(const waveal_prompt_desc* desc 
  * (128 rows some of whose results are not finite, or whose scores' exponentials exceed 2^16 (fp16) or 2^100 (bf16) times those of their first 16, are
  * computed a second time in a slower way, behind all others: a call with many of them takes two to three times as long.)
  * q, k, v, o: 16-byte aligned, strides multiples of 8 elements and not negative (that of a dimension with one entry: anything); o must overlap neither the others nor
- * itself, which is checked (it may lie between the elements of one that has the same strides, as in a buffer with one row a token for all of
- * them).  At most 2^25 tokens, 10^9 rows (tokens * q_heads) and 10^9 row tiles ((tokens / (128 / group) + batch) * kv_heads, with group = q_heads
+ * itself, which is checked (it may lie between the elements of one that has the same stride along one dimension, as in a buffer with one row
+ * a token for all of them; beside one that has neither, its bytes from the first to the last must be apart from the other's).  At most 2^25 tokens, 10^9 rows (tokens * q_heads) and 10^9 row tiles ((tokens / (128 / group) + batch) * kv_heads, with group = q_heads
  * / kv_heads).  scale <= 0 means 1/sqrt(head_dim).  Scores, sums and the
  * accumulated output are fp32; the probabilities, relative to one of the row's scores, enter the second product in the tensors' type
  * (fp16: to multiples of 2^-24 below 2^-14, which adds up to 2^-25 sum |v| to a result).

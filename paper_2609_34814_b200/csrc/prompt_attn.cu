@@ -1014,23 +1014,39 @@ bool lands(Wide at, Wide step, Wide low, Wide high, Wide dim) {
   return false;
 }
 
-// Does o share an element with an input of `heads` heads?  Exact where both have the same strides, so that o may lie between an input's elements (one row a
-// token for all tensors); otherwise the bytes from the first to the last element decide.
+// Does o share an element with an input of `heads` heads?  Exact where their strides agree along one dimension, so that o may lie between an input's elements
+// (one row a token for all tensors, an input's heads repeated by a stride of 0); otherwise the bytes from the first to the last element decide.
 bool meets(const waveal_prompt_desc* d, const void* o, const void* x, int heads, const int64_t* stride) {
   const Wide D = d->head_dim, T = d->tokens, H = d->q_heads;
   const Wide ot = T > 1 ? d->o_stride[1] : 0, xt = T > 1 ? stride[1] : 0;
-  const Wide oh = H > 1 ? d->o_stride[0] : heads > 1 ? stride[0] : 0, xh = heads > 1 ? stride[0] : oh;
+  const Wide oh = H > 1 ? d->o_stride[0] : 0, xh = heads > 1 ? stride[0] : oh;
   const Wide apart = ((Wide) reinterpret_cast<intptr_t>(o) - (Wide) reinterpret_cast<intptr_t>(x)) / 2;   // elements (both are aligned to eight)
   if (apart >= (heads - 1) * xh + (T - 1) * xt + D || -apart >= (H - 1) * oh + (T - 1) * ot + D) return false;
-  if (ot != xt || oh != xh) return true;
-  // two rows that are i heads and k tokens apart, 1 - heads <= i < H, -T < k < T: the fewer of them one by one (at most 2 x 31,623: 10^9 rows)
-  if (H + heads <= 2 * T) {
-    for (Wide i = 1 - heads; i < H; ++i)
-      if (lands(apart + i * oh, ot, 1 - T, T - 1, D)) return true;
-  } else {
-    for (Wide k = 1 - T; k < T; ++k)
-      if (lands(apart + k * ot, oh, 1 - heads, H - 1, D)) return true;
+  if (ot != xt && oh != xh) return true;
+  if (ot == xt && oh == xh) {
+    // two rows that are i heads and k tokens apart, 1 - heads <= i < H, -T < k < T: the fewer of them one by one (at most 2 x 31,623: 10^9 rows)
+    if (H + heads <= 2 * T) {
+      for (Wide i = 1 - heads; i < H; ++i)
+        if (lands(apart + i * oh, ot, 1 - T, T - 1, D)) return true;
+    } else {
+      for (Wide k = 1 - T; k < T; ++k)
+        if (lands(apart + k * ot, oh, 1 - heads, H - 1, D)) return true;
+    }
+    return false;
   }
+  // `step` is common; for each distance along it that can matter, o's rows along the other dimension one by one
+  const bool by_token = ot == xt;
+  const Wide step = by_token ? ot : oh, on = by_token ? H : T, xn = by_token ? (Wide)heads : T, os = by_token ? oh : ot, xs = by_token ? xh : xt;
+  Wide low = by_token ? 1 - T : 1 - (Wide)heads, high = by_token ? T - 1 : H - 1;
+  if (step) {
+    low = std::max(low, (-(on - 1) * os - D - apart) / step - 1), high = std::min(high, ((xn - 1) * xs + D - apart) / step + 1);
+  } else {
+    low = high = 0;
+  }
+  if (low <= high && (high - low + 1) * on > 1 << 20) return true;   // (some ms of the host's time; the bytes' ranges overlap)
+  for (Wide k = low; k <= high; ++k)
+    for (Wide i = 0; i < on; ++i)
+      if (lands(-(apart + k * step + i * os), xs, 0, xn - 1, D)) return true;
   return false;
 }
 

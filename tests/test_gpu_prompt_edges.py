@@ -164,3 +164,23 @@ def test_an_infinite_value_with_a_small_probability(dim, dtype, bits):
     assert ((seen == math.inf) | seen.isnan()).all() and ((seen == math.inf).all() if bits == 10 else True)
     o[:, 150:, 3] = want[:, 150:, 3].to(dtype)
     compare(o, lse, want, want_lse, tol, lse_tol)
+
+
+def test_results_between_the_heads_of_one_buffer():
+    """Every other head of the buffer's rows is q's or o's, every fourth k's or v's: one stride in common, no element."""
+    lens = [200, 1, 99]
+    q, k, v = tensors(sum(lens), 6, 3, 64, BF, seed=27)
+    want = run(q, k, v, ends(lens))
+    wide = torch.full((sum(lens), 36, 64), 7.0, dtype=BF, device="cuda")
+    x, y, z, o = (wide[:, a:b:s].transpose(0, 1) for a, b, s in ((0, 12, 2), (12, 24, 4), (24, 36, 4), (1, 12, 2)))
+    x.copy_(q), y.copy_(k), z.copy_(v)
+    start = torch.tensor(ends(lens), dtype=torch.int32, device="cuda")
+    wb.prompt_attn(x, y, z, start, o=o)
+    assert torch.equal(o, want[0]) and torch.equal(x, q) and torch.equal(y, k) and torch.equal(z, v) and (wide[:, 13:24:4] == 7).all()
+    # one key head, repeated without a copy, in front of o in every row
+    y, z = (t[:1].expand(6, -1, -1) for t in (y, z))
+    want = run(q, k[:1], v[:1], ends(lens))
+    wb.prompt_attn(x, y, z, start, o=wide[:, 25:36:2].transpose(0, 1)[:6])
+    assert torch.equal(wide[:, 25:36:2].transpose(0, 1), want[0])
+    with pytest.raises(wb.WavealError):
+        wb.prompt_attn(x, y, z, start, o=wide[:, 24:36:2].transpose(0, 1))

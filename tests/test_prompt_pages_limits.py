@@ -89,6 +89,52 @@ def test_prompt_overlap_against_sets(lib):
     assert met > 300 and let > 300
 
 
+def test_prompt_overlap_with_one_stride_in_common(lib):
+    """The same where head strides differ (repeated heads with a stride of 0 among them), or token strides: still exact."""
+    r = random.Random(7)
+    dim, met, let = 64, 0, 0
+    for _ in range(6000):
+        heads, tokens = r.choice([(2, 1), (2, 3), (4, 3), (3, 2), (6, 5), (4, 9)])
+        kv_heads = r.choice([h for h in (1, 2, 3, 4, 6) if heads % h == 0])
+        if r.random() < 0.6:
+            common = 8 * r.randint(0, 300)
+            k = (r.choice([0, 64, 128, 8 * r.randint(0, 60)]), common)
+            o = (64 + 8 * r.randint(0, 30), max(common, 8))
+            common = o[1]
+            k = (k[0], common)
+        else:
+            common = 64 + 8 * r.randint(0, 300)
+            k = (common, r.choice([0, 64, 8 * r.randint(0, 60)]))
+            o = (common, 64 + 8 * r.randint(0, 30))
+        rows = sorted(h * o[0] + t * o[1] for h in range(heads) for t in range(tokens))
+        if any(b - a < dim for a, b in zip(rows, rows[1:])):
+            continue                                                      # o over itself is refused before
+
+        def elements(at, heads, stride):
+            return {at + h * stride[0] + t * stride[1] + c for h in range(heads) for t in range(tokens) for c in range(0, dim, 8)}
+        at = [5_000_000, 8 * r.randint(0, 200), 2_000_000, 8 * r.randint(0, 400)]
+        meets = bool(elements(at[1], kv_heads, k) & elements(at[3], heads, o))
+        got = prompt(lib, heads, kv_heads, tokens, dim, at, [(64, 64 * heads), k, (64, 64 * kv_heads), o])
+        assert got == (wb.ERR_INVALID_ARG if meets else TAKEN), (heads, kv_heads, tokens, at, k, o)
+        met, let = met + meets, let + (not meets)
+    assert met > 500 and let > 500
+
+
+def test_prompt_overlap_of_the_largest(lib):
+    """Two strides in common, one, none: 10^9 rows are decided about without a walk through all of them."""
+    heads = tokens = 31000
+    row = 128 * heads
+    strides = lambda k, o: [(128, row), k, (128, row), o]  # noqa: E731
+    far = 1 << 45
+    for k, o, at, status in (((128, 2 * row), (128, 2 * row), row, TAKEN), ((128, 2 * row), (128, 2 * row), row - 8, wb.ERR_INVALID_ARG),
+                             # (o's heads fill the second half of every 2 * row elements, the repeated key head is at the front of the first)
+                             ((0, 2 * row), (128, 2 * row), row, TAKEN), ((0, 2 * row), (128, 2 * row), 0, wb.ERR_INVALID_ARG),
+                             ((136, 4 * row), (128, 2 * row), 0, wb.ERR_INVALID_ARG), ((136, 4 * row), (128, 2 * row), 1 << 44, TAKEN)):
+        assert prompt(lib, heads, heads, tokens, 128, [far, 0, 2 * far, at], strides(k, o)) == status, (k, o, at)
+    # three heads a token that read one repeated key head
+    assert prompt(lib, 3, 3, 1 << 24, 64, [far, 0, 2 * far, 64], [(64, 192), (0, 256), (64, 192), (64, 256)]) == TAKEN
+
+
 def pool(n_pages=10, head_dim=128):
     return wb.CacheDesc(n_pages, 16, 2, head_dim, wb.BF16, (32 * head_dim, 16 * head_dim, head_dim), (32 * head_dim, 16 * head_dim, head_dim))
 
